@@ -58,7 +58,8 @@ typedef enum {
   CATQ_ERR_TIMEOUT = 6,     /* a bounded device-side wait expired (latched) */
   CATQ_ERR_NONFINITE = 7,   /* reserved: non-finite data detected (latched) */
   CATQ_ERR_UNSUPPORTED = 8, /* valid request this build does not implement (e.g. no sm_100-class GPU) */
-  CATQ_ERR_WORKSPACE = 9    /* workspace missing or smaller than the *_workspace_bytes() result */
+  CATQ_ERR_WORKSPACE = 9,   /* workspace missing or smaller than the *_workspace_bytes() result */
+  CATQ_ERR_INDEX = 10       /* a page number, row offset or length read on the device was out of range (latched) */
 } catq_status;
 
 typedef enum { CATQ_F32 = 0, CATQ_BF16 = 1 } catq_dtype;
@@ -588,6 +589,116 @@ catq_status catq_attention_fwd(const void* Q, const void* K, const void* V, int3
 catq_status catq_attention_bwd(const void* Q, const void* K, const void* V, const void* O, const void* dO,
                                const float* lse, int32_t B, int32_t S, int32_t n_heads, int32_t n_kv_heads,
                                int32_t d, float* delta, void* dQ, void* dK, void* dV, catq_stream stream);
+
+/* ------------------------------------------------------------------ decoding over a paged 8-bit cache
+ * What a deployed model does between its packed linears (catq_ternary_infer): the new tokens' queries and
+ * keys are rotated to their positions, keys and values go into a cache, and the queries attend to what the
+ * cache holds of their sequence.  (This library's addition; the paper leaves decoding to another runtime.)
+ * Errors as for the decoder-block layers. */
+
+typedef enum {
+  CATQ_ROPE_HALF = 0,       /* pair i: elements i and i + rot/2 of the head */
+  CATQ_ROPE_INTERLEAVED = 1 /* pair i: elements 2i and 2i + 1 */
+} catq_rope_layout;
+
+/* How the pairs' frequencies f_i = base^(-2i/rot) (radians a token) are scaled for contexts longer than
+ * those a model was trained on. */
+typedef enum {
+  CATQ_ROPE_PLAIN = 0,  /* f_i */
+  CATQ_ROPE_LINEAR = 1, /* f_i / factor (interpolated positions) */
+  CATQ_ROPE_BANDS = 2,  /* by the turns t_i = original f_i / 2 pi that a pair makes in the original context: f_i where
+                           t_i >= high, f_i / factor where t_i <= low, between them (1 - w) f_i / factor + w f_i with
+                           w = (t_i - low) / (high - low) */
+  CATQ_ROPE_YARN = 3    /* by the pair's index: f_i up to a, f_i / factor from b on, linear in i between, where
+                           a = floor(x(high)), b = ceil(x(low)), x(t) = rot ln(original / (2 pi t)) / (2 ln base), a >= 0,
+                           b <= rot - 1, b - a at least 0.001; magnitude 0.1 ln(factor) + 1 */
+} catq_rope_scaling;
+
+/* A rotation by position.  turns: device [rot/2], 8-byte aligned, the turns a token of each pair in 64-bit
+ * fixed point (2^64 is one turn; catq_rotation_turns fills a host copy): the product with a position wraps
+ * modulo one turn, so the angle of a far position is as exact as that of a near one. */
+typedef struct {
+  const uint64_t* turns;
+  int32_t rot;      /* rotated elements, the first of every head: even, 2 <= rot <= d; the others pass unchanged */
+  int32_t layout;   /* catq_rope_layout */
+  float magnitude;  /* factor on the rotated elements (1: a rotation), finite */
+  int32_t reserved; /* must be 0 */
+} catq_rotation;
+
+/* Host only: turns [rot/2] and magnitude of a scaled rotation.  rot even, 2 <= rot <= 65536 (else
+ * CATQ_ERR_SHAPE); base > 1, scaling a catq_rope_scaling; where a scaling uses them factor >= 1, original >= 1 and
+ * 0 < low < high, finite.  Other values and null pointers: CATQ_ERR_INVALID_ARG. */
+catq_status catq_rotation_turns(int32_t rot, double base, int32_t scaling, double factor, double low, double high,
+                                double original, uint64_t* turns, float* magnitude);
+
+/* Y = X [T rows of n_heads d] with every head's pairs (a, b) rotated by the angle of the row's position:
+ *   (a, b) -> magnitude (a cos - b sin, a sin + b cos)    (inverse != 0: (a cos + b sin, b cos - a sin), the
+ * backward of the rotation, magnitude included).  X, Y of dtype (CATQ_BF16 or CATQ_F32), rows ldx and ldy elements
+ * apart (>= n_heads d: the queries of a fused q/k/v product can be given in place); Y may be X (then ldy == ldx, else
+ * CATQ_ERR_INVALID_ARG) and must not overlap it otherwise.  positions [T] int32, device.  d even, 2 <= d <= 65536.
+ * Pointers aligned to their element type; 16-byte aligned rows with d and rot multiples of 16 are faster.
+ * T == 0 is a no-op. */
+catq_status catq_rope_at(const void* X, int64_t ldx, void* Y, int64_t ldy, int32_t dtype, const int32_t* positions,
+                         int64_t T, int32_t n_heads, int32_t d, const catq_rotation* rotation, int32_t inverse,
+                         catq_stream stream);
+
+/* A paged key/value cache of e4m3 codes (device memory, caller-owned).  Page p holds `page` consecutive tokens of one
+ * sequence: codes [n_pages, n_kv_heads, page, d], one byte each, and one scale a page and head, [n_pages, n_kv_heads]
+ * fp32, for keys and for values; an element is code * scale.  Page table [B, max_pages] int32: the page of tokens
+ * i page .. of every sequence; entries behind a sequence's last token are not read.  page 16, 32, 64 or 128; d 64 or
+ * 128; n_pages n_kv_heads page < 2^31 (else CATQ_ERR_SHAPE); codes 128-byte aligned, scales and table 4-byte. */
+typedef struct {
+  void* k_codes;
+  void* v_codes;
+  float* k_scale;
+  float* v_scale;
+  const int32_t* table;
+  int32_t n_pages, n_kv_heads, page, d, max_pages;
+  int32_t reserved; /* must be 0 */
+} catq_kv_cache;
+
+/* Appends new tokens to the cache.  Sequence b (of B) has the rows row_start[b] .. row_start[b+1] - 1 of K and V
+ * ([T rows of n_kv_heads d] bf16, ldk and ldv elements apart), which become its last tokens: seq_len[b] is its length
+ * with them, so row row_start[b] + i has position seq_len[b] - (row_start[b+1] - row_start[b]) + i.  row_start [B+1] and
+ * seq_len [B] are device int32.  Keys are rotated to their positions (rotation NULL: not), in fp32 and never rounded
+ * before the code.  With Q [T rows of n_heads d] bf16 (nullable) the same launch writes the rotated queries to Q_out
+ * (bf16; may be Q with ldq_out == ldq).  For every page and head that gets tokens:
+ *   want  = the least power of two, 2^-60 or more, with max |new values| <= 448 want   (0 when all are 0)
+ *   scale = max(scale, want), or want when the page's first token is among the new ones (a recycled page's old scale
+ *           does not count)
+ *   codes already in the page: multiplied by old scale / scale and rounded again (exact but for e4m3's subnormals),
+ *   new codes = e4m3(value / scale), to nearest, ties to even.
+ * A value that is not finite makes the scale NaN until the page begins anew: the queries that see a token of
+ * such a page get NaN, others are not touched.  Tokens at negative positions (rows of an idle slot of length 0) and rows
+ * outside every sequence are not stored.  No two sequences may get tokens in the same page in one call.
+ * Sequences with row offsets outside 0 .. T or decreasing, or a length outside 0 .. max_pages page, and pages outside
+ * 0 .. n_pages - 1 are skipped, latching CATQ_ERR_INDEX (catq_device_status).  rot a multiple of 16, rows 16-byte aligned
+ * (else CATQ_ERR_SHAPE, CATQ_ERR_ALIGN); 0 <= B <= 65535, T < 2^31, n_kv_heads <= 4096, n_heads <= 65536, max_pages page < 2^31.
+ * T == 0 or B == 0 is a no-op. */
+catq_status catq_kv_append(const catq_kv_cache* cache, const int32_t* row_start, const int32_t* seq_len, int32_t B,
+                           const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t T, const void* Q, int64_t ldq,
+                           void* Q_out, int64_t ldq_out, int32_t n_heads, const catq_rotation* rotation,
+                           catq_stream stream);
+
+/* Workspace bytes of catq_kv_attention on the current device. */
+size_t catq_kv_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, int32_t d);
+
+/* Attention of the new tokens over the cache: row r of sequence b (rows, lengths and positions as in catq_kv_append,
+ * normally called just before) and query head h, which uses key/value head h / (n_heads / n_kv_heads):
+ *   O[r, h] = softmax(Q[r, h] K^T / sqrt(d)) V   over the sequence's tokens at positions up to the row's own.
+ * Q, O [T rows of n_heads d] bf16, ldq and ldo elements apart, rows 16-byte aligned; O may be Q with ldo == ldq.
+ * lse [T, n_heads] fp32 (nullable): the natural log-sum-exp of the scaled scores.  Queries enter exactly (as two
+ * e4m3 terms), scores, softmax and sums are fp32, the weights of the values have two e4m3 terms (a relative 2^-8, as
+ * bf16 weights).  A row that sees no token (a negative position) gets 0 and lse -inf; rows outside every
+ * sequence are left as they were.  Codes are never NaN (catq_kv_append writes none) in tokens of the sequence; what lies
+ * behind its last token may be anything.  Scales are powers of two, 0 or NaN.  Out-of-range offsets and lengths as in
+ * catq_kv_append (the sequence's rows are left as they were); a page outside 0 .. n_pages - 1 counts as zeros, latched.
+ * workspace: >= catq_kv_attention_workspace_bytes(), 256-byte aligned, zero before the first call; a call leaves the
+ * part that has to be zero as zero.  Calls that may run at the same time need workspaces of their own.
+ * n_heads % n_kv_heads == 0, n_heads / n_kv_heads <= 64; limits as for catq_kv_append. */
+catq_status catq_kv_attention(const catq_kv_cache* cache, const int32_t* row_start, const int32_t* seq_len, int32_t B,
+                              const void* Q, int64_t ldq, int64_t T, int32_t n_heads, void* O, int64_t ldo, float* lse,
+                              void* workspace, size_t ws_bytes, catq_stream stream);
 
 /* Self-test of the device-side failure detection (no counterpart in the paper): launches
  * one thread that waits, through the library's bounded mbarrier wait, on a barrier nothing

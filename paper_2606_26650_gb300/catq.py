@@ -22,11 +22,14 @@ PHASE_TEACHER, PHASE_SOFT, PHASE_HARD = 0, 1, 2
 THR_HALF, THR_TWN07, THR_ABSMEAN, THR_TWN_STATIC = 0, 1, 2, 3
 REDUCE_MEAN, REDUCE_SUM = 0, 1
 RECON_ALPHA_T, RECON_ALPHA_T_MU = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BANDS, ROPE_YARN = 0, 1, 2, 3
 
 STATUS = {
     0: "CATQ_OK", 1: "CATQ_ERR_INVALID_ARG", 2: "CATQ_ERR_SHAPE", 3: "CATQ_ERR_DTYPE",
     4: "CATQ_ERR_ALIGN", 5: "CATQ_ERR_CUDA", 6: "CATQ_ERR_TIMEOUT", 7: "CATQ_ERR_NONFINITE",
     8: "CATQ_ERR_UNSUPPORTED", 9: "CATQ_ERR_WORKSPACE",
+    10: "CATQ_ERR_INDEX",
 }
 
 
@@ -65,6 +68,18 @@ class catq_infer_layer(ctypes.Structure):
                 ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("X", ctypes.c_void_p), ("Y", ctypes.c_void_p)]
 
 
+class catq_rotation(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("rot", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("magnitude", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class catq_kv_cache(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p), ("n_pages", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("page", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 class catq_adamw(ctypes.Structure):
     _fields_ = [("beta1", ctypes.c_float), ("beta2", ctypes.c_float), ("eps", ctypes.c_float),
                 ("weight_decay", ctypes.c_float), ("margin", ctypes.c_float)]
@@ -82,7 +97,9 @@ def lib() -> ctypes.CDLL:
         raise RuntimeError(f"{LIB_PATH} is missing: build it with __graft_entry__.build()")
     L = ctypes.CDLL(LIB_PATH)
     P, I64, I32, F, S = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
-    LP, GP, IP = (ctypes.POINTER(t) for t in (catq_layer, catq_grouped_layer, catq_infer_layer))
+    LP, GP, IP, RP, KP = (ctypes.POINTER(t) for t in (catq_layer, catq_grouped_layer, catq_infer_layer, catq_rotation,
+                                                     catq_kv_cache))
+    D = ctypes.c_double
     sig = {
         "catq_abi_version": (I32, []),
         "catq_status_string": (ctypes.c_char_p, [I32]),
@@ -127,6 +144,11 @@ def lib() -> ctypes.CDLL:
         "catq_block_output_loss": (I32, [P, P, I64, P, I32, P, P, P, P, S, P]),
         "catq_attention_fwd": (I32, [P, P, P, I32, I32, I32, I32, I32, P, P, P]),
         "catq_attention_bwd": (I32, [P, P, P, P, P, P, I32, I32, I32, I32, I32, P, P, P, P, P]),
+        "catq_rotation_turns": (I32, [I32, D, I32, D, D, D, D, P, ctypes.POINTER(F)]),
+        "catq_rope_at": (I32, [P, I64, P, I64, I32, P, I64, I32, I32, RP, I32, P]),
+        "catq_kv_append": (I32, [KP, P, P, I32, P, I64, P, I64, I64, P, I64, P, I64, I32, RP, P]),
+        "catq_kv_attention_workspace_bytes": (S, [I32, I32, I32]),
+        "catq_kv_attention": (I32, [KP, P, P, I32, P, I64, I64, I32, P, I64, P, P, S, P]),
         "catq_grouped_soft_ternary_linear_fwd_loss": (I32, [GP, catq_schedule, P, P, I32, P, I32, P, P, P, P, S, P]),
     }
     for name, (res, args) in sig.items():
@@ -734,3 +756,165 @@ def catq_attention_bwd(Q, K, V, O, dO, lse, delta, dQ, dK, dV, B, S, n_heads, n_
     ls, de = _buf(lse, "lse", ns, w), _buf(delta, "delta", ns, w)
     _check(lib().catq_attention_bwd(q, k, v, o, do, ls, int(B), int(S), int(n_heads), int(n_kv_heads), int(d), de, dq,
                                     dk, dv, _stream(stream)), w)
+
+
+# ------------------------------------------------------------------ decoding over a paged 8-bit cache
+# Rows of activations [T, n_heads * d] or [T, n_heads, d] whose rows may lie apart (the queries, keys and values of
+# a fused product): contiguous but for the first dimension's stride.
+
+_ROTATION = struct.Struct("Qiifi")
+_KV = struct.Struct("5Q6i")
+
+
+def _rows(t, name: str, T: int, width: int, where: str):
+    """(address, elements from a row to the next) of T rows of `width` elements."""
+    if not t.is_cuda:
+        raise ValueError(f"{where}: {name} must be a CUDA tensor")
+    shape = t.shape
+    if len(shape) not in (2, 3) or shape[0] != T or t.numel() != T * width:
+        raise ValueError(f"{where}: {name} has shape {tuple(shape)}, the call needs {T} rows of {width}")
+    st = t.stride()
+    if st[-1] != 1 or (len(shape) == 3 and shape[1] > 1 and st[1] != shape[2]) or (T > 1 and st[0] < width):
+        raise ValueError(f"{where}: {name}'s rows must be contiguous and in order")
+    return t.data_ptr(), st[0] if T > 1 else width
+
+
+def _i32(t, name: str, count: int, where: str):
+    if str(t.dtype) != "torch.int32":
+        raise ValueError(f"{where}: {name} must be int32")
+    return _buf(t, name, 4 * count, where)
+
+
+@dataclasses.dataclass
+class Rope:
+    """A rotation by position: `turns` int64 [rot / 2] (64-bit fixed point, see catq_rotation_turns) on the GPU."""
+    turns: object
+    rot: int
+    layout: int = ROPE_HALF
+    magnitude: float = 1.0
+
+    @classmethod
+    def create(cls, rot, base, device, layout=ROPE_HALF, scaling=ROPE_PLAIN, factor=1.0, low=1.0, high=4.0,
+               original=8192.0):
+        """The turns of base^(-2i/rot) under a scaling for long contexts (catq_rope_scaling)."""
+        import torch
+        turns, magnitude = catq_rotation_turns(rot, base, scaling, factor, low, high, original)
+        return cls(torch.tensor(turns, dtype=torch.int64).to(device), int(rot), int(layout), magnitude)
+
+    def struct(self) -> catq_rotation:
+        r = catq_rotation()
+        _ROTATION.pack_into(r, 0, _buf(self.turns, "turns", 4 * self.rot, "Rope"), self.rot, self.layout,
+                            self.magnitude, 0)
+        return r
+
+
+@dataclasses.dataclass
+class KVCache:
+    """A paged cache of e4m3 codes: k_codes, v_codes float8_e4m3fn (or uint8) [n_pages, n_kv_heads, page, d], k_scale,
+    v_scale fp32 [n_pages, n_kv_heads], table int32 [B, max_pages]."""
+    k_codes: object
+    v_codes: object
+    k_scale: object
+    v_scale: object
+    table: object
+
+    @classmethod
+    def create(cls, n_pages, n_kv_heads, page, d, table):
+        """Allocates codes and scales for the pages that `table` numbers."""
+        import torch
+        kw = dict(device=table.device)
+        codes = [torch.zeros(n_pages, n_kv_heads, page, d, dtype=torch.uint8, **kw).view(torch.float8_e4m3fn)
+                 for _ in range(2)]
+        scales = [torch.zeros(n_pages, n_kv_heads, dtype=torch.float32, **kw) for _ in range(2)]
+        return cls(*codes, *scales, table)
+
+    def struct(self) -> catq_kv_cache:
+        w = "KVCache"
+        n_pages, nkv, page, d = self.k_codes.shape
+        B, max_pages = self.table.shape
+        if self.k_codes.element_size() != 1 or self.v_codes.element_size() != 1:
+            raise ValueError(f"{w}: codes are one byte an element")
+        n, m = n_pages * nkv * page * d, 4 * n_pages * nkv
+        c = catq_kv_cache()
+        _KV.pack_into(c, 0, _buf(self.k_codes, "k_codes", n, w), _buf(self.v_codes, "v_codes", n, w),
+                      _f32(self.k_scale, "k_scale", m, w), _f32(self.v_scale, "v_scale", m, w),
+                      _i32(self.table, "table", B * max_pages, w), n_pages, nkv, page, d, max_pages, 0)
+        return c
+
+
+def catq_rotation_turns(rot: int, base: float, scaling: int = ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
+                        high: float = 4.0, original: float = 8192.0):
+    """(turns as a list of signed 64-bit integers, magnitude) of a scaled rotation (host only)."""
+    turns, m = (ctypes.c_int64 * max(1, int(rot) // 2))(), ctypes.c_float()
+    _check(lib().catq_rotation_turns(int(rot), float(base), int(scaling), float(factor), float(low), float(high),
+                                     float(original), turns, ctypes.byref(m)), "catq_rotation_turns")
+    return list(turns), float(m.value)
+
+
+def catq_rope_at(X, positions, rope: Rope, n_heads: int, d: int, Y=None, inverse: bool = False, stream=None):
+    """Y (X itself when None) = the rows of X [T, n_heads * d] rotated to their positions (int32 [T]); inverse: the
+    backward.  X, Y bf16 or fp32."""
+    w, T = "catq_rope_at", X.shape[0]
+    x, ldx = _rows(X, "X", T, n_heads * d, w)
+    y, ldy = (x, ldx) if Y is None else _rows(Y, "Y", T, n_heads * d, w)
+    dt = _dtype_code(X)
+    if Y is not None and Y.dtype != X.dtype:
+        raise ValueError(f"{w}: Y must have X's dtype")
+    _check(lib().catq_rope_at(x, ldx, y, ldy, dt, _i32(positions, "positions", T, w), T, n_heads, d, rope.struct(),
+                              1 if inverse else 0, _stream(stream)), w)
+
+
+def _kv_meta(cache, row_start, seq_len, where):
+    """The cache's struct, the addresses of the row offsets and lengths, and the sequences."""
+    B = cache.table.shape[0]
+    return cache.struct(), _i32(row_start, "row_start", B + 1, where), _i32(seq_len, "seq_len", B, where), B
+
+
+def _bf16_rows(t, name, T, width, where):
+    if _known_dtype(t) != BF16:
+        raise ValueError(f"{where}: {name} must be bfloat16")
+    return _rows(t, name, T, width, where)
+
+
+def catq_kv_append(cache: KVCache, row_start, seq_len, K, V, rope: Rope = None, Q=None, Q_out=None, n_heads: int = 0,
+                   stream=None):
+    """Appends the rows of K, V [T, n_kv_heads * d] (bf16) to the cache, keys rotated (rope None: not); with Q [T,
+    n_heads * d] the rotated queries go to Q_out (Q itself when None).  row_start [B + 1], seq_len [B] int32: the rows of
+    each sequence and its length with them."""
+    w = "catq_kv_append"
+    c, rs, sl, B = _kv_meta(cache, row_start, seq_len, w)
+    T = K.shape[0]
+    k, ldk = _bf16_rows(K, "K", T, c.n_kv_heads * c.d, w)
+    v, ldv = _bf16_rows(V, "V", T, c.n_kv_heads * c.d, w)
+    q = qo = None
+    ldq = ldqo = 0
+    if Q is not None:
+        q, ldq = _bf16_rows(Q, "Q", T, n_heads * c.d, w)
+        qo, ldqo = (q, ldq) if Q_out is None else _bf16_rows(Q_out, "Q_out", T, n_heads * c.d, w)
+    _check(lib().catq_kv_append(c, rs, sl, B, k, ldk, v, ldv, T, q, ldq, qo, ldqo, n_heads,
+                                None if rope is None else rope.struct(), _stream(stream)), w)
+
+
+def catq_kv_attention_workspace_bytes(n_heads: int, n_kv_heads: int, d: int) -> int:
+    return int(lib().catq_kv_attention_workspace_bytes(int(n_heads), int(n_kv_heads), int(d)))
+
+
+def kv_attention_workspace(cache: KVCache, n_heads: int):
+    """A zeroed workspace for catq_kv_attention over this cache."""
+    import torch
+    _, nkv, _, d = cache.k_codes.shape
+    return torch.zeros(catq_kv_attention_workspace_bytes(n_heads, nkv, d), dtype=torch.uint8,
+                       device=cache.k_codes.device)
+
+
+def catq_kv_attention(cache: KVCache, row_start, seq_len, Q, O, n_heads: int, workspace, lse=None, stream=None):
+    """O [T, n_heads * d] = attention of the rows of Q over the cached tokens up to each row's position; lse [T,
+    n_heads] fp32 (optional).  workspace: kv_attention_workspace, one for every call that may run at the same time."""
+    w = "catq_kv_attention"
+    c, rs, sl, B = _kv_meta(cache, row_start, seq_len, w)
+    T = Q.shape[0]
+    q, ldq = _bf16_rows(Q, "Q", T, n_heads * c.d, w)
+    o, ldo = _bf16_rows(O, "O", T, n_heads * c.d, w)
+    ws, ws_bytes = _ws(workspace, w)
+    _check(lib().catq_kv_attention(c, rs, sl, B, q, ldq, T, n_heads, o, ldo, _f32(lse, "lse", 4 * T * n_heads, w), ws,
+                                   ws_bytes, _stream(stream)), w)

@@ -166,6 +166,7 @@ const char* catq_status_string(int32_t s) {
     case CATQ_ERR_NONFINITE: return "CATQ_ERR_NONFINITE";
     case CATQ_ERR_UNSUPPORTED: return "CATQ_ERR_UNSUPPORTED";
     case CATQ_ERR_WORKSPACE: return "CATQ_ERR_WORKSPACE";
+    case CATQ_ERR_INDEX: return "CATQ_ERR_INDEX";
     default: return "CATQ_ERR_UNKNOWN";
   }
 }
@@ -954,6 +955,190 @@ catq_status catq_attention_bwd(const void* Q, const void* K, const void* V, cons
   io.lse = const_cast<float*>(lse);
   io.delta = delta;
   return cuda_status(launch_attention(io, B, S, n_heads, n_kv_heads, d, true, as_stream(stream)));
+}
+
+// ------------------------------------------------------------------ decoding over a paged 8-bit cache
+
+namespace {
+
+// A rotation of heads of d elements as the kernels see it.
+catq_status check_rotation(const catq_rotation* r, int32_t d, RotDev* out) {
+  if (!r || !r->turns) return CATQ_ERR_INVALID_ARG;
+  if (r->rot < 2 || r->rot % 2 != 0 || r->rot > d) return CATQ_ERR_SHAPE;
+  if ((r->layout != CATQ_ROPE_HALF && r->layout != CATQ_ROPE_INTERLEAVED) || r->reserved != 0 ||
+      !std::isfinite(r->magnitude))
+    return CATQ_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(r->turns) & 7u) return CATQ_ERR_ALIGN;
+  *out = RotDev{r->turns, r->rot, r->layout, r->magnitude};
+  return CATQ_OK;
+}
+
+bool rows_ok(const void* p, int64_t ld) { return aligned16(p) && ld % 8 == 0; }
+
+catq_status check_kv(const catq_kv_cache* c, const int32_t* row_start, const int32_t* seq_len, int32_t B, int64_t T) {
+  if (!c) return CATQ_ERR_INVALID_ARG;
+  if (B < 0 || B > 65535 || T < 0 || T > 0x7fffffff) return CATQ_ERR_SHAPE;
+  if ((c->d != 64 && c->d != 128) || (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) ||
+      c->n_kv_heads < 1 || c->n_kv_heads > 4096 || c->n_pages < 1 || c->max_pages < 1 ||
+      static_cast<int64_t>(c->n_pages) * c->n_kv_heads * c->page > 0x7fffffff ||
+      static_cast<int64_t>(c->max_pages) * c->page > 0x7fffffff)
+    return CATQ_ERR_SHAPE;
+  if (c->reserved != 0) return CATQ_ERR_INVALID_ARG;
+  if (T == 0 || B == 0) return CATQ_OK;
+  if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !c->table || !row_start || !seq_len)
+    return CATQ_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(c->k_codes) & 127u) || (reinterpret_cast<uintptr_t>(c->v_codes) & 127u) ||
+      !aligned4(c->k_scale) || !aligned4(c->v_scale) || !aligned4(c->table) || !aligned4(row_start) || !aligned4(seq_len))
+    return CATQ_ERR_ALIGN;
+  return CATQ_OK;
+}
+
+KvCacheDev kv_dev(const catq_kv_cache* c) {
+  KvCacheDev d;
+  d.k_codes = static_cast<uint8_t*>(c->k_codes);
+  d.v_codes = static_cast<uint8_t*>(c->v_codes);
+  d.k_scale = c->k_scale;
+  d.v_scale = c->v_scale;
+  d.table = c->table;
+  d.n_pages = c->n_pages;
+  d.nkv = c->n_kv_heads;
+  d.page = c->page;
+  d.d = c->d;
+  d.max_pages = c->max_pages;
+  return d;
+}
+
+// Frequencies of a scaled rotation, in radians a token (the formulas of catq_rope_scaling).
+double scaled_frequency(int32_t i, int32_t rot, double base, int32_t scaling, double factor, double low, double high,
+                        double original) {
+  constexpr double kTwoPi = 6.283185307179586476925;
+  const double f = std::pow(base, -2.0 * i / rot);
+  if (scaling == CATQ_ROPE_LINEAR) return f / factor;
+  if (scaling == CATQ_ROPE_BANDS) {
+    const double w = std::min(1.0, std::max(0.0, (original * f / kTwoPi - low) / (high - low)));
+    return (1.0 - w) * f / factor + w * f;
+  }
+  if (scaling == CATQ_ROPE_YARN) {
+    auto index_of = [&](double t) { return rot * std::log(original / (t * kTwoPi)) / (2.0 * std::log(base)); };
+    const double a = std::max(std::floor(index_of(high)), 0.0), b = std::min(std::ceil(index_of(low)), rot - 1.0);
+    const double w = std::min(1.0, std::max(0.0, (i - a) / std::max(b - a, 0.001)));
+    return w * f / factor + (1.0 - w) * f;
+  }
+  return f;
+}
+
+}  // namespace
+
+catq_status catq_rotation_turns(int32_t rot, double base, int32_t scaling, double factor, double low, double high,
+                                double original, uint64_t* turns, float* magnitude) {
+  if (rot < 2 || rot % 2 != 0 || rot > 65536) return CATQ_ERR_SHAPE;
+  if (!(base > 1.0) || !std::isfinite(base) || scaling < CATQ_ROPE_PLAIN || scaling > CATQ_ROPE_YARN || !turns ||
+      !magnitude)
+    return CATQ_ERR_INVALID_ARG;
+  if (scaling != CATQ_ROPE_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor))) return CATQ_ERR_INVALID_ARG;
+  if ((scaling == CATQ_ROPE_BANDS || scaling == CATQ_ROPE_YARN) &&
+      (!(low > 0.0) || !(high > low) || !std::isfinite(high) || !(original >= 1.0) || !std::isfinite(original)))
+    return CATQ_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < rot / 2; ++i) {
+    const double t = scaled_frequency(i, rot, base, scaling, factor, low, high, original) / 6.283185307179586476925;
+    turns[i] = static_cast<uint64_t>(std::nearbyint(std::ldexp(t, 62))) * 4u;  // t <= 1 / (2 pi): below 2^60
+  }
+  *magnitude = scaling == CATQ_ROPE_YARN ? static_cast<float>(0.1 * std::log(factor) + 1.0) : 1.0f;
+  return CATQ_OK;
+}
+
+catq_status catq_rope_at(const void* X, int64_t ldx, void* Y, int64_t ldy, int32_t dtype, const int32_t* positions,
+                         int64_t T, int32_t n_heads, int32_t d, const catq_rotation* rotation, int32_t inverse,
+                         catq_stream stream) {
+  if (dtype != CATQ_BF16 && dtype != CATQ_F32) return CATQ_ERR_DTYPE;
+  if (T < 0 || T > 0x7fffffff || n_heads < 1 || n_heads > 65536 || d < 2 || d > 65536 || d % 2 != 0)
+    return CATQ_ERR_SHAPE;
+  RotDev rot{};
+  const catq_status st = check_rotation(rotation, d, &rot);
+  if (st != CATQ_OK) return st;
+  const int64_t width = static_cast<int64_t>(n_heads) * d;
+  if (ldx < width || ldy < width) return CATQ_ERR_SHAPE;
+  if (T == 0) return CATQ_OK;
+  if (!X || !Y || !positions || (X == Y && ldx != ldy)) return CATQ_ERR_INVALID_ARG;
+  const uintptr_t mask = dtype == CATQ_F32 ? 3u : 1u;
+  if ((reinterpret_cast<uintptr_t>(X) & mask) || (reinterpret_cast<uintptr_t>(Y) & mask) || !aligned4(positions))
+    return CATQ_ERR_ALIGN;
+  return cuda_status(launch_rope_at(X, ldx, Y, ldy, dtype == CATQ_F32, positions, T, n_heads, d, rot, inverse != 0,
+                                    as_stream(stream)));
+}
+
+catq_status catq_kv_append(const catq_kv_cache* cache, const int32_t* row_start, const int32_t* seq_len, int32_t B,
+                           const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t T, const void* Q, int64_t ldq,
+                           void* Q_out, int64_t ldq_out, int32_t n_heads, const catq_rotation* rotation,
+                           catq_stream stream) {
+  catq_status st = check_kv(cache, row_start, seq_len, B, T);
+  if (st != CATQ_OK) return st;
+  KvAppendArgs a{};
+  if (rotation) {
+    if ((st = check_rotation(rotation, cache->d, &a.rot)) != CATQ_OK) return st;
+    if (a.rot.rot % 16 != 0) return CATQ_ERR_SHAPE;
+  }
+  const int64_t width = static_cast<int64_t>(cache->n_kv_heads) * cache->d;
+  if (ldk < width || ldv < width) return CATQ_ERR_SHAPE;
+  if (Q && (n_heads < 1 || n_heads > 65536 || ldq < static_cast<int64_t>(n_heads) * cache->d ||
+            ldq_out < static_cast<int64_t>(n_heads) * cache->d))
+    return CATQ_ERR_SHAPE;
+  if (T == 0 || B == 0) return CATQ_OK;
+  if (!K || !V || (Q && !Q_out) || (Q && Q == Q_out && ldq != ldq_out)) return CATQ_ERR_INVALID_ARG;
+  if (!rows_ok(K, ldk) || !rows_ok(V, ldv) || (Q && (!rows_ok(Q, ldq) || !rows_ok(Q_out, ldq_out))))
+    return CATQ_ERR_ALIGN;
+  a.cache = kv_dev(cache);
+  a.row_start = row_start;
+  a.seq_len = seq_len;
+  a.B = B;
+  a.T = T;
+  a.k = static_cast<const uint16_t*>(K);
+  a.v = static_cast<const uint16_t*>(V);
+  a.ldk = ldk;
+  a.ldv = ldv;
+  a.q = static_cast<const uint16_t*>(Q);
+  a.q_out = static_cast<uint16_t*>(Q_out);
+  a.ldq = ldq;
+  a.ldqo = ldq_out;
+  a.nh = n_heads;
+  return cuda_status(launch_kv_append(a, as_stream(stream)));
+}
+
+size_t catq_kv_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, int32_t d) {
+  if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || (d != 64 && d != 128)) return 0;
+  return kv_attention_ws_bytes(n_heads, n_kv_heads, d);
+}
+
+catq_status catq_kv_attention(const catq_kv_cache* cache, const int32_t* row_start, const int32_t* seq_len, int32_t B,
+                              const void* Q, int64_t ldq, int64_t T, int32_t n_heads, void* O, int64_t ldo, float* lse,
+                              void* workspace, size_t ws_bytes, catq_stream stream) {
+  catq_status st = check_kv(cache, row_start, seq_len, B, T);
+  if (st != CATQ_OK) return st;
+  const int32_t nkv = cache->n_kv_heads, d = cache->d;
+  if (n_heads < 1 || n_heads > 65536 || n_heads % nkv != 0 || n_heads / nkv > 64 ||
+      ldq < static_cast<int64_t>(n_heads) * d || ldo < static_cast<int64_t>(n_heads) * d)
+    return CATQ_ERR_SHAPE;
+  if (T == 0 || B == 0) return CATQ_OK;
+  if (!Q || !O || (Q == O && ldq != ldo)) return CATQ_ERR_INVALID_ARG;
+  if (!rows_ok(Q, ldq) || !rows_ok(O, ldo) || (lse && !aligned4(lse))) return CATQ_ERR_ALIGN;
+  if (!workspace || ws_bytes < kv_attention_ws_bytes(n_heads, nkv, d)) return CATQ_ERR_WORKSPACE;
+  if (!aligned256(workspace)) return CATQ_ERR_ALIGN;
+  if ((st = check_tensor_core_device()) != CATQ_OK) return st;
+  KvAttnArgs a{};
+  a.cache = kv_dev(cache);
+  a.row_start = row_start;
+  a.seq_len = seq_len;
+  a.B = B;
+  a.T = T;
+  a.q = static_cast<const uint16_t*>(Q);
+  a.o = static_cast<uint16_t*>(O);
+  a.ldq = ldq;
+  a.ldo = ldo;
+  a.nh = n_heads;
+  a.scale_log2 = 1.4426950408889634f / std::sqrt(static_cast<float>(d));
+  a.lse = lse;
+  a.workspace = workspace;
+  return cuda_status(launch_kv_attention(a, as_stream(stream)));
 }
 
 }  // extern "C"

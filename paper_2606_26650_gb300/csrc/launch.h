@@ -7,6 +7,7 @@
 #include <cstdint>
 
 #include "catq_math.cuh"
+#include "rope.cuh"
 
 namespace catq {
 
@@ -201,6 +202,51 @@ cudaError_t launch_attention_fwd_tc(const void* q, const void* k, const void* v,
 cudaError_t launch_attention_bwd_tc(const void* q, const void* k, const void* v, const void* dO, const float* lse,
                                     const float* delta, void* dq, void* dk, void* dv, int32_t B, int32_t S, int32_t nh,
                                     int32_t nkv, int32_t d, cudaStream_t st);
+// kv_cache.cu
+// Rows of nh heads of d, ldx and ldy elements apart; x == y in place (then ldx == ldy).
+cudaError_t launch_rope_at(const void* x, int64_t ldx, void* y, int64_t ldy, bool f32, const int32_t* pos, int64_t T,
+                           int32_t nh, int32_t d, const RotDev& rot, bool inverse, cudaStream_t st);
+// Device view of catq_kv_cache.
+struct KvCacheDev {
+  uint8_t *k_codes, *v_codes;  // [n_pages, nkv, page, d] e4m3
+  float *k_scale, *v_scale;    // [n_pages, nkv]
+  const int32_t* table;        // [B, max_pages]
+  int32_t n_pages, nkv, page, d, max_pages;
+};
+struct KvAppendArgs {
+  KvCacheDev cache;
+  const int32_t *row_start, *seq_len;
+  int32_t B;
+  int64_t T;
+  const uint16_t *k, *v;
+  int64_t ldk, ldv;
+  const uint16_t* q;  // nullable: no queries
+  uint16_t* q_out;
+  int64_t ldq, ldqo;
+  int32_t nh;
+  RotDev rot;  // rot.rot == 0: no rotation
+  int32_t* status;  // set by the launcher
+};
+cudaError_t launch_kv_append(KvAppendArgs a, cudaStream_t st);
+
+// kv_attn_tc.cu
+struct KvAttnArgs {
+  KvCacheDev cache;
+  const int32_t *row_start, *seq_len;
+  int32_t B;
+  int64_t T;
+  const uint16_t* q;
+  uint16_t* o;
+  int64_t ldq, ldo;
+  int32_t nh;
+  float scale_log2;  // log2(e) / sqrt(d)
+  float* lse;        // [T, nh], nullable
+  void* workspace;
+  int32_t* status;   // set by the launcher
+};
+size_t kv_attention_ws_bytes(int32_t nh, int32_t nkv, int32_t d);
+cudaError_t launch_kv_attention(KvAttnArgs a, cudaStream_t st);
+
 // Status word latched by device-side bounded waits (0 = none); read-and-clear.
 cudaError_t read_and_clear_device_status(int32_t* out);
 bool tensor_map_encoder_available();
