@@ -695,7 +695,7 @@ size_t catq_kv_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, in
  * catq_kv_append (the sequence's rows are left as they were); a page outside 0 .. n_pages - 1 counts as zeros, latched.
  * workspace: >= catq_kv_attention_workspace_bytes(), 256-byte aligned, zero before the first call; a call leaves the
  * part that has to be zero as zero.  Calls that may run at the same time need workspaces of their own.
- * n_heads % n_kv_heads == 0, n_heads / n_kv_heads <= 64; limits as for catq_kv_append. */
+ * n_heads % n_kv_heads == 0, n_heads / n_kv_heads <= 64, T n_heads / n_kv_heads <= 2^26; other limits as for catq_kv_append. */
 catq_status catq_kv_attention(const catq_kv_cache* cache, const int32_t* row_start, const int32_t* seq_len, int32_t B,
                               const void* Q, int64_t ldq, int64_t T, int32_t n_heads, void* O, int64_t ldo, float* lse,
                               void* workspace, size_t ws_bytes, catq_stream stream);

@@ -1116,7 +1116,7 @@ catq_status catq_kv_attention(const catq_kv_cache* cache, const int32_t* row_sta
   if (st != CATQ_OK) return st;
   const int32_t nkv = cache->n_kv_heads, d = cache->d;
   if (n_heads < 1 || n_heads > 65536 || n_heads % nkv != 0 || n_heads / nkv > 64 ||
-      T * (n_heads / nkv) > 0x7fffff00 || ldq < static_cast<int64_t>(n_heads) * d ||
+      T * (n_heads / nkv) > (1 << 26) || ldq < static_cast<int64_t>(n_heads) * d ||
       ldo < static_cast<int64_t>(n_heads) * d)
     return CATQ_ERR_SHAPE;
   if (T == 0 || B == 0) return CATQ_OK;

@@ -41,28 +41,30 @@ namespace catq {
 namespace {
 
 constexpr int kTok = 128;                    // cached tokens per tile (MMA M of S^T, contraction of O^T)
-constexpr int kSoft = 128;                   // softmax threads
-constexpr int kTmaWarp = 4, kMmaWarp = 5;
-constexpr int kThreads = 6 * 32;
-constexpr float kNominal = 5.0f;             // log2 of a weight at the maximum taken
+constexpr int kGroup = 128;                  // threads of a softmax group
+constexpr float kNominal = 3.0f;             // log2 of a weight at the maximum taken
 constexpr float kOver = 8.75f;               // raise the maximum past this (2^8.75 < 448)
 constexpr float kNoMax = -3e38f;             // maximum of a row that has seen nothing
 constexpr float kLoUnit = 0.0625f;           // a lo term's unit
+constexpr int kScaleRing = 16;               // tiles whose scales are kept (see the TMA warp)
 
 template <int HD, int R>
 struct KvLay {
   static constexpr int kCols = 2 * R;                                // N of both products
-  static constexpr int kChunk = R < 16 ? R : 16;                     // rows handled at a time
-  static constexpr int kCtas = R <= 32 ? 2 : 1;                      // CTAs an SM
+  static constexpr int kChunk = R < 16 ? R : 16;                     // rows of a softmax group
+  static constexpr int kGroups = R / kChunk;
+  static constexpr int kSoft = kGroups * kGroup;
+  static constexpr int kTmaWarp = 4 * kGroups, kMmaWarp = kTmaWarp + 1, kThreads = kSoft + 64;
+  static constexpr int kCtas = R == 8 ? 3 : R <= 32 ? 2 : 1;         // CTAs an SM
   static constexpr uint32_t kTile = kTok * HD;                       // a tile of codes
   static constexpr uint32_t kQ = kCols * HD, kP = kTok * kCols;
-  static constexpr uint32_t kRowBytes = R * 4;
-  // barriers, tensor-memory address, start of the run | per row: query factor, maximum, last position, sums by warp |
-  // Q, P twice, ring
-  static constexpr uint32_t kOffF = 512, kOffM = kOffF + kRowBytes, kOffLim = kOffM + kRowBytes,
-                            kOffRed = kOffLim + kRowBytes, kOffQ = (kOffRed + 4 * kRowBytes + 127) / 128 * 128,
-                            kOffP = kOffQ + kQ, kOffRing = (kOffP + 2 * kP + 1023) / 1024 * 1024;
-  static constexpr uint32_t kBudget = kCtas == 2 ? 112 * 1024 : 224 * 1024;
+  // barriers, tensor-memory address, start of the run | scales of the tiles in flight | per row: query factor, maximum,
+  // its last raise, last position, output offset (8 bytes), sums by warp | Q, P twice, ring
+  static constexpr uint32_t kOffScale = 640, kOffF = kOffScale + kScaleRing * 64, kOffM = kOffF + 4 * R,
+                            kOffFac = kOffM + 4 * R, kOffLim = kOffFac + 4 * R, kOffRow = kOffLim + 4 * R,
+                            kOffRed = kOffRow + 8 * R, kOffQ = (kOffRed + 16 * R + 127) / 128 * 128, kOffP = kOffQ + kQ,
+                            kOffRing = (kOffP + 2 * kP + 1023) / 1024 * 1024;
+  static constexpr uint32_t kBudget = (kCtas == 3 ? 75 : kCtas == 2 ? 112 : 224) * 1024;
   static constexpr int kSlots0 = (kBudget - 1024 - kOffRing) / kTile;
   static constexpr int kSlots = kSlots0 > 12 ? 12 : kSlots0;
   static constexpr uint32_t kSmem = kOffRing + kSlots * kTile + 1024;
@@ -80,18 +82,21 @@ struct KvSeq {
 struct KvGeom {
   const int32_t *row_start, *seq_len;
   int32_t B, group, nkv;
+  uint32_t group_inv;  // ceil(2^32 / group): rows below 2^26 are divided by one product
   int64_t T, max_len;
+  __device__ __forceinline__ int32_t token_of(int32_t row) const {
+    return group == 1 ? row : static_cast<int32_t>(__umulhi(static_cast<uint32_t>(row), group_inv));
+  }
 };
 
 // Tokens that the row tile `q` of a sequence can see.
 template <int R>
 __device__ __forceinline__ int32_t visible(const KvGeom& g, const KvSeq& s, int32_t q) {
-  const int64_t last = min(static_cast<int64_t>(q + 1) * R, static_cast<int64_t>(s.n) * g.group) - 1;
-  return max(s.len - s.n + static_cast<int32_t>(last / g.group) + 1, 0);
+  return max(s.len - s.n + g.token_of(min((q + 1) * R, s.n * g.group) - 1) + 1, 0);
 }
 template <int R>
 __device__ __forceinline__ int32_t row_tiles(const KvGeom& g, const KvSeq& s) {
-  return static_cast<int32_t>((static_cast<int64_t>(s.n) * g.group + R - 1) / R);
+  return (s.n * g.group + R - 1) / R;
 }
 // A row tile that sees nothing still has a tile: its rows are written.
 __device__ __forceinline__ int32_t tiles_of(int32_t vis) { return max((vis + kTok - 1) / kTok, 1); }
@@ -124,9 +129,10 @@ struct KvWalk {
   int32_t n;             // its tiles
   int32_t t0;            // first of them
   int32_t all, vis;      // the row tile's tiles and visible tokens
-  int64_t begin;         // line position of the row tile's first tile
   int32_t sb, sh, sq;    // its sequence, head, row tile
-  KvSeq ss;
+  int32_t r0, rows_n, len;  // its sequence's first row, rows, cached tokens
+  // line position of the row tile's first tile
+  __device__ __forceinline__ int64_t begin() const { return at - n - t0; }
   __device__ __forceinline__ bool next(const KvGeom& g) {
     if (at >= end) return false;
     if (s.per_head == 0 || h == g.nkv) {
@@ -136,12 +142,11 @@ struct KvWalk {
       } while (s.per_head == 0);
       h = q = t = 0;
     }
-    sb = b; sh = h; sq = q; ss = s;
+    sb = b; sh = h; sq = q; r0 = s.r0; rows_n = s.n; len = s.len;
     vis = visible<R>(g, s, q);
     all = tiles_of(vis);
     t0 = t;
     n = static_cast<int32_t>(min(static_cast<int64_t>(all - t), end - at));
-    begin = at - t;
     at += n;
     t = 0;
     if (++q == row_tiles<R>(g, s)) {
@@ -208,50 +213,63 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// The hi and lo columns of chunk c (rows c kChunk ..) at `base`: 16 columns of both for 8 rows, else 16 and 16.
-template <int R>
-__device__ __forceinline__ void load_chunk(uint32_t base, int c, uint32_t (&v)[R < 16 ? 16 : 32]) {
-  if constexpr (R < 16) {
+// A group's hi and lo columns (its CH rows, lo R columns behind hi) at `base`.
+template <int R, int CH>
+__device__ __forceinline__ void load_cols(uint32_t base, uint32_t (&v)[2 * CH]) {
+  if constexpr (CH < 16) {
     tmem_ld16(base, v);
   } else {
     uint32_t(&hi)[16] = *reinterpret_cast<uint32_t(*)[16]>(&v[0]);
     uint32_t(&lo)[16] = *reinterpret_cast<uint32_t(*)[16]>(&v[16]);
-    tmem_ld16(base + 16u * c, hi);
-    tmem_ld16(base + R + 16u * c, lo);
+    tmem_ld16(base, hi);
+    tmem_ld16(base + R, lo);
   }
   tmem_ld_wait();
 }
-template <int R>
-__device__ __forceinline__ void store_chunk(uint32_t base, int c, const uint32_t (&v)[R < 16 ? 16 : 32]) {
-  if constexpr (R < 16) {
+template <int R, int CH>
+__device__ __forceinline__ void store_cols(uint32_t base, const uint32_t (&v)[2 * CH]) {
+  if constexpr (CH < 16) {
     tmem_st16(base, v);
   } else {
-    tmem_st16(base + 16u * c, *reinterpret_cast<const uint32_t(*)[16]>(&v[0]));
-    tmem_st16(base + R + 16u * c, *reinterpret_cast<const uint32_t(*)[16]>(&v[16]));
+    tmem_st16(base, *reinterpret_cast<const uint32_t(*)[16]>(&v[0]));
+    tmem_st16(base + R, *reinterpret_cast<const uint32_t(*)[16]>(&v[16]));
   }
 }
 
-__device__ __forceinline__ void soft_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void bar_sync(int id, int threads) {
+  asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
 
-// Sums over a warp of v[0 .. R): afterwards lane l holds those of rows l R / 32 .. in v[0 .. R / 32), or, where R < 32,
-// that of row l / (32 / R) in v[0].
-template <int R>
-__device__ __forceinline__ void warp_row_sums(float (&v)[R], int lane) {
-  int n = R;
+// Sums (or maxima) over a warp of v[0 .. CH), CH <= 32: afterwards v[0] of lane l holds that of row l / (32 / CH).
+template <int CH, bool MAX>
+__device__ __forceinline__ void warp_rows(float (&v)[CH], int lane) {
+  int n = CH;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     if (n > 1) {
       n /= 2;
       const bool up = (lane & o) != 0;
 #pragma unroll
-      for (int i = 0; i < R / 2; ++i)
+      for (int i = 0; i < CH / 2; ++i)
         if (i < n) {
           const float send = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
-          v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+          const float got = __shfl_xor_sync(0xffffffffu, send, o);
+          v[i] = MAX ? fmaxf(keep, got) : keep + got;
         }
     } else {
-      v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+      const float got = __shfl_xor_sync(0xffffffffu, v[0], o);
+      v[0] = MAX ? fmaxf(v[0], got) : v[0] + got;
     }
+  }
+}
+
+// n floats of shared memory (16-byte aligned).
+template <int N>
+__device__ __forceinline__ void load_row(const float* p, float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    const float4 q = reinterpret_cast<const float4*>(p)[i];
+    v[4 * i] = q.x; v[4 * i + 1] = q.y; v[4 * i + 2] = q.z; v[4 * i + 3] = q.w;
   }
 }
 
@@ -271,26 +289,30 @@ struct KvTcArgs {
 };
 
 template <int HD, int R>
-__global__ void __launch_bounds__(kThreads, KvLay<HD, R>::kCtas)
+__global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
     kv_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const KvTcArgs p) {
   using Y = KvLay<HD, R>;
-  constexpr int NC = Y::kCols, CH = Y::kChunk, NS = Y::kSlots;
+  constexpr int NC = Y::kCols, CH = Y::kChunk, NS = Y::kSlots, kThreads = Y::kThreads, kSoft = Y::kSoft;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* const gbase = smem_raw + (base - raw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t full0 = base, empty0 = base + 8u * NS, s_full0 = base + 16u * NS, p_full0 = s_full0 + 16,
-                 pv_done0 = p_full0 + 16, q_full = pv_done0 + 16, final_bar = q_full + 8;
-  static_assert(16 * NS + 3 * 16 + 2 * 8 <= 272, "barriers");
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(gbase + 272);
-  int32_t* const merge_flag = reinterpret_cast<int32_t*>(gbase + 276);
-  int64_t* const scan = reinterpret_cast<int64_t*>(gbase + 280);             // warps' sums [6]
-  int32_t* const start = reinterpret_cast<int32_t*>(gbase + 336);           // b, h, q, t of the run's first tile
+                 pv_done0 = p_full0 + 16, q_full = pv_done0 + 16, final_bar = q_full + 8, scale_full0 = final_bar + 8;
+  static_assert(16 * NS + 3 * 16 + 2 * 8 + 8 * kScaleRing <= 400, "barriers");
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(gbase + 400);
+  int32_t* const merge_flag = reinterpret_cast<int32_t*>(gbase + 404);
+  int32_t* const start = reinterpret_cast<int32_t*>(gbase + 408);           // b, h, q, t of the run's first tile
+  int64_t* const scan = reinterpret_cast<int64_t*>(gbase + 424);            // warps' sums
+  static_assert(424 + 8 * (kThreads / 32) <= Y::kOffScale, "start");
+  float* const scales = reinterpret_cast<float*>(gbase + Y::kOffScale);     // [kScaleRing][8 key, 8 value scales]
   float* const row_f = reinterpret_cast<float*>(gbase + Y::kOffF);
   float* const row_m = reinterpret_cast<float*>(gbase + Y::kOffM);
+  float* const row_fac = reinterpret_cast<float*>(gbase + Y::kOffFac);
   int32_t* const row_lim = reinterpret_cast<int32_t*>(gbase + Y::kOffLim);
-  float* const red = reinterpret_cast<float*>(gbase + Y::kOffRed);           // [4][R]
+  int64_t* const row_at = reinterpret_cast<int64_t*>(gbase + Y::kOffRow);
+  float* const red = reinterpret_cast<float*>(gbase + Y::kOffRed);          // [groups][4][CH]
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < NS; ++i) {
@@ -299,14 +321,15 @@ __global__ void __launch_bounds__(kThreads, KvLay<HD, R>::kCtas)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full0 + 8u * i, 1);
-      mbar_init(p_full0 + 8u * i, 4);
+      mbar_init(p_full0 + 8u * i, kSoft / 32);
       mbar_init(pv_done0 + 8u * i, 1);
     }
-    mbar_init(q_full, 4);
+    for (int i = 0; i < kScaleRing; ++i) mbar_init(scale_full0 + 8u * i, 1);
+    mbar_init(q_full, kSoft / 32);
     mbar_init(final_bar, 1);
     fence_mbar_init_cluster();
   }
-  if (warp == kMmaWarp) tmem_alloc<1>(smem_u32(tmem_slot), Y::kTmem);
+  if (warp == Y::kMmaWarp) tmem_alloc<1>(smem_u32(tmem_slot), Y::kTmem);
 
   // The run of this CTA: every CTA adds up all sequences' tiles, a thread a stretch of them.
   const KvGeom& g = p.g;
@@ -369,41 +392,80 @@ __global__ void __launch_bounds__(kThreads, KvLay<HD, R>::kCtas)
   const int32_t ppt = kTok / kv.page;  // pages a tile
   bool ok = true;
 
-  if (warp == kTmaWarp) {
+  if (warp == Y::kTmaWarp) {
     if (lane == 0) {
       prefetch_tmap(&tmk);
       prefetch_tmap(&tmv);
     }
     int slot = 0, loads = 0;
-    uint32_t ph = 1;
-    // tile j of the segment into the next slot, a lane a page
-    auto load = [&](const CUtensorMap* map, int32_t j) -> bool {
-      const int32_t tok = (w.t0 + j) * kTok;
-      const int32_t pages = min(max((w.vis - tok + kv.page - 1) / kv.page, 0), ppt);
-      int32_t row = 0;
-      if (lane < pages) {
-        const int32_t id = __ldg(kv.table + static_cast<int64_t>(w.sb) * kv.max_pages + tok / kv.page + lane);
-        const bool in = id >= 0 && id < kv.n_pages;
-        if (!in) atomicCAS(p.a.status, 0, 10 /* CATQ_ERR_INDEX */);
-        row = in ? (id * kv.nkv + w.sh) * kv.page : kv.n_pages * kv.nkv * kv.page;  // (behind the last row: zeros)
+    uint32_t ph = 1, gt = 0;
+    // A lane a page: the lane's page in tile t of the segment (first row of its block, -1: none), its scales.
+    struct Page {
+      int32_t row;
+      float ks, vs;
+    };
+    auto page_of = [&](int32_t j) -> int32_t {
+      const int32_t tok = (w.t0 + j) * kTok + lane * kv.page;
+      if (j >= w.n || lane >= ppt || tok >= w.vis) return -1;
+      return __ldg(kv.table + static_cast<int64_t>(w.sb) * kv.max_pages + tok / kv.page);
+    };
+    auto block_of = [&](int32_t j, int32_t id) {
+      Page g{-1, 0.0f, 0.0f};
+      if (j >= w.n || lane >= ppt || (w.t0 + j) * kTok + lane * kv.page >= w.vis) return g;
+      if (id < 0 || id >= kv.n_pages) {
+        atomicCAS(p.a.status, 0, 10 /* CATQ_ERR_INDEX */);
+        g.row = kv.n_pages * kv.nkv * kv.page;  // behind the last row: zeros
+        return g;
       }
+      const int32_t block = id * kv.nkv + w.sh;
+      g.row = block * kv.page;
+      g.ks = __ldg(kv.k_scale + block);
+      g.vs = __ldg(kv.v_scale + block);
+      return g;
+    };
+    // A tile into the next slot; with its keys go its scales, into a ring of kScaleRing tiles of their own.  That is
+    // deep enough without an empty barrier: while a tile's scales are read its values hold their slot, and the NS slots
+    // from there on hold the keys of at most NS / 2 + 3 further tiles.
+    static_assert(NS / 2 + 4 <= kScaleRing, "ring of scales");
+    auto load = [&](const CUtensorMap* map, const Page& g, bool keys) -> bool {
+      const uint32_t pages = __popc(__ballot_sync(0xffffffffu, g.row >= 0));
       if (!mbar_wait_warp(empty0 + 8u * slot, ph, p.wc)) return false;
-      if (lane == 0) mbar_arrive_expect_tx(full0 + 8u * slot, static_cast<uint32_t>(pages * kv.page * HD));
+      if (keys && lane < 8) {
+        float* const to = scales + (gt % kScaleRing) * 16;
+        to[lane] = g.ks;
+        to[8 + lane] = g.vs;
+      }
       __syncwarp();
-      if (lane < pages)
-        tma_load_2d(base + Y::kOffRing + slot * Y::kTile + lane * kv.page * HD, map, full0 + 8u * slot, 0, row);
+      if (lane == 0) {
+        if (keys) mbar_arrive_local(scale_full0 + 8u * (gt % kScaleRing));
+        mbar_arrive_expect_tx(full0 + 8u * slot, pages * kv.page * HD);
+      }
+      __syncwarp();
+      if (g.row >= 0)
+        tma_load_2d(base + Y::kOffRing + slot * Y::kTile + lane * kv.page * HD, map, full0 + 8u * slot, 0, g.row);
       ++loads;
+      gt += keys;
       if (++slot == NS) { slot = 0; ph ^= 1u; }
       return true;
     };
     while (ok && w.next(g)) {
-      // in the order in which the products take them
-      ok = load(&tmk, 0) && (w.n < 2 || load(&tmk, 1));
-      for (int32_t j = 0; ok && j < w.n; ++j) ok = load(&tmv, j) && (j + 2 >= w.n || load(&tmk, j + 2));
+      // In the order in which the products take them: K0 K1 V0 K2 V1 ...; a tile's page number is asked for two tiles
+      // ahead and its scales one, so that only a segment's first wait for memory.
+      const int32_t id0 = page_of(0), id1 = page_of(1);
+      int32_t id = page_of(2);
+      Page g0 = block_of(0, id0), g1 = block_of(1, id1), g2{-1, 0.0f, 0.0f};
+      ok = load(&tmk, g0, true) && (w.n < 2 || load(&tmk, g1, true));
+      for (int32_t j = 0; ok && j < w.n; ++j) {
+        g2 = block_of(j + 2, id);
+        id = page_of(j + 3);
+        ok = load(&tmv, g0, false) && (j + 2 >= w.n || load(&tmk, g2, true));
+        g0 = g1;
+        g1 = g2;
+      }
     }
     // copies still in flight land before the CTA exits
     for (int t = max(0, loads - NS); t < loads; ++t) drain(full0 + 8u * (t % NS), (t / NS) & 1);
-  } else if (warp == kMmaWarp) {
+  } else if (warp == Y::kMmaWarp) {
     constexpr uint32_t kSwizzle = HD == 128 ? 2 : 4;
     constexpr uint32_t idesc_s = idesc_e4m3(kTok, NC, false, false), idesc_o = idesc_e4m3(HD, NC, true, true);
     constexpr uint32_t kHi = desc_hi(8 * HD, kSwizzle);  // code tiles: 8 rows of HD bytes from one group to the next
@@ -458,249 +520,258 @@ __global__ void __launch_bounds__(kThreads, KvLay<HD, R>::kCtas)
     __syncwarp();
     drain(final_bar, 0);  // every MMA has completed before TMEM is released
   } else {
-    // softmax: token tid of every tile
-    const int tid = threadIdx.x;
-    const uint32_t lanes = tmem + (static_cast<uint32_t>(warp * 32) << 16);
+    // softmax: group wg has rows CH wg .. of the row tile, thread tid of it token tid of every tile
+    const int wg = warp >> 2, tid = threadIdx.x & (kGroup - 1), bar = 1 + wg, bar_every = 1 + Y::kGroups;
+    const int r0 = CH * wg;
+    const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + r0;
+    float* const my_red = red + wg * 4 * CH;
+    const int page_at = tid / kv.page;
     uint32_t gt = 0, ring = 0;  // tiles and loads before the segment's
-    // page of the thread's token in tile t of the segment's sequence, -1 behind what is visible
-    auto page_of = [&](int32_t t) -> int32_t {
-      const int32_t tok = t * kTok + tid;
-      if (t >= w.t0 + w.n || tok >= w.vis) return -1;
-      const int32_t id = __ldg(kv.table + static_cast<int64_t>(w.sb) * kv.max_pages + tok / kv.page);
-      return id < kv.n_pages ? id : -1;
-    };
-    auto scale_at = [&](const float* s, int32_t id) { return id < 0 ? 0.0f : __ldg(s + static_cast<int64_t>(id) * kv.nkv + w.sh); };
     // Products with the values up to tile t of the run have completed.  A barrier for every other tile: the scores of
     // tile t that the caller has seen followed the product of tile t - 2, so the barrier is at most one phase behind,
     // where a single one could be two behind and show the awaited parity.
     auto wait_pv = [&](uint32_t t) { return mbar_wait_warp(pv_done0 + 8u * (t & 1), (t >> 1) & 1, p.wc); };
     while (w.next(g)) {
-      if (!bar_all(1, kSoft, ok)) { ok = false; break; }  // the rows' arrays are free
-      const int32_t rows = min(R, w.ss.n * g.group - w.sq * R);
-      int32_t id1 = page_of(w.t0);
-      float ks1 = scale_at(kv.k_scale, id1), vs1 = scale_at(kv.v_scale, id1);
-      id1 = page_of(w.t0 + 1);
-      // queries: HD / 8 threads a row
-      for (int r = tid / (HD / 8); r < R; r += kSoft / (HD / 8)) {
-        const int i = tid % (HD / 8), row = w.sq * R + r;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (r < rows)
-          v = *reinterpret_cast<const uint4*>(p.a.q + (w.ss.r0 + row / g.group) * p.a.ldq +
-                                              (w.sh * g.group + row % g.group) * HD + 8 * i);
-        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-        float x[8];
-        uint32_t top = 0;
+      if (!bar_all(bar_every, kSoft, ok)) { ok = false; break; }  // the rows' arrays are free
+      const int32_t rows = min(R, w.rows_n * g.group - w.sq * R);
+      const bool active = r0 < rows;
+      // queries: HD / 8 threads a row, all loads first
+      constexpr int kPerRow = HD / 8, kPass = kGroup / kPerRow, kPasses = (CH + kPass - 1) / kPass;
+      if (active) {
+        uint4 raw[kPasses];
+        const int i = tid % kPerRow;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          x[2 * k] = __uint_as_float(u[k] << 16);
-          x[2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
-          top = max(top, max(u[k] << 16 & 0x7fffffffu, u[k] & 0x7fff0000u));
+        for (int k = 0; k < kPasses; ++k) {
+          const int r = r0 + k * kPass + tid / kPerRow, row = w.sq * R + r;
+          raw[k] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < rows && r < r0 + CH) {
+            const int32_t tk = g.token_of(row);
+            raw[k] = *reinterpret_cast<const uint4*>(p.a.q + (w.r0 + tk) * p.a.ldq +
+                                                     (w.sh * g.group + row - tk * g.group) * HD + 8 * i);
+          }
+        }
+        if (tid < CH) {
+          const int row = w.sq * R + r0 + tid;
+          const int32_t tk = g.token_of(row);
+          row_m[r0 + tid] = kNoMax;
+          row_lim[r0 + tid] = r0 + tid < rows ? w.len - w.rows_n + tk : -1;
+          row_at[r0 + tid] = (w.r0 + tk) * p.a.ldo + (w.sh * g.group + row - tk * g.group) * HD;
         }
 #pragma unroll
-        for (int o = 1; o < HD / 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        // 2^-e brings the largest element into (224, 448]; a row that is not finite has NaN as its factor
-        const int e = max(static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), -100);
-        const bool bad = top >= 0x7f800000u;
-        const float by = bad ? 0.0f : __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+        for (int k = 0; k < kPasses; ++k) {
+          const int r = k * kPass + tid / kPerRow;
+          const uint32_t u[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+          float x[8];
+          uint32_t top = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = bad ? 0.0f : x[k] * by;
-        uint2 hi, lo;
-        split8(x, hi, lo);
-        // K-major without swizzle: 16 bytes of a row, the next 7 rows, the next rows' groups; then the next 16 bytes
-        uint8_t* const at = gbase + Y::kOffQ + (i / 2) * (16 * NC) + (r / 8) * 128 + (r % 8) * 16 + (i % 2) * 8;
-        *reinterpret_cast<uint2*>(at) = hi;
-        *reinterpret_cast<uint2*>(at + 16 * R) = lo;
-        if (i == 0) {
-          row_f[r] = bad ? __uint_as_float(0x7fffffffu) : __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * p.a.scale_log2;
-          row_m[r] = kNoMax;
-          row_lim[r] = r < rows ? w.ss.len - w.ss.n + row / g.group : -1;
+          for (int e = 0; e < 4; ++e) {
+            x[2 * e] = __uint_as_float(u[e] << 16);
+            x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+            top = max(top, max(u[e] << 16 & 0x7fffffffu, u[e] & 0x7fff0000u));
+          }
+#pragma unroll
+          for (int o = 1; o < kPerRow; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+          // 2^-e brings the largest element into (224, 448]; a row that is not finite has NaN as its factor
+          const int e = max(static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), -100);
+          const bool bad = top >= 0x7f800000u;
+          const float by = bad ? 0.0f : __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) x[q] = bad ? 0.0f : x[q] * by;
+          uint2 hi, lo;
+          split8(x, hi, lo);
+          if (r < CH) {
+            // K-major without swizzle: 16 bytes of a row, the next 7 rows, the next rows' groups; then the next 16 bytes
+            uint8_t* const at = gbase + Y::kOffQ + (i / 2) * (16 * NC) + (r0 + r) * 16 + (i % 2) * 8;
+            *reinterpret_cast<uint2*>(at) = hi;
+            *reinterpret_cast<uint2*>(at + 16 * R) = lo;
+            if (i == 0)
+              row_f[r0 + r] = bad ? __uint_as_float(0x7fffffffu)
+                                  : __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * p.a.scale_log2;
+          }
         }
+        fence_proxy_async_smem();
       }
-      fence_proxy_async_smem();
-      soft_sync();
+      bar_sync(bar, kGroup);
       if (lane == 0) mbar_arrive_local(q_full);
-      const int32_t sees_all = row_lim[0] + 1;  // tokens that the first row sees, the others at least as many
-      float l[R];
+      // tokens that the group's first row sees (the others at least as many)
+      const int32_t sees_all = active ? row_lim[r0] + 1 : 0;
+      float l[CH];
 #pragma unroll
-      for (int r = 0; r < R; ++r) l[r] = 0.0f;
+      for (int i = 0; i < CH; ++i) l[i] = 0.0f;
 
+      bool failed = false;
+#pragma unroll 1
       for (int32_t j = 0; j < w.n; ++j, ++gt) {
         const uint32_t buf = gt & 1;
-        const float ks = ks1, vs = vs1;
-        ks1 = scale_at(kv.k_scale, id1);
-        vs1 = scale_at(kv.v_scale, id1);
-        id1 = page_of(w.t0 + j + 2);
-        const int32_t tok = (w.t0 + j) * kTok + tid;
-        const bool masked = (w.t0 + j + 1) * kTok > sees_all;
-        // log2 and reciprocal of the values' scale; codes under a scale of 0 are zeros, any scale serves them
-        uint32_t vb = __float_as_uint(vs);
+        if (!active) {  // rows behind the last: the group only keeps pace
+          ok = mbar_wait_warp(s_full0 + 8u * buf, (gt >> 1) & 1, p.wc) && ok;
+          if (!bar_all(bar, kGroup, ok)) { failed = true; break; }
+          if (lane == 0) mbar_arrive_local(p_full0 + 8u * buf);
+          continue;
+        }
+        ok = mbar_wait_warp(scale_full0 + 8u * (gt % kScaleRing), (gt / kScaleRing) & 1, p.wc) && ok;
+        float ks = scales[(gt % kScaleRing) * 16 + page_at];
+        uint32_t vb = __float_as_uint(scales[(gt % kScaleRing) * 16 + 8 + page_at]);
+        // log2 and reciprocal of the values' scale; codes under a scale of 0 are zeros, any scale serves them; one that
+        // is not finite makes the scores of the rows that see the token NaN
         if (vb == 0u) vb = (127u - 20u) << 23;
-        const bool fin = vb < 0x7f800000u;
-        const float lsv = fin ? static_cast<float>(static_cast<int>(vb >> 23) - 127) : vs;
-        const float inv = fin ? __uint_as_float((254u - (vb >> 23)) << 23) : vs;
+        if (vb >= 0x7f800000u) {
+          ks = __uint_as_float(0x7fffffffu);
+          vb = 127u << 23;
+        }
+        const float lsv = static_cast<float>(static_cast<int>(vb >> 23) - 127);
+        const float inv = __uint_as_float((254u - (vb >> 23)) << 23);
+        const int32_t tile = (w.t0 + j) * kTok;
+        const bool masked = tile + kTok > sees_all;
         ok = mbar_wait_warp(s_full0 + 8u * buf, (gt >> 1) & 1, p.wc) && ok;
         tc_fence_after();
-        if (masked && (w.t0 + j + 1) * kTok > w.vis) {
+        if (wg == 0 && tile + kTok > w.vis) {
           // the values behind the last visible token become zeros
           const uint32_t at = ring + min(2, w.n) + j + max(0, min(j, w.n - 2)), sl = at % NS;
           ok = mbar_wait_warp(full0 + 8u * sl, (at / NS) & 1, p.wc) && ok;
-          const int32_t left = max(w.vis - (w.t0 + j) * kTok, 0);
           uint4* const v = reinterpret_cast<uint4*>(gbase + Y::kOffRing + sl * Y::kTile);
-          for (int32_t i = left * (HD / 16) + tid; i < kTok * (HD / 16); i += kSoft) v[i] = make_uint4(0u, 0u, 0u, 0u);
+          for (int32_t i = max(w.vis - tile, 0) * (HD / 16) + tid; i < kTok * (HD / 16); i += kGroup)
+            v[i] = make_uint4(0u, 0u, 0u, 0u);
         }
-        bool failed = false;
+        float s[CH], y[CH];
+        {
+          uint32_t both[2 * CH];
+          load_cols<R, CH>(lanes + buf * NC, both);
+          float f[CH];
+          load_row<CH>(row_f + r0, f);
 #pragma unroll
-        for (int c = 0; c < R / CH; ++c) {
-          uint32_t s[R < 16 ? 16 : 32];
-          load_chunk<R>(lanes + buf * NC, c, s);
-          float x[CH], m[CH];
-          bool over = false;
+          for (int i = 0; i < CH; ++i)
+            s[i] = fmaf(__uint_as_float(both[i + CH]), kLoUnit, __uint_as_float(both[i])) * (ks * f[i]);
+        }
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < CH; ++i)
+            if (tile + tid > row_lim[r0 + i]) s[i] = -INFINITY;
+        }
+        for (;;) {
+          float m[CH], top = -INFINITY;
+          load_row<CH>(row_m + r0, m);
 #pragma unroll
           for (int i = 0; i < CH; ++i) {
-            m[i] = row_m[c * CH + i];
-            x[i] = fmaf(__uint_as_float(s[i + CH]), kLoUnit, __uint_as_float(s[i])) * (ks * row_f[c * CH + i]);
-            const float y = x[i] + (lsv - m[i]);
-            if (masked && tok > row_lim[c * CH + i]) x[i] = -INFINITY;
-            else over |= y > kOver;
+            y[i] = s[i] + (lsv - m[i]);
+            top = fmaxf(top, y[i]);
           }
-          if (!bar_all(1, kSoft, ok && !over)) {
-            if (!bar_all(1, kSoft, ok)) { failed = true; break; }
-            // new maxima of the chunk's rows, and what they were worth before
+          if (bar_all(bar, kGroup, ok && !(top > kOver))) break;
+          if (!bar_all(bar, kGroup, ok)) { failed = true; break; }
+          // new maxima of the group's rows and what a weight of the old is worth under them: a lane a row
+#pragma unroll
+          for (int i = 0; i < CH; ++i) m[i] = s[i] + lsv;
+          warp_rows<CH, true>(m, lane);
+          const int row = lane / (32 / CH);
+          if (lane % (32 / CH) == 0) my_red[(warp & 3) * CH + row] = m[0];
+          bar_sync(bar, kGroup);
+          const float t = fmaxf(fmaxf(my_red[row], my_red[CH + row]), fmaxf(my_red[2 * CH + row], my_red[3 * CH + row]));
+          const float old = row_m[r0 + row], raised = t - old > kNominal ? t - kNominal : old;
+          const float fac = raised == old ? 1.0f : fast_exp2(old - raised);
+          bar_sync(bar, kGroup);  // everyone has read the old maxima
+          if ((warp & 3) == 0 && lane % (32 / CH) == 0) {
+            row_m[r0 + row] = raised;
+            row_fac[r0 + row] = fac;
+          }
+          bar_sync(bar, kGroup);
+          load_row<CH>(row_fac + r0, m);
+#pragma unroll
+          for (int i = 0; i < CH; ++i) l[i] *= m[i];
+          if (j > 0) {
+            ok = wait_pv(gt - 1) && ok;
+            tc_fence_after();
+            uint32_t o[2 * CH];
+            load_cols<R, CH>(lanes + kColO, o);
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-              float t = x[i] + lsv;
-#pragma unroll
-              for (int o = 16; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
-              if (lane == 0) red[warp * R + i] = t;
+              o[i] = __float_as_uint(__uint_as_float(o[i]) * m[i]);
+              o[i + CH] = __float_as_uint(__uint_as_float(o[i + CH]) * m[i]);
             }
-            soft_sync();
-            float f[CH];
-            bool any = false;
-#pragma unroll
-            for (int i = 0; i < CH; ++i) {
-              const float t = fmaxf(fmaxf(red[i], red[R + i]), fmaxf(red[2 * R + i], red[3 * R + i]));
-              const float raised = t - m[i] > kNominal ? t - kNominal : m[i];
-              f[i] = raised == m[i] ? 1.0f : fast_exp2(m[i] - raised);
-              any |= raised != m[i];
-              m[i] = raised;
-              l[c * CH + i] *= f[i];
-            }
-            if (j > 0 && any) {
-              ok = wait_pv(gt - 1) && ok;
-              tc_fence_after();
-              uint32_t o[R < 16 ? 16 : 32];
-              load_chunk<R>(lanes + kColO, c, o);
-#pragma unroll
-              for (int i = 0; i < CH; ++i) {
-                o[i] = __float_as_uint(__uint_as_float(o[i]) * f[i]);
-                o[i + CH] = __float_as_uint(__uint_as_float(o[i + CH]) * f[i]);
-              }
-              store_chunk<R>(lanes + kColO, c, o);
-              tmem_st_wait();
-            }
-            soft_sync();  // everyone has read the old maxima and the parts of the new
-            if (tid == 0) {
-#pragma unroll
-              for (int i = 0; i < CH; ++i) row_m[c * CH + i] = m[i];
-            }
-            soft_sync();
-          }
-          float wt[CH];
-#pragma unroll
-          for (int i = 0; i < CH; ++i) {
-            wt[i] = fast_exp2(x[i] + (lsv - m[i]));
-            if (masked) {
-              const bool sees = tok <= row_lim[c * CH + i];
-              wt[i] = sees ? wt[i] : 0.0f;
-              l[c * CH + i] += sees ? wt[i] * inv : 0.0f;
-            } else {
-              l[c * CH + i] = fmaf(wt[i], inv, l[c * CH + i]);
-            }
-          }
-          // MN-major without swizzle: 16 columns of a token, the next tokens; then the next 16 columns
-          uint8_t* const at = gbase + Y::kOffP + buf * Y::kP + tid * 16;
-          uint2 hi[CH / 8], lo[CH / 8];
-#pragma unroll
-          for (int i = 0; i < CH / 8; ++i) split8(wt + 8 * i, hi[i], lo[i]);
-          if constexpr (R < 16) {
-            *reinterpret_cast<uint4*>(at) = make_uint4(hi[0].x, hi[0].y, lo[0].x, lo[0].y);
-          } else {
-            *reinterpret_cast<uint4*>(at + c * (16 * kTok)) = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y);
-            *reinterpret_cast<uint4*>(at + (R / 16 + c) * (16 * kTok)) = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y);
+            store_cols<R, CH>(lanes + kColO, o);
+            tmem_st_wait();
           }
         }
-        if (failed) { ok = false; break; }
+        if (failed) break;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+          y[i] = fast_exp2(y[i]);
+          l[i] = fmaf(y[i], inv, l[i]);
+        }
+        // MN-major without swizzle: 16 columns of a token, the next tokens; then the next 16 columns
+        uint8_t* const at = gbase + Y::kOffP + buf * Y::kP + tid * 16;
+        uint2 hi[CH / 8], lo[CH / 8];
+#pragma unroll
+        for (int i = 0; i < CH / 8; ++i) split8(y + 8 * i, hi[i], lo[i]);
+        if constexpr (CH < 16) {
+          *reinterpret_cast<uint4*>(at) = make_uint4(hi[0].x, hi[0].y, lo[0].x, lo[0].y);
+        } else {
+          *reinterpret_cast<uint4*>(at + wg * (16 * kTok)) = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y);
+          *reinterpret_cast<uint4*>(at + (Y::kGroups + wg) * (16 * kTok)) = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y);
+        }
         tc_fence_before();
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive_local(p_full0 + 8u * buf);
       }
-      if (!bar_all(1, kSoft, ok)) { ok = false; break; }
       ring += 2 * w.n;
-
-      // the rows' sums
-      warp_row_sums<R>(l, lane);
-      if constexpr (R >= 32) {
-#pragma unroll
-        for (int i = 0; i < R / 32; ++i) red[warp * R + lane * (R / 32) + i] = l[i];
-      } else {
-        if (lane % (32 / R) == 0) red[warp * R + lane / (32 / R)] = l[0];
-      }
-      soft_sync();
-      ok = wait_pv(gt - 1);
-      tc_fence_after();
       const bool whole = w.n == w.all;
-      const int dl = HD == 128 ? tid : warp * 16 + lane;  // the thread's column of the head (64: lanes 0 .. 15)
-      const bool mine = HD == 128 || lane < 16;
-      float* const part = p.parts + (2 * static_cast<int64_t>(blockIdx.x) + (w.begin >= first ? 1 : 0)) * Y::kPartFloats;
+      float* const part = p.parts + (2 * static_cast<int64_t>(blockIdx.x) + (w.begin() >= first ? 1 : 0)) * Y::kPartFloats;
+      if (active && !failed) {
+        warp_rows<CH, false>(l, lane);  // the rows' sums
+        if (lane % (32 / CH) == 0) my_red[(warp & 3) * CH + lane / (32 / CH)] = l[0];
+        bar_sync(bar, kGroup);
+        if (tid < CH && r0 + tid < rows) {
+          const float sum = (my_red[tid] + my_red[CH + tid]) + (my_red[2 * CH + tid] + my_red[3 * CH + tid]);
+          const float m = row_m[r0 + tid];
+          if (!whole) {
+            part[r0 + tid] = m;
+            part[R + r0 + tid] = sum;
+          } else if (p.a.lse) {
+            const int row = w.sq * R + r0 + tid;
+            const int32_t tk = g.token_of(row);
+            p.a.lse[static_cast<int64_t>(w.r0 + tk) * p.a.nh + w.sh * g.group + row - tk * g.group] =
+                sum == 0.0f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
+          }
+          row_fac[r0 + tid] = sum == 0.0f ? 0.0f : 1.0f / sum;
+        }
+        bar_sync(bar, kGroup);
+        ok = wait_pv(gt - 1) && ok;
+        tc_fence_after();
+        const int dl = HD == 128 ? tid : (warp & 3) * 16 + lane;  // the thread's column of the head (64: lanes 0 .. 15)
+        uint32_t o[2 * CH];
+        load_cols<R, CH>(lanes + kColO, o);
+        if (ok && (HD == 128 || lane < 16)) {
 #pragma unroll
-      for (int c = 0; c < R / CH; ++c) {
-        uint32_t o[R < 16 ? 16 : 32];
-        load_chunk<R>(lanes + kColO, c, o);
-#pragma unroll
-        for (int i = 0; i < CH; ++i) {
-          const int r = c * CH + i;
-          if (!ok || !mine || r >= rows) continue;
-          const float v = fmaf(__uint_as_float(o[i + CH]), kLoUnit, __uint_as_float(o[i]));
-          if (whole) {
-            const float sum = (red[r] + red[R + r]) + (red[2 * R + r] + red[3 * R + r]);
-            const int row = w.sq * R + r;
-            const __nv_bfloat16 out = __float2bfloat16_rn(sum == 0.0f ? 0.0f : v / sum);
-            p.a.o[(w.ss.r0 + row / g.group) * p.a.ldo + (w.sh * g.group + row % g.group) * HD + dl] =
-                *reinterpret_cast<const uint16_t*>(&out);
-          } else {
-            part[2 * R + r * HD + dl] = v;
+          for (int i = 0; i < CH; ++i) {
+            const float v = fmaf(__uint_as_float(o[i + CH]), kLoUnit, __uint_as_float(o[i]));
+            if (r0 + i >= rows) break;
+            if (whole) {
+              const float f = row_fac[r0 + i];
+              const __nv_bfloat16 out = __float2bfloat16_rn(f == 0.0f ? 0.0f : v * f);
+              p.a.o[row_at[r0 + i] + dl] = *reinterpret_cast<const uint16_t*>(&out);
+            } else {
+              part[2 * R + (r0 + i) * HD + dl] = v;
+            }
           }
         }
+        tc_fence_before();
       }
-      tc_fence_before();
-      if (ok && tid < rows) {
-        const float sum = (red[tid] + red[R + tid]) + (red[2 * R + tid] + red[3 * R + tid]);
-        const int row = w.sq * R + tid;
-        if (!whole) {
-          part[tid] = row_m[tid];
-          part[R + tid] = sum;
-        } else if (p.a.lse) {
-          p.a.lse[static_cast<int64_t>(w.ss.r0 + row / g.group) * p.a.nh + w.sh * g.group + row % g.group] =
-              sum == 0.0f ? -INFINITY : (row_m[tid] + log2f(sum)) * 0.6931471805599453f;
-        }
-      }
+      ok = ok && !failed;
       if (whole) continue;
       // the last of the row tile's runs joins their parts
-      if (!bar_all(1, kSoft, ok)) { ok = false; break; }
-      const int32_t c0 = static_cast<int32_t>(w.begin / run), c1 = static_cast<int32_t>((w.begin + w.all - 1) / run);
       __threadfence();
-      soft_sync();
-      if (tid == 0) {
+      if (!bar_all(bar_every, kSoft, ok)) { ok = false; break; }
+      const int32_t c0 = static_cast<int32_t>(w.begin() / run), c1 = static_cast<int32_t>((w.begin() + w.all - 1) / run);
+      if (threadIdx.x == 0) {
         const uint32_t last = static_cast<uint32_t>(c1 - c0);
         *merge_flag = atomicInc(p.counters + c0, last) == last;
       }
-      soft_sync();
+      bar_sync(bar_every, kSoft);
       if (*merge_flag) {
         __threadfence();
         constexpr int kLanes = HD / 4;  // threads a row
-        for (int r = tid / kLanes; r < rows; r += kSoft / kLanes) {
-          const int i = tid % kLanes;
+        for (int r = threadIdx.x / kLanes; r < rows; r += kSoft / kLanes) {
+          const int i = threadIdx.x % kLanes;
           float m = kNoMax, sum = 0.0f, o[4] = {0.f, 0.f, 0.f, 0.f};
           for (int32_t c = c0; c <= c1; c += 8) {
             float pm[8], pl[8];
@@ -709,7 +780,7 @@ __global__ void __launch_bounds__(kThreads, KvLay<HD, R>::kCtas)
             for (int k = 0; k < 8; ++k) {
               const float* const q = p.parts + (2 * static_cast<int64_t>(min(c + k, c1)) + (c + k == c0 ? 1 : 0)) * Y::kPartFloats;
               pm[k] = __ldcg(q + r);
-              pl[k] = c + k <= c1 ? __ldcg(q + R + r) : 0.0f;
+              pl[k] = __ldcg(q + R + r);
               po[k] = __ldcg(reinterpret_cast<const float4*>(q + 2 * R + r * HD) + i);
             }
 #pragma unroll
@@ -725,21 +796,23 @@ __global__ void __launch_bounds__(kThreads, KvLay<HD, R>::kCtas)
               }
           }
           const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-          const int row = w.sq * R + r;
-          const int64_t tk = w.ss.r0 + row / g.group, hd = w.sh * g.group + row % g.group;
           uint2 out;
           asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(out.x) : "f"(o[1] * by), "f"(o[0] * by));
           asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(out.y) : "f"(o[3] * by), "f"(o[2] * by));
-          *reinterpret_cast<uint2*>(p.a.o + tk * p.a.ldo + hd * HD + 4 * i) = out;
-          if (p.a.lse && i == 0)
-            p.a.lse[tk * p.a.nh + hd] = sum == 0.0f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
+          *reinterpret_cast<uint2*>(p.a.o + row_at[r] + 4 * i) = out;
+          if (p.a.lse && i == 0) {
+            const int row = w.sq * R + r;
+            const int32_t tk = g.token_of(row);
+            p.a.lse[static_cast<int64_t>(w.r0 + tk) * p.a.nh + w.sh * g.group + row - tk * g.group] =
+                sum == 0.0f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
+          }
         }
       }
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == kMmaWarp) {
+  if (warp == Y::kMmaWarp) {
     tc_fence_after();
     tmem_dealloc<1>(tmem, Y::kTmem);
   }
@@ -786,7 +859,8 @@ cudaError_t run_kv(const KvAttnArgs& a, cudaStream_t st) {
   p.a = a;
   if (!launch_wait_ctl(&p.wc)) return cudaErrorInvalidDevice;
   p.a.status = p.wc.status_word;
-  p.g = KvGeom{a.row_start, a.seq_len, a.B, a.nh / a.cache.nkv, a.cache.nkv, a.T,
+  p.g = KvGeom{a.row_start, a.seq_len, a.B, a.nh / a.cache.nkv, a.cache.nkv,
+               static_cast<uint32_t>(((uint64_t(1) << 32) + a.nh / a.cache.nkv - 1) / (a.nh / a.cache.nkv)), a.T,
                static_cast<int64_t>(a.cache.max_pages) * a.cache.page};
   p.counters = static_cast<uint32_t*>(a.workspace);
   p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + kCounterBytes);
@@ -794,7 +868,7 @@ cudaError_t run_kv(const KvAttnArgs& a, cudaStream_t st) {
   auto kern = kv_attn_kernel<HD, R>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Y::kSmem);
   if (e != cudaSuccess) return e;
-  kern<<<static_cast<unsigned>(std::min(Y::kCtas * sm_count(), 1024)), kThreads, Y::kSmem, st>>>(tk, tv, p);
+  kern<<<static_cast<unsigned>(std::min(Y::kCtas * sm_count(), 1024)), Y::kThreads, Y::kSmem, st>>>(tk, tv, p);
   return cudaGetLastError();
 }
 
@@ -811,8 +885,8 @@ cudaError_t run_kv_rows(const KvAttnArgs& a, cudaStream_t st) {
 }  // namespace
 
 size_t kv_attention_ws_bytes(int32_t, int32_t, int32_t d) {
-  // two parts of up to 32 rows for each of two CTAs an SM, or of 64 for one
-  const size_t ctas = static_cast<size_t>(std::min(2 * sm_count(), 1024));
+  // two parts for each CTA: three CTAs an SM of 8 rows, two of up to 32, one of 64
+  const size_t ctas = 2 * static_cast<size_t>(sm_count());
   const size_t parts = ctas * 2 * 32 * (static_cast<size_t>(d) + 2) * sizeof(float);
   return (kCounterBytes + parts + 255) / 256 * 256;
 }

@@ -7,8 +7,9 @@ Tolerances, from the arithmetic:
              half a step of the output's type (bf16: 2^-8 |y|)
   codes      of values: the oracle's, bit for bit.  Of rotated keys: the nearest e4m3 number to a value that is the
              oracle's within the rotation's error
-  attention  half a step of bf16 (2^-8 |o|); the two-term weights, 2^-8 sum p |v|, and their floor, 2^-20 of the largest
-             weight for every token; 2^-14 sum p |v| for scores, exponentials and sums in fp32
+  attention  half a step of bf16 (2^-8 |o|); the two-term weights, 2^-8 sum p |v|, and their floor (half of e4m3's least
+             step in units of 1/16, 2^-14, where the largest weight is 2^3 or more), 2^-17 of the largest weight for
+             every token; 2^-14 sum p |v| for scores, exponentials and sums in fp32
   lse        2^-16 (1 + |lse|)
 """
 import numpy as np
@@ -99,7 +100,7 @@ def check_attention(paged, row_start, seq_len, q, nh, got, lse):
                                         syn.round_bf16(np.asarray(q, np.float32)), q.shape[0], nh)
     outside = np.isnan(want_lse)
     assert (got[outside] == 7).all()
-    bound = 2.0 ** -8 * np.abs(O) + (2.0 ** -8 + 2.0 ** -14) * mag + 2.0 ** -20 * low
+    bound = 2.0 ** -8 * np.abs(O) + (2.0 ** -8 + 2.0 ** -14) * mag + 2.0 ** -17 * low
     off = np.abs(got - O)[~outside] - bound[~outside]
     assert (off <= 0).all(), f"largest excess {off.max():.3g} at bound {bound[~outside].flat[off.argmax()]:.3g}"
     if lse is not None:
