@@ -768,30 +768,43 @@ _KV = struct.Struct("5Q6i")
 
 def _rows(t, name: str, T: int, width: int, where: str):
     """(address, elements from a row to the next) of T rows of `width` elements."""
+    shape, st = t.shape, t.stride()
+    if (t.is_cuda and len(shape) == 2 and shape[0] == T and shape[1] == width and st[1] == 1
+            and (st[0] >= width or T < 2)):
+        return t.data_ptr(), st[0] if T > 1 else width
     if not t.is_cuda:
         raise ValueError(f"{where}: {name} must be a CUDA tensor")
-    shape = t.shape
     if len(shape) not in (2, 3) or shape[0] != T or t.numel() != T * width:
         raise ValueError(f"{where}: {name} has shape {tuple(shape)}, the call needs {T} rows of {width}")
-    st = t.stride()
-    if st[-1] != 1 or (len(shape) == 3 and shape[1] > 1 and st[1] != shape[2]) or (T > 1 and st[0] < width):
+    if t.numel() and (st[-1] != 1 or (len(shape) == 3 and shape[1] > 1 and st[1] != shape[2])
+                      or (T > 1 and st[0] < width)):
         raise ValueError(f"{where}: {name}'s rows must be contiguous and in order")
     return t.data_ptr(), st[0] if T > 1 else width
 
 
 def _i32(t, name: str, count: int, where: str):
-    if str(t.dtype) != "torch.int32":
+    if "i32" not in _DTYPES_I:
+        import torch
+        _DTYPES_I["i32"] = torch.int32
+    if t.dtype != _DTYPES_I["i32"]:
         raise ValueError(f"{where}: {name} must be int32")
     return _buf(t, name, 4 * count, where)
 
 
-@dataclasses.dataclass
+_DTYPES_I: dict = {}
+
+
 class Rope:
-    """A rotation by position: `turns` int64 [rot / 2] (64-bit fixed point, see catq_rotation_turns) on the GPU."""
-    turns: object
-    rot: int
-    layout: int = ROPE_HALF
-    magnitude: float = 1.0
+    """A rotation by position: `turns` int64 [rot / 2] (64-bit fixed point, see catq_rotation_turns) on the GPU.  A handle:
+    it checks its arguments and takes the tensor's address when it is made, and holds the tensor."""
+
+    def __init__(self, turns, rot, layout=ROPE_HALF, magnitude=1.0):
+        if turns.element_size() != 8:
+            raise ValueError("Rope: turns are 64-bit integers")
+        self.turns, self.rot, self.layout, self.magnitude = turns, int(rot), int(layout), float(magnitude)
+        self._struct = catq_rotation()
+        _ROTATION.pack_into(self._struct, 0, _buf(turns, "turns", 4 * self.rot, "Rope"), self.rot, self.layout,
+                            self.magnitude, 0)
 
     @classmethod
     def create(cls, rot, base, device, layout=ROPE_HALF, scaling=ROPE_PLAIN, factor=1.0, low=1.0, high=4.0,
@@ -799,24 +812,30 @@ class Rope:
         """The turns of base^(-2i/rot) under a scaling for long contexts (catq_rope_scaling)."""
         import torch
         turns, magnitude = catq_rotation_turns(rot, base, scaling, factor, low, high, original)
-        return cls(torch.tensor(turns, dtype=torch.int64).to(device), int(rot), int(layout), magnitude)
+        return cls(torch.tensor(turns, dtype=torch.int64).to(device), rot, layout, magnitude)
 
     def struct(self) -> catq_rotation:
-        r = catq_rotation()
-        _ROTATION.pack_into(r, 0, _buf(self.turns, "turns", 4 * self.rot, "Rope"), self.rot, self.layout,
-                            self.magnitude, 0)
-        return r
+        return self._struct
 
 
-@dataclasses.dataclass
 class KVCache:
     """A paged cache of e4m3 codes: k_codes, v_codes float8_e4m3fn (or uint8) [n_pages, n_kv_heads, page, d], k_scale,
-    v_scale fp32 [n_pages, n_kv_heads], table int32 [B, max_pages]."""
-    k_codes: object
-    v_codes: object
-    k_scale: object
-    v_scale: object
-    table: object
+    v_scale fp32 [n_pages, n_kv_heads], table int32 [B, max_pages].  A handle: it checks the tensors and takes their
+    addresses when it is made, and holds the tensors; their contents may change, the table's too."""
+
+    def __init__(self, k_codes, v_codes, k_scale, v_scale, table):
+        w = "KVCache"
+        n_pages, nkv, page, d = k_codes.shape
+        self.B, max_pages = table.shape
+        if k_codes.element_size() != 1 or v_codes.element_size() != 1:
+            raise ValueError(f"{w}: codes are one byte an element")
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale, self.table = k_codes, v_codes, k_scale, v_scale, table
+        self.n_kv_heads, self.page, self.d = nkv, page, d
+        n, m = n_pages * nkv * page * d, 4 * n_pages * nkv
+        self._struct = catq_kv_cache()
+        _KV.pack_into(self._struct, 0, _buf(k_codes, "k_codes", n, w), _buf(v_codes, "v_codes", n, w),
+                      _f32(k_scale, "k_scale", m, w), _f32(v_scale, "v_scale", m, w),
+                      _i32(table, "table", self.B * max_pages, w), n_pages, nkv, page, d, max_pages, 0)
 
     @classmethod
     def create(cls, n_pages, n_kv_heads, page, d, table):
@@ -829,17 +848,7 @@ class KVCache:
         return cls(*codes, *scales, table)
 
     def struct(self) -> catq_kv_cache:
-        w = "KVCache"
-        n_pages, nkv, page, d = self.k_codes.shape
-        B, max_pages = self.table.shape
-        if self.k_codes.element_size() != 1 or self.v_codes.element_size() != 1:
-            raise ValueError(f"{w}: codes are one byte an element")
-        n, m = n_pages * nkv * page * d, 4 * n_pages * nkv
-        c = catq_kv_cache()
-        _KV.pack_into(c, 0, _buf(self.k_codes, "k_codes", n, w), _buf(self.v_codes, "v_codes", n, w),
-                      _f32(self.k_scale, "k_scale", m, w), _f32(self.v_scale, "v_scale", m, w),
-                      _i32(self.table, "table", B * max_pages, w), n_pages, nkv, page, d, max_pages, 0)
-        return c
+        return self._struct
 
 
 def catq_rotation_turns(rot: int, base: float, scaling: int = ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
@@ -860,14 +869,8 @@ def catq_rope_at(X, positions, rope: Rope, n_heads: int, d: int, Y=None, inverse
     dt = _dtype_code(X)
     if Y is not None and Y.dtype != X.dtype:
         raise ValueError(f"{w}: Y must have X's dtype")
-    _check(lib().catq_rope_at(x, ldx, y, ldy, dt, _i32(positions, "positions", T, w), T, n_heads, d, rope.struct(),
+    _check(lib().catq_rope_at(x, ldx, y, ldy, dt, _i32(positions, "positions", T, w), T, n_heads, d, rope._struct,
                               1 if inverse else 0, _stream(stream)), w)
-
-
-def _kv_meta(cache, row_start, seq_len, where):
-    """The cache's struct, the addresses of the row offsets and lengths, and the sequences."""
-    B = cache.table.shape[0]
-    return cache.struct(), _i32(row_start, "row_start", B + 1, where), _i32(seq_len, "seq_len", B, where), B
 
 
 def _bf16_rows(t, name, T, width, where):
@@ -882,17 +885,17 @@ def catq_kv_append(cache: KVCache, row_start, seq_len, K, V, rope: Rope = None, 
     n_heads * d] the rotated queries go to Q_out (Q itself when None).  row_start [B + 1], seq_len [B] int32: the rows of
     each sequence and its length with them."""
     w = "catq_kv_append"
-    c, rs, sl, B = _kv_meta(cache, row_start, seq_len, w)
-    T = K.shape[0]
-    k, ldk = _bf16_rows(K, "K", T, c.n_kv_heads * c.d, w)
-    v, ldv = _bf16_rows(V, "V", T, c.n_kv_heads * c.d, w)
+    B, T, width = cache.B, K.shape[0], cache.n_kv_heads * cache.d
+    rs, sl = _i32(row_start, "row_start", B + 1, w), _i32(seq_len, "seq_len", B, w)
+    k, ldk = _bf16_rows(K, "K", T, width, w)
+    v, ldv = _bf16_rows(V, "V", T, width, w)
     q = qo = None
     ldq = ldqo = 0
     if Q is not None:
-        q, ldq = _bf16_rows(Q, "Q", T, n_heads * c.d, w)
-        qo, ldqo = (q, ldq) if Q_out is None else _bf16_rows(Q_out, "Q_out", T, n_heads * c.d, w)
-    _check(lib().catq_kv_append(c, rs, sl, B, k, ldk, v, ldv, T, q, ldq, qo, ldqo, n_heads,
-                                None if rope is None else rope.struct(), _stream(stream)), w)
+        q, ldq = _bf16_rows(Q, "Q", T, n_heads * cache.d, w)
+        qo, ldqo = (q, ldq) if Q_out is None else _bf16_rows(Q_out, "Q_out", T, n_heads * cache.d, w)
+    _check(lib().catq_kv_append(cache._struct, rs, sl, B, k, ldk, v, ldv, T, q, ldq, qo, ldqo, n_heads,
+                                None if rope is None else rope._struct, _stream(stream)), w)
 
 
 def catq_kv_attention_workspace_bytes(n_heads: int, n_kv_heads: int, d: int) -> int:
@@ -902,8 +905,7 @@ def catq_kv_attention_workspace_bytes(n_heads: int, n_kv_heads: int, d: int) -> 
 def kv_attention_workspace(cache: KVCache, n_heads: int):
     """A zeroed workspace for catq_kv_attention over this cache."""
     import torch
-    _, nkv, _, d = cache.k_codes.shape
-    return torch.zeros(catq_kv_attention_workspace_bytes(n_heads, nkv, d), dtype=torch.uint8,
+    return torch.zeros(catq_kv_attention_workspace_bytes(n_heads, cache.n_kv_heads, cache.d), dtype=torch.uint8,
                        device=cache.k_codes.device)
 
 
@@ -911,10 +913,10 @@ def catq_kv_attention(cache: KVCache, row_start, seq_len, Q, O, n_heads: int, wo
     """O [T, n_heads * d] = attention of the rows of Q over the cached tokens up to each row's position; lse [T,
     n_heads] fp32 (optional).  workspace: kv_attention_workspace, one for every call that may run at the same time."""
     w = "catq_kv_attention"
-    c, rs, sl, B = _kv_meta(cache, row_start, seq_len, w)
-    T = Q.shape[0]
-    q, ldq = _bf16_rows(Q, "Q", T, n_heads * c.d, w)
-    o, ldo = _bf16_rows(O, "O", T, n_heads * c.d, w)
+    B, T, width = cache.B, Q.shape[0], n_heads * cache.d
+    rs, sl = _i32(row_start, "row_start", B + 1, w), _i32(seq_len, "seq_len", B, w)
+    q, ldq = _bf16_rows(Q, "Q", T, width, w)
+    o, ldo = _bf16_rows(O, "O", T, width, w)
     ws, ws_bytes = _ws(workspace, w)
-    _check(lib().catq_kv_attention(c, rs, sl, B, q, ldq, T, n_heads, o, ldo, _f32(lse, "lse", 4 * T * n_heads, w), ws,
-                                   ws_bytes, _stream(stream)), w)
+    _check(lib().catq_kv_attention(cache._struct, rs, sl, B, q, ldq, T, n_heads, o, ldo,
+                                   _f32(lse, "lse", 4 * T * n_heads, w), ws, ws_bytes, _stream(stream)), w)

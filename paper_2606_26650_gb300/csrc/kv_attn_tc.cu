@@ -32,6 +32,7 @@
 #include <cudaTypedefs.h>
 
 #include <algorithm>
+#include <atomic>
 #include <mutex>
 
 #include "launch.h"
@@ -330,6 +331,13 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
     fence_mbar_init_cluster();
   }
   if (warp == Y::kMmaWarp) tmem_alloc<1>(smem_u32(tmem_slot), Y::kTmem);
+  if (warp == Y::kTmaWarp && lane == 0) {
+    prefetch_tmap(&tmk);
+    prefetch_tmap(&tmv);
+  }
+  // so far nothing that the launch ahead may have written was read
+  grid_launch_dependents();
+  grid_dependency_wait();
 
   // The run of this CTA: every CTA adds up all sequences' tiles, a thread a stretch of them.
   const KvGeom& g = p.g;
@@ -393,10 +401,6 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
   bool ok = true;
 
   if (warp == Y::kTmaWarp) {
-    if (lane == 0) {
-      prefetch_tmap(&tmk);
-      prefetch_tmap(&tmv);
-    }
     int slot = 0, loads = 0;
     uint32_t ph = 1, gt = 0;
     // A lane a page: the lane's page in tile t of the segment (first row of its block, -1: none), its scales.
@@ -430,21 +434,21 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
     auto load = [&](const CUtensorMap* map, const Page& g, bool keys) -> bool {
       const uint32_t pages = __popc(__ballot_sync(0xffffffffu, g.row >= 0));
       if (!mbar_wait_warp(empty0 + 8u * slot, ph, p.wc)) return false;
-      if (keys && lane < 8) {
-        float* const to = scales + (gt % kScaleRing) * 16;
-        to[lane] = g.ks;
-        to[8 + lane] = g.vs;
-      }
-      __syncwarp();
-      if (lane == 0) {
-        if (keys) mbar_arrive_local(scale_full0 + 8u * (gt % kScaleRing));
-        mbar_arrive_expect_tx(full0 + 8u * slot, pages * kv.page * HD);
-      }
+      if (lane == 0) mbar_arrive_expect_tx(full0 + 8u * slot, pages * kv.page * HD);
       __syncwarp();
       if (g.row >= 0)
         tma_load_2d(base + Y::kOffRing + slot * Y::kTile + lane * kv.page * HD, map, full0 + 8u * slot, 0, g.row);
+      if (keys) {
+        if (lane < 8) {
+          float* const to = scales + (gt % kScaleRing) * 16;
+          to[lane] = g.ks;
+          to[8 + lane] = g.vs;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive_local(scale_full0 + 8u * (gt % kScaleRing));
+        ++gt;
+      }
       ++loads;
-      gt += keys;
       if (++slot == NS) { slot = 0; ph ^= 1u; }
       return true;
     };
@@ -759,53 +763,92 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
       ok = ok && !failed;
       if (whole) continue;
       // the last of the row tile's runs joins their parts
-      __threadfence();
       if (!bar_all(bar_every, kSoft, ok)) { ok = false; break; }
       const int32_t c0 = static_cast<int32_t>(w.begin() / run), c1 = static_cast<int32_t>((w.begin() + w.all - 1) / run);
       if (threadIdx.x == 0) {
         const uint32_t last = static_cast<uint32_t>(c1 - c0);
-        *merge_flag = atomicInc(p.counters + c0, last) == last;
+        uint32_t old;  // releases what the barrier's threads wrote, acquires what the runs before did
+        asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(old) : "l"(p.counters + c0), "r"(last) : "memory");
+        *merge_flag = old == last;
       }
       bar_sync(bar_every, kSoft);
       if (*merge_flag) {
-        __threadfence();
-        constexpr int kLanes = HD / 4;  // threads a row
-        for (int r = threadIdx.x / kLanes; r < rows; r += kSoft / kLanes) {
-          const int i = threadIdx.x % kLanes;
-          float m = kNoMax, sum = 0.0f, o[4] = {0.f, 0.f, 0.f, 0.f};
-          for (int32_t c = c0; c <= c1; c += 8) {
-            float pm[8], pl[8];
-            float4 po[8];
+        auto part_of = [&](int32_t c) { return p.parts + (2 * static_cast<int64_t>(c) + (c == c0 ? 1 : 0)) * Y::kPartFloats; };
+        // the rows' maxima and sums over all parts: the threads of a row share them
+        constexpr int kPer = kSoft / R;  // 8 or 16
+        const int mr = threadIdx.x / kPer, mi = threadIdx.x % kPer;
+        float m = kNoMax, sum = 0.0f;
+        for (int32_t c = c0 + mi; c <= c1; c += kPer) {
+          const float pm = __ldcg(part_of(c) + mr), pl = __ldcg(part_of(c) + R + mr);
+          if (mr < rows) {
+            const float top = fmaxf(m, pm);
+            sum = sum * fast_exp2(m - top) + pl * fast_exp2(pm - top);
+            m = top;
+          }
+        }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const float* const q = p.parts + (2 * static_cast<int64_t>(min(c + k, c1)) + (c + k == c0 ? 1 : 0)) * Y::kPartFloats;
-              pm[k] = __ldcg(q + r);
-              pl[k] = __ldcg(q + R + r);
-              po[k] = __ldcg(reinterpret_cast<const float4*>(q + 2 * R + r * HD) + i);
+        for (int o = 1; o < kPer; o <<= 1) {
+          const float om = __shfl_xor_sync(0xffffffffu, m, o), os = __shfl_xor_sync(0xffffffffu, sum, o);
+          const float top = fmaxf(m, om);
+          // (written alike in both lanes: they get the same bits)
+          const float mine = sum * fast_exp2(m - top), other = os * fast_exp2(om - top);
+          sum = (mi & o) ? other + mine : mine + other;
+          m = top;
+        }
+        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+        if (p.a.lse && mi == 0 && mr < rows) {
+          const int row = w.sq * R + mr;
+          const int32_t tk = g.token_of(row);
+          p.a.lse[static_cast<int64_t>(w.r0 + tk) * p.a.nh + w.sh * g.group + row - tk * g.group] =
+              sum == 0.0f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
+        }
+        // the parts' weights, 128 parts at a time, over the weights' buffers (no product is under way), then the
+        // accumulators: kItems vectors of four columns a thread, kAt of them at a time (few rows have many parts, many
+        // rows few), 16 loads at once
+        float* const weight = reinterpret_cast<float*>(gbase + Y::kOffP);  // [R][128]
+        constexpr int kItems = R * HD / 4 / kSoft, kAt = R == 8 ? 1 : kItems, kDeep = 16 / kAt;
+        float acc[kItems][4] = {};
+        for (int32_t cb = c0; cb <= c1; cb += 128) {
+          const int32_t count = min(128, c1 + 1 - cb);
+          for (int32_t c = mi; c < count; c += kPer)
+            weight[mr * 128 + c] = mr < rows ? fast_exp2(__ldcg(part_of(cb + c) + mr) - m) * by : 0.0f;
+          bar_sync(bar_every, kSoft);
+#pragma unroll
+          for (int e0 = 0; e0 < kItems; e0 += kAt) {
+            if ((e0 * kSoft + static_cast<int>(threadIdx.x)) / (HD / 4) >= rows) break;
+            for (int32_t c = 0; c < count; c += kDeep) {
+              float4 v[kDeep][kAt];
+#pragma unroll
+              for (int k = 0; k < kDeep; ++k)
+#pragma unroll
+                for (int e = 0; e < kAt; ++e) {
+                  const int at = (e0 + e) * kSoft + threadIdx.x;
+                  v[k][e] = make_float4(0.f, 0.f, 0.f, 0.f);
+                  if (c + k < count && at / (HD / 4) < rows)
+                    v[k][e] = __ldcg(reinterpret_cast<const float4*>(part_of(cb + c + k) + 2 * R) + at);
+                }
+#pragma unroll
+              for (int k = 0; k < kDeep; ++k)
+#pragma unroll
+                for (int e = 0; e < kAt; ++e) {
+                  const int r = ((e0 + e) * kSoft + static_cast<int>(threadIdx.x)) / (HD / 4);
+                  const float f = c + k < count ? weight[r * 128 + c + k] : 0.0f;
+                  acc[e0 + e][0] = fmaf(v[k][e].x, f, acc[e0 + e][0]);
+                  acc[e0 + e][1] = fmaf(v[k][e].y, f, acc[e0 + e][1]);
+                  acc[e0 + e][2] = fmaf(v[k][e].z, f, acc[e0 + e][2]);
+                  acc[e0 + e][3] = fmaf(v[k][e].w, f, acc[e0 + e][3]);
+                }
             }
+          }
+          bar_sync(bar_every, kSoft);
+        }
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-              if (c + k <= c1) {
-                const float top = fmaxf(m, pm[k]), f = fast_exp2(m - top), e = fast_exp2(pm[k] - top);
-                sum = sum * f + pl[k] * e;
-                o[0] = o[0] * f + po[k].x * e;
-                o[1] = o[1] * f + po[k].y * e;
-                o[2] = o[2] * f + po[k].z * e;
-                o[3] = o[3] * f + po[k].w * e;
-                m = top;
-              }
-          }
-          const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+        for (int e = 0; e < kItems; ++e) {
+          const int at = e * kSoft + threadIdx.x, r = at / (HD / 4);
           uint2 out;
-          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(out.x) : "f"(o[1] * by), "f"(o[0] * by));
-          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(out.y) : "f"(o[3] * by), "f"(o[2] * by));
-          *reinterpret_cast<uint2*>(p.a.o + row_at[r] + 4 * i) = out;
-          if (p.a.lse && i == 0) {
-            const int row = w.sq * R + r;
-            const int32_t tk = g.token_of(row);
-            p.a.lse[static_cast<int64_t>(w.r0 + tk) * p.a.nh + w.sh * g.group + row - tk * g.group] =
-                sum == 0.0f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
-          }
+          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(out.x) : "f"(acc[e][1]), "f"(acc[e][0]));
+          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(out.y) : "f"(acc[e][3]), "f"(acc[e][2]));
+          if (r < rows) *reinterpret_cast<uint2*>(p.a.o + row_at[r] + 4 * (at % (HD / 4))) = out;
         }
       }
     }
@@ -866,10 +909,28 @@ cudaError_t run_kv(const KvAttnArgs& a, cudaStream_t st) {
   p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + kCounterBytes);
   p.min_run = 2;
   auto kern = kv_attn_kernel<HD, R>;
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Y::kSmem);
+  static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  kern<<<static_cast<unsigned>(std::min(Y::kCtas * sm_count(), 1024)), Y::kThreads, Y::kSmem, st>>>(tk, tv, p);
-  return cudaGetLastError();
+  const uint64_t bit = uint64_t(1) << (dev & 63);
+  if (!(ready.load(std::memory_order_relaxed) & bit)) {
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Y::kSmem);
+    if (e != cudaSuccess) return e;
+    ready.fetch_or(bit, std::memory_order_relaxed);
+  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(std::min(Y::kCtas * sm_count(), 1024)));
+  cfg.blockDim = dim3(Y::kThreads);
+  cfg.dynamicSmemBytes = Y::kSmem;
+  cfg.stream = st;
+  // the kernel waits by itself for the launch ahead; its first steps run beside that one's end
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, tk, tv, p);
 }
 
 // Rows of a tile: what an average sequence has a key/value head (any number is right).
