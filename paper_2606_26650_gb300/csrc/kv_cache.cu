@@ -20,21 +20,7 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return r;
 }
 
-// Eight consecutive elements (16-byte aligned) to and from fp32.
-__device__ __forceinline__ void load8(const uint16_t* p, float* f) {
-  const uint4 v = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = __uint_as_float(w[i] << 16);
-    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void load8(const float* p, float* f) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-  f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
+// Eight consecutive elements (16-byte aligned) from fp32.
 __device__ __forceinline__ void store8(uint16_t* p, const float* f) {
   *reinterpret_cast<uint4*>(p) = make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
 }
@@ -59,7 +45,77 @@ struct RopeAtArgs {
   bool inverse;
 };
 
-// One thread per (token, unit, run of `hpt` heads): its eight angles serve the run.
+// Eight elements as loaded, kept packed until they are needed.
+template <typename E>
+struct Eight;
+template <>
+struct Eight<uint16_t> {
+  uint4 q;
+  __device__ __forceinline__ void load(const uint16_t* p) { q = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float* f) const {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+};
+template <>
+struct Eight<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = reinterpret_cast<const float4*>(p)[0];
+    b = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void get(float* f) const {
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  }
+};
+
+// Heads h0 .. h1 - 1 of one token, unit q, rotated by angles that are computed once: the first heads' loads go out
+// before the angles, which cover their latency, and always kAhead heads' before any store.
+template <typename E>
+__device__ __forceinline__ void rotate_heads(const E* x, E* y, int32_t h0, int32_t h1, int32_t d, const RotDev& rot,
+                                             int32_t u, const RotUnit& q, int32_t pos, bool inverse) {
+  constexpr int kAhead = sizeof(E) == 2 ? 4 : 2;
+  Eight<E> a[kAhead], b[kAhead];
+  auto load = [&](int32_t h) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (h + k < h1) {
+        a[k].load(x + (h + k) * d + q.a);
+        b[k].load(x + (h + k) * d + q.b);
+      }
+  };
+  load(h0);
+  float c[8], s[8];
+  if (q.turned) rot_angles(rot, u, pos, inverse, c, s);
+  for (int32_t h = h0; h < h1; h += kAhead) {
+    if (h > h0) load(h);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (h + k < h1) {
+        float v[16];
+        a[k].get(v);
+        b[k].get(v + 8);
+        if (q.turned) rot_apply(rot.interleaved != 0, c, s, v);
+        store8(y + (h + k) * d + q.a, v);
+        store8(y + (h + k) * d + q.b, v + 8);
+      }
+  }
+}
+
+// Heads a thread takes at once: the longest run (fewest repeated angles) that still gives every SM a full set of
+// threads.
+int32_t heads_per_thread(int64_t tokens, int32_t nh, int32_t units) {
+  int32_t hpt = 8;
+  while (hpt > 1 && tokens * units * ((nh + hpt - 1) / hpt) < 152 * 2048) hpt /= 2;
+  return hpt;
+}
+
+// One thread per (token, unit, run of `hpt` heads).
 template <typename E>
 __global__ void __launch_bounds__(kThreads) rope_at_vec_kernel(const RopeAtArgs a, int32_t hpt) {
   const int32_t units = a.d / 16, runs = (a.nh + hpt - 1) / hpt;
@@ -67,22 +123,11 @@ __global__ void __launch_bounds__(kThreads) rope_at_vec_kernel(const RopeAtArgs 
   const E* const x = static_cast<const E*>(a.x);
   E* const y = static_cast<E*>(a.y);
   for (int64_t e = blockIdx.x * (int64_t)kThreads + threadIdx.x; e < items; e += (int64_t)gridDim.x * kThreads) {
-    const int32_t u = static_cast<int32_t>(e % units);
-    const int64_t tr = e / units;
-    const int32_t h0 = static_cast<int32_t>(tr % runs) * hpt, h1 = min(h0 + hpt, a.nh);
-    const int64_t t = tr / runs;
+    const int64_t tr = e / units, t = tr / runs;
+    const int32_t u = static_cast<int32_t>(e - tr * units), h0 = static_cast<int32_t>(tr - t * runs) * hpt;
     const RotUnit q = rot_unit(a.rot, u);
     if (!q.turned && a.x == a.y) continue;
-    float c[8], s[8];
-    if (q.turned) rot_angles(a.rot, u, a.pos[t], a.inverse, c, s);
-    for (int32_t h = h0; h < h1; ++h) {
-      float v[16];
-      load8(x + t * a.ldx + h * a.d + q.a, v);
-      load8(x + t * a.ldx + h * a.d + q.b, v + 8);
-      if (q.turned) rot_apply(a.rot.interleaved != 0, c, s, v);
-      store8(y + t * a.ldy + h * a.d + q.a, v);
-      store8(y + t * a.ldy + h * a.d + q.b, v + 8);
-    }
+    rotate_heads(x + t * a.ldx, y + t * a.ldy, h0, min(h0 + hpt, a.nh), a.d, a.rot, u, q, a.pos[t], a.inverse);
   }
 }
 
@@ -158,94 +203,132 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t codes, __half2 by) {
 
 __device__ __forceinline__ void latch_index_error(int32_t* status) { atomicCAS(status, 0, 10 /* CATQ_ERR_INDEX */); }
 
-// Grid (sequence, key heads then value heads then query blocks, share of the sequence's pages): a CTA
-// takes the tokens of one page at a time, twice: once for the largest magnitude, once for the codes.
-__global__ void __launch_bounds__(kThreads) kv_append_kernel(const KvAppendArgs a) {
-  __shared__ uint32_t red[kThreads / 32];
+// Maximum over an item's threads (whole warps).
+template <int W>
+__device__ __forceinline__ uint32_t item_max(uint32_t v, uint32_t* red) {
+  v = __reduce_max_sync(0xffffffffu, v);
+  if constexpr (W > 1) {
+    __syncthreads();  // red is free
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) v = max(v, red[w]);
+  }
+  return v;
+}
+
+// An item is the new tokens of one page and head, keys or values: W warps hold its units (16 elements of a token), kHeld
+// a thread, in registers between the search for the largest magnitude and the codes; an item of more units is read (and
+// rotated) twice.  Grid (sequence, items then shares of the queries).  W = 1 serves calls of a token or a few a sequence:
+// many items of little work, and no barrier; W = 8 whole pages.
+// Bound by HBM where prompts are appended (an element read in 16 bits, written in 8, queries read and written), by
+// latency where tokens are: row offsets, then page number, then scale.
+template <int W, int kHeld>
+__global__ void __launch_bounds__(kThreads, 2) kv_append_kernel(const KvAppendArgs a, int32_t zkv, int32_t zq, int32_t hpt) {
+  constexpr int kItemThreads = 32 * W;
+  __shared__ uint32_t red[W];
+  grid_launch_dependents();
+  grid_dependency_wait();
   const int b = blockIdx.x;
+  const int32_t tid = threadIdx.x % kItemThreads;
   const int64_t r0 = a.row_start[b], r1 = a.row_start[b + 1];
   const int32_t len = a.seq_len[b];
-  if (r0 < 0 || r1 < r0 || r1 > a.T || len < 0 || len > static_cast<int64_t>(a.cache.max_pages) * a.cache.page) {
+  const int32_t d = a.cache.d, nkv = a.cache.nkv, page = a.cache.page, units = d / 16;
+  if (r0 < 0 || r1 < r0 || r1 > a.T || len < 0 || len > a.cache.max_pages * page) {
     if (threadIdx.x == 0) latch_index_error(a.status);
     return;
   }
   const int32_t n = static_cast<int32_t>(r1 - r0), first = len - n;  // position of the sequence's row r0
-  const int32_t d = a.cache.d, nkv = a.cache.nkv, page = a.cache.page, units = d / 16;
-  if (static_cast<int>(blockIdx.y) >= 2 * nkv) {  // queries
-    const int32_t per = a.nh * units;
-    for (int64_t e = (blockIdx.z * static_cast<int64_t>(gridDim.y - 2 * nkv) + blockIdx.y - 2 * nkv) * kThreads +
-                     threadIdx.x;
-         e < static_cast<int64_t>(n) * per; e += static_cast<int64_t>(gridDim.z) * (gridDim.y - 2 * nkv) * kThreads) {
-      const int32_t i = static_cast<int32_t>(e / per), hu = static_cast<int32_t>(e % per), u = hu % units;
+  const int32_t item_blocks = gridDim.y - zq;
+  if (static_cast<int>(blockIdx.y) >= item_blocks) {  // queries
+    const int32_t runs = (a.nh + hpt - 1) / hpt, per = runs * units;
+    const int64_t items = static_cast<int64_t>(n) * per;
+    for (int64_t e = static_cast<int64_t>(blockIdx.y - item_blocks) * kThreads + threadIdx.x; e < items;
+         e += static_cast<int64_t>(zq) * kThreads) {
+      const int32_t i = static_cast<int32_t>(e / per), ru = static_cast<int32_t>(e - static_cast<int64_t>(i) * per);
+      const int32_t run = ru / units, u = ru - run * units;
       const RotUnit q = rot_unit(a.rot, u);
-      const uint16_t* const x = a.q + (r0 + i) * a.ldq + (hu / units) * d;
-      uint16_t* const y = a.q_out + (r0 + i) * a.ldqo + (hu / units) * d;
-      float v[16], c[8], s[8];
-      load8(x + q.a, v);
-      load8(x + q.b, v + 8);
-      if (q.turned) {
-        rot_angles(a.rot, u, first + i, false, c, s);
-        rot_apply(a.rot.interleaved != 0, c, s, v);
-      }
-      store8(y + q.a, v);
-      store8(y + q.b, v + 8);
+      if (!q.turned && a.q == a.q_out) continue;
+      rotate_heads(a.q + (r0 + i) * a.ldq, a.q_out + (r0 + i) * a.ldqo, run * hpt, min(run * hpt + hpt, a.nh), d, a.rot,
+                   u, q, first + i, false);
     }
     return;
   }
-  const bool is_v = static_cast<int>(blockIdx.y) >= nkv;
-  const int32_t h = blockIdx.y - (is_v ? nkv : 0);
-  const uint16_t* const src = is_v ? a.v : a.k;
+  // item: share of the sequence's pages, head, keys or values
+  const int32_t item = blockIdx.y * (kThreads / kItemThreads) + threadIdx.x / kItemThreads;
+  const int32_t z = item / (2 * nkv), hv = item - z * 2 * nkv;
+  if (z >= zkv) return;
+  const bool is_v = hv >= nkv;
+  const int32_t h = hv - (is_v ? nkv : 0);
   const int64_t ld = is_v ? a.ldv : a.ldk;
+  const uint16_t* const src = (is_v ? a.v : a.k) + r0 * ld + h * d;
   uint8_t* const codes = is_v ? a.cache.v_codes : a.cache.k_codes;
   float* const scales = is_v ? a.cache.v_scale : a.cache.k_scale;
-  // the units of a row: values behind no rotation
   RotDev rot = a.rot;
   if (is_v) rot.rot = 0;
   const int32_t p0 = max(first, 0);
-  for (int32_t pg = p0 / page + blockIdx.z; pg * page < len; pg += gridDim.z) {
+  for (int32_t pg = p0 / page + z; pg * page < len; pg += zkv) {
     const int32_t lo = max(p0, pg * page), hi = min(len, (pg + 1) * page);
     const int32_t id = a.cache.table[static_cast<int64_t>(b) * a.cache.max_pages + pg];
+    const int32_t kept = lo - pg * page, items = (hi - lo) * units;
+    Eight<uint16_t> va[kHeld], vb[kHeld];
+    auto fetch = [&](int32_t e, Eight<uint16_t>& x, Eight<uint16_t>& y) {
+      const int32_t i = e / units;
+      const RotUnit q = rot_unit(rot, e - i * units);
+      const uint16_t* const row = src + (lo - first + i) * ld;
+      x.load(row + q.a);
+      y.load(row + q.b);
+    };
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+      if (tid + k * kItemThreads < items) fetch(tid + k * kItemThreads, va[k], vb[k]);
     if (id < 0 || id >= a.cache.n_pages) {
-      if (threadIdx.x == 0) latch_index_error(a.status);
+      if (tid == 0) latch_index_error(a.status);
       continue;
     }
     const int64_t block = static_cast<int64_t>(id) * nkv + h;
     uint8_t* const dst = codes + block * page * d;
-    const int32_t kept = lo - pg * page, items = (hi - lo) * units;
     const float old = kept > 0 ? scales[block] : 0.0f;
-    auto row = [&](int32_t e, float (&v)[16]) -> RotUnit {
+    // a unit's values
+    auto turn = [&](int32_t e, const Eight<uint16_t>& x, const Eight<uint16_t>& y, float (&v)[16]) {
+      x.get(v);
+      y.get(v + 8);
       const int32_t i = e / units, u = e - i * units;
-      const RotUnit q = rot_unit(rot, u);
-      const uint16_t* const x = src + (r0 + lo - first + i) * ld + h * d;
-      load8(x + q.a, v);
-      load8(x + q.b, v + 8);
-      if (q.turned) {
+      if (16 * u < rot.rot) {
         float c[8], s[8];
         rot_angles(rot, u, lo + i, false, c, s);
         rot_apply(rot.interleaved != 0, c, s, v);
       }
-      return q;
     };
-    uint32_t top = 0;
-    for (int32_t e = threadIdx.x; e < items; e += kThreads) {
-      float v[16];
-      row(e, v);
+    auto largest = [](const float (&v)[16], uint32_t top) {
 #pragma unroll
       for (int j = 0; j < 16; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-    }
-    top = __reduce_max_sync(0xffffffffu, top);
-    __syncthreads();  // red is free
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = top;
-    __syncthreads();
+      return top;
+    };
+    uint32_t top = 0;
+    float v[kHeld][16];
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) top = max(top, red[w]);
+    for (int k = 0; k < kHeld; ++k)
+      if (tid + k * kItemThreads < items) {
+        turn(tid + k * kItemThreads, va[k], vb[k], v[k]);
+        top = largest(v[k], top);
+      }
+    for (int32_t e = tid + kHeld * kItemThreads; e < items; e += kItemThreads) {
+      Eight<uint16_t> x, y;
+      float more[16];
+      fetch(e, x, y);
+      turn(e, x, y, more);
+      top = largest(more, top);
+    }
+    top = item_max<W>(top, red);
     const float want = scale_of(top);
     const bool bad = !(want == want) || !(old == old);
     const float now = bad ? __uint_as_float(0x7fffffffu) : fmaxf(old, want);
-    if (threadIdx.x == 0) scales[block] = now;
-    if (!bad && kept > 0 && old > 0.0f && now > old) {
+    if constexpr (W == 1) __syncwarp();  // (every thread has read the old scale: with more warps, item_max's barriers)
+    if (tid == 0) scales[block] = now;
+    if (!bad && old > 0.0f && now > old) {
       const __half2 by = __float2half2_rn(fmaxf(old / now, 5.9604645e-8f));
-      for (int32_t e = threadIdx.x; e < kept * d / 16; e += kThreads) {
+      for (int32_t e = tid; e < kept * d / 16; e += kItemThreads) {
         uint4 w = reinterpret_cast<const uint4*>(dst)[e];
         w.x = rescale4(w.x, by);
         w.y = rescale4(w.y, by);
@@ -256,16 +339,26 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const KvAppendArgs 
     }
     // a page that holds what is not finite has NaN as its scale, and finite codes
     const float by = bad ? 0.0f : (now > 0.0f ? 1.0f / now : 1.0f);
-    for (int32_t e = threadIdx.x; e < items; e += kThreads) {
-      float v[16];
-      const RotUnit q = row(e, v);
+    auto put = [&](int32_t e, float (&f)[16]) {
+      const int32_t i = e / units;
+      const RotUnit q = rot_unit(rot, e - i * units);
+      uint8_t* const at = dst + (kept + i) * d;
       if (bad) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = 0.0f;
+        for (int j = 0; j < 16; ++j) f[j] = 0.0f;
       }
-      uint8_t* const at = dst + (kept + e / units) * d;
-      *reinterpret_cast<uint2*>(at + q.a) = codes8(v, by);
-      *reinterpret_cast<uint2*>(at + q.b) = codes8(v + 8, by);
+      *reinterpret_cast<uint2*>(at + q.a) = codes8(f, by);
+      *reinterpret_cast<uint2*>(at + q.b) = codes8(f + 8, by);
+    };
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+      if (tid + k * kItemThreads < items) put(tid + k * kItemThreads, v[k]);
+    for (int32_t e = tid + kHeld * kItemThreads; e < items; e += kItemThreads) {
+      Eight<uint16_t> x, y;
+      float more[16];
+      fetch(e, x, y);
+      turn(e, x, y, more);
+      put(e, more);
     }
   }
 }
@@ -283,8 +376,7 @@ cudaError_t launch_rope_at(const void* x, int64_t ldx, void* y, int64_t ldy, boo
   const bool vec = d % 16 == 0 && rot.rot % 16 == 0 && ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y)) & 15u) == 0 &&
                    ldx * e % 16 == 0 && ldy * e % 16 == 0;
   if (vec) {
-    int32_t hpt = 8;
-    while (hpt > 1 && T * (d / 16) * ((nh + hpt - 1) / hpt) < 152 * 2048) hpt /= 2;
+    const int32_t hpt = heads_per_thread(T, nh, d / 16);
     const int grid = grid_for(T * (d / 16) * ((nh + hpt - 1) / hpt));
     if (f32)
       rope_at_vec_kernel<float><<<grid, kThreads, 0, st>>>(a, hpt);
@@ -304,11 +396,28 @@ cudaError_t launch_kv_append(KvAppendArgs a, cudaStream_t st) {
   WaitCtl wc;
   if (!launch_wait_ctl(&wc)) return cudaErrorInvalidDevice;
   a.status = wc.status_word;
-  // shares of a sequence's pages: what an average sequence touches, and one (any number is right)
-  const int64_t z = std::min<int64_t>(a.T / (static_cast<int64_t>(a.B) * a.cache.page) + 1, 1024);
-  const int32_t qblocks = a.q ? std::max(1, a.nh * (a.cache.d / 16) / 64) : 0;
-  kv_append_kernel<<<dim3(a.B, 2 * a.cache.nkv + qblocks, static_cast<unsigned>(z)), kThreads, 0, st>>>(a);
-  return cudaGetLastError();
+  // shares of a sequence's pages and queries: what an average sequence has of them (any number is right)
+  const int32_t units = a.cache.d / 16;
+  const int64_t each = (a.T + a.B - 1) / a.B;
+  const int32_t zkv = static_cast<int32_t>(std::min<int64_t>((each + a.cache.page - 1) / a.cache.page, 32768 / (2 * a.cache.nkv)));
+  const int32_t hpt = a.q ? heads_per_thread(a.T, a.nh, units) : 1, runs = a.q ? (a.nh + hpt - 1) / hpt : 0;
+  const int32_t zq = a.q ? static_cast<int32_t>(std::min<int64_t>((each * runs * units + kThreads - 1) / kThreads, 4096)) : 0;
+  // a warp for an item of up to 8 tokens, the CTA for longer ones (64 sequences, 32 / 8 heads of 128, one token each:
+  // TODO us against TODO)
+  const bool narrow = each <= 8;
+  const int32_t items = 2 * a.cache.nkv * zkv, blocks = narrow ? (items + kThreads / 32 - 1) / (kThreads / 32) : items;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(a.B), static_cast<unsigned>(blocks + zq));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};  // the kernel waits by itself for the launch ahead
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (narrow) return cudaLaunchKernelEx(&cfg, kv_append_kernel<1, 2>, a, zkv, zq, hpt);
+  return a.cache.page * units <= 2 * kThreads ? cudaLaunchKernelEx(&cfg, kv_append_kernel<8, 2>, a, zkv, zq, hpt)
+                                              : cudaLaunchKernelEx(&cfg, kv_append_kernel<8, 4>, a, zkv, zq, hpt);
 }
 
 }  // namespace catq

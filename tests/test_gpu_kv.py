@@ -135,3 +135,198 @@ def test_attention_matches_oracle(device, d, nh, nkv, page, lens, news):
     q = r.standard_normal((rs[-1], nh, d)) * 2.0
     got, lse = attend(paged, rs, lens, q, nh, device)
     check_attention(paged, rs, np.array(lens), q, nh, got, lse)
+
+
+# ------------------------------------------------------------------ rotary positions
+
+def rope_bound(x, freq, interleaved, magnitude):
+    """2^-22 (|a| + |b|) magnitude for the elements of a pair, 0 for the others."""
+    out = np.zeros(x.shape)
+    half = len(freq)
+    for i in range(half):
+        a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
+        out[..., a] = out[..., b] = 2.0 ** -22 * magnitude * (np.abs(x[..., a]) + np.abs(x[..., b]))
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,nh,d,rot,interleaved,scaling,gap,far", [
+    (1, 1, 128, 128, False, "plain", 0, 1),          # position 0: nothing turns
+    (1, 3, 64, 32, True, "plain", 0, 1 << 20),       # far positions
+    (67, 5, 128, 128, False, "bands", 64, 131072),   # rows apart
+    (33, 9, 128, 64, True, "yarn", 0, 131072),       # part of the head, a magnitude
+    (20, 2, 96, 48, False, "linear", 8, 4096),
+    (19, 3, 40, 20, False, "plain", 0, 4096),        # sizes off the vector path
+    (19, 3, 10, 6, True, "plain", 3, 4096),          # rows of odd alignment
+    (300, 32, 64, 64, True, "plain", 0, 2 ** 31 - 1),
+])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rope_at_matches_oracle(device, dtype, T, nh, d, rot, interleaved, scaling, gap, far, inverse):
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(4, f"rope/{T}/{nh}/{d}/{rot}")
+    kw = dict(factor=8.0, low=1.0, high=32.0 if scaling == "yarn" else 4.0, original=8192.0)
+    freq, magnitude = K.frequencies(rot, 500000.0, scaling, **kw)
+    rope = C.Rope.create(rot, 500000.0, device, C.ROPE_INTERLEAVED if interleaved else C.ROPE_HALF,
+                         ["plain", "linear", "bands", "yarn"].index(scaling), **kw)
+    x = r.standard_normal((T, nh, d)).astype(np.float32)
+    x = syn.round_bf16(x) if dtype == "bf16" else x
+    pos = r.integers(0, far, T)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    whole = torch.full((T, nh * d + gap), 5.0, dtype=dt, device=device)
+    X = whole[:, :nh * d]
+    X.copy_(U.to_device(x.reshape(T, nh * d), dtype, device))
+    Y = torch.empty(T, nh * d, dtype=dt, device=device)
+    C.catq_rope_at(X, i32(pos, device), rope, nh, d, Y, inverse=inverse)
+    want = K.rope(x, pos, freq, interleaved, magnitude, inverse)
+    # positions below 2^31 and turns to 2^-62: the angle is off by 2^-31 turns at most (none of the near ones)
+    bound = rope_bound(x, freq, interleaved, magnitude) * (1 + far * 2.0 ** -62 * 2 * np.pi * 2.0 ** 22)
+    bound += np.abs(want) * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24)
+    got = Y.float().cpu().numpy().reshape(T, nh, d)
+    assert (np.abs(got - want) <= bound).all(), (np.abs(got - want) - bound).max()
+    C.catq_rope_at(X, i32(pos, device), rope, nh, d, inverse=inverse)  # in place
+    assert torch.equal(X, Y) and (whole[:, nh * d:] == 5).all()
+    assert C.catq_device_status() == 0
+
+
+def test_rope_backward_is_the_gradient(device):
+    """<dY, rope(X)> has the gradient rope_at(dY, inverse) in X: against the formula's transpose and central differences
+    of the fp64 oracle."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(5, "rope/grad")
+    T, nh, d, rot = 7, 2, 32, 16
+    freq, magnitude = K.frequencies(rot, 10000.0, "yarn", factor=4.0, low=1.0, high=32.0, original=64.0)
+    rope = C.Rope.create(rot, 10000.0, device, C.ROPE_INTERLEAVED, C.ROPE_YARN, factor=4.0, low=1.0, high=32.0,
+                         original=64.0)
+    x, dy = r.standard_normal((2, T, nh, d))
+    dy = dy.astype(np.float32)
+    pos = np.arange(T) * 37
+    dX = torch.empty(T, nh * d, device=device)
+    C.catq_rope_at(U.to_device(dy.reshape(T, -1), "f32", device), i32(pos, device), rope, nh, d, dX, inverse=True)
+    got = dX.cpu().numpy().reshape(T, nh, d)
+    h = 1e-3
+    for at in [(0, 0, 0), (3, 1, 5), (6, 0, 14), (6, 1, 15), (2, 1, 31)]:
+        e = np.zeros_like(x)
+        e[at] = h
+        num = ((K.rope(x + e, pos, freq, True, magnitude) - K.rope(x - e, pos, freq, True, magnitude)) * dy).sum() / (2 * h)
+        assert abs(got[at] - num) <= 2.0 ** -21 * magnitude * np.abs(dy[at[:2]]).sum() + 1e-9
+
+
+# ------------------------------------------------------------------ append
+
+@pytest.mark.parametrize("d,nkv,nh,page,lens,news,rot,interleaved", [
+    (128, 2, 4, 64, [1], [1], 128, False),                      # the first token of a sequence
+    (128, 2, 2, 64, [64, 65, 130], [1, 1, 1], 128, False),      # the last of a page, the first of one, one inside
+    (64, 3, 6, 16, [7, 16, 17, 40, 3], [1, 1, 1, 1, 1], 16, True),
+    (128, 1, 5, 128, [200, 128], [150, 128], 128, False),       # whole pages, beginning and ending inside
+    (64, 4, 4, 16, [50, 33, 90], [37, 1, 90], 32, True),
+    (64, 2, 2, 32, [9, 12], [9, 3], 0, False),                  # no rotation
+    (128, 3, 3, 64, [70], [9], 64, True),
+    (64, 1, 1, 128, [300, 20], [290, 20], 64, False),
+])
+@pytest.mark.parametrize("kind", ["normal", "quiet", "growing"])
+def test_append_matches_oracle(device, d, nkv, nh, page, lens, news, rot, interleaved, kind):
+    """kind: values like the cached ones; far smaller (old scales stay, e4m3's subnormals); far larger (the codes of
+    open pages are rounded again)."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(6, f"append/{d}/{nkv}/{page}/{lens}/{news}/{kind}")
+    paged = Paged(r, lens, nkv, page, d, device)
+    rs, T = starts(news), int(sum(news))
+    gain = {"normal": 1.0, "quiet": 2.0 ** -9, "growing": 64.0}[kind]
+    k, v = (syn.round_bf16((r.standard_normal((T, nkv, d)) * gain).astype(np.float32)) for _ in range(2))
+    v[0, 0] = 0.0  # a row of zeros
+    q = syn.round_bf16(r.standard_normal((T, nh, d)).astype(np.float32))
+    freq, rope = np.zeros(0), None
+    if rot:
+        freq, _ = K.frequencies(rot, 10000.0)
+        rope = C.Rope.create(rot, 10000.0, device, C.ROPE_INTERLEAVED if interleaved else C.ROPE_HALF)
+    fused = torch.empty(T, 2 * nkv * d + 16, dtype=torch.bfloat16, device=device)
+    Kt, Vt = fused[:, :nkv * d], fused[:, nkv * d:2 * nkv * d]
+    Kt.copy_(bf16(k.reshape(T, -1), device))
+    Vt.copy_(bf16(v.reshape(T, -1), device))
+    Q = bf16(q.reshape(T, -1), device)
+    Qo = torch.empty_like(Q)
+    C.catq_kv_append(paged.cache, i32(rs, device), i32(lens, device), Kt, Vt, rope=rope, Q=Q, Q_out=Qo, n_heads=nh)
+    torch.cuda.synchronize()
+    assert C.catq_device_status() == 0
+    pos = np.concatenate([np.arange(n - m, n) for n, m in zip(lens, news)])
+    codes, scale = paged.host()
+    want_q = K.rope(q, pos, freq, interleaved)
+    off = np.abs(Qo.float().cpu().numpy().reshape(T, nh, d) - want_q)
+    assert (off <= rope_bound(q, freq, interleaved, 1.0) + 2.0 ** -8 * np.abs(want_q)).all()
+    K.append(paged.codes[1], paged.scale[1], paged.table, page, rs, lens, v.astype(np.float64))
+    assert np.array_equal(scale[1], paged.scale[1])
+    assert np.array_equal(K.E4M3[codes[1]], K.E4M3[paged.codes[1]])
+    # keys: the nearest code to the rotated value, within the rotation's error; what is not new as the values' codes
+    rotated = K.rope(k, pos, freq, interleaved)
+    asked = K.append(paged.codes[0], paged.scale[0], paged.table, page, rs, lens, rotated)
+    assert np.array_equal(scale[0], paged.scale[0])
+    new = ~np.isnan(asked)
+    assert np.array_equal(K.E4M3[codes[0]][~new], K.E4M3[paged.codes[0]][~new])
+    slack = np.full(codes[0].shape, np.nan)
+    err, r0 = rope_bound(k, freq, interleaved, 1.0), 0
+    for b, (n, m) in enumerate(zip(lens, news)):
+        for i in range(m):
+            p, at = paged.table[b][(n - m + i) // page], (n - m + i) % page
+            slack[p, :, at] = err[r0 + i] / np.maximum(scale[0][p], 1e-300)[:, None]
+        r0 += m
+    got = K.E4M3[codes[0]][new]
+    assert (np.abs(got - asked[new]) <= K.half_step(asked[new]) * (1 + 2.0 ** -20) + slack[new]).all()
+
+
+def test_append_then_attention_then_packed_linear(device):
+    """Decoding as it is used: a prompt of unequal lengths is appended, then tokens one by one, each with attention over
+    the cache and the packed output projection; the oracle walks its own cache beside it."""
+    import torch
+
+    from oracle import catq_oracle as O
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(7, "kv/loop")
+    nh, nkv, d, page, B, H, g = 8, 2, 64, 16, 3, 192, 128
+    N, Kdim = H, nh * d
+    W = syn.round_bf16(r.standard_normal((N, Kdim)).astype(np.float32) * 0.02)
+    layer = C.Layer.create(U.to_device(W, "bf16", device), g)
+    C.catq_group_stats(layer)
+    codes = torch.empty(N * Kdim // 4, dtype=torch.uint8, device=device)
+    alpha = torch.empty(N * Kdim // g, dtype=torch.float32, device=device)
+    C.catq_hard_ternarize_pack(layer, codes, alpha)
+    freq, _ = K.frequencies(d, 10000.0)
+    rope = C.Rope.create(d, 10000.0, device)
+    prompt = np.array([21, 5, 40])
+    steps = 4
+    paged = Paged(r, prompt + steps, nkv, page, d, device)
+    lens = i32(prompt, device)
+    ws = C.kv_attention_workspace(paged.cache, nh)
+    for step in range(steps + 1):
+        news = prompt if step == 0 else np.ones(3, np.int64)
+        now = prompt + step
+        rs, T = starts(news), int(news.sum())
+        q, k, v = (syn.round_bf16(r.standard_normal((T, h, d)).astype(np.float32)) for h in (nh, nkv, nkv))
+        Q = bf16(q.reshape(T, -1), device)
+        Kt, Vt = bf16(k.reshape(T, -1), device), bf16(v.reshape(T, -1), device)
+        if step:
+            lens += 1
+        row_start = i32(rs, device)
+        C.catq_kv_append(paged.cache, row_start, lens, Kt, Vt, rope=rope, Q=Q, n_heads=nh)
+        A = torch.empty(T, nh * d, dtype=torch.bfloat16, device=device)
+        C.catq_kv_attention(paged.cache, row_start, lens, Q, A, nh, ws)
+        last = A[[int(e) - 1 for e in rs[1:]]].contiguous()
+        Y = torch.empty(B, N, dtype=torch.bfloat16, device=device)
+        C.catq_ternary_infer(codes, alpha, N, Kdim, g, last, Y)
+        torch.cuda.synchronize()
+        assert C.catq_device_status() == 0
+        pos = np.concatenate([np.arange(n - m, n) for n, m in zip(now, news)])
+        K.append(paged.codes[0], paged.scale[0], paged.table, page, rs, now, K.rope(k, pos, freq, False))
+        K.append(paged.codes[1], paged.scale[1], paged.table, page, rs, now, v.astype(np.float64))
+        assert np.array_equal(K.E4M3[paged.host()[0][1]], K.E4M3[paged.codes[1]])
+        paged.codes[0], paged.scale[0] = paged.host()[0][0], paged.host()[1][0]  # a key on a border may differ
+        want, _, _, _ = K.attention(*paged.codes, *paged.scale, paged.table, page, rs, now,
+                                    Q.float().cpu().numpy().reshape(T, nh, d), T, nh)
+        assert U.fro_rel(A.float().cpu().numpy(), want.reshape(T, -1)) <= 2.0 ** -7
+        want_y = O.ternary_infer(U.to_host(codes), U.to_host(alpha), N, Kdim, g, U.to_host(last))
+        assert U.fro_rel(U.to_host(Y), want_y) <= U.TOL_BF16
