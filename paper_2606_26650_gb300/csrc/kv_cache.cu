@@ -90,8 +90,8 @@ __device__ __forceinline__ void rotate_heads(const E* x, E* y, int32_t h0, int32
       }
   };
   load(h0);
-  float c[8], s[8];
-  if (q.turned) rot_angles(rot, u, pos, inverse, c, s);
+  RotAngles ang;
+  if (q.turned) rot_angles(rot, u, pos, inverse, ang);
   for (int32_t h = h0; h < h1; h += kAhead) {
     if (h > h0) load(h);
 #pragma unroll
@@ -100,7 +100,7 @@ __device__ __forceinline__ void rotate_heads(const E* x, E* y, int32_t h0, int32
         float v[16];
         a[k].get(v);
         b[k].get(v + 8);
-        if (q.turned) rot_apply(rot.interleaved != 0, c, s, v);
+        if (q.turned) rot_apply(rot.interleaved != 0, ang, v);
         store8(y + (h + k) * d + q.a, v);
         store8(y + (h + k) * d + q.b, v + 8);
       }
@@ -115,19 +115,24 @@ int32_t heads_per_thread(int64_t tokens, int32_t nh, int32_t units) {
   return hpt;
 }
 
-// One thread per (token, unit, run of `hpt` heads).
+// One thread per (token, unit, run of `hpt` heads); `part` items a token (below 2^31), a CTA's tokens side by side.
 template <typename E>
-__global__ void __launch_bounds__(kThreads) rope_at_vec_kernel(const RopeAtArgs a, int32_t hpt) {
-  const int32_t units = a.d / 16, runs = (a.nh + hpt - 1) / hpt;
-  const int64_t items = a.T * units * runs;
+__global__ void __launch_bounds__(kThreads, 2) rope_at_vec_kernel(const RopeAtArgs a, int32_t hpt, Divisor by_units,
+                                                                     Divisor by_part, int32_t part) {
+  const int32_t units = a.d / 16;
   const E* const x = static_cast<const E*>(a.x);
   E* const y = static_cast<E*>(a.y);
-  for (int64_t e = blockIdx.x * (int64_t)kThreads + threadIdx.x; e < items; e += (int64_t)gridDim.x * kThreads) {
-    const int64_t tr = e / units, t = tr / runs;
-    const int32_t u = static_cast<int32_t>(e - tr * units), h0 = static_cast<int32_t>(tr - t * runs) * hpt;
+  const int64_t items = a.T * part;
+  for (int64_t e0 = blockIdx.x * (int64_t)kThreads; e0 < items; e0 += (int64_t)gridDim.x * kThreads) {
+    const int64_t t0 = e0 / part;  // (the CTA's first token)
+    const int32_t e = static_cast<int32_t>(e0 - t0 * part) + static_cast<int32_t>(threadIdx.x), over = by_part.of(e);
+    const int64_t t = t0 + over;
+    if (t >= a.T) continue;
+    const int32_t ru = e - over * part, run = by_units.of(ru), u = ru - run * units;
     const RotUnit q = rot_unit(a.rot, u);
     if (!q.turned && a.x == a.y) continue;
-    rotate_heads(x + t * a.ldx, y + t * a.ldy, h0, min(h0 + hpt, a.nh), a.d, a.rot, u, q, a.pos[t], a.inverse);
+    rotate_heads(x + t * a.ldx, y + t * a.ldy, run * hpt, min(run * hpt + hpt, a.nh), a.d, a.rot, u, q, a.pos[t],
+                 a.inverse);
   }
 }
 
@@ -150,9 +155,8 @@ __global__ void __launch_bounds__(kThreads) rope_at_kernel(const RopeAtArgs a) {
       continue;
     }
     float c, s;
-    rot_cos_sin(a.pos[t], a.rot.turns[j], c, s);
-    c *= a.rot.magnitude;
-    s *= a.inverse ? -a.rot.magnitude : a.rot.magnitude;
+    rot_cos_sin(a.pos[t], a.rot.turns[j], a.rot.magnitude, c, s);
+    if (a.inverse) s = -s;
     const int32_t i0 = a.rot.interleaved ? 2 * j : j, i1 = a.rot.interleaved ? 2 * j + 1 : j + half;
     const float p = load1(xr + i0), q = load1(xr + i1);
     store1(yr + i0, p * c - q * s);
@@ -223,9 +227,10 @@ __device__ __forceinline__ uint32_t item_max(uint32_t v, uint32_t* red) {
 // many items of little work, and no barrier; W = 8 whole pages.
 // Bound by HBM where prompts are appended (an element read in 16 bits, written in 8, queries read and written), by
 // latency where tokens are: row offsets, then page number, then scale.
-template <int W, int kHeld>
-__global__ void __launch_bounds__(kThreads, 2) kv_append_kernel(const KvAppendArgs a, int32_t zkv, int32_t zq, int32_t hpt) {
-  constexpr int kItemThreads = 32 * W;
+template <int D, int W, int kHeld>
+__global__ void __launch_bounds__(kThreads, 2) kv_append_kernel(const KvAppendArgs a, int32_t zkv, int32_t zq, int32_t hpt,
+                                                                Divisor by_part, Divisor by_page) {
+  constexpr int kItemThreads = 32 * W, d = D, units = D / 16;
   __shared__ uint32_t red[W];
   grid_launch_dependents();
   grid_dependency_wait();
@@ -233,7 +238,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_append_kernel(const KvAppendAr
   const int32_t tid = threadIdx.x % kItemThreads;
   const int64_t r0 = a.row_start[b], r1 = a.row_start[b + 1];
   const int32_t len = a.seq_len[b];
-  const int32_t d = a.cache.d, nkv = a.cache.nkv, page = a.cache.page, units = d / 16;
+  const int32_t nkv = a.cache.nkv, page = a.cache.page;
   if (r0 < 0 || r1 < r0 || r1 > a.T || len < 0 || len > a.cache.max_pages * page) {
     if (threadIdx.x == 0) latch_index_error(a.status);
     return;
@@ -245,7 +250,8 @@ __global__ void __launch_bounds__(kThreads, 2) kv_append_kernel(const KvAppendAr
     const int64_t items = static_cast<int64_t>(n) * per;
     for (int64_t e = static_cast<int64_t>(blockIdx.y - item_blocks) * kThreads + threadIdx.x; e < items;
          e += static_cast<int64_t>(zq) * kThreads) {
-      const int32_t i = static_cast<int32_t>(e / per), ru = static_cast<int32_t>(e - static_cast<int64_t>(i) * per);
+      const int32_t i = e >> 31 ? static_cast<int32_t>(e / per) : by_part.of(static_cast<int32_t>(e));
+      const int32_t ru = static_cast<int32_t>(e - static_cast<int64_t>(i) * per);
       const int32_t run = ru / units, u = ru - run * units;
       const RotUnit q = rot_unit(a.rot, u);
       if (!q.turned && a.q == a.q_out) continue;
@@ -267,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_append_kernel(const KvAppendAr
   RotDev rot = a.rot;
   if (is_v) rot.rot = 0;
   const int32_t p0 = max(first, 0);
-  for (int32_t pg = p0 / page + z; pg * page < len; pg += zkv) {
+  for (int32_t pg = by_page.of(p0) + z; pg * page < len; pg += zkv) {
     const int32_t lo = max(p0, pg * page), hi = min(len, (pg + 1) * page);
     const int32_t id = a.cache.table[static_cast<int64_t>(b) * a.cache.max_pages + pg];
     const int32_t kept = lo - pg * page, items = (hi - lo) * units;
@@ -295,32 +301,33 @@ __global__ void __launch_bounds__(kThreads, 2) kv_append_kernel(const KvAppendAr
       y.get(v + 8);
       const int32_t i = e / units, u = e - i * units;
       if (16 * u < rot.rot) {
-        float c[8], s[8];
-        rot_angles(rot, u, lo + i, false, c, s);
-        rot_apply(rot.interleaved != 0, c, s, v);
+        RotAngles ang;
+        rot_angles(rot, u, lo + i, false, ang);
+        rot_apply(rot.interleaved != 0, ang, v);
       }
     };
-    auto largest = [](const float (&v)[16], uint32_t top) {
+    auto largest = [](const float (&v)[16], float top) {  // (NaN if any is)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+      for (int j = 0; j < 16; ++j)
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(top), "f"(fabsf(v[j])));
       return top;
     };
-    uint32_t top = 0;
+    float most = 0.0f;
     float v[kHeld][16];
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
       if (tid + k * kItemThreads < items) {
         turn(tid + k * kItemThreads, va[k], vb[k], v[k]);
-        top = largest(v[k], top);
+        most = largest(v[k], most);
       }
     for (int32_t e = tid + kHeld * kItemThreads; e < items; e += kItemThreads) {
       Eight<uint16_t> x, y;
       float more[16];
       fetch(e, x, y);
       turn(e, x, y, more);
-      top = largest(more, top);
+      most = largest(more, most);
     }
-    top = item_max<W>(top, red);
+    const uint32_t top = item_max<W>(__float_as_uint(most) & 0x7fffffffu, red);
     const float want = scale_of(top);
     const bool bad = !(want == want) || !(old == old);
     const float now = bad ? __uint_as_float(0x7fffffffu) : fmaxf(old, want);
@@ -377,11 +384,12 @@ cudaError_t launch_rope_at(const void* x, int64_t ldx, void* y, int64_t ldy, boo
                    ldx * e % 16 == 0 && ldy * e % 16 == 0;
   if (vec) {
     const int32_t hpt = heads_per_thread(T, nh, d / 16);
-    const int grid = grid_for(T * (d / 16) * ((nh + hpt - 1) / hpt));
+    const int32_t part = (d / 16) * ((nh + hpt - 1) / hpt);
+    const int grid = grid_for(T * part);
     if (f32)
-      rope_at_vec_kernel<float><<<grid, kThreads, 0, st>>>(a, hpt);
+      rope_at_vec_kernel<float><<<grid, kThreads, 0, st>>>(a, hpt, divisor(d / 16), divisor(part), part);
     else
-      rope_at_vec_kernel<uint16_t><<<grid, kThreads, 0, st>>>(a, hpt);
+      rope_at_vec_kernel<uint16_t><<<grid, kThreads, 0, st>>>(a, hpt, divisor(d / 16), divisor(part), part);
   } else {
     const int grid = grid_for(T * nh * (d - rot.rot / 2));
     if (f32)
@@ -415,9 +423,13 @@ cudaError_t launch_kv_append(KvAppendArgs a, cudaStream_t st) {
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  if (narrow) return cudaLaunchKernelEx(&cfg, kv_append_kernel<1, 2>, a, zkv, zq, hpt);
-  return a.cache.page * units <= 2 * kThreads ? cudaLaunchKernelEx(&cfg, kv_append_kernel<8, 2>, a, zkv, zq, hpt)
-                                              : cudaLaunchKernelEx(&cfg, kv_append_kernel<8, 4>, a, zkv, zq, hpt);
+  const auto go = [&](auto kern) {
+    return cudaLaunchKernelEx(&cfg, kern, a, zkv, zq, hpt, divisor(runs * units), divisor(a.cache.page));
+  };
+  const bool d128 = a.cache.d == 128;
+  if (narrow) return d128 ? go(kv_append_kernel<128, 1, 2>) : go(kv_append_kernel<64, 1, 2>);
+  if (a.cache.page * units <= 2 * kThreads) return d128 ? go(kv_append_kernel<128, 8, 2>) : go(kv_append_kernel<64, 8, 2>);
+  return go(kv_append_kernel<128, 8, 4>);  // pages of 128 tokens of 128 elements
 }
 
 }  // namespace catq

@@ -6,6 +6,8 @@
 
 #include <cstdint>
 
+#include "catq_math.cuh"
+
 namespace catq {
 
 // Device view of catq_rotation.
@@ -16,28 +18,58 @@ struct RotDev {
   float magnitude;        // factor on the rotated elements
 };
 
-// cos and sin of pos * turn.  The product wraps modulo 2^64, which is modulo one turn, so that the angle
-// of a far position is as exact as that of a near one (32-bit floats would lose 2^-24 of the whole angle:
-// 0.008 rad at 131072).  Its upper 32 bits fall into the nearest quarter turn and a rest of at most an
-// eighth, whose sine and cosine are their Taylor series up to x^9 and x^10 (remainders x^11 / 11! and
-// x^12 / 12! at pi / 4: 1.8e-9 and 1.2e-10, under half a unit in the last place).
-__device__ __forceinline__ void rot_cos_sin(int32_t pos, uint64_t turn, float& c, float& s) {
-  const uint32_t frac = static_cast<uint32_t>((static_cast<uint64_t>(static_cast<int64_t>(pos)) * turn) >> 32);
-  const uint32_t quarter = (frac + 0x20000000u) >> 30;
-  const float x = static_cast<float>(static_cast<int32_t>(frac - (quarter << 30))) * 1.4629180792671596e-9f;  // 2 pi / 2^32
-  const float y = x * x;
-  float sn = fmaf(y, 1.0f / 362880.0f, -1.0f / 5040.0f);
-  sn = fmaf(y, sn, 1.0f / 120.0f);
-  sn = fmaf(y, sn, -1.0f / 6.0f);
-  sn = fmaf(x * y, sn, x);
-  float cs = fmaf(y, -1.0f / 3628800.0f, 1.0f / 40320.0f);
-  cs = fmaf(y, cs, -1.0f / 720.0f);
-  cs = fmaf(y, cs, 1.0f / 24.0f);
-  cs = fmaf(y, cs, -0.5f);
-  cs = fmaf(y, cs, 1.0f);
-  const float a = (quarter & 1u) ? sn : cs, b = (quarter & 1u) ? cs : sn;
-  c = ((quarter + 1u) & 2u) ? -a : a;
-  s = (quarter & 2u) ? -b : b;
+// Pairs of fp32 values in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  unpack_f32x2(fma_f32x2(pack_f32x2(a.x, a.y), pack_f32x2(b.x, b.y), pack_f32x2(c.x, c.y)), d.x, d.y);
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  unpack_f32x2(mul_f32x2(pack_f32x2(a.x, a.y), pack_f32x2(b.x, b.y)), d.x, d.y);
+  return d;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// cos and sin, times m, of pos * turn for two pairs.  The product wraps modulo 2^64, which is modulo one turn, so that
+// the angle of a far position is as exact as that of a near one (32-bit floats would lose 2^-24 of the whole angle: 0.008
+// rad at 131072).  Its upper 32 bits fall into the nearest half turn, which is a sign of both, and a rest of at most a
+// quarter, whose sine and cosine are their Taylor series up to x^13 and x^14 (remainders x^15 / 15! and x^16 / 16! at pi / 2:
+// 6.7e-10 and 6.6e-11, far under half a unit in the last place), evaluated for the two pairs at once.  Quarter turns would
+// save three terms and cost twice their instructions in exchanging sine and cosine.
+__device__ __forceinline__ uint32_t turn_of(int32_t pos, uint64_t turn) {
+  const uint32_t lo = static_cast<uint32_t>(turn), hi = static_cast<uint32_t>(turn >> 32);
+  return __umulhi(static_cast<uint32_t>(pos), lo) + static_cast<uint32_t>(pos) * hi - (pos < 0 ? lo : 0u);
+}
+__device__ __forceinline__ void rot_cos_sin2(int32_t pos, uint64_t t0, uint64_t t1, float m, float2& c, float2& s) {
+  const uint32_t f0 = turn_of(pos, t0), f1 = turn_of(pos, t1);
+  const uint32_t h0 = (f0 + 0x40000000u) & 0x80000000u, h1 = (f1 + 0x40000000u) & 0x80000000u;
+  const float2 x = mul2(make_float2(static_cast<float>(static_cast<int32_t>(f0 ^ h0)),
+                                    static_cast<float>(static_cast<int32_t>(f1 ^ h1))),
+                        both(1.4629180792671596e-9f));  // 2 pi / 2^32
+  const float2 y = mul2(x, x);
+  float2 sn = fma2(y, both(1.0f / 6227020800.0f), both(-1.0f / 39916800.0f));
+  sn = fma2(y, sn, both(1.0f / 362880.0f));
+  sn = fma2(y, sn, both(-1.0f / 5040.0f));
+  sn = fma2(y, sn, both(1.0f / 120.0f));
+  sn = fma2(y, sn, both(-1.0f / 6.0f));
+  sn = fma2(mul2(x, y), sn, x);
+  float2 cs = fma2(y, both(-1.0f / 87178291200.0f), both(1.0f / 479001600.0f));
+  cs = fma2(y, cs, both(-1.0f / 3628800.0f));
+  cs = fma2(y, cs, both(1.0f / 40320.0f));
+  cs = fma2(y, cs, both(-1.0f / 720.0f));
+  cs = fma2(y, cs, both(1.0f / 24.0f));
+  cs = fma2(y, cs, both(-0.5f));
+  cs = fma2(y, cs, both(1.0f));
+  const float2 sign = make_float2(__uint_as_float(__float_as_uint(m) ^ h0), __uint_as_float(__float_as_uint(m) ^ h1));
+  c = mul2(cs, sign);
+  s = mul2(sn, sign);
+}
+__device__ __forceinline__ void rot_cos_sin(int32_t pos, uint64_t turn, float m, float& c, float& s) {
+  float2 c2, s2;
+  rot_cos_sin2(pos, turn, turn, m, c2, s2);
+  c = c2.x;
+  s = s2.x;
 }
 
 // A head of d = 16 n elements as units of 16: the two vectors of eight elements that a rotated unit pairs
@@ -56,34 +88,51 @@ __device__ __forceinline__ RotUnit rot_unit(const RotDev& r, int32_t u) {
   return q;
 }
 
-// The unit's eight cosines and sines (times the magnitude; sines negated for the inverse).
-__device__ __forceinline__ void rot_angles(const RotDev& r, int32_t u, int32_t pos, bool inverse, float (&c)[8],
-                                           float (&s)[8]) {
+// The unit's eight cosines and sines (times the magnitude; sines negated for the inverse) by pairs.
+struct RotAngles {
+  float2 c[4], s[4];
+};
+__device__ __forceinline__ void rot_angles(const RotDev& r, int32_t u, int32_t pos, bool inverse, RotAngles& a) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    rot_cos_sin(pos, __ldg(reinterpret_cast<const unsigned long long*>(r.turns) + 8 * u + j), c[j], s[j]);
-    c[j] *= r.magnitude;
-    s[j] *= inverse ? -r.magnitude : r.magnitude;
+  for (int j = 0; j < 4; ++j) {
+    const auto* t = reinterpret_cast<const unsigned long long*>(r.turns) + 8 * u + 2 * j;
+    rot_cos_sin2(pos, __ldg(t), __ldg(t + 1), r.magnitude, a.c[j], a.s[j]);
+    if (inverse) a.s[j] = make_float2(-a.s[j].x, -a.s[j].y);
   }
 }
 
+// (p, q) of two pairs rotated in place.
+__device__ __forceinline__ void rot_pairs(float2 c, float2 s, float& p0, float& p1, float& q0, float& q1) {
+  const float2 p = make_float2(p0, p1), q = make_float2(q0, q1);
+  const float2 o = fma2(q, make_float2(-s.x, -s.y), mul2(p, c)), w = fma2(q, c, mul2(p, s));
+  p0 = o.x; p1 = o.y;
+  q0 = w.x; q1 = w.y;
+}
+
 // x[0..7] and x[8..15] (the unit's vectors a and b) rotated in place.
-__device__ __forceinline__ void rot_apply(bool interleaved, const float (&c)[8], const float (&s)[8], float (&x)[16]) {
-  if (interleaved) {
+__device__ __forceinline__ void rot_apply(bool interleaved, const RotAngles& a, float (&x)[16]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float p = x[2 * j], q = x[2 * j + 1];
-      x[2 * j] = p * c[j] - q * s[j];
-      x[2 * j + 1] = p * s[j] + q * c[j];
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float p = x[j], q = x[j + 8];
-      x[j] = p * c[j] - q * s[j];
-      x[j + 8] = p * s[j] + q * c[j];
-    }
+  for (int j = 0; j < 4; ++j) {
+    if (interleaved)
+      rot_pairs(a.c[j], a.s[j], x[4 * j], x[4 * j + 2], x[4 * j + 1], x[4 * j + 3]);
+    else
+      rot_pairs(a.c[j], a.s[j], x[2 * j], x[2 * j + 1], x[2 * j + 8], x[2 * j + 9]);
   }
+}
+
+// n / d for 0 <= n < 2^31 by one product: m = floor(2^(31 + l) / d) + 1 with l = ceil(log2 d), so that n m / 2^(31 + l)
+// exceeds n / d by less than 1 / d.
+struct Divisor {
+  uint32_t m, shift;  // d == 1: m == 0
+  __device__ __forceinline__ int32_t of(int32_t n) const {
+    return m == 0u ? n : static_cast<int32_t>(__umulhi(static_cast<uint32_t>(n), m) >> shift);
+  }
+};
+inline Divisor divisor(int32_t d) {
+  if (d <= 1) return Divisor{0u, 0u};
+  uint32_t l = 0;
+  while ((int64_t(1) << l) < d) ++l;
+  return Divisor{static_cast<uint32_t>((uint64_t(1) << (31 + l)) / static_cast<uint64_t>(d) + 1), l - 1};
 }
 
 }  // namespace catq
