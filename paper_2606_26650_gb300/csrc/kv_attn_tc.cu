@@ -204,37 +204,43 @@ __host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t M, uint32_t N, bool a
   return (1u << 4) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);
 }
 
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
-          taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// A group's hi and lo columns (its CH rows, lo R columns behind hi) at `base`.
-template <int R, int CH>
-__device__ __forceinline__ void load_cols(uint32_t base, uint32_t (&v)[2 * CH]) {
-  if constexpr (CH < 16) {
-    tmem_ld16(base, v);
-  } else {
-    uint32_t(&hi)[16] = *reinterpret_cast<uint32_t(*)[16]>(&v[0]);
-    uint32_t(&lo)[16] = *reinterpret_cast<uint32_t(*)[16]>(&v[16]);
-    tmem_ld16(base, hi);
-    tmem_ld16(base + R, lo);
-  }
-  tmem_ld_wait();
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
 }
-template <int R, int CH>
-__device__ __forceinline__ void store_cols(uint32_t base, const uint32_t (&v)[2 * CH]) {
-  if constexpr (CH < 16) {
-    tmem_st16(base, v);
-  } else {
-    tmem_st16(base, *reinterpret_cast<const uint32_t(*)[16]>(&v[0]));
-    tmem_st16(base + R, *reinterpret_cast<const uint32_t(*)[16]>(&v[16]));
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+
+// Eight rows' products from their hi columns at `base` and their lo columns R behind: hi + lo / 16, by pairs.
+template <int R>
+__device__ __forceinline__ void load_rows8(uint32_t base, float2 (&t)[4]) {
+  uint32_t hi[8], lo[8];
+  tmem_ld8(base, hi);
+  tmem_ld8(base + R, lo);
+  tmem_ld_wait();
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    t[i] = fma2(make_float2(__uint_as_float(lo[2 * i]), __uint_as_float(lo[2 * i + 1])), both(kLoUnit),
+                make_float2(__uint_as_float(hi[2 * i]), __uint_as_float(hi[2 * i + 1])));
+}
+// Eight columns at `base` times f.
+__device__ __forceinline__ void scale_cols8(uint32_t base, const float2 (&f)[4]) {
+  uint32_t v[8];
+  tmem_ld8(base, v);
+  tmem_ld_wait();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 w = mul2(make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), f[i]);
+    v[2 * i] = __float_as_uint(w.x);
+    v[2 * i + 1] = __float_as_uint(w.y);
   }
+  tmem_st8(base, v);
 }
 
 __device__ __forceinline__ void bar_sync(int id, int threads) {
@@ -264,14 +270,13 @@ __device__ __forceinline__ void warp_rows(float (&v)[CH], int lane) {
   }
 }
 
-// n floats of shared memory (16-byte aligned).
-template <int N>
-__device__ __forceinline__ void load_row(const float* p, float (&v)[N]) {
-#pragma unroll
-  for (int i = 0; i < N / 4; ++i) {
-    const float4 q = reinterpret_cast<const float4*>(p)[i];
-    v[4 * i] = q.x; v[4 * i + 1] = q.y; v[4 * i + 2] = q.z; v[4 * i + 3] = q.w;
-  }
+// Eight floats of shared memory (16-byte aligned) by pairs.
+__device__ __forceinline__ void load_row8(const float* p, float2 (&v)[4]) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  v[0] = make_float2(a.x, a.y);
+  v[1] = make_float2(a.z, a.w);
+  v[2] = make_float2(b.x, b.y);
+  v[3] = make_float2(b.z, b.w);
 }
 
 __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
@@ -637,37 +642,52 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
           for (int32_t i = max(w.vis - tile, 0) * (HD / 16) + tid; i < kTok * (HD / 16); i += kGroup)
             v[i] = make_uint4(0u, 0u, 0u, 0u);
         }
-        float s[CH], y[CH];
-        {
-          uint32_t both[2 * CH];
-          load_cols<R, CH>(lanes + buf * NC, both);
-          float f[CH];
-          load_row<CH>(row_f + r0, f);
-#pragma unroll
-          for (int i = 0; i < CH; ++i)
-            s[i] = fmaf(__uint_as_float(both[i + CH]), kLoUnit, __uint_as_float(both[i])) * (ks * f[i]);
-        }
-        if (masked) {
-#pragma unroll
-          for (int i = 0; i < CH; ++i)
-            if (tile + tid > row_lim[r0 + i]) s[i] = -INFINITY;
-        }
+        float y[CH];
         for (;;) {
-          float m[CH], top = -INFINITY;
-          load_row<CH>(row_m + r0, m);
+          float top = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < CH; ++i) {
-            y[i] = s[i] + (lsv - m[i]);
-            top = fmaxf(top, y[i]);
+          for (int c = 0; c < CH; c += 8) {
+            float2 t[4], f[4], m[4];
+            load_row8(row_f + r0 + c, f);
+            load_row8(row_m + r0 + c, m);
+            load_rows8<R>(lanes + buf * NC + c, t);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 v = fma2(t[i], mul2(both(ks), f[i]), fma2(m[i], both(-1.0f), both(lsv)));
+              y[c + 2 * i] = v.x;
+              y[c + 2 * i + 1] = v.y;
+            }
           }
+          if (masked) {
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+              if (tile + tid > row_lim[r0 + i]) y[i] = -INFINITY;
+          }
+#pragma unroll
+          for (int i = 0; i < CH; ++i) top = fmaxf(top, y[i]);
           if (bar_all(bar, kGroup, ok && !(top > kOver))) break;
           if (!bar_all(bar, kGroup, ok)) { failed = true; break; }
           // new maxima of the group's rows and what a weight of the old is worth under them: a lane a row
 #pragma unroll
-          for (int i = 0; i < CH; ++i) m[i] = s[i] + lsv;
-          warp_rows<CH, true>(m, lane);
+          for (int c = 0; c < CH; c += 8) {
+            float2 t[4], f[4];
+            load_row8(row_f + r0 + c, f);
+            load_rows8<R>(lanes + buf * NC + c, t);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 v = fma2(t[i], mul2(both(ks), f[i]), both(lsv));
+              y[c + 2 * i] = v.x;
+              y[c + 2 * i + 1] = v.y;
+            }
+          }
+          if (masked) {
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+              if (tile + tid > row_lim[r0 + i]) y[i] = -INFINITY;
+          }
+          warp_rows<CH, true>(y, lane);
           const int row = lane / (32 / CH);
-          if (lane % (32 / CH) == 0) my_red[(warp & 3) * CH + row] = m[0];
+          if (lane % (32 / CH) == 0) my_red[(warp & 3) * CH + row] = y[0];
           bar_sync(bar, kGroup);
           const float t = fmaxf(fmaxf(my_red[row], my_red[CH + row]), fmaxf(my_red[2 * CH + row], my_red[3 * CH + row]));
           const float old = row_m[r0 + row], raised = t - old > kNominal ? t - kNominal : old;
@@ -678,28 +698,34 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
             row_fac[r0 + row] = fac;
           }
           bar_sync(bar, kGroup);
-          load_row<CH>(row_fac + r0, m);
-#pragma unroll
-          for (int i = 0; i < CH; ++i) l[i] *= m[i];
           if (j > 0) {
             ok = wait_pv(gt - 1) && ok;
             tc_fence_after();
-            uint32_t o[2 * CH];
-            load_cols<R, CH>(lanes + kColO, o);
-#pragma unroll
-            for (int i = 0; i < CH; ++i) {
-              o[i] = __float_as_uint(__uint_as_float(o[i]) * m[i]);
-              o[i + CH] = __float_as_uint(__uint_as_float(o[i + CH]) * m[i]);
-            }
-            store_cols<R, CH>(lanes + kColO, o);
-            tmem_st_wait();
           }
+#pragma unroll
+          for (int c = 0; c < CH; c += 8) {
+            float2 f[4];
+            load_row8(row_fac + r0 + c, f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              l[c + 2 * i] *= f[i].x;
+              l[c + 2 * i + 1] *= f[i].y;
+            }
+            if (j > 0) {
+              scale_cols8(lanes + kColO + c, f);
+              scale_cols8(lanes + kColO + R + c, f);
+            }
+          }
+          tmem_st_wait();
         }
         if (failed) break;
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
+        for (int i = 0; i < CH; i += 2) {
           y[i] = fast_exp2(y[i]);
-          l[i] = fmaf(y[i], inv, l[i]);
+          y[i + 1] = fast_exp2(y[i + 1]);
+          const float2 v = fma2(make_float2(y[i], y[i + 1]), both(inv), make_float2(l[i], l[i + 1]));
+          l[i] = v.x;
+          l[i + 1] = v.y;
         }
         // MN-major without swizzle: 16 columns of a token, the next tokens; then the next 16 columns
         uint8_t* const at = gbase + Y::kOffP + buf * Y::kP + tid * 16;
@@ -742,19 +768,22 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
         ok = wait_pv(gt - 1) && ok;
         tc_fence_after();
         const int dl = HD == 128 ? tid : (warp & 3) * 16 + lane;  // the thread's column of the head (64: lanes 0 .. 15)
-        uint32_t o[2 * CH];
-        load_cols<R, CH>(lanes + kColO, o);
-        if (ok && (HD == 128 || lane < 16)) {
 #pragma unroll
-          for (int i = 0; i < CH; ++i) {
-            const float v = fmaf(__uint_as_float(o[i + CH]), kLoUnit, __uint_as_float(o[i]));
-            if (r0 + i >= rows) break;
+        for (int c = 0; c < CH; c += 8) {
+          float2 o[4];
+          load_rows8<R>(lanes + kColO + c, o);
+          if (!ok || (HD == 64 && lane >= 16)) continue;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = r0 + c + i;
+            const float v = i & 1 ? o[i / 2].y : o[i / 2].x;
+            if (r >= rows) break;
             if (whole) {
-              const float f = row_fac[r0 + i];
+              const float f = row_fac[r];
               const __nv_bfloat16 out = __float2bfloat16_rn(f == 0.0f ? 0.0f : v * f);
-              p.a.o[row_at[r0 + i] + dl] = *reinterpret_cast<const uint16_t*>(&out);
+              p.a.o[row_at[r] + dl] = *reinterpret_cast<const uint16_t*>(&out);
             } else {
-              part[2 * R + (r0 + i) * HD + dl] = v;
+              part[2 * R + r * HD + dl] = v;
             }
           }
         }
