@@ -41,40 +41,50 @@
 namespace catq {
 namespace {
 
-constexpr int kTok = 128;                    // cached tokens per tile (MMA M of S^T, contraction of O^T)
 constexpr int kGroup = 128;                  // threads of a softmax group
 constexpr float kNominal = 3.0f;             // log2 of a weight at the maximum taken
 constexpr float kOver = 8.75f;               // raise the maximum past this (2^8.75 < 448)
 constexpr float kNoMax = -3e38f;             // maximum of a row that has seen nothing
 constexpr float kLoUnit = 0.0625f;           // a lo term's unit
 constexpr int kScaleRing = 16;               // tiles whose scales are kept (see the TMA warp)
+constexpr int kRows = 128;                   // shared-memory rows of a tile of codes, 128 bytes each
 
 template <int HD, int R>
 struct KvLay {
+  static constexpr int kR = R;                                       // rows of a row tile
+  static constexpr int kTpr = 128 / HD;                              // tokens a shared-memory row
+  static constexpr int kTok = kRows * kTpr;                          // cached tokens a tile
+  // What a row tile's beginning and end cost, in tiles (one GB300; no such cost: 32 us for drafted tokens, 66 for heads of
+  // 64, 53 for one long sequence; with it 29, 55 and 51; 4 for the heads of 64: 60, 1 for the drafted tokens: 32).
+  static constexpr int kHead = R == 8 ? (HD == 64 ? 1 : 2) : 4;
+  static constexpr int kPages = kTok / 16;                           // most pages a tile
   static constexpr int kCols = 2 * R;                                // N of both products
-  static constexpr int kChunk = R < 16 ? R : 16;                     // rows of a softmax group
+  static constexpr int kMaxChunk = HD == 128 ? 32 : 16;
+  static constexpr int kChunk = R < kMaxChunk ? R : kMaxChunk;       // rows of a softmax group
   static constexpr int kGroups = R / kChunk;
   static constexpr int kSoft = kGroups * kGroup;
   static constexpr int kTmaWarp = 4 * kGroups, kMmaWarp = kTmaWarp + 1, kThreads = kSoft + 64;
-  static constexpr int kCtas = R == 8 ? 3 : R <= 32 ? 2 : 1;         // CTAs an SM
-  static constexpr uint32_t kTile = kTok * HD;                       // a tile of codes
+  static constexpr uint32_t kColO = 2 * kTpr * kCols;                // two buffers of scores, then the accumulators
+  static constexpr uint32_t kTmem = kColO + kCols <= 64 ? 64 : kColO + kCols <= 128 ? 128 : kColO + kCols <= 256 ? 256 : 512;
+  static constexpr int kCtas = kTmem <= 256 ? 2 : 1;                 // CTAs an SM
+  static constexpr uint32_t kTile = kRows * 128;                     // a tile of codes
   static constexpr uint32_t kQ = kCols * HD, kP = kTok * kCols;
   // barriers, tensor-memory address, start of the run | scales of the tiles in flight | per row: query factor, maximum,
   // its last raise, last position, output offset (8 bytes), sums by warp | Q, P twice, ring
-  static constexpr uint32_t kOffScale = 640, kOffF = kOffScale + kScaleRing * 64, kOffM = kOffF + 4 * R,
+  static constexpr uint32_t kOffScale = 640, kOffF = kOffScale + kScaleRing * 8 * kPages, kOffM = kOffF + 4 * R,
                             kOffFac = kOffM + 4 * R, kOffLim = kOffFac + 4 * R, kOffRow = kOffLim + 4 * R,
-                            kOffRed = kOffRow + 8 * R, kOffQ = (kOffRed + 16 * R + 127) / 128 * 128, kOffP = kOffQ + kQ,
+                            kOffZero = kOffRow + 8 * R, kOffRed = kOffZero + 4 * R, kOffQ = (kOffRed + 16 * R + 127) / 128 * 128, kOffP = kOffQ + kQ,
                             kOffRing = (kOffP + 2 * kP + 1023) / 1024 * 1024;
-  static constexpr uint32_t kBudget = (kCtas == 3 ? 75 : kCtas == 2 ? 112 : 224) * 1024;
+  static constexpr uint32_t kBudget = (kCtas == 2 ? 112 : 224) * 1024;
   static constexpr int kSlots0 = (kBudget - 1024 - kOffRing) / kTile;
   static constexpr int kSlots = kSlots0 > 12 ? 12 : kSlots0;
   static constexpr uint32_t kSmem = kOffRing + kSlots * kTile + 1024;
-  static constexpr uint32_t kTmem = 3 * kCols <= 64 ? 64 : 3 * kCols <= 128 ? 128 : 3 * kCols <= 256 ? 256 : 512;
   static constexpr int kPartFloats = R * (HD + 2);                   // maxima, sums, accumulators of a part
 };
 
 // ---------------------------------------------------------------- the line of tiles
-// One sequence's share of the line: `per_head` tiles for each key/value head.
+// One sequence's share of the line: `per_head` positions for each key/value head.  Every row tile has a stretch of kHead
+// positions and one for each of its tiles: runs of equal length are then runs of nearly equal time.
 struct KvSeq {
   int32_t r0, n, len;  // first row, rows, cached tokens
   int64_t per_head;
@@ -91,18 +101,19 @@ struct KvGeom {
 };
 
 // Tokens that the row tile `q` of a sequence can see.
-template <int R>
+template <class Y>
 __device__ __forceinline__ int32_t visible(const KvGeom& g, const KvSeq& s, int32_t q) {
-  return max(s.len - s.n + g.token_of(min((q + 1) * R, s.n * g.group) - 1) + 1, 0);
+  return max(s.len - s.n + g.token_of(min((q + 1) * Y::kR, s.n * g.group) - 1) + 1, 0);
 }
-template <int R>
+template <class Y>
 __device__ __forceinline__ int32_t row_tiles(const KvGeom& g, const KvSeq& s) {
-  return (s.n * g.group + R - 1) / R;
+  return (s.n * g.group + Y::kR - 1) / Y::kR;
 }
 // A row tile that sees nothing still has a tile: its rows are written.
-__device__ __forceinline__ int32_t tiles_of(int32_t vis) { return max((vis + kTok - 1) / kTok, 1); }
+template <class Y>
+__device__ __forceinline__ int32_t tiles_of(int32_t vis) { return max((vis + Y::kTok - 1) / Y::kTok, 1); }
 
-template <int R>
+template <class Y>
 __device__ __forceinline__ KvSeq load_seq(const KvGeom& g, int32_t b, int32_t* status) {
   KvSeq s;
   s.r0 = g.row_start[b];
@@ -115,46 +126,51 @@ __device__ __forceinline__ KvSeq load_seq(const KvGeom& g, int32_t b, int32_t* s
     s.n = 0;
     return s;
   }
-  const int32_t nq = row_tiles<R>(g, s);
-  for (int32_t q = 0; q < nq; ++q) s.per_head += tiles_of(visible<R>(g, s, q));
+  const int32_t nq = row_tiles<Y>(g, s);
+#pragma unroll 1
+  for (int32_t q = 0; q < nq; ++q) s.per_head += Y::kHead + tiles_of<Y>(visible<Y>(g, s, q));
   return s;
 }
 
 // Walks a run's segments: a segment is the run's part of one row tile.
-template <int R>
+template <class Y>
 struct KvWalk {
   int64_t at, end;       // line positions still to do
-  int32_t b, h, q, t;    // the next tile: sequence, head, row tile, tile of the row tile
+  int32_t b, h, q, t;    // the next position: sequence, head, row tile, place in the row tile's stretch
   KvSeq s;
   // the segment
   int32_t n;             // its tiles
   int32_t t0;            // first of them
   int32_t all, vis;      // the row tile's tiles and visible tokens
+  int64_t begin;         // line position of the row tile's first tile
   int32_t sb, sh, sq;    // its sequence, head, row tile
   int32_t r0, rows_n, len;  // its sequence's first row, rows, cached tokens
-  // line position of the row tile's first tile
-  __device__ __forceinline__ int64_t begin() const { return at - n - t0; }
   __device__ __forceinline__ bool next(const KvGeom& g) {
-    if (at >= end) return false;
-    if (s.per_head == 0 || h == g.nkv) {
-      do {
-        ++b;
-        s = load_seq<R>(g, b, nullptr);
-      } while (s.per_head == 0);
-      h = q = t = 0;
+    for (;;) {
+      if (at >= end) return false;
+      if (s.per_head == 0 || h == g.nkv) {
+#pragma unroll 1
+        do {
+          if (++b >= g.B) return false;  // (the lengths changed under the kernel)
+          s = load_seq<Y>(g, b, nullptr);
+        } while (s.per_head == 0);
+        h = q = t = 0;
+      }
+      sb = b; sh = h; sq = q; r0 = s.r0; rows_n = s.n; len = s.len;
+      vis = visible<Y>(g, s, q);
+      all = tiles_of<Y>(vis);
+      const int32_t part = static_cast<int32_t>(min(static_cast<int64_t>(Y::kHead + all - t), end - at));
+      begin = at - t + Y::kHead;
+      t0 = max(t - Y::kHead, 0);
+      n = t + part - Y::kHead - t0;
+      at += part;
+      t = 0;
+      if (++q == row_tiles<Y>(g, s)) {
+        q = 0;
+        ++h;
+      }
+      if (n > 0) return true;  // (a run that ends in a row tile's head leaves it to the next)
     }
-    sb = b; sh = h; sq = q; r0 = s.r0; rows_n = s.n; len = s.len;
-    vis = visible<R>(g, s, q);
-    all = tiles_of(vis);
-    t0 = t;
-    n = static_cast<int32_t>(min(static_cast<int64_t>(all - t), end - at));
-    at += n;
-    t = 0;
-    if (++q == row_tiles<R>(g, s)) {
-      q = 0;
-      ++h;
-    }
-    return true;
   }
 };
 
@@ -162,6 +178,12 @@ struct KvWalk {
 __device__ __forceinline__ float fast_exp2(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 
@@ -217,17 +239,22 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
                : "memory");
 }
 
-// Eight rows' products from their hi columns at `base` and their lo columns R behind: hi + lo / 16, by pairs.
-template <int R>
-__device__ __forceinline__ void load_rows8(uint32_t base, float2 (&t)[4]) {
-  uint32_t hi[8], lo[8];
-  tmem_ld8(base, hi);
-  tmem_ld8(base + R, lo);
+// N rows' products (8 where R is, else 16) from their hi columns at `base` and their lo columns R behind: hi + lo / 16, by
+// pairs.
+template <int R, int N>
+__device__ __forceinline__ void load_rows(uint32_t base, float2 (&t)[N / 2]) {
+  uint32_t v[2 * N];
+  if constexpr (N == R && N == 8) {
+    tmem_ld16(base, v);
+  } else {
+    tmem_ld16(base, *reinterpret_cast<uint32_t(*)[16]>(&v[0]));
+    tmem_ld16(base + R, *reinterpret_cast<uint32_t(*)[16]>(&v[N]));
+  }
   tmem_ld_wait();
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    t[i] = fma2(make_float2(__uint_as_float(lo[2 * i]), __uint_as_float(lo[2 * i + 1])), both(kLoUnit),
-                make_float2(__uint_as_float(hi[2 * i]), __uint_as_float(hi[2 * i + 1])));
+  for (int i = 0; i < N / 2; ++i)
+    t[i] = fma2(make_float2(__uint_as_float(v[N + 2 * i]), __uint_as_float(v[N + 2 * i + 1])), both(kLoUnit),
+                make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])));
 }
 // Eight columns at `base` times f.
 __device__ __forceinline__ void scale_cols8(uint32_t base, const float2 (&f)[4]) {
@@ -270,13 +297,15 @@ __device__ __forceinline__ void warp_rows(float (&v)[CH], int lane) {
   }
 }
 
-// Eight floats of shared memory (16-byte aligned) by pairs.
-__device__ __forceinline__ void load_row8(const float* p, float2 (&v)[4]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  v[0] = make_float2(a.x, a.y);
-  v[1] = make_float2(a.z, a.w);
-  v[2] = make_float2(b.x, b.y);
-  v[3] = make_float2(b.z, b.w);
+// N floats of shared memory (16-byte aligned) by pairs.
+template <int N>
+__device__ __forceinline__ void load_row(const float* p, float2 (&v)[N / 2]) {
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    const float4 a = reinterpret_cast<const float4*>(p)[i];
+    v[2 * i] = make_float2(a.x, a.y);
+    v[2 * i + 1] = make_float2(a.z, a.w);
+  }
 }
 
 __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
@@ -298,7 +327,8 @@ template <int HD, int R>
 __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
     kv_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const KvTcArgs p) {
   using Y = KvLay<HD, R>;
-  constexpr int NC = Y::kCols, CH = Y::kChunk, NS = Y::kSlots, kThreads = Y::kThreads, kSoft = Y::kSoft;
+  constexpr int NC = Y::kCols, CH = Y::kChunk, NS = Y::kSlots, kThreads = Y::kThreads, kSoft = Y::kSoft,
+                kTok = Y::kTok, TPR = Y::kTpr;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -312,12 +342,13 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
   int32_t* const start = reinterpret_cast<int32_t*>(gbase + 408);           // b, h, q, t of the run's first tile
   int64_t* const scan = reinterpret_cast<int64_t*>(gbase + 424);            // warps' sums
   static_assert(424 + 8 * (kThreads / 32) <= Y::kOffScale, "start");
-  float* const scales = reinterpret_cast<float*>(gbase + Y::kOffScale);     // [kScaleRing][8 key, 8 value scales]
+  float* const scales = reinterpret_cast<float*>(gbase + Y::kOffScale);     // [kScaleRing][key scales, value scales of kPages]
   float* const row_f = reinterpret_cast<float*>(gbase + Y::kOffF);
   float* const row_m = reinterpret_cast<float*>(gbase + Y::kOffM);
   float* const row_fac = reinterpret_cast<float*>(gbase + Y::kOffFac);
   int32_t* const row_lim = reinterpret_cast<int32_t*>(gbase + Y::kOffLim);
   int64_t* const row_at = reinterpret_cast<int64_t*>(gbase + Y::kOffRow);
+  float* const row_zero = reinterpret_cast<float*>(gbase + Y::kOffZero);
   float* const red = reinterpret_cast<float*>(gbase + Y::kOffRed);          // [groups][4][CH]
 
   if (threadIdx.x == 0) {
@@ -351,8 +382,9 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
     const int32_t per = (g.B + kThreads - 1) / kThreads;
     const int32_t b0 = min(static_cast<int32_t>(threadIdx.x) * per, g.B), b1 = min(b0 + per, g.B);
     int64_t mine = 0;
+#pragma unroll 1
     for (int32_t b = b0; b < b1; ++b)
-      mine += load_seq<R>(g, b, blockIdx.x == 0 ? p.a.status : nullptr).per_head * g.nkv;
+      mine += load_seq<Y>(g, b, blockIdx.x == 0 ? p.a.status : nullptr).per_head * g.nkv;
     int64_t upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -362,6 +394,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
     if (lane == 31) scan[warp] = upto;
     __syncthreads();
     total = 0;
+#pragma unroll 1
     for (int w = 0; w < kThreads / 32; ++w) {
       if (w < warp) upto += scan[w];
       total += scan[w];
@@ -371,15 +404,17 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
     if (upto - mine <= first && first < upto) {  // the thread whose stretch holds the run's first tile
       int64_t rest = first - (upto - mine);
       int32_t b = b0;
-      KvSeq s = load_seq<R>(g, b, nullptr);
-      while (rest >= s.per_head * g.nkv) {
+      KvSeq s = load_seq<Y>(g, b, nullptr);
+#pragma unroll 1
+      while (rest >= s.per_head * g.nkv && b + 1 < b1) {
         rest -= s.per_head * g.nkv;
-        s = load_seq<R>(g, ++b, nullptr);
+        s = load_seq<Y>(g, ++b, nullptr);
       }
-      const int32_t h = static_cast<int32_t>(rest / s.per_head);
+      const int32_t h = static_cast<int32_t>(rest / max(s.per_head, static_cast<int64_t>(1)));
       rest -= h * s.per_head;
       int32_t q = 0;
-      for (int32_t n; rest >= (n = tiles_of(visible<R>(g, s, q))); ++q) rest -= n;
+#pragma unroll 1
+      for (int32_t n; q < row_tiles<Y>(g, s) - 1 && rest >= (n = Y::kHead + tiles_of<Y>(visible<Y>(g, s, q))); ++q) rest -= n;
       start[0] = b;
       start[1] = h;
       start[2] = q;
@@ -390,8 +425,8 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  constexpr uint32_t kColO = 2 * NC;
-  KvWalk<R> w;
+  constexpr uint32_t kColO = Y::kColO;
+  KvWalk<Y> w;
   w.at = first;
   w.end = min(first + run, total);
   if (w.at < w.end) {
@@ -399,7 +434,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
     w.h = start[1];
     w.q = start[2];
     w.t = start[3];
-    w.s = load_seq<R>(g, w.b, nullptr);
+    w.s = load_seq<Y>(g, w.b, nullptr);
   }
   const KvCacheDev& kv = p.a.cache;
   const int32_t ppt = kTok / kv.page;  // pages a tile
@@ -423,11 +458,11 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
       if (j >= w.n || lane >= ppt || (w.t0 + j) * kTok + lane * kv.page >= w.vis) return g;
       if (id < 0 || id >= kv.n_pages) {
         atomicCAS(p.a.status, 0, 10 /* CATQ_ERR_INDEX */);
-        g.row = kv.n_pages * kv.nkv * kv.page;  // behind the last row: zeros
+        g.row = kv.n_pages * kv.nkv * (kv.page / TPR);  // behind the last row: zeros
         return g;
       }
       const int32_t block = id * kv.nkv + w.sh;
-      g.row = block * kv.page;
+      g.row = block * (kv.page / TPR);
       g.ks = __ldg(kv.k_scale + block);
       g.vs = __ldg(kv.v_scale + block);
       return g;
@@ -444,10 +479,10 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
       if (g.row >= 0)
         tma_load_2d(base + Y::kOffRing + slot * Y::kTile + lane * kv.page * HD, map, full0 + 8u * slot, 0, g.row);
       if (keys) {
-        if (lane < 8) {
-          float* const to = scales + (gt % kScaleRing) * 16;
+        if (lane < Y::kPages) {
+          float* const to = scales + (gt % kScaleRing) * (2 * Y::kPages);
           to[lane] = g.ks;
-          to[8 + lane] = g.vs;
+          to[Y::kPages + lane] = g.vs;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive_local(scale_full0 + 8u * (gt % kScaleRing));
@@ -473,12 +508,12 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
       }
     }
     // copies still in flight land before the CTA exits
+#pragma unroll 1
     for (int t = max(0, loads - NS); t < loads; ++t) drain(full0 + 8u * (t % NS), (t / NS) & 1);
   } else if (warp == Y::kMmaWarp) {
-    constexpr uint32_t kSwizzle = HD == 128 ? 2 : 4;
-    constexpr uint32_t idesc_s = idesc_e4m3(kTok, NC, false, false), idesc_o = idesc_e4m3(HD, NC, true, true);
-    constexpr uint32_t kHi = desc_hi(8 * HD, kSwizzle);  // code tiles: 8 rows of HD bytes from one group to the next
-    constexpr uint32_t kHiQ = desc_hi(128, 0), kHiP = desc_hi(16 * kTok, 0);
+    constexpr uint32_t idesc_s = idesc_e4m3(kRows, NC, false, false), idesc_o = idesc_e4m3(HD, NC, true, true);
+    constexpr uint32_t kHi = desc_hi(1024, 2);  // code tiles: 8 swizzled rows of 128 bytes from one group to the next
+    constexpr uint32_t kHiQ = desc_hi(128, 0), kHiP = desc_hi(16 * kRows, 0);
     const bool issuer = elect_one();
     int slot = 0;
     uint32_t ph = 0, gt = 0, seg = 0;  // gt: tiles so far
@@ -491,8 +526,9 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
       if (issuer) {
         const uint32_t ad = desc_lo(base + Y::kOffRing + slot * Y::kTile, 16), bd = desc_lo(base + Y::kOffQ, 16 * NC);
 #pragma unroll
-        for (int k = 0; k < HD / 32; ++k)
-          umma_f8(tmem + buf * NC, ad + 2 * k, kHi, bd + 2 * NC * k, kHiQ, idesc_s, k > 0 ? 1u : 0u);
+        for (int k = 0; k < 4; ++k)  // 32 bytes of a row: HD / 32 steps a token
+          umma_f8(tmem + buf * (TPR * NC) + k / (HD / 32) * NC, ad + 2 * k, kHi, bd + 2 * NC * (k % (HD / 32)), kHiQ, idesc_s,
+                  k % (HD / 32) > 0 ? 1u : 0u);
         umma_commit<1>(s_full0 + 8u * buf);
         umma_commit<1>(empty0 + 8u * slot);
       }
@@ -516,8 +552,9 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
           const uint32_t ad = desc_lo(base + Y::kOffRing + slot * Y::kTile, 16),
                          bd = desc_lo(base + Y::kOffP + buf * Y::kP, 128);
 #pragma unroll
-          for (int k = 0; k < kTok / 32; ++k)
-            umma_f8(tmem + kColO, ad + 2 * HD * k, kHi, bd + 32 * k, kHiP, idesc_o, (j > 0 || k > 0) ? 1u : 0u);
+          for (int k = 0; k < 4 * TPR; ++k)  // 32 rows, one token of each at a time
+            umma_f8(tmem + kColO, ad + 256 * (k % 4) + 4 * (k / 4), kHi, bd + 32 * (k % 4) + 8 * NC * (k / 4), kHiP, idesc_o,
+                    (j > 0 || k > 0) ? 1u : 0u);
           umma_commit<1>(pv_done0 + 8u * buf);
           umma_commit<1>(empty0 + 8u * slot);
         }
@@ -529,40 +566,49 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
     __syncwarp();
     drain(final_bar, 0);  // every MMA has completed before TMEM is released
   } else {
-    // softmax: group wg has rows CH wg .. of the row tile, thread tid of it token tid of every tile
+    // softmax: group wg has rows CH wg .. of the row tile, thread tid of it the tokens of row tid of every tile
     const int wg = warp >> 2, tid = threadIdx.x & (kGroup - 1), bar = 1 + wg, bar_every = 1 + Y::kGroups;
     const int r0 = CH * wg;
     const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + r0;
     float* const my_red = red + wg * 4 * CH;
-    const int page_at = tid / kv.page;
+    const int page_at = TPR * tid / kv.page;
     uint32_t gt = 0, ring = 0;  // tiles and loads before the segment's
     // Products with the values up to tile t of the run have completed.  A barrier for every other tile: the scores of
     // tile t that the caller has seen followed the product of tile t - 2, so the barrier is at most one phase behind,
     // where a single one could be two behind and show the awaited parity.
     auto wait_pv = [&](uint32_t t) { return mbar_wait_warp(pv_done0 + 8u * (t & 1), (t >> 1) & 1, p.wc); };
-    while (w.next(g)) {
+    // Queries, HD / 8 threads a row: a segment's are asked for while the segment before it is under way.
+    constexpr int kPerRow = HD / 8, kPass = kGroup / kPerRow, kPasses = (CH + kPass - 1) / kPass;
+    uint4 raw[kPasses];
+    auto ask = [&](const KvWalk<Y>& v) {
+#pragma unroll
+      for (int k = 0; k < kPasses; ++k) {
+        const int r = k * kPass + tid / kPerRow, row = v.sq * R + r0 + r;
+        raw[k] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < CH && row < v.rows_n * g.group) {
+          const int32_t tk = g.token_of(row);
+          raw[k] = *reinterpret_cast<const uint4*>(p.a.q + (v.r0 + tk) * p.a.ldq +
+                                                   (v.sh * g.group + row - tk * g.group) * HD + 8 * (tid % kPerRow));
+        }
+      }
+    };
+    constexpr bool kAhead = CH <= 16;  // (32 rows a group: the registers are needed, and a segment is mostly long)
+    bool more = w.next(g);
+    if (kAhead && more) ask(w);
+    KvWalk<Y> ahead;
+#pragma unroll 1
+    for (; more; w = ahead) {
       if (!bar_all(bar_every, kSoft, ok)) { ok = false; break; }  // the rows' arrays are free
       const int32_t rows = min(R, w.rows_n * g.group - w.sq * R);
       const bool active = r0 < rows;
-      // queries: HD / 8 threads a row, all loads first
-      constexpr int kPerRow = HD / 8, kPass = kGroup / kPerRow, kPasses = (CH + kPass - 1) / kPass;
       if (active) {
-        uint4 raw[kPasses];
+        if (!kAhead) ask(w);
         const int i = tid % kPerRow;
-#pragma unroll
-        for (int k = 0; k < kPasses; ++k) {
-          const int r = r0 + k * kPass + tid / kPerRow, row = w.sq * R + r;
-          raw[k] = make_uint4(0u, 0u, 0u, 0u);
-          if (r < rows && r < r0 + CH) {
-            const int32_t tk = g.token_of(row);
-            raw[k] = *reinterpret_cast<const uint4*>(p.a.q + (w.r0 + tk) * p.a.ldq +
-                                                     (w.sh * g.group + row - tk * g.group) * HD + 8 * i);
-          }
-        }
         if (tid < CH) {
           const int row = w.sq * R + r0 + tid;
           const int32_t tk = g.token_of(row);
           row_m[r0 + tid] = kNoMax;
+          row_zero[r0 + tid] = 0.0f;
           row_lim[r0 + tid] = r0 + tid < rows ? w.len - w.rows_n + tk : -1;
           row_at[r0 + tid] = (w.r0 + tk) * p.a.ldo + (w.sh * g.group + row - tk * g.group) * HD;
         }
@@ -602,6 +648,9 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
       }
       bar_sync(bar, kGroup);
       if (lane == 0) mbar_arrive_local(q_full);
+      ahead = w;
+      more = ahead.next(g);
+      if (kAhead && more) ask(ahead);
       // tokens that the group's first row sees (the others at least as many)
       const int32_t sees_all = active ? row_lim[r0] + 1 : 0;
       float l[CH];
@@ -619,8 +668,9 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
           continue;
         }
         ok = mbar_wait_warp(scale_full0 + 8u * (gt % kScaleRing), (gt / kScaleRing) & 1, p.wc) && ok;
-        float ks = scales[(gt % kScaleRing) * 16 + page_at];
-        uint32_t vb = __float_as_uint(scales[(gt % kScaleRing) * 16 + 8 + page_at]);
+        const float* const at_scale = scales + (gt % kScaleRing) * (2 * Y::kPages) + page_at;
+        float ks = at_scale[0];
+        uint32_t vb = __float_as_uint(at_scale[Y::kPages]);
         // log2 and reciprocal of the values' scale; codes under a scale of 0 are zeros, any scale serves them; one that
         // is not finite makes the scores of the rows that see the token NaN
         if (vb == 0u) vb = (127u - 20u) << 23;
@@ -639,55 +689,60 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
           const uint32_t at = ring + min(2, w.n) + j + max(0, min(j, w.n - 2)), sl = at % NS;
           ok = mbar_wait_warp(full0 + 8u * sl, (at / NS) & 1, p.wc) && ok;
           uint4* const v = reinterpret_cast<uint4*>(gbase + Y::kOffRing + sl * Y::kTile);
-          for (int32_t i = max(w.vis - tile, 0) * (HD / 16) + tid; i < kTok * (HD / 16); i += kGroup)
-            v[i] = make_uint4(0u, 0u, 0u, 0u);
+          for (int32_t i = max(w.vis - tile, 0) / TPR * 8 + tid; i < kRows * 8; i += kGroup)  // (chunks of a row are swizzled)
+            if (tile + TPR * (i / 8) + ((i ^ (i / 8)) & 7) / (HD / 16) >= w.vis) v[i] = make_uint4(0u, 0u, 0u, 0u);
         }
-        float y[CH];
-        for (;;) {
+        // element e CH + i: token e of the thread's, row i of the group's
+        float y[TPR * CH];
+        constexpr int kStep = CH < 16 ? 8 : 16;
+        const int tok = tile + TPR * tid;
+        // x as it is rounded, then less the maximum, so that a weight is at most 2^kNominal after a raise however large the
+        // scores are (a fused x - m could exceed it by the rounding of x)
+        auto score = [&](const float* less) {
+#pragma unroll
+          for (int c = 0; c < CH; c += kStep) {
+            float2 t[kStep / 2], f[kStep / 2], m[kStep / 2];
+            load_row<kStep>(row_f + r0 + c, f);
+            load_row<kStep>(less + r0 + c, m);
+#pragma unroll
+            for (int i = 0; i < kStep / 2; ++i) f[i] = mul2(both(ks), f[i]);
+#pragma unroll
+            for (int e = 0; e < TPR; ++e) {
+              load_rows<R, kStep>(lanes + buf * (TPR * NC) + e * NC + c, t);
+#pragma unroll
+              for (int i = 0; i < kStep / 2; ++i) {
+                const float2 v = fma2(m[i], both(-1.0f), fma2(t[i], f[i], both(lsv)));
+                y[e * CH + c + 2 * i] = v.x;
+                y[e * CH + c + 2 * i + 1] = v.y;
+              }
+            }
+          }
+          if (masked) {
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+              for (int e = 0; e < TPR; ++e)
+                if (tok + e > row_lim[r0 + i]) y[e * CH + i] = -INFINITY;
+          }
+        };
+        bool keep = false;  // the maxima serve this tile too (a segment's first has none yet)
+        if (j > 0) {
+          score(row_m);
           float top = -INFINITY;
 #pragma unroll
-          for (int c = 0; c < CH; c += 8) {
-            float2 t[4], f[4], m[4];
-            load_row8(row_f + r0 + c, f);
-            load_row8(row_m + r0 + c, m);
-            load_rows8<R>(lanes + buf * NC + c, t);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float2 v = fma2(t[i], mul2(both(ks), f[i]), fma2(m[i], both(-1.0f), both(lsv)));
-              y[c + 2 * i] = v.x;
-              y[c + 2 * i + 1] = v.y;
-            }
-          }
-          if (masked) {
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-              if (tile + tid > row_lim[r0 + i]) y[i] = -INFINITY;
-          }
-#pragma unroll
-          for (int i = 0; i < CH; ++i) top = fmaxf(top, y[i]);
-          if (bar_all(bar, kGroup, ok && !(top > kOver))) break;
+          for (int i = 0; i < TPR * CH; i += 2) top = max3(top, y[i], y[i + 1]);
+          keep = bar_all(bar, kGroup, ok && !(top > kOver));
+        }
+        if (!keep) {
           if (!bar_all(bar, kGroup, ok)) { failed = true; break; }
           // new maxima of the group's rows and what a weight of the old is worth under them: a lane a row
+          score(row_zero);
+          float x[CH];
 #pragma unroll
-          for (int c = 0; c < CH; c += 8) {
-            float2 t[4], f[4];
-            load_row8(row_f + r0 + c, f);
-            load_rows8<R>(lanes + buf * NC + c, t);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float2 v = fma2(t[i], mul2(both(ks), f[i]), both(lsv));
-              y[c + 2 * i] = v.x;
-              y[c + 2 * i + 1] = v.y;
-            }
-          }
-          if (masked) {
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-              if (tile + tid > row_lim[r0 + i]) y[i] = -INFINITY;
-          }
-          warp_rows<CH, true>(y, lane);
+          for (int i = 0; i < CH; ++i) x[i] = TPR == 1 ? y[i] : fmaxf(y[i], y[(TPR - 1) * CH + i]);
+          warp_rows<CH, true>(x, lane);
           const int row = lane / (32 / CH);
-          if (lane % (32 / CH) == 0) my_red[(warp & 3) * CH + row] = y[0];
+          if (lane % (32 / CH) == 0) my_red[(warp & 3) * CH + row] = x[0];
           bar_sync(bar, kGroup);
           const float t = fmaxf(fmaxf(my_red[row], my_red[CH + row]), fmaxf(my_red[2 * CH + row], my_red[3 * CH + row]));
           const float old = row_m[r0 + row], raised = t - old > kNominal ? t - kNominal : old;
@@ -705,7 +760,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
 #pragma unroll
           for (int c = 0; c < CH; c += 8) {
             float2 f[4];
-            load_row8(row_fac + r0 + c, f);
+            load_row<8>(row_fac + r0 + c, f);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               l[c + 2 * i] *= f[i].x;
@@ -717,26 +772,36 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
             }
           }
           tmem_st_wait();
+          score(row_m);
         }
-        if (failed) break;
 #pragma unroll
-        for (int i = 0; i < CH; i += 2) {
-          y[i] = fast_exp2(y[i]);
-          y[i + 1] = fast_exp2(y[i + 1]);
-          const float2 v = fma2(make_float2(y[i], y[i + 1]), both(inv), make_float2(l[i], l[i + 1]));
-          l[i] = v.x;
-          l[i + 1] = v.y;
-        }
-        // MN-major without swizzle: 16 columns of a token, the next tokens; then the next 16 columns
-        uint8_t* const at = gbase + Y::kOffP + buf * Y::kP + tid * 16;
-        uint2 hi[CH / 8], lo[CH / 8];
+        for (int e = 0; e < TPR; ++e) {
+          float* const z = y + e * CH;
 #pragma unroll
-        for (int i = 0; i < CH / 8; ++i) split8(y + 8 * i, hi[i], lo[i]);
-        if constexpr (CH < 16) {
-          *reinterpret_cast<uint4*>(at) = make_uint4(hi[0].x, hi[0].y, lo[0].x, lo[0].y);
-        } else {
-          *reinterpret_cast<uint4*>(at + wg * (16 * kTok)) = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y);
-          *reinterpret_cast<uint4*>(at + (Y::kGroups + wg) * (16 * kTok)) = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y);
+          for (int i = 0; i < CH; i += 2) {
+            z[i] = fast_exp2(z[i]);
+            z[i + 1] = fast_exp2(z[i + 1]);
+            const float2 v = fma2(make_float2(z[i], z[i + 1]), both(inv), make_float2(l[i], l[i + 1]));
+            l[i] = v.x;
+            l[i + 1] = v.y;
+          }
+          // MN-major without swizzle: 16 columns of a token, the next rows' tokens; then the next 16 columns
+          uint8_t* const at = gbase + Y::kOffP + buf * Y::kP + e * (kRows * NC) + tid * 16;
+          if constexpr (CH < 16) {
+            uint2 hi, lo;
+            split8(z, hi, lo);
+            *reinterpret_cast<uint4*>(at) = make_uint4(hi.x, hi.y, lo.x, lo.y);
+          } else {
+#pragma unroll
+            for (int c = 0; c < CH; c += 16) {
+              uint2 hi[2], lo[2];
+              split8(z + c, hi[0], lo[0]);
+              split8(z + c + 8, hi[1], lo[1]);
+              const int k = (r0 + c) / 16;
+              *reinterpret_cast<uint4*>(at + k * (16 * kRows)) = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y);
+              *reinterpret_cast<uint4*>(at + (R / 16 + k) * (16 * kRows)) = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y);
+            }
+          }
         }
         tc_fence_before();
         fence_proxy_async_smem();
@@ -745,7 +810,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
       }
       ring += 2 * w.n;
       const bool whole = w.n == w.all;
-      float* const part = p.parts + (2 * static_cast<int64_t>(blockIdx.x) + (w.begin() >= first ? 1 : 0)) * Y::kPartFloats;
+      float* const part = p.parts + (2 * static_cast<int64_t>(blockIdx.x) + (w.begin >= first ? 1 : 0)) * Y::kPartFloats;
       if (active && !failed) {
         warp_rows<CH, false>(l, lane);  // the rows' sums
         if (lane % (32 / CH) == 0) my_red[(warp & 3) * CH + lane / (32 / CH)] = l[0];
@@ -767,14 +832,15 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
         bar_sync(bar, kGroup);
         ok = wait_pv(gt - 1) && ok;
         tc_fence_after();
+        constexpr int kCols = CH < 16 ? 8 : 16;
         const int dl = HD == 128 ? tid : (warp & 3) * 16 + lane;  // the thread's column of the head (64: lanes 0 .. 15)
 #pragma unroll
-        for (int c = 0; c < CH; c += 8) {
-          float2 o[4];
-          load_rows8<R>(lanes + kColO + c, o);
+        for (int c = 0; c < CH; c += kCols) {
+          float2 o[kCols / 2];
+          load_rows<R, kCols>(lanes + kColO + c, o);
           if (!ok || (HD == 64 && lane >= 16)) continue;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
+          for (int i = 0; i < kCols; ++i) {
             const int r = r0 + c + i;
             const float v = i & 1 ? o[i / 2].y : o[i / 2].x;
             if (r >= rows) break;
@@ -793,7 +859,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
       if (whole) continue;
       // the last of the row tile's runs joins their parts
       if (!bar_all(bar_every, kSoft, ok)) { ok = false; break; }
-      const int32_t c0 = static_cast<int32_t>(w.begin() / run), c1 = static_cast<int32_t>((w.begin() + w.all - 1) / run);
+      const int32_t c0 = static_cast<int32_t>(w.begin / run), c1 = static_cast<int32_t>((w.begin + w.all - 1) / run);
       if (threadIdx.x == 0) {
         const uint32_t last = static_cast<uint32_t>(c1 - c0);
         uint32_t old;  // releases what the barrier's threads wrote, acquires what the runs before did
@@ -835,7 +901,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
         // accumulators: kItems vectors of four columns a thread, kAt of them at a time (few rows have many parts, many
         // rows few), 16 loads at once
         float* const weight = reinterpret_cast<float*>(gbase + Y::kOffP);  // [R][128]
-        constexpr int kItems = R * HD / 4 / kSoft, kAt = R == 8 ? 1 : kItems, kDeep = 16 / kAt;
+        constexpr int kItems = R * HD / 4 / kSoft, kAt = R == 8 ? 1 : kItems > 4 ? 4 : kItems, kDeep = 16 / kAt;
         float acc[kItems][4] = {};
         for (int32_t cb = c0; cb <= c1; cb += 128) {
           const int32_t count = min(128, c1 + 1 - cb);
@@ -893,7 +959,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
 PFN_cuTensorMapEncodeTiled_v12000 g_enc = nullptr;
 std::once_flag g_enc_once;
 
-// Codes as [n_pages n_kv_heads page] rows of d bytes, boxes of one page and head, rows swizzled over their own length.
+// Codes as rows of 128 bytes (a token of 128 elements, or two of 64), boxes of one page and head.
 bool tmap_codes(CUtensorMap* m, const void* ptr, int32_t d, int64_t rows, int32_t page) {
   std::call_once(g_enc_once, [] {
     void* fn = nullptr;
@@ -903,12 +969,12 @@ bool tmap_codes(CUtensorMap* m, const void* ptr, int32_t d, int64_t rows, int32_
       g_enc = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
   });
   if (!g_enc) return false;
-  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(d)};
-  const cuuint32_t box[2] = {static_cast<cuuint32_t>(d), static_cast<cuuint32_t>(page)};
+  const cuuint64_t dims[2] = {128, static_cast<cuuint64_t>(rows * d / 128)};
+  const cuuint64_t strides[1] = {128};
+  const cuuint32_t box[2] = {128, static_cast<cuuint32_t>(page * d / 128)};
   const cuuint32_t estr[2] = {1, 1};
   return g_enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, estr,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -936,7 +1002,7 @@ cudaError_t run_kv(const KvAttnArgs& a, cudaStream_t st) {
                static_cast<int64_t>(a.cache.max_pages) * a.cache.page};
   p.counters = static_cast<uint32_t*>(a.workspace);
   p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + kCounterBytes);
-  p.min_run = 2;
+  p.min_run = Y::kHead + 2;
   auto kern = kv_attn_kernel<HD, R>;
   static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
   int dev = 0;
@@ -968,8 +1034,8 @@ cudaError_t run_kv_rows(const KvAttnArgs& a, cudaStream_t st) {
   const int64_t rows = (a.T + a.B - 1) / a.B * (a.nh / a.cache.nkv);
   if (rows <= 8) return run_kv<HD, 8>(a, st);
   if (rows <= 16) return run_kv<HD, 16>(a, st);
-  if (rows <= 32) return run_kv<HD, 32>(a, st);
-  return run_kv<HD, 64>(a, st);
+  if (rows <= 32 || HD == 64) return run_kv<HD, 32>(a, st);  // (heads of 64: 64 rows' scores exceed the tensor memory)
+  return run_kv<128, 64>(a, st);
 }
 
 }  // namespace

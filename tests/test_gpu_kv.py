@@ -127,6 +127,15 @@ def check_attention(paged, row_start, seq_len, q, nh, got, lse):
     (128, 16, 1, 64, [400, 333], [1, 50]),          # 16 heads share one
     (128, 64, 1, 64, [200], [2]),                   # 64 heads share one
     (64, 7, 1, 16, [5, 6, 7, 130], [5, 1, 3, 2]),   # 7 heads share one
+    (64, 2, 2, 16, [700, 255, 256, 257], [1, 1, 1, 1]),   # every page size, single tokens and a few
+    (64, 2, 2, 32, [700, 255, 256, 257], [1, 1, 1, 1]),
+    (64, 2, 1, 64, [700, 31], [1, 1]),
+    (64, 2, 1, 128, [129, 600], [1, 1]),
+    (128, 2, 2, 16, [500, 127, 128], [1, 1, 1]),
+    (128, 2, 1, 32, [500, 33], [1, 1]),
+    (128, 2, 2, 128, [500, 1], [1, 1]),
+    (64, 4, 1, 32, [300, 77], [4, 3]),
+    (64, 4, 1, 128, [300, 77], [3, 4]),
 ])
 def test_attention_matches_oracle(device, d, nh, nkv, page, lens, news):
     r = syn.rng(3, f"kv/{d}/{nh}/{nkv}/{page}/{lens}/{news}")
