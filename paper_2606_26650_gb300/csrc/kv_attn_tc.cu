@@ -51,6 +51,7 @@ constexpr int kRows = 128;                   // shared-memory rows of a tile of 
 
 template <int HD, int R>
 struct KvLay {
+  static constexpr int kHd = HD;
   static constexpr int kR = R;                                       // rows of a row tile
   static constexpr int kTpr = 128 / HD;                              // tokens a shared-memory row
   static constexpr int kTok = kRows * kTpr;                          // cached tokens a tile
@@ -78,6 +79,7 @@ struct KvLay {
   static constexpr uint32_t kBudget = (kCtas == 2 ? 112 : 224) * 1024;
   static constexpr int kSlots0 = (kBudget - 1024 - kOffRing) / kTile;
   static constexpr int kSlots = kSlots0 > 12 ? 12 : kSlots0;
+  static constexpr uint32_t kBarFull = 0, kBarEmpty = 8 * kSlots, kBarScale = 16 * kSlots, kBarRest = kBarScale + 8 * kScaleRing;
   static constexpr uint32_t kSmem = kOffRing + kSlots * kTile + 1024;
   static constexpr int kPartFloats = R * (HD + 2);                   // maxima, sums, accumulators of a part
 };
@@ -323,6 +325,155 @@ struct KvTcArgs {
   WaitCtl wc;
 };
 
+// The run of this CTA: every CTA adds up all sequences' tiles, a thread a stretch of them.  scan [warps] and start [4]: shared
+// memory.  Every thread of the CTA comes here, and what it wrote before is visible to all afterwards, tensor memory's
+// address too.
+template <class Y>
+__device__ __forceinline__ KvWalk<Y> find_run(const KvTcArgs& p, int64_t* scan, int32_t* start, int64_t& run, int64_t& first) {
+  const KvGeom& g = p.g;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int64_t total;
+  {
+    const int32_t per = (g.B + Y::kThreads - 1) / Y::kThreads;
+    const int32_t b0 = min(static_cast<int32_t>(threadIdx.x) * per, g.B), b1 = min(b0 + per, g.B);
+    int64_t mine = 0;
+#pragma unroll 1
+    for (int32_t b = b0; b < b1; ++b)
+      mine += load_seq<Y>(g, b, blockIdx.x == 0 ? p.a.status : nullptr).per_head * g.nkv;
+    int64_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    if (lane == 31) scan[warp] = upto;
+    __syncthreads();
+    total = 0;
+#pragma unroll 1
+    for (int w = 0; w < Y::kThreads / 32; ++w) {
+      if (w < warp) upto += scan[w];
+      total += scan[w];
+    }
+    run = max((total + gridDim.x - 1) / gridDim.x, static_cast<int64_t>(p.min_run));
+    first = run * blockIdx.x;
+    if (upto - mine <= first && first < upto) {  // the thread whose stretch holds the run's first tile
+      int64_t rest = first - (upto - mine);
+      int32_t b = b0;
+      KvSeq s = load_seq<Y>(g, b, nullptr);
+#pragma unroll 1
+      while (rest >= s.per_head * g.nkv && b + 1 < b1) {
+        rest -= s.per_head * g.nkv;
+        s = load_seq<Y>(g, ++b, nullptr);
+      }
+      const int32_t h = static_cast<int32_t>(rest / max(s.per_head, static_cast<int64_t>(1)));
+      rest -= h * s.per_head;
+      int32_t q = 0;
+#pragma unroll 1
+      for (int32_t n; q < row_tiles<Y>(g, s) - 1 && rest >= (n = Y::kHead + tiles_of<Y>(visible<Y>(g, s, q))); ++q) rest -= n;
+      start[0] = b;
+      start[1] = h;
+      start[2] = q;
+      start[3] = static_cast<int32_t>(rest);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  KvWalk<Y> w;
+  w.at = first;
+  w.end = min(first + run, total);
+  if (w.at < w.end) {
+    w.b = start[0];
+    w.h = start[1];
+    w.q = start[2];
+    w.t = start[3];
+    w.s = load_seq<Y>(g, w.b, nullptr);
+  }
+  return w;
+}
+
+// The copying warp of a CTA: every tile of its run through the ring of NS slots.
+template <class Y>
+__device__ __forceinline__ void copy_tiles(const CUtensorMap& tmk, const CUtensorMap& tmv, const KvTcArgs& p, KvWalk<Y> w,
+                                           uint32_t base, float* scales) {
+  constexpr int NS = Y::kSlots, kTok = Y::kTok, TPR = Y::kTpr, HD = Y::kHd;
+  const uint32_t full0 = base + Y::kBarFull, empty0 = base + Y::kBarEmpty, scale_full0 = base + Y::kBarScale;
+  const int lane = threadIdx.x & 31;
+  const KvGeom& g = p.g;
+  const KvCacheDev& kv = p.a.cache;
+  const int32_t ppt = kTok / kv.page;  // pages a tile
+  bool ok = true;
+  int slot = 0, loads = 0;
+  uint32_t ph = 1, gt = 0;
+  // A lane a page: the lane's page in tile t of the segment (first row of its block, -1: none), its scales.
+  struct Page {
+    int32_t row;
+    float ks, vs;
+  };
+  auto page_of = [&](int32_t j) -> int32_t {
+    const int32_t tok = (w.t0 + j) * kTok + lane * kv.page;
+    if (j >= w.n || lane >= ppt || tok >= w.vis) return -1;
+    return __ldg(kv.table + static_cast<int64_t>(w.sb) * kv.max_pages + tok / kv.page);
+  };
+  auto block_of = [&](int32_t j, int32_t id) {
+    Page g{-1, 0.0f, 0.0f};
+    if (j >= w.n || lane >= ppt || (w.t0 + j) * kTok + lane * kv.page >= w.vis) return g;
+    if (id < 0 || id >= kv.n_pages) {
+      atomicCAS(p.a.status, 0, 10 /* CATQ_ERR_INDEX */);
+      g.row = kv.n_pages * kv.nkv * (kv.page / TPR);  // behind the last row: zeros
+      return g;
+    }
+    const int32_t block = id * kv.nkv + w.sh;
+    g.row = block * (kv.page / TPR);
+    g.ks = __ldg(kv.k_scale + block);
+    g.vs = __ldg(kv.v_scale + block);
+    return g;
+  };
+  // A tile into the next slot; with its keys go its scales, into a ring of kScaleRing tiles of their own.  That is
+  // deep enough without an empty barrier: while a tile's scales are read its values hold their slot, and the NS slots
+  // from there on hold the keys of at most NS / 2 + 3 further tiles.
+  static_assert(NS / 2 + 4 <= kScaleRing, "ring of scales");
+  auto load = [&](const CUtensorMap* map, const Page& g, bool keys) -> bool {
+    const uint32_t pages = __popc(__ballot_sync(0xffffffffu, g.row >= 0));
+    if (!mbar_wait_warp(empty0 + 8u * slot, ph, p.wc)) return false;
+    if (lane == 0) mbar_arrive_expect_tx(full0 + 8u * slot, pages * kv.page * HD);
+    __syncwarp();
+    if (g.row >= 0)
+      tma_load_2d(base + Y::kOffRing + slot * Y::kTile + lane * kv.page * HD, map, full0 + 8u * slot, 0, g.row);
+    if (keys) {
+      if (lane < Y::kPages) {
+        float* const to = scales + (gt % kScaleRing) * (2 * Y::kPages);
+        to[lane] = g.ks;
+        to[Y::kPages + lane] = g.vs;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive_local(scale_full0 + 8u * (gt % kScaleRing));
+      ++gt;
+    }
+    ++loads;
+    if (++slot == NS) { slot = 0; ph ^= 1u; }
+    return true;
+  };
+  while (ok && w.next(g)) {
+    // In the order in which the products take them: K0 K1 V0 K2 V1 ...; a tile's page number is asked for two tiles
+    // ahead and its scales one, so that only a segment's first wait for memory.
+    const int32_t id0 = page_of(0), id1 = page_of(1);
+    int32_t id = page_of(2);
+    Page g0 = block_of(0, id0), g1 = block_of(1, id1), g2{-1, 0.0f, 0.0f};
+    ok = load(&tmk, g0, true) && (w.n < 2 || load(&tmk, g1, true));
+    for (int32_t j = 0; ok && j < w.n; ++j) {
+      g2 = block_of(j + 2, id);
+      id = page_of(j + 3);
+      ok = load(&tmv, g0, false) && (j + 2 >= w.n || load(&tmk, g2, true));
+      g0 = g1;
+      g1 = g2;
+    }
+  }
+  // copies still in flight land before the CTA exits
+#pragma unroll 1
+  for (int t = max(0, loads - NS); t < loads; ++t) drain(full0 + 8u * (t % NS), (t / NS) & 1);
+}
+
 template <int HD, int R>
 __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
     kv_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const KvTcArgs p) {
@@ -334,9 +485,10 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* const gbase = smem_raw + (base - raw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t full0 = base, empty0 = base + 8u * NS, s_full0 = base + 16u * NS, p_full0 = s_full0 + 16,
-                 pv_done0 = p_full0 + 16, q_full = pv_done0 + 16, final_bar = q_full + 8, scale_full0 = final_bar + 8;
-  static_assert(16 * NS + 3 * 16 + 2 * 8 + 8 * kScaleRing <= 400, "barriers");
+  const uint32_t full0 = base + Y::kBarFull, empty0 = base + Y::kBarEmpty, scale_full0 = base + Y::kBarScale,
+                 s_full0 = base + Y::kBarRest, p_full0 = s_full0 + 16, pv_done0 = p_full0 + 16, q_full = pv_done0 + 16,
+                 final_bar = q_full + 8;
+  static_assert(Y::kBarRest + 3 * 16 + 2 * 8 <= 400, "barriers");
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(gbase + 400);
   int32_t* const merge_flag = reinterpret_cast<int32_t*>(gbase + 404);
   int32_t* const start = reinterpret_cast<int32_t*>(gbase + 408);           // b, h, q, t of the run's first tile
@@ -375,141 +527,16 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
   grid_launch_dependents();
   grid_dependency_wait();
 
-  // The run of this CTA: every CTA adds up all sequences' tiles, a thread a stretch of them.
   const KvGeom& g = p.g;
-  int64_t run, total, first;
-  {
-    const int32_t per = (g.B + kThreads - 1) / kThreads;
-    const int32_t b0 = min(static_cast<int32_t>(threadIdx.x) * per, g.B), b1 = min(b0 + per, g.B);
-    int64_t mine = 0;
-#pragma unroll 1
-    for (int32_t b = b0; b < b1; ++b)
-      mine += load_seq<Y>(g, b, blockIdx.x == 0 ? p.a.status : nullptr).per_head * g.nkv;
-    int64_t upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += v;
-    }
-    if (lane == 31) scan[warp] = upto;
-    __syncthreads();
-    total = 0;
-#pragma unroll 1
-    for (int w = 0; w < kThreads / 32; ++w) {
-      if (w < warp) upto += scan[w];
-      total += scan[w];
-    }
-    run = max((total + gridDim.x - 1) / gridDim.x, static_cast<int64_t>(p.min_run));
-    first = run * blockIdx.x;
-    if (upto - mine <= first && first < upto) {  // the thread whose stretch holds the run's first tile
-      int64_t rest = first - (upto - mine);
-      int32_t b = b0;
-      KvSeq s = load_seq<Y>(g, b, nullptr);
-#pragma unroll 1
-      while (rest >= s.per_head * g.nkv && b + 1 < b1) {
-        rest -= s.per_head * g.nkv;
-        s = load_seq<Y>(g, ++b, nullptr);
-      }
-      const int32_t h = static_cast<int32_t>(rest / max(s.per_head, static_cast<int64_t>(1)));
-      rest -= h * s.per_head;
-      int32_t q = 0;
-#pragma unroll 1
-      for (int32_t n; q < row_tiles<Y>(g, s) - 1 && rest >= (n = Y::kHead + tiles_of<Y>(visible<Y>(g, s, q))); ++q) rest -= n;
-      start[0] = b;
-      start[1] = h;
-      start[2] = q;
-      start[3] = static_cast<int32_t>(rest);
-    }
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
+  int64_t run, first;
+  KvWalk<Y> w = find_run<Y>(p, scan, start, run, first);
   const uint32_t tmem = *tmem_slot;
   constexpr uint32_t kColO = Y::kColO;
-  KvWalk<Y> w;
-  w.at = first;
-  w.end = min(first + run, total);
-  if (w.at < w.end) {
-    w.b = start[0];
-    w.h = start[1];
-    w.q = start[2];
-    w.t = start[3];
-    w.s = load_seq<Y>(g, w.b, nullptr);
-  }
   const KvCacheDev& kv = p.a.cache;
-  const int32_t ppt = kTok / kv.page;  // pages a tile
   bool ok = true;
 
   if (warp == Y::kTmaWarp) {
-    int slot = 0, loads = 0;
-    uint32_t ph = 1, gt = 0;
-    // A lane a page: the lane's page in tile t of the segment (first row of its block, -1: none), its scales.
-    struct Page {
-      int32_t row;
-      float ks, vs;
-    };
-    auto page_of = [&](int32_t j) -> int32_t {
-      const int32_t tok = (w.t0 + j) * kTok + lane * kv.page;
-      if (j >= w.n || lane >= ppt || tok >= w.vis) return -1;
-      return __ldg(kv.table + static_cast<int64_t>(w.sb) * kv.max_pages + tok / kv.page);
-    };
-    auto block_of = [&](int32_t j, int32_t id) {
-      Page g{-1, 0.0f, 0.0f};
-      if (j >= w.n || lane >= ppt || (w.t0 + j) * kTok + lane * kv.page >= w.vis) return g;
-      if (id < 0 || id >= kv.n_pages) {
-        atomicCAS(p.a.status, 0, 10 /* CATQ_ERR_INDEX */);
-        g.row = kv.n_pages * kv.nkv * (kv.page / TPR);  // behind the last row: zeros
-        return g;
-      }
-      const int32_t block = id * kv.nkv + w.sh;
-      g.row = block * (kv.page / TPR);
-      g.ks = __ldg(kv.k_scale + block);
-      g.vs = __ldg(kv.v_scale + block);
-      return g;
-    };
-    // A tile into the next slot; with its keys go its scales, into a ring of kScaleRing tiles of their own.  That is
-    // deep enough without an empty barrier: while a tile's scales are read its values hold their slot, and the NS slots
-    // from there on hold the keys of at most NS / 2 + 3 further tiles.
-    static_assert(NS / 2 + 4 <= kScaleRing, "ring of scales");
-    auto load = [&](const CUtensorMap* map, const Page& g, bool keys) -> bool {
-      const uint32_t pages = __popc(__ballot_sync(0xffffffffu, g.row >= 0));
-      if (!mbar_wait_warp(empty0 + 8u * slot, ph, p.wc)) return false;
-      if (lane == 0) mbar_arrive_expect_tx(full0 + 8u * slot, pages * kv.page * HD);
-      __syncwarp();
-      if (g.row >= 0)
-        tma_load_2d(base + Y::kOffRing + slot * Y::kTile + lane * kv.page * HD, map, full0 + 8u * slot, 0, g.row);
-      if (keys) {
-        if (lane < Y::kPages) {
-          float* const to = scales + (gt % kScaleRing) * (2 * Y::kPages);
-          to[lane] = g.ks;
-          to[Y::kPages + lane] = g.vs;
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive_local(scale_full0 + 8u * (gt % kScaleRing));
-        ++gt;
-      }
-      ++loads;
-      if (++slot == NS) { slot = 0; ph ^= 1u; }
-      return true;
-    };
-    while (ok && w.next(g)) {
-      // In the order in which the products take them: K0 K1 V0 K2 V1 ...; a tile's page number is asked for two tiles
-      // ahead and its scales one, so that only a segment's first wait for memory.
-      const int32_t id0 = page_of(0), id1 = page_of(1);
-      int32_t id = page_of(2);
-      Page g0 = block_of(0, id0), g1 = block_of(1, id1), g2{-1, 0.0f, 0.0f};
-      ok = load(&tmk, g0, true) && (w.n < 2 || load(&tmk, g1, true));
-      for (int32_t j = 0; ok && j < w.n; ++j) {
-        g2 = block_of(j + 2, id);
-        id = page_of(j + 3);
-        ok = load(&tmv, g0, false) && (j + 2 >= w.n || load(&tmk, g2, true));
-        g0 = g1;
-        g1 = g2;
-      }
-    }
-    // copies still in flight land before the CTA exits
-#pragma unroll 1
-    for (int t = max(0, loads - NS); t < loads; ++t) drain(full0 + 8u * (t % NS), (t / NS) & 1);
+    copy_tiles<Y>(tmk, tmv, p, w, base, scales);
   } else if (warp == Y::kMmaWarp) {
     constexpr uint32_t idesc_s = idesc_e4m3(kRows, NC, false, false), idesc_o = idesc_e4m3(HD, NC, true, true);
     constexpr uint32_t kHi = desc_hi(1024, 2);  // code tiles: 8 swizzled rows of 128 bytes from one group to the next
@@ -956,6 +983,418 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
   }
 }
 
+// ---------------------------------------------------------------- many rows a key/value head
+// Row tiles of 128 rows (heads of 128): the rows are the M of both products, a thread pair's each,
+//   S [128 rows, 128 tokens] = (Q_hi + Q_lo) K^T,      O [128 rows, 128] += (P_hi + P_lo) V,
+// with queries and weights in tensor memory and the codes as B operands, K as it lies, V MN-major.  Against the other
+// kernel's products, whose operands both come from shared memory (1,300 cycles for a tile of 128 tokens and 64 rows), a tile
+// of 128 rows takes 1,024.  hi and lo add into one accumulator, so lo has hi's unit: x = hi + lo with lo = e4m3(x - hi), 4 + 4
+// significant bits down to lo's least step, 2^-9: of a query whose largest element lies in (224, 448] all but 2^-19 of that;
+// of weights 2^-10 at most, which is 2^-17 of the largest where that is 2^kNominalRows.
+// Thread (row, half c) has the row's tokens 64 c .. 64 c + 63 of a tile.  The two agree on the row's maximum through shared
+// memory; raising it is lazy, as there, row by row.
+constexpr float kNominalRows = 7.0f;
+struct KvMany {
+  static constexpr int kHd = 128, kR = 128, kTpr = 1, kTok = kRows, kHead = 4, kPages = kTok / 16;
+  static constexpr int kSoft = 256, kTmaWarp = 8, kMmaWarp = 9, kThreads = 320, kSlots = 12;
+  static constexpr uint32_t kTile = kRows * 128, kTmem = 512;
+  static constexpr uint32_t kColO = 256, kColQ = 384;  // scores twice, accumulators, queries (32 columns hi, 32 lo)
+  static constexpr uint32_t kBarFull = 0, kBarEmpty = 8 * kSlots, kBarScale = 16 * kSlots, kBarRest = kBarScale + 8 * kScaleRing;
+  static constexpr uint32_t kOffScale = 640, kOffEx = kOffScale + kScaleRing * 8 * kPages, kOffRing = 6 * 1024;
+  static constexpr uint32_t kSmem = kOffRing + kSlots * kTile + 1024;
+  static constexpr int kPartFloats = kR * (kHd + 2);
+  static_assert(kOffEx + 4 * 128 * 4 <= kOffRing, "exchange");
+};
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
+          taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+// D[tmem] (+)= A[tmem] B[smem], A: a row a lane, four e4m3 elements a column.
+__device__ __forceinline__ void umma_f8_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                           uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 db, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], db, %4, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// Four values as the words of either term, hi + lo.
+__device__ __forceinline__ void split4(const float* x, uint32_t& hi, uint32_t& lo) {
+  uint16_t h[2], l[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t h16, back;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h16) : "f"(x[2 * i + 1]), "f"(x[2 * i]));
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(h[i]) : "r"(h16));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(h[i]));
+    const __half2 rest = __hsub2(*reinterpret_cast<const __half2*>(&h16), *reinterpret_cast<const __half2*>(&back));
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(l[i]) : "r"(*reinterpret_cast<const uint32_t*>(&rest)));
+  }
+  hi = h[0] | static_cast<uint32_t>(h[1]) << 16;
+  lo = l[0] | static_cast<uint32_t>(l[1]) << 16;
+}
+
+__global__ void __launch_bounds__(KvMany::kThreads, 1)
+    kv_attn_rows_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const KvTcArgs p) {
+  using Y = KvMany;
+  constexpr int NS = Y::kSlots, HD = 128, R = Y::kR, kTok = Y::kTok;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* const gbase = smem_raw + (base - raw);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t full0 = base + Y::kBarFull, empty0 = base + Y::kBarEmpty, scale_full0 = base + Y::kBarScale,
+                 s_full0 = base + Y::kBarRest, p_full0 = s_full0 + 16, pv_done0 = p_full0 + 16, q_full = pv_done0 + 16,
+                 final_bar = q_full + 8;
+  static_assert(Y::kBarRest + 3 * 16 + 2 * 8 <= 400, "barriers");
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(gbase + 400);
+  int32_t* const merge_flag = reinterpret_cast<int32_t*>(gbase + 404);
+  int32_t* const start = reinterpret_cast<int32_t*>(gbase + 408);
+  int64_t* const scan = reinterpret_cast<int64_t*>(gbase + 424);
+  static_assert(424 + 8 * (Y::kThreads / 32) <= Y::kOffScale, "start");
+  float* const scales = reinterpret_cast<float*>(gbase + Y::kOffScale);
+  float* const ex = reinterpret_cast<float*>(gbase + Y::kOffEx);  // [2][2][128]: what the halves of a row tell each other
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < NS; ++i) {
+      mbar_init(full0 + 8u * i, 1);
+      mbar_init(empty0 + 8u * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_full0 + 8u * i, 1);
+      mbar_init(p_full0 + 8u * i, Y::kSoft / 32);
+      mbar_init(pv_done0 + 8u * i, 1);
+    }
+    for (int i = 0; i < kScaleRing; ++i) mbar_init(scale_full0 + 8u * i, 1);
+    mbar_init(q_full, Y::kSoft / 32);
+    mbar_init(final_bar, 1);
+    fence_mbar_init_cluster();
+  }
+  if (warp == Y::kMmaWarp) tmem_alloc<1>(smem_u32(tmem_slot), Y::kTmem);
+  if (warp == Y::kTmaWarp && lane == 0) {
+    prefetch_tmap(&tmk);
+    prefetch_tmap(&tmv);
+  }
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const KvGeom& g = p.g;
+  int64_t run, first;
+  KvWalk<Y> w = find_run<Y>(p, scan, start, run, first);
+  const uint32_t tmem = *tmem_slot;
+  const KvCacheDev& kv = p.a.cache;
+  bool ok = true;
+
+  if (warp == Y::kTmaWarp) {
+    copy_tiles<Y>(tmk, tmv, p, w, base, scales);
+  } else if (warp == Y::kMmaWarp) {
+    constexpr uint32_t idesc_s = idesc_e4m3(R, kTok, false, false), idesc_o = idesc_e4m3(R, HD, false, true);
+    constexpr uint32_t kHi = desc_hi(1024, 2);
+    const bool issuer = elect_one();
+    int slot = 0;
+    uint32_t ph = 0, gt = 0, seg = 0;
+    auto step = [&] {
+      if (++slot == NS) { slot = 0; ph ^= 1u; }
+    };
+    auto issue_s = [&](uint32_t buf) -> bool {
+      if (!mbar_wait_warp(full0 + 8u * slot, ph, p.wc)) return false;
+      tc_fence_after();
+      if (issuer) {
+        const uint32_t bd = desc_lo(base + Y::kOffRing + slot * Y::kTile, 16);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)  // hi, then lo
+          umma_f8_ts(tmem + 128 * buf, tmem + Y::kColQ + 8 * k, bd + 2 * (k % 4), kHi, idesc_s, k > 0 ? 1u : 0u);
+        umma_commit<1>(s_full0 + 8u * buf);
+        umma_commit<1>(empty0 + 8u * slot);
+      }
+      step();
+      return true;
+    };
+    while (ok && w.next(g)) {
+      if (!mbar_wait_warp(q_full, seg & 1, p.wc)) { ok = false; break; }
+      tc_fence_after();
+      if (!issue_s(gt & 1) || (w.n > 1 && !issue_s((gt + 1) & 1))) { ok = false; break; }
+      ++seg;
+#pragma unroll 1
+      for (int32_t j = 0; j < w.n; ++j, ++gt) {
+        const uint32_t buf = gt & 1;
+        if (!mbar_wait_warp(full0 + 8u * slot, ph, p.wc) || !mbar_wait_warp(p_full0 + 8u * buf, (gt >> 1) & 1, p.wc)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        if (issuer) {
+          const uint32_t bd = desc_lo(base + Y::kOffRing + slot * Y::kTile, 16);
+#pragma unroll
+          for (int k = 0; k < 8; ++k)  // 32 tokens at a time: halves of 64, hi words in their first 16 columns, lo in the next
+            umma_f8_ts(tmem + Y::kColO, tmem + 128 * buf + 64 * (k % 4 / 2) + 8 * (k % 2) + 16 * (k / 4), bd + 256 * (k % 4), kHi,
+                       idesc_o, (j > 0 || k > 0) ? 1u : 0u);
+          umma_commit<1>(pv_done0 + 8u * buf);
+          umma_commit<1>(empty0 + 8u * slot);
+        }
+        step();
+        if (j + 2 < w.n && !issue_s(buf)) { ok = false; break; }
+      }
+    }
+    if (issuer) umma_commit<1>(final_bar);
+    __syncwarp();
+    drain(final_bar, 0);  // every MMA has completed before TMEM is released
+  } else {
+    const int quarter = warp & 3, c = warp >> 2, row = quarter * 32 + lane;
+    constexpr int kEvery = 5;
+    const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+    uint32_t gt = 0, ring = 0;
+    // (see the other kernel's)
+    auto wait_pv = [&](uint32_t t) { return mbar_wait_warp(pv_done0 + 8u * (t & 1), (t >> 1) & 1, p.wc); };
+    while (w.next(g)) {
+      if (!bar_all(kEvery, Y::kSoft, ok)) { ok = false; break; }
+      const int32_t at = w.sq * R + row, tk = g.token_of(at), head = w.sh * g.group + at - tk * g.group;
+      const bool mine = at < w.rows_n * g.group;
+      const int32_t lim = mine ? w.len - w.rows_n + tk : -1;
+      const int32_t sees_all = w.len - w.rows_n + g.token_of(w.sq * R) + 1;  // (the first row's, the others' at least that)
+      float f;
+      {
+        uint4 q[8];
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          q[k] = make_uint4(0u, 0u, 0u, 0u);
+          if (mine) q[k] = *reinterpret_cast<const uint4*>(p.a.q + (w.r0 + tk) * p.a.ldq + head * HD + 64 * c + 8 * k);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t u[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = max(top, max(u[e] << 16 & 0x7fffffffu, u[e] & 0x7fff0000u));
+        }
+        ex[c * 128 + row] = __uint_as_float(top);
+        bar_sync(1 + quarter, 64);
+        top = max(top, __float_as_uint(ex[(c ^ 1) * 128 + row]));
+        // 2^-e brings the largest element into (224, 448]; a row that is not finite has NaN as its factor
+        const int e = max(static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), -100);
+        const bool bad = top >= 0x7f800000u;
+        const float by = bad ? 0.0f : __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+        f = bad ? __uint_as_float(0x7fffffffu) : __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * p.a.scale_log2;
+        uint32_t hi[16], lo[16];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t u[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[2 * i] = bad ? 0.0f : __uint_as_float(u[i] << 16) * by;
+            x[2 * i + 1] = bad ? 0.0f : __uint_as_float(u[i] & 0xffff0000u) * by;
+          }
+          split4(x, hi[2 * k], lo[2 * k]);
+          split4(x + 4, hi[2 * k + 1], lo[2 * k + 1]);
+        }
+        tmem_st16(lanes + Y::kColQ + 16 * c, hi);
+        tmem_st16(lanes + Y::kColQ + 32 + 16 * c, lo);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_local(q_full);
+      }
+      float m = kNoMax, l = 0.0f;
+      bool failed = false;
+#pragma unroll 1
+      for (int32_t j = 0; j < w.n; ++j, ++gt) {
+        const uint32_t buf = gt & 1, sbuf = lanes + 128 * buf + 64 * c;
+        const int32_t tile = (w.t0 + j) * kTok;
+        ok = mbar_wait_warp(scale_full0 + 8u * (gt % kScaleRing), (gt / kScaleRing) & 1, p.wc) && ok;
+        const float* const sc = scales + (gt % kScaleRing) * (2 * Y::kPages);
+        float ks[4], lsv[4], inv[4];  // of 16 tokens each (see the other kernel)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int at_page = (64 * c + 16 * i) / kv.page;
+          ks[i] = sc[at_page];
+          uint32_t vb = __float_as_uint(sc[Y::kPages + at_page]);
+          if (vb == 0u) vb = (127u - 20u) << 23;
+          if (vb >= 0x7f800000u) {
+            ks[i] = __uint_as_float(0x7fffffffu);
+            vb = 127u << 23;
+          }
+          lsv[i] = static_cast<float>(static_cast<int>(vb >> 23) - 127);
+          inv[i] = __uint_as_float((254u - (vb >> 23)) << 23);
+        }
+        ok = mbar_wait_warp(s_full0 + 8u * buf, (gt >> 1) & 1, p.wc) && ok;
+        tc_fence_after();
+        if (c == 0 && tile + kTok > w.vis) {
+          // the values behind the last visible token become zeros
+          const uint32_t vat = ring + min(2, w.n) + j + max(0, min(j, w.n - 2)), sl = vat % NS;
+          ok = mbar_wait_warp(full0 + 8u * sl, (vat / NS) & 1, p.wc) && ok;
+          uint4* const v = reinterpret_cast<uint4*>(gbase + Y::kOffRing + sl * Y::kTile);
+#pragma unroll 1
+          for (int32_t i = max(w.vis - tile, 0) * 8 + row; i < kRows * 8; i += 128) v[i] = make_uint4(0u, 0u, 0u, 0u);
+          fence_proxy_async_smem();
+        }
+        uint32_t v[2][32];
+        tmem_ld32(sbuf, v[0]);
+        tmem_ld32(sbuf + 32, v[1]);
+        tmem_ld_wait();
+        float x[64], top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 64; i += 2) {
+          const float2 t = fma2(make_float2(__uint_as_float(v[i / 32][i % 32]), __uint_as_float(v[i / 32][i % 32 + 1])),
+                                both(f * ks[i / 16]), both(lsv[i / 16]));
+          x[i] = t.x;
+          x[i + 1] = t.y;
+        }
+        if (tile + kTok > sees_all) {
+          const int32_t sees = lim - tile - 64 * c;  // the thread's last visible token
+#pragma unroll
+          for (int i = 0; i < 64; ++i)
+            if (i > sees) x[i] = -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < 64; i += 2) top = max3(top, x[i], x[i + 1]);
+        ex[buf * 256 + c * 128 + row] = top;
+        if (!bar_all(1 + quarter, 64, ok)) { failed = true; break; }
+        top = fmaxf(top, ex[buf * 256 + (c ^ 1) * 128 + row]);
+        const bool raise = top - m > kOver;
+        if (__any_sync(0xffffffffu, raise)) {
+          const float to = raise ? top - kNominalRows : m, fac = raise ? fast_exp2(m - to) : 1.0f;
+          m = to;
+          l *= fac;
+          if (j > 0) {
+            ok = wait_pv(gt - 1) && ok;
+            tc_fence_after();
+            const float2 f4[4] = {both(fac), both(fac), both(fac), both(fac)};
+#pragma unroll 1
+            for (int i = 0; i < 64; i += 8) scale_cols8(lanes + Y::kColO + 64 * c + i, f4);
+            tmem_st_wait();
+          }
+        }
+        uint32_t hi[16], lo[16];
+#pragma unroll
+        for (int i = 0; i < 64; i += 16) {
+          float2 sum = both(0.0f);
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) {
+            const float2 y = fma2(both(m), both(-1.0f), make_float2(x[i + e], x[i + e + 1]));
+            x[i + e] = fast_exp2(y.x);
+            x[i + e + 1] = fast_exp2(y.y);
+            sum = fma2(make_float2(x[i + e], x[i + e + 1]), both(1.0f), sum);
+          }
+          l = fmaf(sum.x + sum.y, inv[i / 16], l);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) split4(x + i + 4 * e, hi[i / 4 + e], lo[i / 4 + e]);
+        }
+        tmem_st16(sbuf, hi);
+        tmem_st16(sbuf + 16, lo);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_local(p_full0 + 8u * buf);
+      }
+      ring += 2 * w.n;
+      const bool whole = w.n == w.all;
+      float* const part = p.parts + (2 * static_cast<int64_t>(blockIdx.x) + (w.begin >= first ? 1 : 0)) * Y::kPartFloats;
+      uint16_t* const out = p.a.o + (w.r0 + tk) * p.a.ldo + head * HD + 64 * c;
+      const int64_t lse_at = static_cast<int64_t>(w.r0 + tk) * p.a.nh + head;
+      if (!failed) {
+        // (the exchange of the tile before last is free: this pair has met since)
+        ex[(gt & 1) * 256 + c * 128 + row] = l;
+        bar_sync(1 + quarter, 64);
+        const float sum = c == 0 ? l + ex[(gt & 1) * 256 + 128 + row] : ex[(gt & 1) * 256 + row] + l;
+        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+        if (mine && c == 0) {
+          if (!whole) {
+            part[row] = m;
+            part[R + row] = sum;
+          } else if (p.a.lse) {
+            p.a.lse[lse_at] = sum == 0.0f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
+          }
+        }
+        ok = wait_pv(gt - 1) && ok;
+        tc_fence_after();
+#pragma unroll 1
+        for (int i = 0; i < 64; i += 16) {
+          uint32_t o[16];
+          tmem_ld16(lanes + Y::kColO + 64 * c + i, o);
+          tmem_ld_wait();
+          if (!mine || !ok) continue;
+          if (whole) {
+            uint32_t two[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float a = by == 0.0f ? 0.0f : __uint_as_float(o[2 * e]) * by;
+              const float b = by == 0.0f ? 0.0f : __uint_as_float(o[2 * e + 1]) * by;
+              asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(two[e]) : "f"(b), "f"(a));
+            }
+            *reinterpret_cast<uint4*>(out + i) = make_uint4(two[0], two[1], two[2], two[3]);
+            *reinterpret_cast<uint4*>(out + i + 8) = make_uint4(two[4], two[5], two[6], two[7]);
+          } else {
+            uint4* const to = reinterpret_cast<uint4*>(part + 2 * R + row * HD + 64 * c + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) to[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          }
+        }
+        tc_fence_before();
+      }
+      ok = ok && !failed;
+      if (whole) continue;
+      // the last of the row tile's runs joins their parts, a thread its half of its row
+      if (!bar_all(kEvery, Y::kSoft, ok)) { ok = false; break; }
+      const int32_t c0 = static_cast<int32_t>(w.begin / run), c1 = static_cast<int32_t>((w.begin + w.all - 1) / run);
+      if (threadIdx.x == 0) {
+        const uint32_t last = static_cast<uint32_t>(c1 - c0);
+        uint32_t old;
+        asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(old) : "l"(p.counters + c0), "r"(last) : "memory");
+        *merge_flag = old == last;
+      }
+      bar_sync(kEvery, Y::kSoft);
+      if (*merge_flag && mine) {
+        float top = kNoMax, sum = 0.0f, acc[64];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) acc[i] = 0.0f;
+#pragma unroll 1
+        for (int32_t r = c0; r <= c1; ++r) {
+          const float* const q = p.parts + (2 * static_cast<int64_t>(r) + (r == c0 ? 1 : 0)) * Y::kPartFloats;
+          float4 v[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = __ldcg(reinterpret_cast<const float4*>(q + 2 * R + row * HD + 64 * c) + i);
+          const float pm = __ldcg(q + row), pl = __ldcg(q + R + row), to = fmaxf(top, pm);
+          const float fa = fast_exp2(top - to), fb = fast_exp2(pm - to);
+          sum = sum * fa + pl * fb;
+          top = to;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            acc[4 * i] = acc[4 * i] * fa + v[i].x * fb;
+            acc[4 * i + 1] = acc[4 * i + 1] * fa + v[i].y * fb;
+            acc[4 * i + 2] = acc[4 * i + 2] * fa + v[i].z * fb;
+            acc[4 * i + 3] = acc[4 * i + 3] * fa + v[i].w * fb;
+          }
+        }
+        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+        if (p.a.lse && c == 0) p.a.lse[lse_at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+#pragma unroll
+        for (int i = 0; i < 64; i += 8) {
+          uint32_t two[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;"
+                : "=r"(two[e])
+                : "f"(by == 0.0f ? 0.0f : acc[i + 2 * e + 1] * by), "f"(by == 0.0f ? 0.0f : acc[i + 2 * e] * by));
+          *reinterpret_cast<uint4*>(out + i) = make_uint4(two[0], two[1], two[2], two[3]);
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == Y::kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc<1>(tmem, Y::kTmem);
+  }
+}
+
 PFN_cuTensorMapEncodeTiled_v12000 g_enc = nullptr;
 std::once_flag g_enc_once;
 
@@ -986,9 +1425,9 @@ int sm_count() {
 
 constexpr size_t kCounterBytes = 4096;  // up to 1024 CTAs
 
-template <int HD, int R>
-cudaError_t run_kv(const KvAttnArgs& a, cudaStream_t st) {
-  using Y = KvLay<HD, R>;
+template <class Y>
+cudaError_t run_kv(void (*kern)(CUtensorMap, CUtensorMap, KvTcArgs), int ctas, const KvAttnArgs& a, cudaStream_t st) {
+  constexpr int HD = Y::kHd;
   CUtensorMap tk, tv;
   const int64_t rows = static_cast<int64_t>(a.cache.n_pages) * a.cache.nkv * a.cache.page;
   if (!tmap_codes(&tk, a.cache.k_codes, HD, rows, a.cache.page) || !tmap_codes(&tv, a.cache.v_codes, HD, rows, a.cache.page))
@@ -1003,7 +1442,6 @@ cudaError_t run_kv(const KvAttnArgs& a, cudaStream_t st) {
   p.counters = static_cast<uint32_t*>(a.workspace);
   p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + kCounterBytes);
   p.min_run = Y::kHead + 2;
-  auto kern = kv_attn_kernel<HD, R>;
   static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -1015,7 +1453,7 @@ cudaError_t run_kv(const KvAttnArgs& a, cudaStream_t st) {
     ready.fetch_or(bit, std::memory_order_relaxed);
   }
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(std::min(Y::kCtas * sm_count(), 1024)));
+  cfg.gridDim = dim3(static_cast<unsigned>(std::min(ctas * sm_count(), 1024)));
   cfg.blockDim = dim3(Y::kThreads);
   cfg.dynamicSmemBytes = Y::kSmem;
   cfg.stream = st;
@@ -1029,21 +1467,24 @@ cudaError_t run_kv(const KvAttnArgs& a, cudaStream_t st) {
 }
 
 // Rows of a tile: what an average sequence has a key/value head (any number is right).
+template <int HD, int R>
+cudaError_t run_few(const KvAttnArgs& a, cudaStream_t st) {
+  return run_kv<KvLay<HD, R>>(kv_attn_kernel<HD, R>, KvLay<HD, R>::kCtas, a, st);
+}
 template <int HD>
 cudaError_t run_kv_rows(const KvAttnArgs& a, cudaStream_t st) {
   const int64_t rows = (a.T + a.B - 1) / a.B * (a.nh / a.cache.nkv);
-  if (rows <= 8) return run_kv<HD, 8>(a, st);
-  if (rows <= 16) return run_kv<HD, 16>(a, st);
-  if (rows <= 32 || HD == 64) return run_kv<HD, 32>(a, st);  // (heads of 64: 64 rows' scores exceed the tensor memory)
-  return run_kv<128, 64>(a, st);
+  if (rows <= 8) return run_few<HD, 8>(a, st);
+  if (rows <= 16) return run_few<HD, 16>(a, st);
+  if (rows <= 32 || HD == 64) return run_few<HD, 32>(a, st);
+  return run_kv<KvMany>(kv_attn_rows_kernel, 1, a, st);
 }
 
 }  // namespace
 
 size_t kv_attention_ws_bytes(int32_t, int32_t, int32_t d) {
-  // two parts for each CTA: three CTAs an SM of 8 rows, two of up to 32, one of 64
-  const size_t ctas = 2 * static_cast<size_t>(sm_count());
-  const size_t parts = ctas * 2 * 32 * (static_cast<size_t>(d) + 2) * sizeof(float);
+  // two parts for each CTA: two CTAs an SM of up to 32 rows, one of 128
+  const size_t parts = static_cast<size_t>(sm_count()) * 2 * (d == 128 ? 128 : 64) * (static_cast<size_t>(d) + 2) * sizeof(float);
   return (kCounterBytes + parts + 255) / 256 * 256;
 }
 
