@@ -991,29 +991,21 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
 // of 128 rows takes 1,024.  hi and lo add into one accumulator, so lo has hi's unit: x = hi + lo with lo = e4m3(x - hi), 4 + 4
 // significant bits down to lo's least step, 2^-9: of a query whose largest element lies in (224, 448] all but 2^-19 of that;
 // of weights 2^-10 at most, which is 2^-17 of the largest where that is 2^kNominalRows.
-// Thread (row, half c) has the row's tokens 64 c .. 64 c + 63 of a tile.  The two agree on the row's maximum through shared
-// memory; raising it is lazy, as there, row by row.
+// Thread (row, quarter c) has the row's tokens 32 c .. 32 c + 31 of a tile.  The four agree on the row's maximum through
+// shared memory; raising it is lazy, as there, row by row.
 constexpr float kNominalRows = 7.0f;
 struct KvMany {
   static constexpr int kHd = 128, kR = 128, kTpr = 1, kTok = kRows, kHead = 4, kPages = kTok / 16;
-  static constexpr int kSoft = 256, kTmaWarp = 8, kMmaWarp = 9, kThreads = 320, kSlots = 12;
+  static constexpr int kShare = 4;  // threads a row
+  static constexpr int kSoft = 128 * kShare, kTmaWarp = 4 * kShare, kMmaWarp = kTmaWarp + 1, kThreads = kSoft + 64, kSlots = 12;
   static constexpr uint32_t kTile = kRows * 128, kTmem = 512;
   static constexpr uint32_t kColO = 256, kColQ = 384;  // scores twice, accumulators, queries (32 columns hi, 32 lo)
   static constexpr uint32_t kBarFull = 0, kBarEmpty = 8 * kSlots, kBarScale = 16 * kSlots, kBarRest = kBarScale + 8 * kScaleRing;
-  static constexpr uint32_t kOffScale = 640, kOffEx = kOffScale + kScaleRing * 8 * kPages, kOffRing = 6 * 1024;
+  static constexpr uint32_t kOffScale = 640, kOffEx = kOffScale + kScaleRing * 8 * kPages, kOffRing = 7 * 1024;
   static constexpr uint32_t kSmem = kOffRing + kSlots * kTile + 1024;
   static constexpr int kPartFloats = kR * (kHd + 2);
-  static_assert(kOffEx + 4 * 128 * 4 <= kOffRing, "exchange");
+  static_assert(kOffEx + 2 * kShare * 128 * 4 <= kOffRing, "exchange");
 };
-
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
-          taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
 
 // D[tmem] (+)= A[tmem] B[smem], A: a row a lane, four e4m3 elements a column.
 __device__ __forceinline__ void umma_f8_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
@@ -1044,7 +1036,7 @@ __device__ __forceinline__ void split4(const float* x, uint32_t& hi, uint32_t& l
 __global__ void __launch_bounds__(KvMany::kThreads, 1)
     kv_attn_rows_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const KvTcArgs p) {
   using Y = KvMany;
-  constexpr int NS = Y::kSlots, HD = 128, R = Y::kR, kTok = Y::kTok;
+  constexpr int NS = Y::kSlots, HD = 128, R = Y::kR, kTok = Y::kTok, C = Y::kShare, W = 128 / C;  // W columns a thread
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -1060,7 +1052,7 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
   int64_t* const scan = reinterpret_cast<int64_t*>(gbase + 424);
   static_assert(424 + 8 * (Y::kThreads / 32) <= Y::kOffScale, "start");
   float* const scales = reinterpret_cast<float*>(gbase + Y::kOffScale);
-  float* const ex = reinterpret_cast<float*>(gbase + Y::kOffEx);  // [2][2][128]: what the halves of a row tell each other
+  float* const ex = reinterpret_cast<float*>(gbase + Y::kOffEx);  // [2][C][128]: what the threads of a row tell each other
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < NS; ++i) {
@@ -1132,9 +1124,9 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
         if (issuer) {
           const uint32_t bd = desc_lo(base + Y::kOffRing + slot * Y::kTile, 16);
 #pragma unroll
-          for (int k = 0; k < 8; ++k)  // 32 tokens at a time: halves of 64, hi words in their first 16 columns, lo in the next
-            umma_f8_ts(tmem + Y::kColO, tmem + 128 * buf + 64 * (k % 4 / 2) + 8 * (k % 2) + 16 * (k / 4), bd + 256 * (k % 4), kHi,
-                       idesc_o, (j > 0 || k > 0) ? 1u : 0u);
+          for (int k = 0; k < 8; ++k)  // 32 tokens at a time, whose words lie over their scores: 8 columns hi, 8 lo
+            umma_f8_ts(tmem + Y::kColO, tmem + 128 * buf + 32 * (k % 4) + 8 * (k / 4), bd + 256 * (k % 4), kHi, idesc_o,
+                       (j > 0 || k > 0) ? 1u : 0u);
           umma_commit<1>(pv_done0 + 8u * buf);
           umma_commit<1>(empty0 + 8u * slot);
         }
@@ -1148,6 +1140,14 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
   } else {
     const int quarter = warp & 3, c = warp >> 2, row = quarter * 32 + lane;
     constexpr int kEvery = 5;
+    const int page_shift = 31 - __clz(kv.page);
+    // the row's threads meet; their word k, theirs in order
+    auto others = [&](int k, float mine, auto join) {
+      float v = mine;
+#pragma unroll
+      for (int i = 1; i < C; ++i) v = join(v, ex[k * (128 * C) + ((c + i) % C) * 128 + row]);
+      return v;
+    };
     const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
     uint32_t gt = 0, ring = 0;
     // (see the other kernel's)
@@ -1160,30 +1160,32 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
       const int32_t sees_all = w.len - w.rows_n + g.token_of(w.sq * R) + 1;  // (the first row's, the others' at least that)
       float f;
       {
-        uint4 q[8];
+        uint4 q[W / 8];
         uint32_t top = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < W / 8; ++k) {
           q[k] = make_uint4(0u, 0u, 0u, 0u);
-          if (mine) q[k] = *reinterpret_cast<const uint4*>(p.a.q + (w.r0 + tk) * p.a.ldq + head * HD + 64 * c + 8 * k);
+          if (mine) q[k] = *reinterpret_cast<const uint4*>(p.a.q + (w.r0 + tk) * p.a.ldq + head * HD + W * c + 8 * k);
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < W / 8; ++k) {
           const uint32_t u[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
 #pragma unroll
           for (int e = 0; e < 4; ++e) top = max(top, max(u[e] << 16 & 0x7fffffffu, u[e] & 0x7fff0000u));
         }
         ex[c * 128 + row] = __uint_as_float(top);
-        bar_sync(1 + quarter, 64);
-        top = max(top, __float_as_uint(ex[(c ^ 1) * 128 + row]));
+        bar_sync(1 + quarter, 32 * C);
+        top = __float_as_uint(others(0, __uint_as_float(top), [](float a, float b) {
+          return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));  // (as integers: NaN is the largest)
+        }));
         // 2^-e brings the largest element into (224, 448]; a row that is not finite has NaN as its factor
         const int e = max(static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), -100);
         const bool bad = top >= 0x7f800000u;
         const float by = bad ? 0.0f : __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
         f = bad ? __uint_as_float(0x7fffffffu) : __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * p.a.scale_log2;
-        uint32_t hi[16], lo[16];
+        uint32_t hi[W / 4], lo[W / 4];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < W / 8; ++k) {
           const uint32_t u[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
           float x[8];
 #pragma unroll
@@ -1194,8 +1196,8 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
           split4(x, hi[2 * k], lo[2 * k]);
           split4(x + 4, hi[2 * k + 1], lo[2 * k + 1]);
         }
-        tmem_st16(lanes + Y::kColQ + 16 * c, hi);
-        tmem_st16(lanes + Y::kColQ + 32 + 16 * c, lo);
+        tmem_st8(lanes + Y::kColQ + W / 4 * c, hi);
+        tmem_st8(lanes + Y::kColQ + 32 + W / 4 * c, lo);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -1205,14 +1207,14 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
       bool failed = false;
 #pragma unroll 1
       for (int32_t j = 0; j < w.n; ++j, ++gt) {
-        const uint32_t buf = gt & 1, sbuf = lanes + 128 * buf + 64 * c;
+        const uint32_t buf = gt & 1, sbuf = lanes + 128 * buf + W * c;
         const int32_t tile = (w.t0 + j) * kTok;
         ok = mbar_wait_warp(scale_full0 + 8u * (gt % kScaleRing), (gt / kScaleRing) & 1, p.wc) && ok;
         const float* const sc = scales + (gt % kScaleRing) * (2 * Y::kPages);
-        float ks[4], lsv[4], inv[4];  // of 16 tokens each (see the other kernel)
+        float ks[W / 16], lsv[W / 16], inv[W / 16];  // of 16 tokens each (see the other kernel)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int at_page = (64 * c + 16 * i) / kv.page;
+        for (int i = 0; i < W / 16; ++i) {
+          const int at_page = (W * c + 16 * i) >> page_shift;
           ks[i] = sc[at_page];
           uint32_t vb = __float_as_uint(sc[Y::kPages + at_page]);
           if (vb == 0u) vb = (127u - 20u) << 23;
@@ -1234,29 +1236,29 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
           for (int32_t i = max(w.vis - tile, 0) * 8 + row; i < kRows * 8; i += 128) v[i] = make_uint4(0u, 0u, 0u, 0u);
           fence_proxy_async_smem();
         }
-        uint32_t v[2][32];
-        tmem_ld32(sbuf, v[0]);
-        tmem_ld32(sbuf + 32, v[1]);
+        uint32_t v[32];
+        static_assert(W == 32, "one load");
+        tmem_ld32(sbuf, v);
         tmem_ld_wait();
-        float x[64], top = -INFINITY;
+        float x[W], top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 64; i += 2) {
-          const float2 t = fma2(make_float2(__uint_as_float(v[i / 32][i % 32]), __uint_as_float(v[i / 32][i % 32 + 1])),
+        for (int i = 0; i < W; i += 2) {
+          const float2 t = fma2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])),
                                 both(f * ks[i / 16]), both(lsv[i / 16]));
           x[i] = t.x;
           x[i + 1] = t.y;
         }
         if (tile + kTok > sees_all) {
-          const int32_t sees = lim - tile - 64 * c;  // the thread's last visible token
+          const int32_t sees = lim - tile - W * c;  // the thread's last visible token
 #pragma unroll
-          for (int i = 0; i < 64; ++i)
+          for (int i = 0; i < W; ++i)
             if (i > sees) x[i] = -INFINITY;
         }
 #pragma unroll
-        for (int i = 0; i < 64; i += 2) top = max3(top, x[i], x[i + 1]);
-        ex[buf * 256 + c * 128 + row] = top;
-        if (!bar_all(1 + quarter, 64, ok)) { failed = true; break; }
-        top = fmaxf(top, ex[buf * 256 + (c ^ 1) * 128 + row]);
+        for (int i = 0; i < W; i += 2) top = max3(top, x[i], x[i + 1]);
+        ex[buf * (128 * C) + c * 128 + row] = top;
+        if (!bar_all(1 + quarter, 32 * C, ok)) { failed = true; break; }
+        top = others(buf, top, [](float a, float b) { return fmaxf(a, b); });
         const bool raise = top - m > kOver;
         if (__any_sync(0xffffffffu, raise)) {
           const float to = raise ? top - kNominalRows : m, fac = raise ? fast_exp2(m - to) : 1.0f;
@@ -1267,13 +1269,13 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
             tc_fence_after();
             const float2 f4[4] = {both(fac), both(fac), both(fac), both(fac)};
 #pragma unroll 1
-            for (int i = 0; i < 64; i += 8) scale_cols8(lanes + Y::kColO + 64 * c + i, f4);
+            for (int i = 0; i < W; i += 8) scale_cols8(lanes + Y::kColO + W * c + i, f4);
             tmem_st_wait();
           }
         }
-        uint32_t hi[16], lo[16];
+        uint32_t hi[W / 4], lo[W / 4];
 #pragma unroll
-        for (int i = 0; i < 64; i += 16) {
+        for (int i = 0; i < W; i += 16) {
           float2 sum = both(0.0f);
 #pragma unroll
           for (int e = 0; e < 16; e += 2) {
@@ -1286,8 +1288,8 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
 #pragma unroll
           for (int e = 0; e < 4; ++e) split4(x + i + 4 * e, hi[i / 4 + e], lo[i / 4 + e]);
         }
-        tmem_st16(sbuf, hi);
-        tmem_st16(sbuf + 16, lo);
+        tmem_st8(sbuf, hi);
+        tmem_st8(sbuf + 8, lo);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -1296,13 +1298,16 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
       ring += 2 * w.n;
       const bool whole = w.n == w.all;
       float* const part = p.parts + (2 * static_cast<int64_t>(blockIdx.x) + (w.begin >= first ? 1 : 0)) * Y::kPartFloats;
-      uint16_t* const out = p.a.o + (w.r0 + tk) * p.a.ldo + head * HD + 64 * c;
+      uint16_t* const out = p.a.o + (w.r0 + tk) * p.a.ldo + head * HD + W * c;
       const int64_t lse_at = static_cast<int64_t>(w.r0 + tk) * p.a.nh + head;
       if (!failed) {
-        // (the exchange of the tile before last is free: this pair has met since)
-        ex[(gt & 1) * 256 + c * 128 + row] = l;
-        bar_sync(1 + quarter, 64);
-        const float sum = c == 0 ? l + ex[(gt & 1) * 256 + 128 + row] : ex[(gt & 1) * 256 + row] + l;
+        // (the exchange of the tile before last is free: the row's threads have met since)
+        float* const sums = ex + (gt & 1) * (128 * C) + row;
+        sums[c * 128] = l;
+        bar_sync(1 + quarter, 32 * C);
+        float sum = sums[0];  // in one order: the same bits in every thread
+#pragma unroll
+        for (int i = 1; i < C; ++i) sum += sums[i * 128];
         const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
         if (mine && c == 0) {
           if (!whole) {
@@ -1315,9 +1320,9 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
         ok = wait_pv(gt - 1) && ok;
         tc_fence_after();
 #pragma unroll 1
-        for (int i = 0; i < 64; i += 16) {
+        for (int i = 0; i < W; i += 16) {
           uint32_t o[16];
-          tmem_ld16(lanes + Y::kColO + 64 * c + i, o);
+          tmem_ld16(lanes + Y::kColO + W * c + i, o);
           tmem_ld_wait();
           if (!mine || !ok) continue;
           if (whole) {
@@ -1331,7 +1336,7 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
             *reinterpret_cast<uint4*>(out + i) = make_uint4(two[0], two[1], two[2], two[3]);
             *reinterpret_cast<uint4*>(out + i + 8) = make_uint4(two[4], two[5], two[6], two[7]);
           } else {
-            uint4* const to = reinterpret_cast<uint4*>(part + 2 * R + row * HD + 64 * c + i);
+            uint4* const to = reinterpret_cast<uint4*>(part + 2 * R + row * HD + W * c + i);
 #pragma unroll
             for (int e = 0; e < 4; ++e) to[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
           }
@@ -1340,7 +1345,7 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
       }
       ok = ok && !failed;
       if (whole) continue;
-      // the last of the row tile's runs joins their parts, a thread its half of its row
+      // the last of the row tile's runs joins their parts, a thread its quarter of its row
       if (!bar_all(kEvery, Y::kSoft, ok)) { ok = false; break; }
       const int32_t c0 = static_cast<int32_t>(w.begin / run), c1 = static_cast<int32_t>((w.begin + w.all - 1) / run);
       if (threadIdx.x == 0) {
@@ -1351,21 +1356,21 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
       }
       bar_sync(kEvery, Y::kSoft);
       if (*merge_flag && mine) {
-        float top = kNoMax, sum = 0.0f, acc[64];
+        float top = kNoMax, sum = 0.0f, acc[W];
 #pragma unroll
-        for (int i = 0; i < 64; ++i) acc[i] = 0.0f;
+        for (int i = 0; i < W; ++i) acc[i] = 0.0f;
 #pragma unroll 1
         for (int32_t r = c0; r <= c1; ++r) {
           const float* const q = p.parts + (2 * static_cast<int64_t>(r) + (r == c0 ? 1 : 0)) * Y::kPartFloats;
-          float4 v[16];
+          float4 v[W / 4];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = __ldcg(reinterpret_cast<const float4*>(q + 2 * R + row * HD + 64 * c) + i);
+          for (int i = 0; i < W / 4; ++i) v[i] = __ldcg(reinterpret_cast<const float4*>(q + 2 * R + row * HD + W * c) + i);
           const float pm = __ldcg(q + row), pl = __ldcg(q + R + row), to = fmaxf(top, pm);
           const float fa = fast_exp2(top - to), fb = fast_exp2(pm - to);
           sum = sum * fa + pl * fb;
           top = to;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
+          for (int i = 0; i < W / 4; ++i) {
             acc[4 * i] = acc[4 * i] * fa + v[i].x * fb;
             acc[4 * i + 1] = acc[4 * i + 1] * fa + v[i].y * fb;
             acc[4 * i + 2] = acc[4 * i + 2] * fa + v[i].z * fb;
@@ -1375,7 +1380,7 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
         const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
         if (p.a.lse && c == 0) p.a.lse[lse_at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 #pragma unroll
-        for (int i = 0; i < 64; i += 8) {
+        for (int i = 0; i < W; i += 8) {
           uint32_t two[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
