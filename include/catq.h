@@ -670,10 +670,11 @@ typedef struct {
  *   new codes = e4m3(value / scale), to nearest, ties to even.
  * A value that is not finite makes the scale NaN until the page begins anew: the queries that see a token of
  * such a page get NaN, others are not touched.  Tokens at negative positions (rows of an idle slot of length 0) and rows
- * outside every sequence are not stored.  No two sequences may get tokens in the same page in one call.
+ * outside every sequence are not stored.  No two sequences may have a row
+ * or get tokens in the same page in one call.
  * Sequences with row offsets outside 0 .. T or decreasing, or a length outside 0 .. max_pages page, and pages outside
  * 0 .. n_pages - 1 are skipped, latching CATQ_ERR_INDEX (catq_device_status).  rot a multiple of 16, rows 16-byte aligned
- * (else CATQ_ERR_SHAPE, CATQ_ERR_ALIGN); 0 <= B <= 65535, T < 2^31, n_kv_heads <= 4096, n_heads <= 65536, max_pages page < 2^31.
+ * (else CATQ_ERR_SHAPE, CATQ_ERR_ALIGN); 0 <= B <= 65535, T < 2^31, n_kv_heads <= 4096, n_heads <= 65536, max_pages page <= 2^30.
  * T == 0 or B == 0 is a no-op. */
 catq_status catq_kv_append(const catq_kv_cache* cache, const int32_t* row_start, const int32_t* seq_len, int32_t B,
                            const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t T, const void* Q, int64_t ldq,
@@ -687,14 +688,17 @@ size_t catq_kv_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, in
  * normally called just before) and query head h, which uses key/value head h / (n_heads / n_kv_heads):
  *   O[r, h] = softmax(Q[r, h] K^T / sqrt(d)) V   over the sequence's tokens at positions up to the row's own.
  * Q, O [T rows of n_heads d] bf16, ldq and ldo elements apart, rows 16-byte aligned; O may be Q with ldo == ldq.
- * lse [T, n_heads] fp32 (nullable): the natural log-sum-exp of the scaled scores.  Queries enter exactly (as two
- * e4m3 terms), scores, softmax and sums are fp32, the weights of the values have two e4m3 terms (a relative 2^-8, as
- * bf16 weights).  A row that sees no token (a negative position) gets 0 and lse -inf; rows outside every
+ * lse [T, n_heads] fp32 (nullable): the natural log-sum-exp of the scaled scores.  Queries and the weights of the values
+ * enter the products as two e4m3 terms each: queries exactly but for 2^-19 of their row's largest element, weights to a
+ * relative 2^-8 (like bf16 ones), or 2^-17 of the row's largest; scores, softmax and sums are fp32.  The same call gives
+ * the same bits on a given device; how a sequence's tokens are shared out depends on all lengths, so a row may round
+ * differently beside other rows.  A row that sees no token (a negative position) gets 0 and lse -inf; rows outside every
  * sequence are left as they were.  Codes are never NaN (catq_kv_append writes none) in tokens of the sequence; what lies
  * behind its last token may be anything.  Scales are powers of two, 0 or NaN.  Out-of-range offsets and lengths as in
  * catq_kv_append (the sequence's rows are left as they were); a page outside 0 .. n_pages - 1 counts as zeros, latched.
  * workspace: >= catq_kv_attention_workspace_bytes(), 256-byte aligned, zero before the first call; a call leaves the
- * part that has to be zero as zero.  Calls that may run at the same time need workspaces of their own.
+ * part that has to be zero as zero (one that latched CATQ_ERR_TIMEOUT may not).  Calls that may run at the same time
+ * (other streams, other graphs) need workspaces of their own.
  * n_heads % n_kv_heads == 0, n_heads / n_kv_heads <= 64, T n_heads / n_kv_heads <= 2^26; other limits as for catq_kv_append. */
 catq_status catq_kv_attention(const catq_kv_cache* cache, const int32_t* row_start, const int32_t* seq_len, int32_t B,
                               const void* Q, int64_t ldq, int64_t T, int32_t n_heads, void* O, int64_t ldo, float* lse,

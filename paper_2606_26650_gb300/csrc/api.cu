@@ -981,7 +981,7 @@ catq_status check_kv(const catq_kv_cache* c, const int32_t* row_start, const int
   if ((c->d != 64 && c->d != 128) || (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) ||
       c->n_kv_heads < 1 || c->n_kv_heads > 4096 || c->n_pages < 1 || c->max_pages < 1 ||
       static_cast<int64_t>(c->n_pages) * c->n_kv_heads * c->page > 0x7fffffff ||
-      static_cast<int64_t>(c->max_pages) * c->page > 0x7fffffff)
+      static_cast<int64_t>(c->max_pages) * c->page > (1 << 30))
     return CATQ_ERR_SHAPE;
   if (c->reserved != 0) return CATQ_ERR_INVALID_ARG;
   if (T == 0 || B == 0) return CATQ_OK;

@@ -339,3 +339,352 @@ def test_append_then_attention_then_packed_linear(device):
         assert U.fro_rel(A.float().cpu().numpy(), want.reshape(T, -1)) <= 2.0 ** -7
         want_y = O.ternary_infer(U.to_host(codes), U.to_host(alpha), N, Kdim, g, U.to_host(last))
         assert U.fro_rel(U.to_host(Y), want_y) <= U.TOL_BF16
+
+
+# ------------------------------------------------------------------ what the calls allow and ordinary cases do not show
+
+@pytest.mark.parametrize("d,nh,nkv,page,lens,news", [
+    (128, 4, 1, 64, [5000], [1]),                   # one sequence over many runs, whose parts are joined
+    (64, 2, 1, 32, [9000, 20], [1, 1]),
+    (128, 8, 2, 32, [1500, 900], [700, 3]),         # many rows a key/value head
+    (128, 5, 1, 16, [2100], [130]),
+    (64, 4, 2, 64, [1100], [200]),
+    (128, 24, 1, 128, [3000], [1]),                 # 24 heads share one, split
+])
+def test_long_attention_matches_oracle(device, d, nh, nkv, page, lens, news):
+    r = syn.rng(8, f"kvlong/{d}/{nh}/{nkv}/{lens}/{news}")
+    paged = Paged(r, lens, nkv, page, d, device)
+    rs = starts(news)
+    q = r.standard_normal((rs[-1], nh, d)) * 2.0
+    got, lse = attend(paged, rs, lens, q, nh, device)
+    check_attention(paged, rs, np.array(lens), q, nh, got, lse)
+    again, _ = attend(paged, rs, lens, q, nh, device, with_lse=False)
+    assert np.array_equal(got, again)  # the same bits
+
+
+@pytest.mark.parametrize("d,news", [(128, [1, 0, 1, 2, 1]), (64, [1, 0, 1, 2, 1]), (128, [1, 0, 1, 90, 1])])
+def test_idle_slots_and_rows_outside(device, d, news):
+    """A sequence without rows, one whose row sees nothing (length 0), one shorter than its rows, rows behind the last."""
+    r = syn.rng(9, f"idle/{d}")
+    lens = [40, 33, 0, 1 if news[3] == 2 else 50, 70]
+    paged = Paged(r, lens, 2, 32, d, device, max_pages=4)
+    rs = starts(news)
+    T = int(rs[-1]) + 3
+    q = r.standard_normal((T, 4, d))
+    got, lse = attend(paged, rs, lens, q, 4, device, ld_gap=16)
+    check_attention(paged, rs, np.array(lens), q, 4, got, lse)
+
+
+@pytest.mark.parametrize("d,new", [(128, 1), (64, 1), (128, 3), (64, 20), (128, 60)])
+def test_bytes_behind_the_last_token_do_not_count(device, d, new):
+    """Every byte of the pages behind the last token, NaN codes among them."""
+    import torch
+    r = syn.rng(10, f"behind/{d}/{new}")
+    lens = [new + 70, new + 129]
+    paged = Paged(r, lens, 2, 64, d, device)
+    for c in (paged.cache.k_codes, paged.cache.v_codes):
+        raw = c.view(torch.uint8)
+        for b, n in enumerate(lens):
+            raw[int(paged.table[b][n // 64]), :, n % 64:] = 0x7F
+    rs = starts([new, new])
+    q = r.standard_normal((rs[-1], 4, d))
+    got, lse = attend(paged, rs, lens, q, 4, device)
+    check_attention(paged, rs, np.array(lens), q, 4, got, lse)
+
+
+@pytest.mark.parametrize("d,new", [(128, 4), (64, 4), (128, 80), (64, 40)])
+def test_values_that_are_not_finite(device, d, new):
+    """An infinite key and a NaN value: the pages' scales are NaN, the rows that see them NaN and no other; a row whose
+    query is not finite is NaN by itself."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(11, f"nonfinite/{d}/{new}")
+    page, nkv, nh, n = 16, 2, 4, 90
+    paged = Paged(r, [n, n, n], nkv, page, d, device)
+    rs = starts([new] * 3)
+    T = 3 * new
+    k, v = (syn.round_bf16(r.standard_normal((T, nkv, d)).astype(np.float32)) for _ in range(2))
+    bad = n - new + new // 2  # the position in sequences 0 (key of head 1) and 1 (value of head 0)
+    k[new // 2, 1, 3] = np.inf
+    v[new + new // 2, 0, 5] = np.nan
+    q = syn.round_bf16(r.standard_normal((T, nh, d)).astype(np.float32))
+    q[2 * new + 1, 2, 0] = np.nan
+    Q = bf16(q.reshape(T, -1), device)
+    rope = None
+    C.catq_kv_append(paged.cache, i32(rs, device), i32([n] * 3, device), bf16(k.reshape(T, -1), device),
+                     bf16(v.reshape(T, -1), device), rope=rope)
+    O = torch.empty_like(Q)
+    C.catq_kv_attention(paged.cache, i32(rs, device), i32([n] * 3, device), Q, O, nh,
+                        C.kv_attention_workspace(paged.cache, nh))
+    torch.cuda.synchronize()
+    assert C.catq_device_status() == 0
+    codes, scale = paged.host()
+    K.append(paged.codes[0], paged.scale[0], paged.table, page, rs, [n] * 3, k.astype(np.float64))
+    K.append(paged.codes[1], paged.scale[1], paged.table, page, rs, [n] * 3, v.astype(np.float64))
+    for got, want in zip(scale, paged.scale):
+        assert np.array_equal(got, want, equal_nan=True)
+    assert np.isnan(scale[0]).sum() == 1 and np.isnan(scale[1]).sum() == 1
+    got = O.float().cpu().numpy().reshape(3, new, nh, d)
+    sees = (n - new + np.arange(new)) >= bad // page * page
+    want_nan = np.zeros((3, new, nh), bool)
+    want_nan[0, sees, 2:] = True
+    want_nan[1, sees, :2] = True
+    want_nan[2, 1, 2] = True
+    assert np.array_equal(np.isnan(got).all(-1), want_nan) and np.array_equal(np.isnan(got).any(-1), want_nan)
+
+
+def test_a_recycled_page_forgets_its_scale(device):
+    """A NaN or huge scale of a page's last use does not outlive its first token's append."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(12, "recycled")
+    paged = Paged(r, [17], 1, 16, 64, device)
+    paged.cache.k_scale[int(paged.table[0][1])] = float("nan")
+    paged.cache.v_scale[int(paged.table[0][1])] = 1e20
+    k = bf16(r.standard_normal((1, 64)), device)
+    C.catq_kv_append(paged.cache, i32([0, 1], device), i32([17], device), k, k)
+    torch.cuda.synchronize()
+    want = K.scale_of(float(k.float().abs().max()))
+    assert paged.cache.k_scale[int(paged.table[0][1])].item() == want
+    assert paged.cache.v_scale[int(paged.table[0][1])].item() == want
+
+
+@pytest.mark.parametrize("d,new", [(128, 1), (64, 1), (128, 6), (128, 70), (64, 30)])
+@pytest.mark.parametrize("gain", [3e4, 1e30])
+def test_large_scores_pick_one_token(device, d, new, gain):
+    """Scores far apart (2^24 and more): the weight of the largest is 1, whatever the others'."""
+    r = syn.rng(13, f"large/{d}/{new}")
+    lens = [new + 300]
+    paged = Paged(r, lens, 1, 64, d, device)
+    q = r.standard_normal((new, 2, d)) * gain
+    got, _ = attend(paged, starts([new]), lens, q, 2, device)
+    qr = syn.round_bf16(np.asarray(q, np.float32)).astype(np.float64)
+    for i in range(new):
+        n = lens[0] - new + i + 1
+        pages = [paged.table[0][j] for j in range(-(-n // 64))]
+        kc, vc = (np.concatenate([K.E4M3[c[p, 0]] * s[p, 0] for p in pages])[:n] for c, s in
+                  ((paged.codes[0], paged.scale[0]), (paged.codes[1], paged.scale[1])))
+        for h in range(2):
+            score = kc @ qr[i, h]
+            best = np.argsort(score)[-2:]
+            if score[best[1]] - score[best[0]] > 1e-4 * np.abs(score).max():  # (fp32 tells them apart)
+                assert np.allclose(got[i, h], vc[best[1]], rtol=2.0 ** -7, atol=0)
+
+
+def test_output_over_the_queries_and_strided_rows(device):
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    for d, new in ((128, 2), (64, 2), (128, 50)):
+        r = syn.rng(14, f"inplace/{d}/{new}")
+        lens = [new + 200, new + 3]
+        paged = Paged(r, lens, 2, 32, d, device)
+        rs = starts([new, new])
+        q = r.standard_normal((2 * new, 4, d))
+        want, _ = attend(paged, rs, lens, q, 4, device)
+        whole = torch.full((2 * new, 4 * d + 32), 9.0, dtype=torch.bfloat16, device=device)
+        Q = whole[:, 16:16 + 4 * d]
+        Q.copy_(bf16(q.reshape(2 * new, -1), device))
+        C.catq_kv_attention(paged.cache, i32(rs, device), i32(lens, device), Q, Q, 4,
+                            C.kv_attention_workspace(paged.cache, 4))
+        torch.cuda.synchronize()
+        assert np.array_equal(Q.float().cpu().numpy().reshape(want.shape), want)
+        assert (whole[:, :16] == 9).all() and (whole[:, 16 + 4 * d:] == 9).all()
+
+
+def test_bad_pages_offsets_and_lengths_are_latched(device):
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(15, "bad")
+    for d, new in ((128, 1), (64, 1), (128, 40)):
+        lens = np.array([new + 60, new + 60, new + 60, new + 60])
+        paged = Paged(r, lens, 2, 32, d, device, max_pages=4)
+        rs = starts([new] * 4)
+        T = int(rs[-1])
+        q = r.standard_normal((T, 4, d))
+        want, _ = attend(paged, rs, lens, q, 4, device)
+        ws = C.kv_attention_workspace(paged.cache, 4)
+        Q = bf16(q.reshape(T, -1), device)
+
+        def call(row_start, seq_len):
+            O = torch.full_like(Q, 7.0)
+            C.catq_kv_attention(paged.cache, i32(row_start, device), i32(seq_len, device), Q, O, 4, ws)
+            status = C.catq_device_status()
+            assert C.catq_device_status() == 0 and not ws[:4096].any()
+            return status, O.float().cpu().numpy().reshape(T, 4, d)
+
+        # pages that do not exist count as zeros: keys and values of that page 0
+        table = paged.cache.table.clone()
+        for sick in (-1, paged.n_pages, 2 ** 31 - 1, -2 ** 31):
+            paged.cache.table[1, 1] = sick
+            status, got = call(rs, lens)
+            assert C.STATUS[status] == "CATQ_ERR_INDEX"
+            keep = [i for i in range(T) if not new <= i < 2 * new]
+            assert np.array_equal(got[keep], want[keep])
+            zero = Paged.__new__(Paged)
+            zero.__dict__.update(paged.__dict__)
+            zero.codes, zero.scale = [c.copy() for c in paged.codes], [s.copy() for s in paged.scale]
+            p = paged.table[1][1]
+            for c in zero.codes:
+                c[p] = 0
+            one = slice(new, 2 * new)
+            ref, _, mag, low = K.attention(*zero.codes, *zero.scale, [paged.table[1]], 32, [0, new], lens[1:2],
+                                           syn.round_bf16(np.asarray(q[one], np.float32)), new, 4)
+            assert (np.abs(got[one] - ref) <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2.0 ** -14) * mag
+                    + 2.0 ** -17 * low).all()
+            if new == 1:  # and nothing is appended to them (position 33 of sequence 1 is the only one)
+                before = paged.host()
+                kv = bf16(r.standard_normal((T, 2 * d)), device)
+                C.catq_kv_append(paged.cache, i32(rs, device), i32(np.array([0, 34, 0, 0]), device), kv, kv)
+                assert C.STATUS[C.catq_device_status()] == "CATQ_ERR_INDEX"
+                after = paged.host()
+                assert all(np.array_equal(x, y) for x, y in zip(before[0] + before[1], after[0] + after[1]))
+            paged.cache.table.copy_(table)
+        # offsets that fall, reach past the rows or begin before them; lengths that do not fit the table
+        for row_start, seq_len, lost in [
+                (np.array([0, new, new - 1, 3 * new, 4 * new]), lens, [1, 2]),
+                (np.array([0, new, 2 * new, 3 * new, 4 * new + 1]), lens, [3]),
+                (np.array([-1, new, 2 * new, 3 * new, 4 * new]), lens, [0]),
+                (rs, np.array([lens[0], -1, lens[2], lens[3]]), [1]),
+                (rs, np.array([lens[0], lens[1], 129, lens[3]]), [2])]:
+            status, got = call(row_start, seq_len)
+            assert C.STATUS[status] == "CATQ_ERR_INDEX"
+            for b in range(4):
+                # (offsets 0, new, new - 1, 3 new: sequence 2 by itself is in order and has row new - 1 too, the last of
+                # sequence 0, so nothing is said about that one)
+                rows = slice(b * new, (b + 1) * new - (b == 0 and lost == [1, 2]))
+                if b not in lost:
+                    assert np.array_equal(got[rows], want[rows])
+                elif lost != [1, 2]:  # (sequence 2's rows there: new - 1 .. 3 new - 1, all of sequence 1's among them)
+                    assert (got[rows] == 7).all()
+
+
+def test_many_sequences(device):
+    """More sequences than the kernels have threads, many of them empty."""
+    r = syn.rng(16, "many")
+    B = 1500
+    lens = r.integers(0, 40, B)
+    news = np.minimum(r.integers(0, 2, B), lens)
+    for d in (128, 64):
+        paged = Paged(r, list(lens), 1, 16, d, device)
+        rs = starts(news)
+        q = r.standard_normal((rs[-1], 2, d))
+        got, lse = attend(paged, rs, lens, q, 2, device)
+        check_attention(paged, rs, lens, q, 2, got, lse)
+
+
+def test_offsets_past_32_bits(device):
+    """Caches of more than 2^32 bytes, the sequence's pages at their end."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(17, "far")
+    for d, new in ((128, 1), (64, 2), (128, 40)):
+        n_pages, page, n = 5 * 2 ** 30 // (64 * d), 64, 200
+        table = np.array([[n_pages - 1 - 7 * i for i in range(4)]], np.int32)
+        kc, vc = (torch.empty(n_pages, 1, page, d, dtype=torch.uint8, device=device) for _ in range(2))
+        ks, vs = (torch.ones(n_pages, 1, device=device) for _ in range(2))
+        cache = C.KVCache(kc.view(torch.float8_e4m3fn), vc.view(torch.float8_e4m3fn), ks, vs, i32(table, device))
+        k, v = (syn.round_bf16(r.standard_normal((n, 1, d)).astype(np.float32)) for _ in range(2))
+        C.catq_kv_append(cache, i32([0, n], device), i32([n], device), bf16(k.reshape(n, d), device),
+                         bf16(v.reshape(n, d), device))
+        q = r.standard_normal((new, 2, d))
+        Q = bf16(q.reshape(new, -1), device)
+        O = torch.empty_like(Q)
+        C.catq_kv_attention(cache, i32([0, new], device), i32([n], device), Q, O, 2, C.kv_attention_workspace(cache, 2))
+        torch.cuda.synchronize()
+        assert C.catq_device_status() == 0
+        small = [np.zeros((4, 1, page, d), np.uint8) for _ in range(2)]
+        scale = [np.zeros((4, 1)) for _ in range(2)]
+        for c, s, x in zip(small, scale, (k, v)):
+            K.append(c, s, [[0, 1, 2, 3]], page, [0, n], [n], x.astype(np.float64))
+        for c, t in zip(small, (kc, vc)):
+            got = t[torch.tensor(table[0], device=device).long()].cpu().numpy()
+            assert np.array_equal(K.E4M3[got].reshape(-1, d)[:n], K.E4M3[c].reshape(-1, d)[:n])
+        ref, _, mag, low = K.attention(*small, *scale, [[0, 1, 2, 3]], page, [0, new], [n],
+                                       syn.round_bf16(np.asarray(q, np.float32)), new, 2)
+        got = O.float().cpu().numpy().reshape(new, 2, d)
+        assert (np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2.0 ** -14) * mag + 2.0 ** -17 * low).all()
+        del kc, vc, ks, vs, cache
+        torch.cuda.empty_cache()
+
+
+def test_a_captured_step_follows_the_lengths(device):
+    """Append and attention captured once, replayed as the sequences grow: lengths and rows are read on the device."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    for d in (128, 64):
+        r = syn.rng(18, f"graph/{d}")
+        B, nh, nkv, page, steps = 3, 4, 2, 16, 40
+        paged, eager = (Paged(syn.rng(18, f"graph/cache/{d}"), [5 + steps, 14 + steps, 31 + steps], nkv, page, d, device)
+                        for _ in range(2))
+        rope = C.Rope.create(d, 10000.0, device)
+        lens = i32([5, 14, 31], device)
+        rs = i32([0, 1, 2, 3], device)
+        K_, V, Q, O = (torch.zeros(B, h * d, dtype=torch.bfloat16, device=device) for h in (nkv, nkv, nh, nh))
+        ws = C.kv_attention_workspace(paged.cache, nh)
+
+        def step(cache, ws):
+            C.catq_kv_append(cache, rs, lens, K_, V, rope=rope, Q=Q, n_heads=nh)
+            C.catq_kv_attention(cache, rs, lens, Q, O, nh, ws)
+
+        side = torch.cuda.Stream()
+        graph = torch.cuda.CUDAGraph()
+        start_lens = lens.clone()
+        with torch.cuda.stream(side):
+            step(paged.cache, ws)
+            side.synchronize()
+            with torch.cuda.graph(graph, stream=side):
+                step(paged.cache, ws)
+        torch.cuda.synchronize()
+        # the warm-up appended zeros at the first position: begin again from the same caches
+        for t in ("k_codes", "v_codes", "k_scale", "v_scale"):
+            getattr(paged.cache, t).view(torch.uint8 if "codes" in t else torch.float32).copy_(
+                getattr(eager.cache, t).view(torch.uint8 if "codes" in t else torch.float32))
+        lens.copy_(start_lens)
+        ws2 = C.kv_attention_workspace(eager.cache, nh)
+        for i in range(steps):
+            k, v, q = (bf16(r.standard_normal((B, h * d)), device) for h in (nkv, nkv, nh))
+            outs = []
+            for run in (lambda: graph.replay(), lambda: step(eager.cache, ws2)):
+                K_.copy_(k), V.copy_(v), Q.copy_(q)
+                run()
+                outs.append(O.clone())
+            lens += 1
+            assert torch.equal(outs[0], outs[1]), i
+        torch.cuda.synchronize()
+        assert C.catq_device_status() == 0
+
+
+def test_two_streams_with_workspaces_of_their_own(device):
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(19, "streams")
+    jobs = []
+    for d, nh, nkv, lens, news in ((128, 8, 2, [3000, 700], [1, 1]), (64, 4, 4, [900, 50], [2, 1]),
+                                   (128, 4, 1, [1200], [100])):
+        paged = Paged(r, lens, nkv, 32, d, device)
+        rs = starts(news)
+        Q = bf16(r.standard_normal((rs[-1], nh * d)), device)
+        jobs.append((paged, i32(rs, device), i32(lens, device), Q, torch.empty_like(Q), nh,
+                     C.kv_attention_workspace(paged.cache, nh), torch.cuda.Stream()))
+    want = []
+    for p, rs, sl, Q, O, nh, ws, _ in jobs:
+        C.catq_kv_attention(p.cache, rs, sl, Q, O, nh, ws)
+        want.append(O.clone())
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for p, rs, sl, Q, O, nh, ws, st in jobs:
+            O.zero_()
+        torch.cuda.synchronize()
+        for p, rs, sl, Q, O, nh, ws, st in jobs:
+            C.catq_kv_attention(p.cache, rs, sl, Q, O, nh, ws, stream=st)
+        torch.cuda.synchronize()
+        for (_, _, _, _, O, _, _, _), w in zip(jobs, want):
+            assert torch.equal(O, w)
+    assert C.catq_device_status() == 0
