@@ -4,6 +4,8 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <atomic>
+#include <type_traits>
 
 #include "launch.h"
 #include "ptx_sm100.cuh"
@@ -207,165 +209,352 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t codes, __half2 by) {
 
 __device__ __forceinline__ void latch_index_error(int32_t* status) { atomicCAS(status, 0, 10 /* CATQ_ERR_INDEX */); }
 
-// Maximum over an item's threads (whole warps).
-template <int W>
-__device__ __forceinline__ uint32_t item_max(uint32_t v, uint32_t* red) {
-  v = __reduce_max_sync(0xffffffffu, v);
-  if constexpr (W > 1) {
-    __syncthreads();  // red is free
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < W; ++w) v = max(v, red[w]);
+// The work of one append is three lines of items, each in the order of the sequences: pages that get few tokens (a team of
+// one or two warps takes one head's keys or values of such a page), pages that get more (a CTA), and the queries in chunks
+// of kThreads units of 16 elements.  Lengths are read on the device and every CTA adds them up, so that a batch of single
+// tokens with a long prompt among them is shared out like any other: 128 single tokens and a prompt of 512 (32 / 8 heads of
+// 128, pages of 64) take 11 us, where a grid over sequences and shares of the mean one's pages took 97 to 135; single
+// tokens alone pay 0.7 us for it (64 sequences: 4.3 against 3.6).
+// Few tokens are 64 units a warp of the team, so that its lanes hold two.
+struct KvSpan {
+  int64_t r0;
+  int32_t n, first, len;         // new rows, position of the first, cached tokens with them
+  int32_t pg, pages;             // first page that gets tokens, their number
+  int32_t head_small, tail_small;  // whether the first and (another) last page are a warp's
+  int32_t chunks;                // of the queries
+};
+
+template <int D, int kTeam>
+struct KvAppendWork {
+  static constexpr int kUnits = D / 16, kSmall = 32 * kTeam * 2 / kUnits;  // tokens of a team's item at most
+  const KvAppendArgs& a;
+  Divisor by_page;
+  int32_t per;  // units of a token's queries, in runs of heads; 0: no queries
+  __device__ __forceinline__ KvSpan span(int32_t b, bool latch) const {
+    KvSpan s;
+    s.r0 = a.row_start[b];
+    const int64_t r1 = a.row_start[b + 1];
+    s.len = a.seq_len[b];
+    s.pages = 0;
+    s.chunks = 0;
+    s.n = 0;
+    s.head_small = s.tail_small = 0;
+    const int32_t page = a.cache.page;
+    if (s.r0 < 0 || r1 < s.r0 || r1 > a.T || s.len < 0 || s.len > a.cache.max_pages * page) {
+      if (latch) latch_index_error(a.status);
+      return s;
+    }
+    s.n = static_cast<int32_t>(r1 - s.r0);
+    s.first = s.len - s.n;
+    s.chunks = static_cast<int32_t>((static_cast<int64_t>(s.n) * per + kThreads - 1) / kThreads);
+    const int32_t p0 = max(s.first, 0);
+    if (p0 >= s.len) return s;
+    s.pg = by_page.of(p0);
+    const int32_t last = by_page.of(s.len - 1);
+    s.pages = last - s.pg + 1;
+    s.head_small = min(s.len, (s.pg + 1) * page) - p0 <= kSmall;
+    s.tail_small = s.pages > 1 && s.len - last * page <= kSmall;
+    return s;
   }
+  // Items of line l (0: warps' pages, 1: CTAs' pages, 2: chunks of the queries) of a sequence.
+  __device__ __forceinline__ int32_t count(const KvSpan& s, int l) const {
+    if (l == 2) return s.chunks;
+    const int32_t small = a.cache.page <= kSmall ? s.pages : s.head_small + s.tail_small;
+    return l == 0 ? small : s.pages - small;
+  }
+  // Page k of the sequence's share of line l.
+  __device__ __forceinline__ int32_t page_of(const KvSpan& s, int l, int32_t k) const {
+    if (a.cache.page <= kSmall) return s.pg + k;
+    if (l == 1) return s.pg + s.head_small + k;
+    return k == 0 && s.head_small ? s.pg : s.pg + s.pages - 1;
+  }
+};
+
+// Maximum over an item's threads: W warps, which meet at barrier `bar`.
+template <int W>
+__device__ __forceinline__ uint32_t item_max(uint32_t v, uint32_t* red, int bar) {
+  v = __reduce_max_sync(0xffffffffu, v);
+  const int warp = threadIdx.x >> 5, team = warp / W * W;
+  asm volatile("barrier.cta.sync %0, %1;" ::"r"(bar), "n"(32 * W) : "memory");  // red is free
+  if ((threadIdx.x & 31) == 0) red[warp] = v;
+  asm volatile("barrier.cta.sync %0, %1;" ::"r"(bar), "n"(32 * W) : "memory");
+#pragma unroll
+  for (int w = 0; w < W; ++w) v = max(v, red[team + w]);
   return v;
 }
 
-// An item is the new tokens of one page and head, keys or values: W warps hold its units (16 elements of a token), kHeld
-// a thread, in registers between the search for the largest magnitude and the codes; an item of more units is read (and
-// rotated) twice.  Grid (sequence, items then shares of the queries).  W = 1 serves calls of a token or a few a sequence:
-// many items of little work, and no barrier; W = 8 whole pages.
-// Bound by HBM where prompts are appended (an element read in 16 bits, written in 8, queries read and written), by
-// latency where tokens are: row offsets, then page number, then scale.
-template <int D, int W, int kHeld>
-__global__ void __launch_bounds__(kThreads, 2) kv_append_kernel(const KvAppendArgs a, int32_t zkv, int32_t zq, int32_t hpt,
-                                                                Divisor by_part, Divisor by_page) {
-  constexpr int kItemThreads = 32 * W, d = D, units = D / 16;
-  __shared__ uint32_t red[W];
-  grid_launch_dependents();
-  grid_dependency_wait();
-  const int b = blockIdx.x;
-  const int32_t tid = threadIdx.x % kItemThreads;
-  const int64_t r0 = a.row_start[b], r1 = a.row_start[b + 1];
-  const int32_t len = a.seq_len[b];
-  const int32_t nkv = a.cache.nkv, page = a.cache.page;
-  if (r0 < 0 || r1 < r0 || r1 > a.T || len < 0 || len > a.cache.max_pages * page) {
-    if (threadIdx.x == 0) latch_index_error(a.status);
-    return;
-  }
-  const int32_t n = static_cast<int32_t>(r1 - r0), first = len - n;  // position of the sequence's row r0
-  const int32_t item_blocks = gridDim.y - zq;
-  if (static_cast<int>(blockIdx.y) >= item_blocks) {  // queries
-    const int32_t runs = (a.nh + hpt - 1) / hpt, per = runs * units;
-    const int64_t items = static_cast<int64_t>(n) * per;
-    for (int64_t e = static_cast<int64_t>(blockIdx.y - item_blocks) * kThreads + threadIdx.x; e < items;
-         e += static_cast<int64_t>(zq) * kThreads) {
-      const int32_t i = e >> 31 ? static_cast<int32_t>(e / per) : by_part.of(static_cast<int32_t>(e));
-      const int32_t ru = static_cast<int32_t>(e - static_cast<int64_t>(i) * per);
-      const int32_t run = ru / units, u = ru - run * units;
-      const RotUnit q = rot_unit(a.rot, u);
-      if (!q.turned && a.q == a.q_out) continue;
-      rotate_heads(a.q + (r0 + i) * a.ldq, a.q_out + (r0 + i) * a.ldqo, run * hpt, min(run * hpt + hpt, a.nh), d, a.rot,
-                   u, q, first + i, false);
-    }
-    return;
-  }
-  // item: share of the sequence's pages, head, keys or values
-  const int32_t item = blockIdx.y * (kThreads / kItemThreads) + threadIdx.x / kItemThreads;
-  const int32_t z = item / (2 * nkv), hv = item - z * 2 * nkv;
-  if (z >= zkv) return;
-  const bool is_v = hv >= nkv;
-  const int32_t h = hv - (is_v ? nkv : 0);
-  const int64_t ld = is_v ? a.ldv : a.ldk;
-  const uint16_t* const src = (is_v ? a.v : a.k) + r0 * ld + h * d;
-  uint8_t* const codes = is_v ? a.cache.v_codes : a.cache.k_codes;
-  float* const scales = is_v ? a.cache.v_scale : a.cache.k_scale;
+// One item: the new tokens of a page and one head, keys or values.
+struct KvItem {
+  const uint16_t* src;  // first token
+  int32_t lo, tokens;   // position of it, their number
+  int32_t kept;         // tokens that the page has already
+  int32_t id, h;        // page number, head
+  bool is_v;
+};
+
+__device__ __forceinline__ KvItem item_of(const KvAppendArgs& a, const KvSpan& s, int32_t b, int32_t pg, int32_t hv) {
+  KvItem t;
+  t.is_v = hv >= a.cache.nkv;
+  t.h = hv - (t.is_v ? a.cache.nkv : 0);
+  t.lo = max(max(s.first, 0), pg * a.cache.page);
+  t.tokens = min(s.len, (pg + 1) * a.cache.page) - t.lo;
+  t.kept = t.lo - pg * a.cache.page;
+  t.id = a.cache.table[static_cast<int64_t>(b) * a.cache.max_pages + pg];
+  const int64_t row = s.r0 + (t.lo - s.first);
+  t.src = (t.is_v ? a.v + row * a.ldv : a.k + row * a.ldk) + t.h * a.cache.d;
+  return t;
+}
+
+// The vectors of an item's unit e.
+template <int D>
+__device__ __forceinline__ RotUnit item_unit(const KvAppendArgs& a, const KvItem& t, int32_t e, const uint16_t*& row) {
+  constexpr int units = D / 16;
   RotDev rot = a.rot;
-  if (is_v) rot.rot = 0;
-  const int32_t p0 = max(first, 0);
-  for (int32_t pg = by_page.of(p0) + z; pg * page < len; pg += zkv) {
-    const int32_t lo = max(p0, pg * page), hi = min(len, (pg + 1) * page);
-    const int32_t id = a.cache.table[static_cast<int64_t>(b) * a.cache.max_pages + pg];
-    const int32_t kept = lo - pg * page, items = (hi - lo) * units;
-    Eight<uint16_t> va[kHeld], vb[kHeld];
-    auto fetch = [&](int32_t e, Eight<uint16_t>& x, Eight<uint16_t>& y) {
-      const int32_t i = e / units;
-      const RotUnit q = rot_unit(rot, e - i * units);
-      const uint16_t* const row = src + (lo - first + i) * ld;
-      x.load(row + q.a);
-      y.load(row + q.b);
-    };
+  if (t.is_v) rot.rot = 0;
+  const int32_t i = e / units;
+  row = t.src + i * (t.is_v ? a.ldv : a.ldk);
+  return rot_unit(rot, e - i * units);
+}
+
+// An item by W warps (thread tid of them), kHeld units a thread, which stay in registers between the search for the largest
+// magnitude and the codes.  load(k, e, x, y) gives unit e, the thread's k-th, turn(k, u, position, angles) its angles; then()
+// is called when all have been taken.
+template <int D, int W, int kHeld, class Load, class Turn, class Then>
+__device__ __forceinline__ void append_item(const KvAppendArgs& a, const KvItem& t, int32_t tid, uint32_t* red, int bar, Load load, Turn turn,
+                                            Then then) {
+  constexpr int kItemThreads = 32 * W, d = D, units = D / 16;
+  const int32_t nkv = a.cache.nkv, page = a.cache.page, items = t.tokens * units;
+  uint8_t* const codes = t.is_v ? a.cache.v_codes : a.cache.k_codes;
+  float* const scales = t.is_v ? a.cache.v_scale : a.cache.k_scale;
+  const bool known = t.id >= 0 && t.id < a.cache.n_pages;
+  const int64_t block = known ? static_cast<int64_t>(t.id) * nkv + t.h : 0;
+  uint8_t* const dst = codes + block * page * d;
+  const float old = known && t.kept > 0 ? scales[block] : 0.0f;
+  RotDev rot = a.rot;
+  if (t.is_v) rot.rot = 0;
+  Eight<uint16_t> va[kHeld], vb[kHeld];
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-      if (tid + k * kItemThreads < items) fetch(tid + k * kItemThreads, va[k], vb[k]);
-    if (id < 0 || id >= a.cache.n_pages) {
-      if (tid == 0) latch_index_error(a.status);
-      continue;
-    }
-    const int64_t block = static_cast<int64_t>(id) * nkv + h;
-    uint8_t* const dst = codes + block * page * d;
-    const float old = kept > 0 ? scales[block] : 0.0f;
-    // a unit's values
-    auto turn = [&](int32_t e, const Eight<uint16_t>& x, const Eight<uint16_t>& y, float (&v)[16]) {
-      x.get(v);
-      y.get(v + 8);
-      const int32_t i = e / units, u = e - i * units;
+  for (int k = 0; k < kHeld; ++k) {
+    const int32_t e = tid + k * kItemThreads;
+    if (e < items) load(k, e, va[k], vb[k]);
+  }
+  float most = 0.0f;
+  float v[kHeld][16];
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    const int32_t e = tid + k * kItemThreads, i = e / units, u = e - i * units;
+    if (e < items) {
+      va[k].get(v[k]);
+      vb[k].get(v[k] + 8);
       if (16 * u < rot.rot) {
         RotAngles ang;
-        rot_angles(rot, u, lo + i, false, ang);
-        rot_apply(rot.interleaved != 0, ang, v);
+        turn(k, u, t.lo + i, ang);
+        rot_apply(rot.interleaved != 0, ang, v[k]);
       }
-    };
-    auto largest = [](const float (&v)[16], float top) {  // (NaN if any is)
 #pragma unroll
-      for (int j = 0; j < 16; ++j)
-        asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(top), "f"(fabsf(v[j])));
-      return top;
-    };
-    float most = 0.0f;
-    float v[kHeld][16];
+      for (int j = 0; j < 16; ++j)  // (NaN if any is)
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(most) : "f"(most), "f"(fabsf(v[k][j])));
+    }
+  }
+  then(most);
+  if (!known) {
+    if (tid == 0) latch_index_error(a.status);
+    return;
+  }
+  const uint32_t top = item_max<W>(__float_as_uint(most) & 0x7fffffffu, red, bar);  // (everyone has read the old scale)
+  const float want = scale_of(top);
+  const bool bad = !(want == want) || !(old == old);
+  const float now = bad ? __uint_as_float(0x7fffffffu) : fmaxf(old, want);
+  if (tid == 0) scales[block] = now;
+  if (!bad && old > 0.0f && now > old) {
+    const __half2 by = __float2half2_rn(fmaxf(old / now, 5.9604645e-8f));
+    for (int32_t e = tid; e < t.kept * d / 16; e += kItemThreads) {
+      uint4 w = reinterpret_cast<const uint4*>(dst)[e];
+      w.x = rescale4(w.x, by);
+      w.y = rescale4(w.y, by);
+      w.z = rescale4(w.z, by);
+      w.w = rescale4(w.w, by);
+      reinterpret_cast<uint4*>(dst)[e] = w;
+    }
+  }
+  // a page that holds what is not finite has NaN as its scale, and finite codes
+  const float by = bad ? 0.0f : (now > 0.0f ? 1.0f / now : 1.0f);
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-      if (tid + k * kItemThreads < items) {
-        turn(tid + k * kItemThreads, va[k], vb[k], v[k]);
-        most = largest(v[k], most);
-      }
-    for (int32_t e = tid + kHeld * kItemThreads; e < items; e += kItemThreads) {
-      Eight<uint16_t> x, y;
-      float more[16];
-      fetch(e, x, y);
-      turn(e, x, y, more);
-      most = largest(more, most);
-    }
-    const uint32_t top = item_max<W>(__float_as_uint(most) & 0x7fffffffu, red);
-    const float want = scale_of(top);
-    const bool bad = !(want == want) || !(old == old);
-    const float now = bad ? __uint_as_float(0x7fffffffu) : fmaxf(old, want);
-    if constexpr (W == 1) __syncwarp();  // (every thread has read the old scale: with more warps, item_max's barriers)
-    if (tid == 0) scales[block] = now;
-    if (!bad && old > 0.0f && now > old) {
-      const __half2 by = __float2half2_rn(fmaxf(old / now, 5.9604645e-8f));
-      for (int32_t e = tid; e < kept * d / 16; e += kItemThreads) {
-        uint4 w = reinterpret_cast<const uint4*>(dst)[e];
-        w.x = rescale4(w.x, by);
-        w.y = rescale4(w.y, by);
-        w.z = rescale4(w.z, by);
-        w.w = rescale4(w.w, by);
-        reinterpret_cast<uint4*>(dst)[e] = w;
-      }
-    }
-    // a page that holds what is not finite has NaN as its scale, and finite codes
-    const float by = bad ? 0.0f : (now > 0.0f ? 1.0f / now : 1.0f);
-    auto put = [&](int32_t e, float (&f)[16]) {
-      const int32_t i = e / units;
+  for (int k = 0; k < kHeld; ++k) {
+    const int32_t e = tid + k * kItemThreads, i = e / units;
+    if (e < items) {
       const RotUnit q = rot_unit(rot, e - i * units);
-      uint8_t* const at = dst + (kept + i) * d;
+      uint8_t* const at = dst + (t.kept + i) * d;
       if (bad) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) f[j] = 0.0f;
+        for (int j = 0; j < 16; ++j) v[k][j] = 0.0f;
       }
-      *reinterpret_cast<uint2*>(at + q.a) = codes8(f, by);
-      *reinterpret_cast<uint2*>(at + q.b) = codes8(f + 8, by);
-    };
+      *reinterpret_cast<uint2*>(at + q.a) = codes8(v[k], by);
+      *reinterpret_cast<uint2*>(at + q.b) = codes8(v[k] + 8, by);
+    }
+  }
+}
+
+__device__ __forceinline__ void copy16(void* smem, const void* global) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(smem)), "l"(global) : "memory");
+}
+
+// CTAs below ctas_kv take keys and values, a run of whole pages and heads each, the next one's elements on their way to
+// shared memory meanwhile (each thread copies what it will read itself), and the angles of a page's tokens kept there
+// from its first head on (without that 45 us for four prompts of 2048, with it 41); the others chunks of the queries.
+// Four prompts of 2048 (32 / 8 heads of 128) move 185 MB in 41 us, 4.5 TB/s, bound by the latency of an item (elements,
+// maximum over the CTA, codes) and the arithmetic beside it; single tokens by a chain of loads: row offsets, page
+// number, scale.  kHeld kThreads units: a page and head at most.
+template <int D, int kTeam, int kHeld>
+__global__ void __launch_bounds__(kThreads, 2) kv_append_kernel(const KvAppendArgs a, uint32_t ctas_kv, int32_t hpt,
+                                                                Divisor by_part, Divisor by_page, Divisor by_heads) {
+  constexpr int kWarps = kThreads / 32, kTeams = kWarps / kTeam, units = D / 16;
+  extern __shared__ uint4 staged[];  // [kHeld][2][kThreads], then the angles [kHeld][4][kThreads]
+  float4* const angles = reinterpret_cast<float4*>(staged + 2 * kHeld * kThreads);
+  __shared__ uint32_t red[kWarps];
+  __shared__ int32_t upto[3][kThreads];  // items of each line in the stretches of sequences up to thread t's
+  __shared__ int32_t sums[3][kWarps];
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const int32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int32_t runs = a.q ? (a.nh + hpt - 1) / hpt : 0, heads = 2 * a.cache.nkv;
+  const KvAppendWork<D, kTeam> work{a, by_page, runs * units};
+  const int32_t stretch = (a.B + kThreads - 1) / kThreads;  // sequences a thread
+  {
+    int32_t mine[3] = {0, 0, 0};
+    const int32_t b0 = min(tid * stretch, a.B), b1 = min(b0 + stretch, a.B);
+#pragma unroll 1
+    for (int32_t b = b0; b < b1; ++b) {
+      const KvSpan s = work.span(b, blockIdx.x == 0);
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-      if (tid + k * kItemThreads < items) put(tid + k * kItemThreads, v[k]);
-    for (int32_t e = tid + kHeld * kItemThreads; e < items; e += kItemThreads) {
-      Eight<uint16_t> x, y;
-      float more[16];
-      fetch(e, x, y);
-      turn(e, x, y, more);
-      put(e, more);
+      for (int l = 0; l < 3; ++l) mine[l] += work.count(s, l);
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+#pragma unroll
+      for (int l = 0; l < 3; ++l) {
+        const int32_t v = __shfl_up_sync(0xffffffffu, mine[l], o);
+        if (lane >= o) mine[l] += v;
+      }
+    }
+#pragma unroll
+    for (int l = 0; l < 3; ++l)
+      if (lane == 31) sums[l][warp] = mine[l];
+    __syncthreads();
+#pragma unroll
+    for (int l = 0; l < 3; ++l) {
+#pragma unroll
+      for (int w = 0; w < kWarps - 1; ++w) mine[l] += w < warp ? sums[l][w] : 0;
+      upto[l][tid] = mine[l];
+    }
+    __syncthreads();
+  }
+  // The sequence of item k of line l, which becomes the place in the sequence's share.  By whole warps.
+  auto locate = [&](int l, int32_t& k, KvSpan& s) {
+    const int32_t eighth = __popc(__ballot_sync(0xffffffffu, upto[l][8 * lane + 7] <= k));
+    const int32_t t = 8 * eighth + __popc(__ballot_sync(0xffffffffu, lane < 8 && upto[l][8 * eighth + (lane & 7)] <= k));
+    if (t > 0) k -= upto[l][t - 1];
+    int32_t b = t * stretch;
+    s = work.span(b, false);
+#pragma unroll 1
+    for (int32_t n; k >= (n = work.count(s, l)) && b + 1 < a.B; k -= n) s = work.span(++b, false);
+    return b;
+  };
+  auto page_at = [&](int64_t e) {
+    return e < 0x7fffffff ? by_heads.of(static_cast<int32_t>(e)) : static_cast<int32_t>(e / heads);
+  };
+  auto item_at = [&](int l, int64_t e) {
+    int32_t k = page_at(e);
+    const int32_t hv = static_cast<int32_t>(e - static_cast<int64_t>(k) * heads);
+    KvSpan s;
+    const int32_t b = locate(l, k, s);
+    return item_of(a, s, b, work.page_of(s, l, k), hv);
+  };
+  if (blockIdx.x < ctas_kv) {
+    const int64_t small = static_cast<int64_t>(upto[0][kThreads - 1]) * heads, big = static_cast<int64_t>(upto[1][kThreads - 1]) * heads;
+#pragma unroll 1
+    for (int64_t e = blockIdx.x * static_cast<int64_t>(kTeams) + warp / kTeam; e < small; e += ctas_kv * static_cast<int64_t>(kTeams)) {
+      const KvItem t = item_at(0, e);
+      append_item<D, kTeam, 2>(a, t, tid % (32 * kTeam), red, 1 + warp / kTeam, [&](int, int32_t at, Eight<uint16_t>& x, Eight<uint16_t>& y) {
+        const uint16_t* row;
+        const RotUnit q = item_unit<D>(a, t, at, row);
+        x.load(row + q.a);
+        y.load(row + q.b);
+      }, [&](int, int32_t u, int32_t pos, RotAngles& g) { rot_angles(a.rot, u, pos, false, g); }, [](float) {});
+    }
+    auto stage = [&](const KvItem& t) {
+      int32_t mine = tid;
+      asm volatile("" : "+r"(mine));  // (nothing that follows from the thread alone is kept over the loop)
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) {
+        const int32_t at = mine + k * kThreads;
+        if (at < t.tokens * units) {
+          const uint16_t* row;
+          const RotUnit q = item_unit<D>(a, t, at, row);
+          copy16(&staged[2 * k * kThreads + mine], row + q.a);
+          copy16(&staged[(2 * k + 1) * kThreads + mine], row + q.b);
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    // (from the other end, where the line before left CTAs free)
+    const int64_t run = (big + ctas_kv - 1) / ctas_kv, end = min((ctas_kv - blockIdx.x) * run, big);
+    int64_t e = (ctas_kv - 1 - blockIdx.x) * run;
+    if (e >= end) return;
+    KvItem t = item_at(1, e);
+    stage(t);
+    int32_t have = -1;  // page (of the line) whose angles are kept
+    int32_t page = page_at(e);
+#pragma unroll 1
+    for (bool more = true; more;) {
+      ++e;
+      more = e < end;
+      const KvItem next = item_at(1, more ? e : e - 1);
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      int32_t mine = tid;
+      asm volatile("" : "+r"(mine));
+      append_item<D, kWarps, kHeld>(a, t, mine, red, 0, [&](int k, int32_t, Eight<uint16_t>& x, Eight<uint16_t>& y) {
+        x.q = staged[(2 * k) * kThreads + mine];
+        y.q = staged[(2 * k + 1) * kThreads + mine];
+      }, [&](int k, int32_t u, int32_t pos, RotAngles& g) {
+        float4* const kept = angles + k * 4 * kThreads + mine;
+        if (have != page) {
+          rot_angles(a.rot, u, pos, false, g);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) kept[j * kThreads] = make_float4(g.c[j].x, g.c[j].y, g.s[j].x, g.s[j].y);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float4 w = kept[j * kThreads];
+            g.c[j] = make_float2(w.x, w.y);
+            g.s[j] = make_float2(w.z, w.w);
+          }
+        }
+      }, [&](float most) {
+        asm volatile("" ::"f"(most) : "memory");  // what was staged has been read
+        if (more) stage(next);
+      });
+      if (!t.is_v) have = page;
+      t = next;
+      page = page_at(e);
+    }
+  } else {
+    const int32_t per = work.per;
+#pragma unroll 1
+    for (int32_t c = blockIdx.x - ctas_kv; c < upto[2][kThreads - 1]; c += gridDim.x - ctas_kv) {
+      int32_t k = c;
+      KvSpan s;
+      locate(2, k, s);
+      int32_t mine = tid;
+      asm volatile("" : "+r"(mine));
+      const int64_t e = static_cast<int64_t>(k) * kThreads + mine;
+      if (e >= static_cast<int64_t>(s.n) * per) continue;
+      const int32_t i = e >> 31 ? static_cast<int32_t>(e / per) : by_part.of(static_cast<int32_t>(e));
+      const int32_t ru = static_cast<int32_t>(e - static_cast<int64_t>(i) * per), run = ru / units, u = ru - run * units;
+      const RotUnit q = rot_unit(a.rot, u);
+      if (!q.turned && a.q == a.q_out) continue;
+      rotate_heads(a.q + (s.r0 + i) * a.ldq, a.q_out + (s.r0 + i) * a.ldqo, run * hpt, min(run * hpt + hpt, a.nh), D,
+                   a.rot, u, q, s.first + i, false);
     }
   }
 }
@@ -404,18 +593,22 @@ cudaError_t launch_kv_append(KvAppendArgs a, cudaStream_t st) {
   WaitCtl wc;
   if (!launch_wait_ctl(&wc)) return cudaErrorInvalidDevice;
   a.status = wc.status_word;
-  // shares of a sequence's pages and queries: what an average sequence has of them (any number is right)
-  const int32_t units = a.cache.d / 16;
-  const int64_t each = (a.T + a.B - 1) / a.B;
-  const int32_t zkv = static_cast<int32_t>(std::min<int64_t>((each + a.cache.page - 1) / a.cache.page, 32768 / (2 * a.cache.nkv)));
+  const int32_t units = a.cache.d / 16, heads = 2 * a.cache.nkv;
   const int32_t hpt = a.q ? heads_per_thread(a.T, a.nh, units) : 1, runs = a.q ? (a.nh + hpt - 1) / hpt : 0;
-  const int32_t zq = a.q ? static_cast<int32_t>(std::min<int64_t>((each * runs * units + kThreads - 1) / kThreads, 4096)) : 0;
-  // a warp for an item of up to 8 tokens, the CTA for longer ones (64 sequences, 32 / 8 heads of 128, one token each:
-  // TODO us against TODO)
-  const bool narrow = each <= 8;
-  const int32_t items = 2 * a.cache.nkv * zkv, blocks = narrow ? (items + kThreads / 32 - 1) / (kThreads / 32) : items;
+  // Teams of a warp up to 8 tokens a sequence in the mean, of two above (32 / 8 heads of 128: 64 sequences of 1, 8, 12 and 16
+  // tokens take 4.3, 8.0, 13.9 and 15.6 us by one warp, 5.7, 8.4, 10.2 and 12.4 by two; four prompts of 2048 in pages of 16
+  // tokens 61.9 and 44.7).
+  // CTAs for keys and values: as many as there can be work for (a sequence's pages: its rows' and two that it gets a part
+  // of), two an SM at most, with queries three for two SMs (32 heads of each, 4 x 1024 tokens: 59 us with one an SM, 47 with
+  // 228; 32 / 8 heads the same from one an SM on).  The queries' CTAs come behind them, for four chunks each where they are
+  // many (one each: 46 us instead of 41 for four prompts of 2048).  Any number is right.
+  const int64_t team = a.T <= 8 * static_cast<int64_t>(a.B) ? 1 : 2, teams = kThreads / 32 / team;
+  const int64_t singles = std::min<int64_t>(a.T, a.B), pages = (a.T - singles) / a.cache.page + (a.T > singles ? singles : 0);
+  const int64_t kv = std::min<int64_t>((singles * heads + teams - 1) / teams + pages * heads, a.q ? 228 : 304);
+  const int64_t chunks = (a.T * runs * units + kThreads - 1) / kThreads + (a.q && a.T > singles ? singles : 0);
+  const int64_t qs = std::min<int64_t>(std::max<int64_t>(chunks / 4, std::min<int64_t>(chunks, 304)), 1 << 20);
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(a.B), static_cast<unsigned>(blocks + zq));
+  cfg.gridDim = dim3(static_cast<unsigned>(kv + qs));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = st;
   cudaLaunchAttribute attr{};  // the kernel waits by itself for the launch ahead
@@ -423,13 +616,30 @@ cudaError_t launch_kv_append(KvAppendArgs a, cudaStream_t st) {
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  const auto go = [&](auto kern) {
-    return cudaLaunchKernelEx(&cfg, kern, a, zkv, zq, hpt, divisor(runs * units), divisor(a.cache.page));
+  const auto go = [&](auto d, auto t, auto held) {
+    constexpr auto kern = kv_append_kernel<decltype(d)::value, decltype(t)::value, decltype(held)::value>;
+    static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
+    cfg.dynamicSmemBytes = held * 6 * 16 * kThreads;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = uint64_t(1) << (dev & 63);
+    if (!(ready.load(std::memory_order_relaxed) & bit)) {
+      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(cfg.dynamicSmemBytes));
+      if (e != cudaSuccess) return e;
+      ready.fetch_or(bit, std::memory_order_relaxed);
+    }
+    return cudaLaunchKernelEx(&cfg, kern, a, static_cast<uint32_t>(kv), hpt, divisor(runs * units), divisor(a.cache.page),
+                              divisor(heads));
   };
-  const bool d128 = a.cache.d == 128;
-  if (narrow) return d128 ? go(kv_append_kernel<128, 1, 2>) : go(kv_append_kernel<64, 1, 2>);
-  if (a.cache.page * units <= 2 * kThreads) return d128 ? go(kv_append_kernel<128, 8, 2>) : go(kv_append_kernel<64, 8, 2>);
-  return go(kv_append_kernel<128, 8, 4>);  // pages of 128 tokens of 128 elements
+  constexpr std::integral_constant<int, 1> c1;
+  constexpr std::integral_constant<int, 2> c2;
+  constexpr std::integral_constant<int, 4> c4;
+  constexpr std::integral_constant<int, 64> c64;
+  constexpr std::integral_constant<int, 128> c128;
+  if (a.cache.d == 64) return team == 1 ? go(c64, c1, c2) : go(c64, c2, c2);
+  if (a.cache.page <= 64) return team == 1 ? go(c128, c1, c2) : go(c128, c2, c2);
+  return team == 1 ? go(c128, c1, c4) : go(c128, c2, c4);  // pages of 128 tokens of 128 elements
 }
 
 }  // namespace catq

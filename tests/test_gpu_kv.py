@@ -288,6 +288,21 @@ def test_append_matches_oracle(device, d, nkv, nh, page, lens, news, rot, interl
     assert (np.abs(got - asked[new]) <= K.half_step(asked[new]) * (1 + 2.0 ** -20) + slack[new]).all()
 
 
+@pytest.mark.parametrize("d,nkv,nh,page,lens,news", [
+    # single tokens, idle slots and a long prompt among them; more sequences than a CTA has threads
+    (128, 2, 4, 64, [90, 0, 17] * 100 + [700] + [64, 129], [1, 0, 1] * 100 + [650] + [1, 1]),
+    (64, 1, 2, 16, [3, 30, 64, 7] * 150, [0, 1, 2, 3] * 150),
+    # more pages than CTAs: a CTA's run of them begins and ends inside a page's heads
+    (128, 3, 3, 32, [2500, 1700, 40], [2480, 1700, 17]),
+    (128, 4, 1, 128, [5000, 3], [4980, 3]),
+    (64, 5, 5, 64, [3333, 2000], [3333, 1993]),
+    (128, 5, 5, 16, [1234, 900], [1230, 900]),
+])
+@pytest.mark.parametrize("kind", ["normal", "growing"])
+def test_append_of_mixed_batches(device, d, nkv, nh, page, lens, news, kind):
+    test_append_matches_oracle(device, d, nkv, nh, page, lens, news, d // 2, False, kind)
+
+
 def test_append_then_attention_then_packed_linear(device):
     """Decoding as it is used: a prompt of unequal lengths is appended, then tokens one by one, each with attention over
     the cache and the packed output projection; the oracle walks its own cache beside it."""
