@@ -696,6 +696,9 @@ size_t catq_kv_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, in
  * sequence are left as they were.  Codes are never NaN (catq_kv_append writes none) in tokens of the sequence; what lies
  * behind its last token may be anything.  Scales are powers of two, 0 or NaN.  Out-of-range offsets and lengths as in
  * catq_kv_append (the sequence's rows are left as they were); a page outside 0 .. n_pages - 1 counts as zeros, latched.
+ * Sequences of very different numbers of rows (single tokens with a prompt among them) give their result in one call,
+ * but take less time in one call a kind: sequences b0 .. b1 - 1 of a batch are row_start + b0, seq_len + b0, the table from
+ * its row b0 on, B = b1 - b0 and T = the end of the last one's rows (short ones first: T / B is taken as their mean).
  * workspace: >= catq_kv_attention_workspace_bytes(), 256-byte aligned, zero before the first call; a call leaves the
  * part that has to be zero as zero (one that latched CATQ_ERR_TIMEOUT may not).  Calls that may run at the same time
  * (other streams, other graphs) need workspaces of their own.

@@ -14,16 +14,26 @@
 // Scores in base 2: x = (S_hi + S_lo / 16) s_k f + log2 s_v for a token of a page with scales s_k, s_v (powers of two) and
 // a row whose query's scale and log2(e) / sqrt(d) are in f; weights of the value codes are w = 2^(x - m), the row's sum adds
 // w / s_v, and at the end O = O^T / sum, lse = (m + log2 sum) ln 2, both exact for whichever m was used.  m is the row's
-// largest x less 5, so that most weights lie well inside e4m3's range (2^-9 .. 448; hi + lo / 16 resolves 2^-14, 2^-19 of
-// the largest), and is raised lazily: only when some x - m passes 8.75 (weights stay below 448) does the CTA agree on new
-// maxima and rescale its sums and accumulators.
+// largest x less 3, so that the largest weights are 8 and most lie well inside e4m3's range (2^-9 .. 448; hi + lo / 16
+// resolves 2^-14, 2^-17 of the largest), and is raised lazily: only when some x - m passes 8.75 (weights stay below 448) does
+// the group agree on new maxima and rescale its sums and accumulators; a tile is scored twice at most.
 //
-// A CTA has 4 softmax warps (thread t owns token t of a tile: TMEM lane t), a TMA warp and an MMA warp; two CTAs an SM up
-// to 32 rows.  Work: the tiles of 128 tokens of all (sequence, key/value head, row tile), in this order as one line, cut
+// A CTA has a softmax group of 128 threads for up to 32 rows (16 of heads of 64, whose threads have two tokens; thread t owns
+// shared-memory row t of a tile: TMEM lane t), a TMA warp and an MMA warp.  Work: the tiles of all (sequence, key/value head, row
+// tile), in this order as one line, each row tile with a head of kHead positions for what its beginning and end cost, cut
 // into equal runs, one a CTA, whatever the sequences' lengths are; they are read on the device, so a captured launch
 // follows them.  A run that holds only a part of a row tile's tokens leaves its maxima, sums and accumulators in the
 // workspace; the last run of the row tile to finish (a counter, which it leaves at zero) joins them in their order, so
 // the result does not depend on which one that is.
+//
+// Bound by the codes' way from HBM where sequences are long: 64 of 300 to 8192 tokens, 32 / 8 heads of 128, one row
+// each, take 91 us for 572 MB, 6.3 TB/s (7 while it streams); a build without the softmax's arithmetic takes as
+// long, the rest is the start (lengths, page numbers, first tile: 5 us) and the last runs' join.  One sequence of
+// 131,071 tokens: 50.5 us for 268 MB.  16 sequences of 1000 to 4500 tokens with 25 rows a head: 29 us for 94 MB, 21 without
+// the softmax's arithmetic.  128 sequences of 17 to 2001 tokens, 12 heads of 64: 55 us for 199 MB, 46 without, bound by the
+// beginnings and ends of 1536 row tiles.
+// Two CTAs an SM: with three (rings of 4 slots) the 64 sequences took 94 us and the long one 54.8, with one (12 slots) 108
+// and 51.5, with two 92.5 and 51.8.
 //
 // Tokens behind a row's own position weigh 0 whatever their scales are; the values behind the last visible token of a tile
 // are zeroed in shared memory (what an unfinished page holds there may be anything, NaN codes too).
@@ -993,6 +1003,9 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
 // of weights 2^-10 at most, which is 2^-17 of the largest where that is 2^kNominalRows.
 // Thread (row, quarter c) has the row's tokens 32 c .. 32 c + 31 of a tile.  The four agree on the row's maximum through
 // shared memory; raising it is lazy, as there, row by row.
+// Two prompts' chunks of 1023 tokens on 6001 and 8191 (32 / 8 heads of 128, 213 GFLOP): 266 us, 0.8 PFLOP/s, bound by the
+// softmax (two threads a row: 284; without its arithmetic 167, the products' time: two terms of the queries and of the
+// weights are twice the multiply-adds).  The other kernel with tiles of 64 rows took 386.
 constexpr float kNominalRows = 7.0f;
 struct KvMany {
   static constexpr int kHd = 128, kR = 128, kTpr = 1, kTok = kRows, kHead = 4, kPages = kTok / 16;
@@ -1471,7 +1484,12 @@ cudaError_t run_kv(void (*kern)(CUtensorMap, CUtensorMap, KvTcArgs), int ctas, c
   return cudaLaunchKernelEx(&cfg, kern, tk, tv, p);
 }
 
-// Rows of a tile: what an average sequence has a key/value head (any number is right).
+// Rows of a tile: by what an average sequence has a key/value head (any number is right).  16 sequences of 4096 tokens, 8
+// key/value heads, us with tiles of 8 / 16 / 32 / 128 rows: heads of 128, 4 rows 29.2 / 29.0 / 31.4 / 47.9, 12 rows 33.7 /
+// 29.7 / 33.3 / 49, 24 rows 44.7 / 36.0 / 34.7 / 50, 64 rows 118 / 67 / 47 / 56, 128 rows 189 / 123 / 83 / 67; heads of 64, 4
+// rows 16.9 / 17.8 / 23, 16 rows 24 / 19 / 24, 128 rows 119 / 80 / 73.  The mean is a poor guide to a batch of single tokens
+// with a prompt among them: 128 single tokens on 2048 and a prompt of 512 (32 / 8 heads of 128) take 146 us in one call, 130
+// in two; 32 on 4096 and a prompt of 2048 183 and 150.
 template <int HD, int R>
 cudaError_t run_few(const KvAttnArgs& a, cudaStream_t st) {
   return run_kv<KvLay<HD, R>>(kv_attn_kernel<HD, R>, KvLay<HD, R>::kCtas, a, st);
@@ -1481,14 +1499,14 @@ cudaError_t run_kv_rows(const KvAttnArgs& a, cudaStream_t st) {
   const int64_t rows = (a.T + a.B - 1) / a.B * (a.nh / a.cache.nkv);
   if (rows <= 8) return run_few<HD, 8>(a, st);
   if (rows <= 16) return run_few<HD, 16>(a, st);
-  if (rows <= 32 || HD == 64) return run_few<HD, 32>(a, st);
+  if (rows <= 64 || HD == 64) return run_few<HD, 32>(a, st);
   return run_kv<KvMany>(kv_attn_rows_kernel, 1, a, st);
 }
 
 }  // namespace
 
 size_t kv_attention_ws_bytes(int32_t, int32_t, int32_t d) {
-  // two parts for each CTA: two CTAs an SM of up to 32 rows, one of 128
+  // two parts for each CTA: two CTAs an SM with tiles of up to 32 rows, one of 128 (heads of 64: of 32)
   const size_t parts = static_cast<size_t>(sm_count()) * 2 * (d == 128 ? 128 : 64) * (static_cast<size_t>(d) + 2) * sizeof(float);
   return (kCounterBytes + parts + 255) / 256 * 256;
 }

@@ -577,6 +577,31 @@ def test_bad_pages_offsets_and_lengths_are_latched(device):
                     assert (got[rows] == 7).all()
 
 
+@pytest.mark.parametrize("d", [128, 64])
+def test_a_batch_in_two_calls(device, d):
+    """Single tokens and prompts of one batch by a call each, on slices of the offsets, lengths and table."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(14, f"attn/two/{d}")
+    lens, news = [40, 300, 1, 120, 270], [1, 1, 1, 77, 33]
+    paged = Paged(r, lens, 2, 16, d, device)
+    rs, nh, T = starts(news), 8, sum(news)
+    q = syn.round_bf16(r.standard_normal((T, nh, d)).astype(np.float32))
+    Q, offsets, lengths = bf16(q.reshape(T, -1), device), i32(rs, device), i32(lens, device)
+    O = torch.full((T, nh * d), 7.0, dtype=torch.bfloat16, device=device)
+    lse = torch.full((T, nh), 7.0, device=device)
+    c = paged.cache
+    ws = C.kv_attention_workspace(c, nh)
+    for b0, b1 in ((0, 3), (3, 5)):
+        part, end = C.KVCache(c.k_codes, c.v_codes, c.k_scale, c.v_scale, c.table[b0:b1]), int(rs[b1])
+        C.catq_kv_attention(part, offsets[b0:b1 + 1], lengths[b0:b1], Q[:end], O[:end], nh, ws, lse[:end])
+        if b0 == 0:
+            assert (O[3:] == 7).all() and (lse[3:] == 7).all()
+    assert C.catq_device_status() == 0
+    check_attention(paged, rs, lens, q, nh, O.float().cpu().numpy().reshape(T, nh, d), lse.cpu().numpy())
+
+
 def test_many_sequences(device):
     """More sequences than the kernels have threads, many of them empty."""
     r = syn.rng(16, "many")
