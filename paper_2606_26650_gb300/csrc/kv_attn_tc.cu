@@ -1003,9 +1003,10 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
 // of weights 2^-10 at most, which is 2^-17 of the largest where that is 2^kNominalRows.
 // Thread (row, quarter c) has the row's tokens 32 c .. 32 c + 31 of a tile.  The four agree on the row's maximum through
 // shared memory; raising it is lazy, as there, row by row.
-// Two prompts' chunks of 1023 tokens on 6001 and 8191 (32 / 8 heads of 128, 213 GFLOP): 266 us, 0.8 PFLOP/s, bound by the
-// softmax (two threads a row: 284; without its arithmetic 167, the products' time: two terms of the queries and of the
-// weights are twice the multiply-adds).  The other kernel with tiles of 64 rows took 386.
+// Two prompts' chunks of 1023 tokens on 6001 and 8191 (32 / 8 heads of 128, 213 GFLOP) take 261 us, 0.8 PFLOP/s, bound by
+// the softmax: without its arithmetic 167, the products' time (two terms of the queries and of the weights are twice the
+// multiply-adds).  Two threads a row: 284; the accumulators raised before the weights are made, and only those of the rows
+// that have to be: 266; never raised: 246.  The other kernel with tiles of 64 rows took 386.
 constexpr float kNominalRows = 7.0f;
 struct KvMany {
   static constexpr int kHd = 128, kR = 128, kTpr = 1, kTok = kRows, kHead = 4, kPages = kTok / 16;
@@ -1272,19 +1273,14 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
         ex[buf * (128 * C) + c * 128 + row] = top;
         if (!bar_all(1 + quarter, 32 * C, ok)) { failed = true; break; }
         top = others(buf, top, [](float a, float b) { return fmaxf(a, b); });
-        const bool raise = top - m > kOver;
-        if (__any_sync(0xffffffffu, raise)) {
-          const float to = raise ? top - kNominalRows : m, fac = raise ? fast_exp2(m - to) : 1.0f;
+        // Where some row has to be raised, those that only could be are too: the accumulators' turn costs the same.
+        const bool any = __any_sync(0xffffffffu, top - m > kOver);
+        float fac = 1.0f;
+        if (any) {
+          const float to = top - m > kNominalRows ? top - kNominalRows : m;
+          fac = to == m ? 1.0f : fast_exp2(m - to);
           m = to;
           l *= fac;
-          if (j > 0) {
-            ok = wait_pv(gt - 1) && ok;
-            tc_fence_after();
-            const float2 f4[4] = {both(fac), both(fac), both(fac), both(fac)};
-#pragma unroll 1
-            for (int i = 0; i < W; i += 8) scale_cols8(lanes + Y::kColO + W * c + i, f4);
-            tmem_st_wait();
-          }
         }
         uint32_t hi[W / 4], lo[W / 4];
 #pragma unroll
@@ -1303,6 +1299,13 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
         }
         tmem_st8(sbuf, hi);
         tmem_st8(sbuf + 8, lo);
+        if (any && j > 0) {  // (by now the product before has mostly completed)
+          ok = wait_pv(gt - 1) && ok;
+          tc_fence_after();
+          const float2 f4[4] = {both(fac), both(fac), both(fac), both(fac)};
+#pragma unroll 1
+          for (int i = 0; i < W; i += 8) scale_cols8(lanes + Y::kColO + W * c + i, f4);
+        }
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
