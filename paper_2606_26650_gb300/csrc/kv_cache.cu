@@ -110,7 +110,8 @@ __device__ __forceinline__ void rotate_heads(const E* x, E* y, int32_t h0, int32
 }
 
 // Heads a thread takes at once: the longest run (fewest repeated angles) that still gives every SM a full set of
-// threads.
+// threads.  An append with queries (32 / 8 heads of 128), us by runs of 1 / 2 / 4 / 8: 64 tokens 3.5 / 3.4 / 3.4 / 4.3, 1024
+// tokens 9.5 / 7.6 / 6.6 / 7.1, 8192 tokens 62.7 / 49.7 / 41.1 / 40.5.
 int32_t heads_per_thread(int64_t tokens, int32_t nh, int32_t units) {
   int32_t hpt = 8;
   while (hpt > 1 && tokens * units * ((nh + hpt - 1) / hpt) < 152 * 2048) hpt /= 2;
@@ -118,6 +119,9 @@ int32_t heads_per_thread(int64_t tokens, int32_t nh, int32_t units) {
 }
 
 // One thread per (token, unit, run of `hpt` heads); `part` items a token (below 2^31), a CTA's tokens side by side.
+// Bound by HBM: 8192 tokens of 32 heads of 128 in bf16 take 25 us for 134 MB, 5.3 TB/s (a copy of the same bytes 21.6), 4999
+// of 40 heads in fp32 38.5 us, 5.3 TB/s.  Two CTAs an SM with four heads' loads ahead: three with four or two ahead
+// (80 registers) 31 and 26 us, four with two 27, two with eight 30.
 template <typename E>
 __global__ void __launch_bounds__(kThreads, 2) rope_at_vec_kernel(const RopeAtArgs a, int32_t hpt, Divisor by_units,
                                                                      Divisor by_part, int32_t part) {
@@ -139,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, 2) rope_at_vec_kernel(const RopeAtAr
 }
 
 // Any even rot and d, rows of the type's alignment: one thread per pair, or per element behind the rotated
-// part.
+// part (the 8192 tokens 97 us; 64 tokens 2.8 against 2.7).
 template <typename E>
 __global__ void __launch_bounds__(kThreads) rope_at_kernel(const RopeAtArgs a) {
   const int32_t half = a.rot.rot / 2, per = half + (a.d - a.rot.rot);
