@@ -455,10 +455,10 @@ __global__ void __launch_bounds__(kThreads, 2) kv_append_kernel(const KvAppendAr
   }
   // The sequence of item k of line l, which becomes the place in the sequence's share.  By whole warps.
   auto locate = [&](int l, int32_t& k, KvSpan& s) {
-    const int32_t eighth = __popc(__ballot_sync(0xffffffffu, upto[l][8 * lane + 7] <= k));
+    const int32_t eighth = min(__popc(__ballot_sync(0xffffffffu, upto[l][8 * lane + 7] <= k)), 31);
     const int32_t t = 8 * eighth + __popc(__ballot_sync(0xffffffffu, lane < 8 && upto[l][8 * eighth + (lane & 7)] <= k));
-    if (t > 0) k -= upto[l][t - 1];
-    int32_t b = t * stretch;
+    if (t > 0) k -= upto[l][min(t, kThreads) - 1];
+    int32_t b = min(t * stretch, a.B - 1);
     s = work.span(b, false);
 #pragma unroll 1
     for (int32_t n; k >= (n = work.count(s, l)) && b + 1 < a.B; k -= n) s = work.span(++b, false);
@@ -472,7 +472,9 @@ __global__ void __launch_bounds__(kThreads, 2) kv_append_kernel(const KvAppendAr
     const int32_t hv = static_cast<int32_t>(e - static_cast<int64_t>(k) * heads);
     KvSpan s;
     const int32_t b = locate(l, k, s);
-    return item_of(a, s, b, work.page_of(s, l, k), hv);
+    KvItem t{a.k, 0, 0, 0, -1, 0, false};
+    if (k >= 0 && k < work.count(s, l)) t = item_of(a, s, b, work.page_of(s, l, k), hv);  // (else lengths changed meanwhile)
+    return t;
   };
   if (blockIdx.x < ctas_kv) {
     const int64_t small = static_cast<int64_t>(upto[0][kThreads - 1]) * heads, big = static_cast<int64_t>(upto[1][kThreads - 1]) * heads;
