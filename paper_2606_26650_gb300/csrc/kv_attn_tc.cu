@@ -331,15 +331,16 @@ struct KvTcArgs {
   KvGeom g;
   uint32_t* counters;  // [gridDim.x]
   float* parts;        // [gridDim.x][2][kPartFloats]
-  int32_t min_run;     // least tiles of a run
   WaitCtl wc;
 };
 
-// The run of this CTA: every CTA adds up all sequences' tiles, a thread a stretch of them.  scan [warps] and start [4]: shared
-// memory.  Every thread of the CTA comes here, and what it wrote before is visible to all afterwards, tensor memory's
+// The run of this CTA: every CTA adds up all sequences' tiles, a thread a stretch of them.  A run is at least a row tile of two
+// tiles, or of one where no sequence has more (prompts of 64 and 100 tokens, 32 / 8 heads of 128: 16.8 and 17.1 us with two,
+// 10.3 and 10.7 with one).  scan [warps], longest [warps] and start [4]: shared memory.  Every thread of the CTA comes here, and what it wrote before is visible to all afterwards, tensor memory's
 // address too.
 template <class Y>
-__device__ __forceinline__ KvWalk<Y> find_run(const KvTcArgs& p, int64_t* scan, int32_t* start, int64_t& run, int64_t& first) {
+__device__ __forceinline__ KvWalk<Y> find_run(const KvTcArgs& p, int64_t* scan, int32_t* longest, int32_t* start, int64_t& run,
+                                              int64_t& first) {
   const KvGeom& g = p.g;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int64_t total;
@@ -347,24 +348,33 @@ __device__ __forceinline__ KvWalk<Y> find_run(const KvTcArgs& p, int64_t* scan, 
     const int32_t per = (g.B + Y::kThreads - 1) / Y::kThreads;
     const int32_t b0 = min(static_cast<int32_t>(threadIdx.x) * per, g.B), b1 = min(b0 + per, g.B);
     int64_t mine = 0;
+    int32_t most = 1;
 #pragma unroll 1
-    for (int32_t b = b0; b < b1; ++b)
-      mine += load_seq<Y>(g, b, blockIdx.x == 0 ? p.a.status : nullptr).per_head * g.nkv;
+    for (int32_t b = b0; b < b1; ++b) {
+      const KvSeq s = load_seq<Y>(g, b, blockIdx.x == 0 ? p.a.status : nullptr);
+      mine += s.per_head * g.nkv;
+      if (s.n > 0) most = max(most, tiles_of<Y>(s.len));
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
     int64_t upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
       if (lane >= o) upto += v;
     }
-    if (lane == 31) scan[warp] = upto;
+    if (lane == 31) {
+      scan[warp] = upto;
+      longest[warp] = most;
+    }
     __syncthreads();
     total = 0;
 #pragma unroll 1
     for (int w = 0; w < Y::kThreads / 32; ++w) {
       if (w < warp) upto += scan[w];
       total += scan[w];
+      most = max(most, longest[w]);
     }
-    run = max((total + gridDim.x - 1) / gridDim.x, static_cast<int64_t>(p.min_run));
+    run = max((total + gridDim.x - 1) / gridDim.x, static_cast<int64_t>(Y::kHead + min(most, 2)));
     first = run * blockIdx.x;
     if (upto - mine <= first && first < upto) {  // the thread whose stretch holds the run's first tile
       int64_t rest = first - (upto - mine);
@@ -503,7 +513,8 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
   int32_t* const merge_flag = reinterpret_cast<int32_t*>(gbase + 404);
   int32_t* const start = reinterpret_cast<int32_t*>(gbase + 408);           // b, h, q, t of the run's first tile
   int64_t* const scan = reinterpret_cast<int64_t*>(gbase + 424);            // warps' sums
-  static_assert(424 + 8 * (kThreads / 32) <= Y::kOffScale, "start");
+  int32_t* const longest = reinterpret_cast<int32_t*>(gbase + 424 + 8 * (kThreads / 32));  // warps' longest sequences, in tiles
+  static_assert(424 + 12 * (kThreads / 32) <= Y::kOffScale, "start");
   float* const scales = reinterpret_cast<float*>(gbase + Y::kOffScale);     // [kScaleRing][key scales, value scales of kPages]
   float* const row_f = reinterpret_cast<float*>(gbase + Y::kOffF);
   float* const row_m = reinterpret_cast<float*>(gbase + Y::kOffM);
@@ -539,7 +550,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
 
   const KvGeom& g = p.g;
   int64_t run, first;
-  KvWalk<Y> w = find_run<Y>(p, scan, start, run, first);
+  KvWalk<Y> w = find_run<Y>(p, scan, longest, start, run, first);
   const uint32_t tmem = *tmem_slot;
   constexpr uint32_t kColO = Y::kColO;
   const KvCacheDev& kv = p.a.cache;
@@ -1064,7 +1075,8 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
   int32_t* const merge_flag = reinterpret_cast<int32_t*>(gbase + 404);
   int32_t* const start = reinterpret_cast<int32_t*>(gbase + 408);
   int64_t* const scan = reinterpret_cast<int64_t*>(gbase + 424);
-  static_assert(424 + 8 * (Y::kThreads / 32) <= Y::kOffScale, "start");
+  int32_t* const longest = reinterpret_cast<int32_t*>(gbase + 424 + 8 * (Y::kThreads / 32));
+  static_assert(424 + 12 * (Y::kThreads / 32) <= Y::kOffScale, "start");
   float* const scales = reinterpret_cast<float*>(gbase + Y::kOffScale);
   float* const ex = reinterpret_cast<float*>(gbase + Y::kOffEx);  // [2][C][128]: what the threads of a row tell each other
 
@@ -1092,7 +1104,7 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
   grid_dependency_wait();
   const KvGeom& g = p.g;
   int64_t run, first;
-  KvWalk<Y> w = find_run<Y>(p, scan, start, run, first);
+  KvWalk<Y> w = find_run<Y>(p, scan, longest, start, run, first);
   const uint32_t tmem = *tmem_slot;
   const KvCacheDev& kv = p.a.cache;
   bool ok = true;
@@ -1462,7 +1474,6 @@ cudaError_t run_kv(void (*kern)(CUtensorMap, CUtensorMap, KvTcArgs), int ctas, c
                static_cast<int64_t>(a.cache.max_pages) * a.cache.page};
   p.counters = static_cast<uint32_t*>(a.workspace);
   p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + kCounterBytes);
-  p.min_run = Y::kHead + 2;
   static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
