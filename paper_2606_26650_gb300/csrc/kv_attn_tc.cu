@@ -1014,10 +1014,10 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
 // of weights 2^-10 at most, which is 2^-17 of the largest where that is 2^kNominalRows.
 // Thread (row, quarter c) has the row's tokens 32 c .. 32 c + 31 of a tile.  The four agree on the row's maximum through
 // shared memory; raising it is lazy, as there, row by row.
-// Two prompts' chunks of 1023 tokens on 6001 and 8191 (32 / 8 heads of 128, 213 GFLOP) take 261 us, 0.8 PFLOP/s, bound by
+// Two prompts' chunks of 1023 tokens on 6001 and 8191 (32 / 8 heads of 128, 213 GFLOP) take 257 us, 0.8 PFLOP/s, bound by
 // the softmax: without its arithmetic 167, the products' time (two terms of the queries and of the weights are twice the
 // multiply-adds).  Two threads a row: 284; the accumulators raised before the weights are made, and only those of the rows
-// that have to be: 266; never raised: 246.  The other kernel with tiles of 64 rows took 386.
+// that have to be: 266; rows read and written by their own lanes: 261.  The other kernel with tiles of 64 rows took 386.
 constexpr float kNominalRows = 7.0f;
 struct KvMany {
   static constexpr int kHd = 128, kR = 128, kTpr = 1, kTok = kRows, kHead = 4, kPages = kTok / 16;
@@ -1056,6 +1056,23 @@ __device__ __forceinline__ void split4(const float* x, uint32_t& hi, uint32_t& l
   }
   hi = h[0] | static_cast<uint32_t>(h[1]) << 16;
   lo = l[0] | static_cast<uint32_t>(l[1]) << 16;
+}
+
+// Four lanes' four vectors each, exchanged: vector i of lane c for vector c of lane i.
+__device__ __forceinline__ void exchange4(uint4 (&r)[4], int lane) {
+  auto swap = [&](uint4& a, uint4& b, int o) {  // the lower lane gives b for the upper one's a
+    const bool up = (lane & o) != 0;
+    uint4 give = up ? a : b;
+    give.x = __shfl_xor_sync(0xffffffffu, give.x, o);
+    give.y = __shfl_xor_sync(0xffffffffu, give.y, o);
+    give.z = __shfl_xor_sync(0xffffffffu, give.z, o);
+    give.w = __shfl_xor_sync(0xffffffffu, give.w, o);
+    (up ? a : b) = give;
+  };
+  swap(r[0], r[1], 1);
+  swap(r[2], r[3], 1);
+  swap(r[0], r[2], 2);
+  swap(r[1], r[3], 2);
 }
 
 __global__ void __launch_bounds__(KvMany::kThreads, 1)
@@ -1178,6 +1195,22 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
     uint32_t gt = 0, ring = 0;
     // (see the other kernel's)
     auto wait_pv = [&](uint32_t t) { return mbar_wait_warp(pv_done0 + 8u * (t & 1), (t >> 1) & 1, p.wc); };
+    // Rows come and go four at a time, 64 bytes of each by the four lanes whose rows they are (by the row's own
+    // lane, a line a row and instruction, 8 prompts of 512 took 78 us instead of 74).  Vector i of the
+    // lane is part of row i of the four: its offset in rows ld elements apart, -1 behind the last row.
+    auto place = [&](const KvWalk<Y>& v, int i, int64_t ld) -> int64_t {
+      const int32_t at = v.sq * R + quarter * 32 + (lane & ~3) + i, tk = g.token_of(at);
+      return at < v.rows_n * g.group ? (v.r0 + tk) * ld + (v.sh * g.group + at - tk * g.group) * HD + W * c + 8 * (lane & 3) : -1;
+    };
+    static_assert(W == 32, "four vectors a row");
+    auto ask = [&](const KvWalk<Y>& v, uint4 (&q)[W / 8]) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t from = place(v, i, p.a.ldq);
+        q[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (from >= 0) q[i] = *reinterpret_cast<const uint4*>(p.a.q + from);
+      }
+    };
     while (w.next(g)) {
       if (!bar_all(kEvery, Y::kSoft, ok)) { ok = false; break; }
       const int32_t at = w.sq * R + row, tk = g.token_of(at), head = w.sh * g.group + at - tk * g.group;
@@ -1187,12 +1220,9 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
       float f;
       {
         uint4 q[W / 8];
+        ask(w, q);
+        exchange4(q, lane);
         uint32_t top = 0;
-#pragma unroll
-        for (int k = 0; k < W / 8; ++k) {
-          q[k] = make_uint4(0u, 0u, 0u, 0u);
-          if (mine) q[k] = *reinterpret_cast<const uint4*>(p.a.q + (w.r0 + tk) * p.a.ldq + head * HD + W * c + 8 * k);
-        }
 #pragma unroll
         for (int k = 0; k < W / 8; ++k) {
           const uint32_t u[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
@@ -1347,23 +1377,35 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
         }
         ok = wait_pv(gt - 1) && ok;
         tc_fence_after();
-#pragma unroll 1
-        for (int i = 0; i < W; i += 16) {
-          uint32_t o[16];
-          tmem_ld16(lanes + Y::kColO + W * c + i, o);
-          tmem_ld_wait();
-          if (!mine || !ok) continue;
-          if (whole) {
-            uint32_t two[8];
+        if (whole) {
+          uint4 two[W / 8];
+#pragma unroll
+          for (int i = 0; i < W; i += 16) {
+            uint32_t o[16], u[8];
+            tmem_ld16(lanes + Y::kColO + W * c + i, o);
+            tmem_ld_wait();
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const float a = by == 0.0f ? 0.0f : __uint_as_float(o[2 * e]) * by;
               const float b = by == 0.0f ? 0.0f : __uint_as_float(o[2 * e + 1]) * by;
-              asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(two[e]) : "f"(b), "f"(a));
+              asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[e]) : "f"(b), "f"(a));
             }
-            *reinterpret_cast<uint4*>(out + i) = make_uint4(two[0], two[1], two[2], two[3]);
-            *reinterpret_cast<uint4*>(out + i + 8) = make_uint4(two[4], two[5], two[6], two[7]);
-          } else {
+            two[i / 8] = make_uint4(u[0], u[1], u[2], u[3]);
+            two[i / 8 + 1] = make_uint4(u[4], u[5], u[6], u[7]);
+          }
+          exchange4(two, lane);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int64_t to = place(w, i, p.a.ldo);
+            if (ok && to >= 0) *reinterpret_cast<uint4*>(p.a.o + to) = two[i];
+          }
+        } else {
+#pragma unroll 1
+          for (int i = 0; i < W; i += 16) {
+            uint32_t o[16];
+            tmem_ld16(lanes + Y::kColO + W * c + i, o);
+            tmem_ld_wait();
+            if (!mine || !ok) continue;
             uint4* const to = reinterpret_cast<uint4*>(part + 2 * R + row * HD + W * c + i);
 #pragma unroll
             for (int e = 0; e < 4; ++e) to[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
