@@ -782,16 +782,18 @@ def _rows(t, name: str, T: int, width: int, where: str):
     return t.data_ptr(), st[0] if T > 1 else width
 
 
+_INT32: dict = {}
+
+
 def _i32(t, name: str, count: int, where: str):
-    if "i32" not in _DTYPES_I:
+    if t.dtype not in _INT32:
         import torch
-        _DTYPES_I["i32"] = torch.int32
-    if t.dtype != _DTYPES_I["i32"]:
-        raise ValueError(f"{where}: {name} must be int32")
+        _INT32[torch.int32] = True
+        if t.dtype not in _INT32:
+            raise ValueError(f"{where}: {name} must be int32")
+    if t.is_cuda and t.is_contiguous() and t.numel() >= count:
+        return t.data_ptr()
     return _buf(t, name, 4 * count, where)
-
-
-_DTYPES_I: dict = {}
 
 
 class Rope:
@@ -874,7 +876,7 @@ def catq_rope_at(X, positions, rope: Rope, n_heads: int, d: int, Y=None, inverse
 
 
 def _bf16_rows(t, name, T, width, where):
-    if _known_dtype(t) != BF16:
+    if _DTYPES.get(t.dtype) != BF16 and _known_dtype(t) != BF16:
         raise ValueError(f"{where}: {name} must be bfloat16")
     return _rows(t, name, T, width, where)
 

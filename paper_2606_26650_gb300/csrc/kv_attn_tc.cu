@@ -84,7 +84,8 @@ struct KvLay {
   // its last raise, last position, output offset (8 bytes), sums by warp | Q, P twice, ring
   static constexpr uint32_t kOffScale = 640, kOffF = kOffScale + kScaleRing * 8 * kPages, kOffM = kOffF + 4 * R,
                             kOffFac = kOffM + 4 * R, kOffLim = kOffFac + 4 * R, kOffRow = kOffLim + 4 * R,
-                            kOffZero = kOffRow + 8 * R, kOffRed = kOffZero + 4 * R, kOffQ = (kOffRed + 16 * R + 127) / 128 * 128, kOffP = kOffQ + kQ,
+                            kOffZero = kOffRow + 8 * R, kOffRed = kOffZero + 4 * R,
+                            kOffQ = (kOffRed + 16 * R + 127) / 128 * 128, kOffP = kOffQ + kQ,
                             kOffRing = (kOffP + 2 * kP + 1023) / 1024 * 1024;
   static constexpr uint32_t kBudget = (kCtas == 2 ? 112 : 224) * 1024;
   static constexpr int kSlots0 = (kBudget - 1024 - kOffRing) / kTile;
@@ -336,8 +337,8 @@ struct KvTcArgs {
 
 // The run of this CTA: every CTA adds up all sequences' tiles, a thread a stretch of them.  A run is at least a row tile of two
 // tiles, or of one where no sequence has more (prompts of 64 and 100 tokens, 32 / 8 heads of 128: 16.8 and 17.1 us with two,
-// 10.3 and 10.7 with one).  scan [warps], longest [warps] and start [4]: shared memory.  Every thread of the CTA comes here, and what it wrote before is visible to all afterwards, tensor memory's
-// address too.
+// 10.3 and 10.7 with one).  scan [warps], longest [warps] and start [4]: shared memory.  Every thread of the CTA comes here,
+// and what it wrote before is visible to all afterwards, tensor memory's address too.
 template <class Y>
 __device__ __forceinline__ KvWalk<Y> find_run(const KvTcArgs& p, int64_t* scan, int32_t* longest, int32_t* start, int64_t& run,
                                               int64_t& first) {
