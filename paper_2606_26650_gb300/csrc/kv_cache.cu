@@ -77,7 +77,8 @@ struct Eight<float> {
 };
 
 // Heads h0 .. h1 - 1 of one token, unit q, rotated by angles that are computed once: the first heads' loads go out
-// before the angles, which cover their latency, and always kAhead heads' before any store.
+// before the angles, which cover their latency, and always kAhead heads' before any store.  (A head's offset has 64 bits: a
+// row may have 2^32 elements.)
 template <typename E>
 __device__ __forceinline__ void rotate_heads(const E* x, E* y, int32_t h0, int32_t h1, int32_t d, const RotDev& rot,
                                              int32_t u, const RotUnit& q, int32_t pos, bool inverse) {
@@ -87,8 +88,8 @@ __device__ __forceinline__ void rotate_heads(const E* x, E* y, int32_t h0, int32
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
       if (h + k < h1) {
-        a[k].load(x + (h + k) * d + q.a);
-        b[k].load(x + (h + k) * d + q.b);
+        a[k].load(x + static_cast<int64_t>(h + k) * d + q.a);
+        b[k].load(x + static_cast<int64_t>(h + k) * d + q.b);
       }
   };
   load(h0);
@@ -103,8 +104,8 @@ __device__ __forceinline__ void rotate_heads(const E* x, E* y, int32_t h0, int32
         a[k].get(v);
         b[k].get(v + 8);
         if (q.turned) rot_apply(rot.interleaved != 0, ang, v);
-        store8(y + (h + k) * d + q.a, v);
-        store8(y + (h + k) * d + q.b, v + 8);
+        store8(y + static_cast<int64_t>(h + k) * d + q.a, v);
+        store8(y + static_cast<int64_t>(h + k) * d + q.b, v + 8);
       }
   }
 }
