@@ -426,7 +426,9 @@ __device__ __forceinline__ void copy_tiles(const CUtensorMap& tmk, const CUtenso
   bool ok = true;
   int slot = 0, loads = 0;
   uint32_t ph = 1, gt = 0;
-  // A lane a page: the lane's page in tile t of the segment (first row of its block, -1: none), its scales.
+  // A lane a page: the lane's page in tile t of the segment (first row of its block, -1: none), its scales.  Ordinary loads: the
+  // launch ahead may have written scales and table while this kernel was resident already, and a non-coherent load (ld.global.nc)
+  // is only defined for what no one writes while the kernel lives.
   struct Page {
     int32_t row;
     float ks, vs;
@@ -434,7 +436,7 @@ __device__ __forceinline__ void copy_tiles(const CUtensorMap& tmk, const CUtenso
   auto page_of = [&](int32_t j) -> int32_t {
     const int32_t tok = (w.t0 + j) * kTok + lane * kv.page;
     if (j >= w.n || lane >= ppt || tok >= w.vis) return -1;
-    return __ldg(kv.table + static_cast<int64_t>(w.sb) * kv.max_pages + tok / kv.page);
+    return kv.table[static_cast<int64_t>(w.sb) * kv.max_pages + tok / kv.page];
   };
   auto block_of = [&](int32_t j, int32_t id) {
     Page g{-1, 0.0f, 0.0f};
@@ -446,8 +448,8 @@ __device__ __forceinline__ void copy_tiles(const CUtensorMap& tmk, const CUtenso
     }
     const int32_t block = id * kv.nkv + w.sh;
     g.row = block * (kv.page / TPR);
-    g.ks = __ldg(kv.k_scale + block);
-    g.vs = __ldg(kv.v_scale + block);
+    g.ks = kv.k_scale[block];
+    g.vs = kv.v_scale[block];
     return g;
   };
   // A tile into the next slot; with its keys go its scales, into a ring of kScaleRing tiles of their own.  That is

@@ -95,8 +95,8 @@ struct RotAngles {
 __device__ __forceinline__ void rot_angles(const RotDev& r, int32_t u, int32_t pos, bool inverse, RotAngles& a) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const auto* t = reinterpret_cast<const unsigned long long*>(r.turns) + 8 * u + 2 * j;
-    rot_cos_sin2(pos, __ldg(t), __ldg(t + 1), r.magnitude, a.c[j], a.s[j]);
+    const uint64_t* const t = r.turns + 8 * u + 2 * j;
+    rot_cos_sin2(pos, t[0], t[1], r.magnitude, a.c[j], a.s[j]);
     if (inverse) a.s[j] = make_float2(-a.s[j].x, -a.s[j].y);
   }
 }

@@ -535,7 +535,8 @@ __global__ void __launch_bounds__(kThreads, 2) ternary_mma_kernel(const __grid_c
     const int32_t nb = f.nb, place = f.place;
     const uint4* const xbase =
         reinterpret_cast<const uint4*>(f.X + static_cast<int64_t>(gid < nb ? gid : 0) * f.ldx + 16 * VW * q);
-    // (32 bytes at a time where X allows: half the passes through L1, which a load of eight token rows
+    // (ordinary loads: X may be what the launch ahead wrote while this kernel was resident already, which a non-coherent load
+    // is not defined for; 32 bytes at a time where X allows: half the passes through L1, which a load of eight token rows
     // at 16 bytes a lane keeps busy; two 8B blocks, 8 tokens: 10 us less, staged 129 -> 101.  A staged
     // launch's X may be an earlier stage's Y: plain loads, after the stage's acquire, or through L2 for
     // a single token, whose row is not read twice: 96 -> 92.)
@@ -548,7 +549,7 @@ __global__ void __launch_bounds__(kThreads, 2) ternary_mma_kernel(const __grid_c
         return;
       }
 #pragma unroll
-      for (int i = 0; i < 2 * VW; ++i) xv[i] = STAGED ? __ldcg(xp + i) : __ldg(xp + i);
+      for (int i = 0; i < 2 * VW; ++i) xv[i] = STAGED ? __ldcg(xp + i) : xp[i];
     };
     uint4 xs[NX][2 * VW];  // activations, up to NX super-chunks ahead
 #pragma unroll

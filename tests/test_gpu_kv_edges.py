@@ -37,3 +37,47 @@ def test_rotation_of_rows_past_32_bits(device, dtype):  # noqa: F811
     assert C.catq_device_status() == 0
     del X, Y, x, y
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("shift", [0, 8])
+def test_a_decode_step_sees_what_the_launch_ahead_wrote(device, shift):  # noqa: F811
+    """Append, attention over its own queries and the packed output projection, back to back, every launch resident while the one
+    ahead runs: the same bits as with a wait between them.  shift: rows of 32-byte and of 16-byte alignment."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    nh, nkv, d, page, B, g, steps = 16, 4, 64, 16, 5, 128, 24
+    N, kdim = 512, nh * d
+    gen = torch.Generator(device=device).manual_seed(11)
+
+    def normal(*shape):
+        return torch.empty(*shape, dtype=torch.bfloat16, device=device).normal_(generator=gen)
+
+    codes = torch.randint(0, 255, (N * kdim // 4,), dtype=torch.uint8, device=device, generator=gen) & 0b01010101
+    alpha = torch.rand(N * kdim // g, device=device, generator=gen)
+    rope = C.Rope.create(d, 10000.0, device)
+    tokens = [(normal(B, nh * d), normal(B, nkv * d), normal(B, nkv * d)) for _ in range(steps)]
+    results = []
+    for wait in (True, False):
+        table = torch.arange(B * 4, dtype=torch.int32, device=device).view(B, 4)
+        cache = C.KVCache.create(B * 4, nkv, page, d, table)
+        ws = C.kv_attention_workspace(cache, nh)
+        rows = i32(np.arange(B + 1), device)
+        lens = [i32(np.arange(B) * 7 + i + 1, device) for i in range(steps)]
+        flat = torch.zeros(B * nh * d + 16, dtype=torch.bfloat16, device=device)
+        Q = flat[shift:shift + B * nh * d].view(B, nh * d)
+        out = [torch.empty(B, N, dtype=torch.bfloat16, device=device) for _ in range(steps)]
+        torch.cuda.synchronize()
+        for i, (q, k, v) in enumerate(tokens):
+            Q.copy_(q)
+            for call in (lambda: C.catq_kv_append(cache, rows, lens[i], k, v, rope=rope, Q=Q, n_heads=nh),
+                         lambda: C.catq_kv_attention(cache, rows, lens[i], Q, Q, nh, ws),
+                         lambda: C.catq_ternary_infer(codes, alpha, N, kdim, g, Q, out[i])):
+                call()
+                if wait:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        assert C.catq_device_status() == 0
+        results.append(torch.stack(out))
+    assert torch.isfinite(results[0].float()).all()
+    assert torch.equal(results[0], results[1])
