@@ -34,9 +34,11 @@ __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 // cos and sin, times m, of pos * turn for two pairs.  The product wraps modulo 2^64, which is modulo one turn, so that
 // the angle of a far position is as exact as that of a near one (32-bit floats would lose 2^-24 of the whole angle: 0.008
 // rad at 131072).  Its upper 32 bits fall into the nearest half turn, which is a sign of both, and a rest of at most a
-// quarter, whose sine and cosine are their Taylor series up to x^13 and x^14 (remainders x^15 / 15! and x^16 / 16! at pi / 2:
-// 6.7e-10 and 6.6e-11, far under half a unit in the last place), evaluated for the two pairs at once.  Quarter turns would
-// save three terms and cost twice their instructions in exchanging sine and cosine.
+// quarter as x + e: x the upper 24 of its bits in radians, rounded to fp32, e the rounding and the lower 8 bits.  sin x and cos x
+// are their Taylor series up to x^13 and x^14 (remainders x^15 / 15! and x^16 / 16! at pi / 2: 6.7e-10 and 6.6e-11), evaluated for
+// the two pairs at once, sin(x + e) = sin x + e cos x, cos(x + e) = cos x - e sin x.  Over all rests either is off by 2^-22.86 at most,
+// 2^-25.3 in the mean square: what is left is the series' own roundings near pi / 2, where x, of 1.5, is rounded to 2^-24; without e 2^-22.13
+// and 2^-24.85.  Quarter turns would save three terms and cost twice their instructions in exchanging sine and cosine.
 __device__ __forceinline__ uint32_t turn_of(int32_t pos, uint64_t turn) {
   const uint32_t lo = static_cast<uint32_t>(turn), hi = static_cast<uint32_t>(turn >> 32);
   return __umulhi(static_cast<uint32_t>(pos), lo) + static_cast<uint32_t>(pos) * hi - (pos < 0 ? lo : 0u);
@@ -44,9 +46,15 @@ __device__ __forceinline__ uint32_t turn_of(int32_t pos, uint64_t turn) {
 __device__ __forceinline__ void rot_cos_sin2(int32_t pos, uint64_t t0, uint64_t t1, float m, float2& c, float2& s) {
   const uint32_t f0 = turn_of(pos, t0), f1 = turn_of(pos, t1);
   const uint32_t h0 = (f0 + 0x40000000u) & 0x80000000u, h1 = (f1 + 0x40000000u) & 0x80000000u;
-  const float2 x = mul2(make_float2(static_cast<float>(static_cast<int32_t>(f0 ^ h0)),
-                                    static_cast<float>(static_cast<int32_t>(f1 ^ h1))),
-                        both(1.4629180792671596e-9f));  // 2 pi / 2^32
+  constexpr float kUnit = 1.4629180792671596e-9f;                                      // 2 pi / 2^32 rounded to fp32,
+  constexpr float kUnitLo = static_cast<float>(1.4629180792671596e-9 - static_cast<double>(kUnit));  // and what that leaves
+  const float2 up = make_float2(static_cast<float>(static_cast<int32_t>((f0 ^ h0) & 0xffffff00u)),
+                                static_cast<float>(static_cast<int32_t>((f1 ^ h1) & 0xffffff00u)));
+  // the lower bits as 2^23 and more (the mantissa's last)
+  const float2 low = make_float2(__uint_as_float(0x4b000000u | (f0 & 0xffu)), __uint_as_float(0x4b000000u | (f1 & 0xffu)));
+  const float2 x = mul2(up, both(kUnit));
+  const float2 off = fma2(up, both(kUnitLo), fma2(up, both(kUnit), make_float2(-x.x, -x.y)));
+  const float2 e = fma2(fma2(low, both(kUnit), both(-8388608.0f * kUnit)), both(1.0f), off);
   const float2 y = mul2(x, x);
   float2 sn = fma2(y, both(1.0f / 6227020800.0f), both(-1.0f / 39916800.0f));
   sn = fma2(y, sn, both(1.0f / 362880.0f));
@@ -62,8 +70,8 @@ __device__ __forceinline__ void rot_cos_sin2(int32_t pos, uint64_t t0, uint64_t 
   cs = fma2(y, cs, both(-0.5f));
   cs = fma2(y, cs, both(1.0f));
   const float2 sign = make_float2(__uint_as_float(__float_as_uint(m) ^ h0), __uint_as_float(__float_as_uint(m) ^ h1));
-  c = mul2(cs, sign);
-  s = mul2(sn, sign);
+  c = mul2(fma2(make_float2(-e.x, -e.y), sn, cs), sign);
+  s = mul2(fma2(e, cs, sn), sign);
 }
 __device__ __forceinline__ void rot_cos_sin(int32_t pos, uint64_t turn, float m, float& c, float& s) {
   float2 c2, s2;

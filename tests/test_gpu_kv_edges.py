@@ -81,3 +81,30 @@ def test_a_decode_step_sees_what_the_launch_ahead_wrote(device, shift):  # noqa:
         results.append(torch.stack(out))
     assert torch.isfinite(results[0].float()).all()
     assert torch.equal(results[0], results[1])
+
+
+@pytest.mark.parametrize("pos", [1, -1, 2 ** 31 - 1])
+def test_sine_and_cosine_by_themselves(device, pos):  # noqa: F811
+    """(1, 0) rotated by a million angles from all around the circle, those at the quarter turns more densely: cosine and sine to
+    2^-22.5.  (The angle's last step, 2^-32 of a turn, is 2^-29.3.)"""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = np.random.default_rng(22)
+    half, nh = 32768, 1
+    X = torch.zeros(1, 2 * half, device=device)
+    X[:, :half] = 1.0
+    for i in range(32):
+        turns = r.integers(0, 2 ** 64, half, dtype=np.uint64)
+        if i % 2:  # within 2^-4 of a quarter turn
+            turns = (turns >> np.uint64(4)) + (turns & np.uint64(3)) * np.uint64(2 ** 62) - np.uint64(2 ** 59)
+        rope = C.Rope(torch.from_numpy(turns.view(np.int64).copy()).to(device), 2 * half)
+        Y = torch.empty_like(X)
+        C.catq_rope_at(X, i32([pos], device), rope, nh, 2 * half, Y)
+        got = Y.cpu().numpy().reshape(2, half).astype(np.float64)
+        with np.errstate(over="ignore"):
+            part = turns * np.uint64(pos % 2 ** 64)  # modulo one turn
+        angle = part.astype(np.longdouble) * (2 * np.pi / np.longdouble(2) ** 64)
+        assert np.abs(got[0] - np.cos(angle)).max() <= 2.0 ** -22.5
+        assert np.abs(got[1] - np.sin(angle)).max() <= 2.0 ** -22.5
+    assert C.catq_device_status() == 0
