@@ -3,20 +3,24 @@
 //
 // With few query rows a key/value head, the cached tokens are the long side: they are the M of both products, the
 // rows (new token, query head of the group), R of them a CTA's tile, the N:
-//   S^T [128 tokens, 2 R] = K [128, d] Q^T,      O^T [d, 2 R] += V^T [d, 128] P^T [128, 2 R].
+//   S^T [128 tokens, 2 R] = K [128, d] Q^T,      O^T [d, 3 R] += V^T [d, 128] P^T [128, 3 R].
 // A operands are the code tiles that TMA brings page by page (K K-major, V MN-major: the tensor core transposes it), e4m3
-// like the cache.  B operands are e4m3 too, as two terms in columns of their own: x = hi + lo / 16 with hi = e4m3(x), lo =
-// e4m3(16 (x - hi)), 4 + 4 significant bits.  A bf16 query (8 bits), scaled by a power of two so that its row's largest
-// element lies in (224, 448], is exact but for what is 2^-22 of that element; a weight of the values is off by a relative
-// 2^-8 at most, as a bf16 weight would be.  (Converting the codes to 16 bits instead would cost the CTAs some 4
-// instructions a pair of elements, at 23 elements a cycle and SM more than the loads themselves.)
+// like the cache.  B operands are 8-bit terms in columns of their own.  Queries are two e4m3 terms, x = hi + lo / 16 with hi =
+// e4m3(x), lo = e4m3(16 (x - hi)), 4 + 4 significant bits: a bf16 query (8 bits), scaled by a power of two so that its row's
+// largest element lies in (224, 448], is exact but for what is 2^-22 of that element.  (Converting the codes to 16 bits instead
+// would cost the CTAs some 4 instructions a pair of elements, at 23 elements a cycle and SM more than the loads themselves.)
+//
+// The weights of the values are three e5m2 terms, h + m / 8 + l / 64: within 2^-9 of the weight (a bf16 one would be within 2^-8), or
+// within 2^-33 of the row's largest, which is 2^10 or more.  That range is needed: one token far above thousands of others is
+// ordinary attention, the others count by their sum, and the divisor has all of them.  (Two e4m3 terms, whose floor was 2^-17 of
+// the largest, lost a third of the output of 131,071 tokens 2^-18 below one.)
 //
 // Scores in base 2: x = (S_hi + S_lo / 16) s_k f + log2 s_v for a token of a page with scales s_k, s_v (powers of two) and
 // a row whose query's scale and log2(e) / sqrt(d) are in f; weights of the value codes are w = 2^(x - m), the row's sum adds
 // w / s_v, and at the end O = O^T / sum, lse = (m + log2 sum) ln 2, both exact for whichever m was used.  m is the row's
-// largest x less 3, so that the largest weights are 8 and most lie well inside e4m3's range (2^-9 .. 448; hi + lo / 16
-// resolves 2^-14, 2^-17 of the largest), and is raised lazily: only when some x - m passes 8.75 (weights stay below 448) does
-// the group agree on new maxima and rescale its sums and accumulators; a tile is scored twice at most.
+// largest x less 10, so that the largest weights are 2^10 and more, and is raised lazily: only when some x - m passes 15.75
+// (weights stay below e5m2's largest, 57344) does the group agree on new maxima and rescale its sums and accumulators; a tile is
+// scored twice at most.
 //
 // A CTA has a softmax group of 128 threads for up to 32 rows (16 of heads of 64, whose threads have two tokens; thread t owns
 // shared-memory row t of a tile: TMEM lane t), a TMA warp and an MMA warp.  Work: the tiles of all (sequence, key/value head, row
@@ -52,10 +56,11 @@ namespace catq {
 namespace {
 
 constexpr int kGroup = 128;                  // threads of a softmax group
-constexpr float kNominal = 3.0f;             // log2 of a weight at the maximum taken
-constexpr float kOver = 8.75f;               // raise the maximum past this (2^8.75 < 448)
+constexpr float kNominal = 10.0f;            // log2 of a weight at the maximum taken
+constexpr float kOver = 15.75f;              // raise the maximum past this (2^15.75 < 57344)
 constexpr float kNoMax = -3e38f;             // maximum of a row that has seen nothing
-constexpr float kLoUnit = 0.0625f;           // a lo term's unit
+constexpr float kLoUnit = 0.0625f;           // unit of a query's lo term
+constexpr float kUnitM = 0.125f, kUnitL = 0.015625f;  // units of a weight's second and third term
 constexpr int kScaleRing = 16;               // tiles whose scales are kept (see the TMA warp)
 constexpr int kRows = 128;                   // shared-memory rows of a tile of codes, 128 bytes each
 
@@ -69,17 +74,19 @@ struct KvLay {
   // 64, 53 for one long sequence; with it 29, 55 and 51; 4 for the heads of 64: 60, 1 for the drafted tokens: 32).
   static constexpr int kHead = R == 8 ? (HD == 64 ? 1 : 2) : 4;
   static constexpr int kPages = kTok / 16;                           // most pages a tile
-  static constexpr int kCols = 2 * R;                                // N of both products
+  static constexpr int kCols = 2 * R;                                // N of the scores: two terms of the queries
+  static constexpr int kPCols = R == 8 ? 32 : 3 * R;                 // N of the values' product: three terms (of 8 rows: and 8
+                                                                     // columns that nothing reads, N is a multiple of 16)
   static constexpr int kMaxChunk = HD == 128 ? 32 : 16;
   static constexpr int kChunk = R < kMaxChunk ? R : kMaxChunk;       // rows of a softmax group
   static constexpr int kGroups = R / kChunk;
   static constexpr int kSoft = kGroups * kGroup;
   static constexpr int kTmaWarp = 4 * kGroups, kMmaWarp = kTmaWarp + 1, kThreads = kSoft + 64;
   static constexpr uint32_t kColO = 2 * kTpr * kCols;                // two buffers of scores, then the accumulators
-  static constexpr uint32_t kTmem = kColO + kCols <= 64 ? 64 : kColO + kCols <= 128 ? 128 : kColO + kCols <= 256 ? 256 : 512;
+  static constexpr uint32_t kTmem = kColO + kPCols <= 64 ? 64 : kColO + kPCols <= 128 ? 128 : kColO + kPCols <= 256 ? 256 : 512;
   static constexpr int kCtas = kTmem <= 256 ? 2 : 1;                 // CTAs an SM
   static constexpr uint32_t kTile = kRows * 128;                     // a tile of codes
-  static constexpr uint32_t kQ = kCols * HD, kP = kTok * kCols;
+  static constexpr uint32_t kQ = kCols * HD, kP = kTok * kPCols;
   // barriers, tensor-memory address, start of the run | scales of the tiles in flight | per row: query factor, maximum,
   // its last raise, last position, output offset (8 bytes), sums by warp | Q, P twice, ring
   static constexpr uint32_t kOffScale = 640, kOffF = kOffScale + kScaleRing * 8 * kPages, kOffM = kOffF + 4 * R,
@@ -211,6 +218,35 @@ __device__ __forceinline__ void split2(float x0, float x1, uint16_t& hi, uint16_
   asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(lo) : "r"(*reinterpret_cast<const uint32_t*>(&rest)));
 }
 
+// Four weights, rounded to fp16, as words of three e5m2 terms, h + m / 8 + l / 64 (SCALED) or h + m + l.  e5m2 is fp16's upper byte:
+// a term is a mask, after half a step's addition where it is rounded, and what it leaves is exact in fp16.  Weights up to 2^15.75,
+// where no term passes e5m2's largest: within 2^-9 of the weight, or 2^-23 (SCALED), 2^-17.  h is rounded so that m and l have
+// either sign: added to one accumulator, which cuts off what is below its last bit, they would lose part of a one-sided sum
+// (h cut off too, 2^19 tokens of equal weight: the output 0.4 % too small instead of 0.08 %).  m is cut off, an instruction a
+// pair less.
+template <bool SCALED>
+__device__ __forceinline__ void split3(const float* x, uint32_t& h, uint32_t& m, uint32_t& l) {
+  uint32_t a[2], b[2], c[2];
+  const auto rest = [](uint32_t v, uint32_t term, float unit) {
+    term &= 0xff00ff00u;
+    __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&term));
+    if (SCALED) r = __hmul2(r, __float2half2_rn(unit));
+    return *reinterpret_cast<const uint32_t*>(&r);
+  };
+  constexpr uint32_t kHalfStep = 0x00800080u;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t w;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(x[2 * i + 1]), "f"(x[2 * i]));
+    a[i] = w + kHalfStep;
+    b[i] = rest(w, a[i], 1.0f / kUnitM);
+    c[i] = rest(b[i], b[i], kUnitM / kUnitL) + kHalfStep;
+  }
+  h = __byte_perm(a[0], a[1], 0x7531);
+  m = __byte_perm(b[0], b[1], 0x7531);
+  l = __byte_perm(c[0], c[1], 0x7531);
+}
+
 // Eight values as eight bytes of either term.
 __device__ __forceinline__ void split8(const float* x, uint2& hi, uint2& lo) {
   uint16_t h[4], l[4];
@@ -234,9 +270,11 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint32_t a_lo, uint32_t
       : "memory");
 }
 
-// Instruction descriptor of kind::f8f6f4: e4m3 A and B, fp32 D.
-__host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t M, uint32_t N, bool a_mn, bool b_mn) {
-  return (1u << 4) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);
+// Instruction descriptor of kind::f8f6f4: A and B e4m3 or, if said, e5m2, fp32 D.
+__host__ __device__ constexpr uint32_t idesc_f8(uint32_t M, uint32_t N, bool a_mn, bool b_mn, bool a_e5m2 = false,
+                                                bool b_e5m2 = false) {
+  return (1u << 4) | ((a_e5m2 ? 1u : 0u) << 7) | ((b_e5m2 ? 1u : 0u) << 10) | ((a_mn ? 1u : 0u) << 15) |
+         ((b_mn ? 1u : 0u) << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);
 }
 
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -269,18 +307,43 @@ __device__ __forceinline__ void load_rows(uint32_t base, float2 (&t)[N / 2]) {
     t[i] = fma2(make_float2(__uint_as_float(v[N + 2 * i]), __uint_as_float(v[N + 2 * i + 1])), both(kLoUnit),
                 make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])));
 }
-// Eight columns at `base` times f.
-__device__ __forceinline__ void scale_cols8(uint32_t base, const float2 (&f)[4]) {
-  uint32_t v[8];
-  tmem_ld8(base, v);
+// N rows' sums (8 where R is, else 16) from their three terms' accumulators, R columns apart, by pairs.
+template <int R, int N>
+__device__ __forceinline__ void load_sums(uint32_t base, float2 (&t)[N / 2]) {
+  uint32_t v[3 * N];
+  if constexpr (N == R && N == 8) {
+    tmem_ld16(base, *reinterpret_cast<uint32_t(*)[16]>(&v[0]));
+    tmem_ld8(base + 16, *reinterpret_cast<uint32_t(*)[8]>(&v[16]));
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k) tmem_ld16(base + k * R, *reinterpret_cast<uint32_t(*)[16]>(&v[k * N]));
+  }
   tmem_ld_wait();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 w = mul2(make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), f[i]);
-    v[2 * i] = __float_as_uint(w.x);
-    v[2 * i + 1] = __float_as_uint(w.y);
+  for (int i = 0; i < N / 2; ++i) {
+    const auto term = [&](int k) {
+      return make_float2(__uint_as_float(v[k * N + 2 * i]), __uint_as_float(v[k * N + 2 * i + 1]));
+    };
+    t[i] = fma2(term(2), both(kUnitL), fma2(term(1), both(kUnitM), term(0)));
   }
-  tmem_st8(base, v);
+}
+// Eight columns at `base`, and those `step` behind them N times, times f.
+template <int N>
+__device__ __forceinline__ void scale_cols8(uint32_t base, int step, const float2 (&f)[4]) {
+  uint32_t v[N][8];
+#pragma unroll
+  for (int k = 0; k < N; ++k) tmem_ld8(base + k * step, v[k]);
+  tmem_ld_wait();
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 w = mul2(make_float2(__uint_as_float(v[k][2 * i]), __uint_as_float(v[k][2 * i + 1])), f[i]);
+      v[k][2 * i] = __float_as_uint(w.x);
+      v[k][2 * i + 1] = __float_as_uint(w.y);
+    }
+    tmem_st8(base + k * step, v[k]);
+  }
 }
 
 __device__ __forceinline__ void bar_sync(int id, int threads) {
@@ -501,7 +564,7 @@ template <int HD, int R>
 __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
     kv_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const KvTcArgs p) {
   using Y = KvLay<HD, R>;
-  constexpr int NC = Y::kCols, CH = Y::kChunk, NS = Y::kSlots, kThreads = Y::kThreads, kSoft = Y::kSoft,
+  constexpr int NC = Y::kCols, PC = Y::kPCols, CH = Y::kChunk, NS = Y::kSlots, kThreads = Y::kThreads, kSoft = Y::kSoft,
                 kTok = Y::kTok, TPR = Y::kTpr;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -562,7 +625,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
   if (warp == Y::kTmaWarp) {
     copy_tiles<Y>(tmk, tmv, p, w, base, scales);
   } else if (warp == Y::kMmaWarp) {
-    constexpr uint32_t idesc_s = idesc_e4m3(kRows, NC, false, false), idesc_o = idesc_e4m3(HD, NC, true, true);
+    constexpr uint32_t idesc_s = idesc_f8(kRows, NC, false, false), idesc_o = idesc_f8(HD, PC, true, true, false, true);
     constexpr uint32_t kHi = desc_hi(1024, 2);  // code tiles: 8 swizzled rows of 128 bytes from one group to the next
     constexpr uint32_t kHiQ = desc_hi(128, 0), kHiP = desc_hi(16 * kRows, 0);
     const bool issuer = elect_one();
@@ -604,7 +667,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
                          bd = desc_lo(base + Y::kOffP + buf * Y::kP, 128);
 #pragma unroll
           for (int k = 0; k < 4 * TPR; ++k)  // 32 rows, one token of each at a time
-            umma_f8(tmem + kColO, ad + 256 * (k % 4) + 4 * (k / 4), kHi, bd + 32 * (k % 4) + 8 * NC * (k / 4), kHiP, idesc_o,
+            umma_f8(tmem + kColO, ad + 256 * (k % 4) + 4 * (k / 4), kHi, bd + 32 * (k % 4) + 8 * PC * (k / 4), kHiP, idesc_o,
                     (j > 0 || k > 0) ? 1u : 0u);
           umma_commit<1>(pv_done0 + 8u * buf);
           umma_commit<1>(empty0 + 8u * slot);
@@ -817,10 +880,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
               l[c + 2 * i] *= f[i].x;
               l[c + 2 * i + 1] *= f[i].y;
             }
-            if (j > 0) {
-              scale_cols8(lanes + kColO + c, f);
-              scale_cols8(lanes + kColO + R + c, f);
-            }
+            if (j > 0) scale_cols8<3>(lanes + kColO + c, R, f);
           }
           tmem_st_wait();
           score(row_m);
@@ -837,20 +897,23 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
             l[i + 1] = v.y;
           }
           // MN-major without swizzle: 16 columns of a token, the next rows' tokens; then the next 16 columns
-          uint8_t* const at = gbase + Y::kOffP + buf * Y::kP + e * (kRows * NC) + tid * 16;
+          uint8_t* const at = gbase + Y::kOffP + buf * Y::kP + e * (kRows * PC) + tid * 16;
           if constexpr (CH < 16) {
-            uint2 hi, lo;
-            split8(z, hi, lo);
-            *reinterpret_cast<uint4*>(at) = make_uint4(hi.x, hi.y, lo.x, lo.y);
+            uint32_t h[2], m[2], l3[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) split3<true>(z + 4 * i, h[i], m[i], l3[i]);
+            *reinterpret_cast<uint4*>(at) = make_uint4(h[0], h[1], m[0], m[1]);
+            *reinterpret_cast<uint2*>(at + 16 * kRows) = make_uint2(l3[0], l3[1]);
           } else {
 #pragma unroll
             for (int c = 0; c < CH; c += 16) {
-              uint2 hi[2], lo[2];
-              split8(z + c, hi[0], lo[0]);
-              split8(z + c + 8, hi[1], lo[1]);
-              const int k = (r0 + c) / 16;
-              *reinterpret_cast<uint4*>(at + k * (16 * kRows)) = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y);
-              *reinterpret_cast<uint4*>(at + (R / 16 + k) * (16 * kRows)) = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y);
+              uint32_t t[3][4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) split3<true>(z + c + 4 * i, t[0][i], t[1][i], t[2][i]);
+#pragma unroll
+              for (int k = 0; k < 3; ++k)
+                *reinterpret_cast<uint4*>(at + ((r0 + c) / 16 + k * (R / 16)) * (16 * kRows)) =
+                    make_uint4(t[k][0], t[k][1], t[k][2], t[k][3]);
             }
           }
         }
@@ -888,7 +951,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
 #pragma unroll
         for (int c = 0; c < CH; c += kCols) {
           float2 o[kCols / 2];
-          load_rows<R, kCols>(lanes + kColO + c, o);
+          load_sums<R, kCols>(lanes + kColO + c, o);
           if (!ok || (HD == 64 && lane >= 16)) continue;
 #pragma unroll
           for (int i = 0; i < kCols; ++i) {
@@ -921,7 +984,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
       if (*merge_flag) {
         auto part_of = [&](int32_t c) { return p.parts + (2 * static_cast<int64_t>(c) + (c == c0 ? 1 : 0)) * Y::kPartFloats; };
         // the rows' maxima and sums over all parts: the threads of a row share them
-        constexpr int kPer = kSoft / R;  // 8 or 16
+        constexpr int kPer = kSoft / R;  // 4 to 16
         const int mr = threadIdx.x / kPer, mi = threadIdx.x % kPer;
         float m = kNoMax, sum = 0.0f;
         for (int32_t c = c0 + mi; c <= c1; c += kPer) {
@@ -1009,19 +1072,20 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
 
 // ---------------------------------------------------------------- many rows a key/value head
 // Row tiles of 128 rows (heads of 128): the rows are the M of both products, a thread pair's each,
-//   S [128 rows, 128 tokens] = (Q_hi + Q_lo) K^T,      O [128 rows, 128] += (P_hi + P_lo) V,
+//   S [128 rows, 128 tokens] = (Q_hi + Q_lo) K^T,      O [128 rows, 128] += (P_h + P_m + P_l) V,
 // with queries and weights in tensor memory and the codes as B operands, K as it lies, V MN-major.  Against the other
-// kernel's products, whose operands both come from shared memory (1,300 cycles for a tile of 128 tokens and 64 rows), a tile
-// of 128 rows takes 1,024.  hi and lo add into one accumulator, so lo has hi's unit: x = hi + lo with lo = e4m3(x - hi), 4 + 4
-// significant bits down to lo's least step, 2^-9: of a query whose largest element lies in (224, 448] all but 2^-19 of that;
-// of weights 2^-10 at most, which is 2^-17 of the largest where that is 2^kNominalRows.
+// kernel's products, whose operands both come from shared memory (1,300 cycles for a tile of 128 tokens and 64 rows with
+// two terms of both), the products of a tile of 128 rows take 1,280.  All terms add into one accumulator, so they have one unit: a
+// query is hi + lo with lo = e4m3(x - hi), 4 + 4 significant bits down to lo's least step, 2^-9, exact but for 2^-19 of its row's
+// largest element, which lies in (224, 448]; a weight is three e5m2 numbers, within 2^-9 of it from 2^-8 on and within e5m2's half
+// step, 2^-17, below: 2^-31 of the row's largest, which is 2^kNominalRows or more.
 // Thread (row, quarter c) has the row's tokens 32 c .. 32 c + 31 of a tile.  The four agree on the row's maximum through
 // shared memory; raising it is lazy, as there, row by row.
 // Two prompts' chunks of 1023 tokens on 6001 and 8191 (32 / 8 heads of 128, 213 GFLOP) take 257 us, 0.8 PFLOP/s, bound by
 // the softmax: without its arithmetic 167, the products' time (two terms of the queries and of the weights are twice the
 // multiply-adds).  Two threads a row: 284; the accumulators raised before the weights are made, and only those of the rows
 // that have to be: 266; rows read and written by their own lanes: 261.  The other kernel with tiles of 64 rows took 386.
-constexpr float kNominalRows = 7.0f;
+constexpr float kNominalRows = 14.0f;
 struct KvMany {
   static constexpr int kHd = 128, kR = 128, kTpr = 1, kTok = kRows, kHead = 4, kPages = kTok / 16;
   static constexpr int kShare = 4;  // threads a row
@@ -1132,7 +1196,7 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
   if (warp == Y::kTmaWarp) {
     copy_tiles<Y>(tmk, tmv, p, w, base, scales);
   } else if (warp == Y::kMmaWarp) {
-    constexpr uint32_t idesc_s = idesc_e4m3(R, kTok, false, false), idesc_o = idesc_e4m3(R, HD, false, true);
+    constexpr uint32_t idesc_s = idesc_f8(R, kTok, false, false), idesc_o = idesc_f8(R, HD, false, true, true);
     constexpr uint32_t kHi = desc_hi(1024, 2);
     const bool issuer = elect_one();
     int slot = 0;
@@ -1170,7 +1234,7 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
         if (issuer) {
           const uint32_t bd = desc_lo(base + Y::kOffRing + slot * Y::kTile, 16);
 #pragma unroll
-          for (int k = 0; k < 8; ++k)  // 32 tokens at a time, whose words lie over their scores: 8 columns hi, 8 lo
+          for (int k = 0; k < 12; ++k)  // 32 tokens at a time, whose words lie over their scores: 8 columns a term
             umma_f8_ts(tmem + Y::kColO, tmem + 128 * buf + 32 * (k % 4) + 8 * (k / 4), bd + 256 * (k % 4), kHi, idesc_o,
                        (j > 0 || k > 0) ? 1u : 0u);
           umma_commit<1>(pv_done0 + 8u * buf);
@@ -1327,7 +1391,7 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
           m = to;
           l *= fac;
         }
-        uint32_t hi[W / 4], lo[W / 4];
+        uint32_t t[3][W / 4];
 #pragma unroll
         for (int i = 0; i < W; i += 16) {
           float2 sum = both(0.0f);
@@ -1340,16 +1404,16 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
           }
           l = fmaf(sum.x + sum.y, inv[i / 16], l);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) split4(x + i + 4 * e, hi[i / 4 + e], lo[i / 4 + e]);
+          for (int e = 0; e < 4; ++e) split3<false>(x + i + 4 * e, t[0][i / 4 + e], t[1][i / 4 + e], t[2][i / 4 + e]);
         }
-        tmem_st8(sbuf, hi);
-        tmem_st8(sbuf + 8, lo);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) tmem_st8(sbuf + 8 * k, t[k]);
         if (any && j > 0) {  // (by now the product before has mostly completed)
           ok = wait_pv(gt - 1) && ok;
           tc_fence_after();
           const float2 f4[4] = {both(fac), both(fac), both(fac), both(fac)};
 #pragma unroll 1
-          for (int i = 0; i < W; i += 8) scale_cols8(lanes + Y::kColO + W * c + i, f4);
+          for (int i = 0; i < W; i += 8) scale_cols8<1>(lanes + Y::kColO + W * c + i, 0, f4);
         }
         tmem_st_wait();
         tc_fence_before();

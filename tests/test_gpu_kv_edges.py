@@ -1,4 +1,5 @@
-"""GPU tests of the decoding calls at the ends of their ranges, against the fp64 oracle: rows of more than 2^31 elements.
+"""GPU tests of the decoding calls at the ends of their ranges, against the fp64 oracle: rows of more than 2^31 elements, launches
+that overlap, sines and cosines by themselves, weights far below a row's largest.
 
 Tolerances, from the arithmetic: a rotation is off by 2^-22 (|a| + |b|) (sine and cosine within 2^-22.5, two products and a
 sum in fp32) and half a step of the output's type."""
@@ -6,7 +7,8 @@ import numpy as np
 import pytest
 
 from oracle import kv_oracle as K
-from tests.test_gpu_kv import device, i32, rope_bound  # noqa: F401 (device: the fixture)
+from paper_2606_26650_gb300 import synthetic as syn
+from tests.test_gpu_kv import bf16, device, i32, rope_bound  # noqa: F401 (device: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -107,4 +109,88 @@ def test_sine_and_cosine_by_themselves(device, pos):  # noqa: F811
         angle = part.astype(np.longdouble) * (2 * np.pi / np.longdouble(2) ** 64)
         assert np.abs(got[0] - np.cos(angle)).max() <= 2.0 ** -22.5
         assert np.abs(got[1] - np.sin(angle)).max() <= 2.0 ** -22.5
+    assert C.catq_device_status() == 0
+
+
+class LoudAndTail:
+    """A token (at position `loud`) far above n - 1 others, whose scores spread by 0.3 nats; every key/value head holds the
+    same, every query head of a group has its own others.  Values: one constant an element, or (silent) a spread around it and nothing
+    for the loud token.  The loud token's key has only the first element, the others' keys all but that, so that a query's
+    first element alone says how far it is above them."""
+    page = 128
+
+    def __init__(self, r, d, n, new, group, nkv, loud, device):
+        import torch
+        self.n, self.d, self.new, self.group, self.loud, self.device = n, d, new, group, loud, device
+        n_pages = -(-n // self.page)
+        k = r.standard_normal((n_pages * self.page, d))
+        k[:, 0] = 0.0
+        k[loud] = 0.0
+        k[loud, 0] = 16.0
+        v = np.tile(np.linspace(1.0, 1.75, d), (n_pages * self.page, 1))
+        w = v * (1 + 0.25 * r.standard_normal(v.shape).clip(-3, 3))
+        w[loud] = 0.0
+        kc, *vc = (K.e4m3_encode(x) for x in (k, v, w))
+
+        def pages(c):
+            c = torch.from_numpy(c.reshape(n_pages, 1, self.page, d)).to(device)
+            return c.expand(-1, nkv, -1, -1).contiguous().view(torch.float8_e4m3fn)
+
+        self.keys, self.values = pages(kc), [pages(c) for c in vc]
+        self.ones = torch.ones(n_pages, nkv, device=device)
+        self.q = syn.round_bf16((0.3 * r.standard_normal((new, group, d))).astype(np.float32)).astype(np.float64)
+        rows = new * group
+        last = n - new + np.arange(new).repeat(group)
+        x = self.q.reshape(rows, d) @ K.E4M3[kc[:n]].T / np.sqrt(d)
+        x[np.arange(n)[None] > last[:, None]] = -np.inf
+        x[:, loud] = -np.inf
+        e = np.exp(x)
+        self.others = e.sum(axis=1).reshape(new, group)
+        self.sums = [(e @ K.E4M3[c[:n]]).reshape(new, group, d) for c in vc]
+        self.loud_value = [K.E4M3[c[loud]] for c in vc]
+
+    def case(self, gap, silent):
+        """Queries whose loud token weighs about 2^gap of another; output and log-sum-exp in fp64."""
+        q0 = syn.round_bf16(np.float32([gap * np.log(2) * np.sqrt(self.d) / 16.0]))[0]
+        q = self.q.copy()
+        q[..., 0] = q0
+        top = np.exp(float(q0) * 16.0 / np.sqrt(self.d))
+        total = self.others + top
+        return q, (self.sums[silent] + top * self.loud_value[silent]) / total[..., None], np.log(total)
+
+    def cache(self, B, silent):
+        from paper_2606_26650_gb300 import catq as C
+        table = np.tile(np.arange(self.keys.shape[0], dtype=np.int32), (B, 1))
+        return C.KVCache(self.keys, self.values[silent], self.ones, self.ones, i32(table, self.device))
+
+
+@pytest.mark.parametrize("d,new,group", [
+    (128, 1, 1), (128, 2, 4), (128, 4, 4), (128, 7, 4), (128, 16, 4), (128, 32, 4), (128, 40, 5),
+    (64, 1, 1), (64, 4, 4), (64, 8, 4), (64, 33, 4)])
+@pytest.mark.parametrize("n,B,nkv,loud", [(8192, 40, 8, 3), (131072, 40, 8, 3), (8192, 2, 2, 5000)])
+def test_the_tail_below_a_loud_token_counts(device, d, new, group, n, B, nkv, loud):  # noqa: F811
+    """One token far above thousands of others, whose weights count by their sum: the output is the constant that all values are, or,
+    where the loud token's value is nothing, what the others give.  A bound that does not grow with the number of tokens: half a
+    step of bf16 (2^-8), weights to 2^-11, what is below their range 2^-31 of the largest (2^-11 of a weight of 2^-20; of a
+    constant's 131,072 terms 2^-14), scores, exponentials and sums 2^-14: 2^-8 + 2^-9 of the output, all of whose terms have one sign.
+    With 40 sequences on the same pages whole rows fall to one CTA; few sequences are cut, long ones in pieces."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    t = LoudAndTail(syn.rng(23, f"tail/{d}/{new}/{group}/{n}"), d, n, new, group, nkv, loud, device)
+    row_start, seq_len = i32(np.arange(B + 1) * new, device), i32([n] * B, device)
+    for silent, gaps in ((0, (14, 16.4, 17.3, 18, 20, 22, 24)), (1, (12, 16, 18, 20))):
+        cache = t.cache(B, silent)
+        ws = C.kv_attention_workspace(cache, nkv * group)
+        for gap in gaps:
+            q, want, want_lse = t.case(gap, silent)
+            Q = bf16(np.tile(q[:, None], (B, nkv, 1, 1)).reshape(B * new, nkv * group * d), device)
+            O = torch.empty_like(Q)
+            lse = torch.empty(B * new, nkv * group, device=device)
+            C.catq_kv_attention(cache, row_start, seq_len, Q, O, nkv * group, ws, lse)
+            got = O.float().cpu().numpy().reshape(B, new, nkv, group, d)
+            off = np.abs(got / want[None, :, None] - 1).max()
+            assert off <= 2.0 ** -8 + 2.0 ** -9, (gap, silent, f"2^{np.log2(off):.2f}")
+            off = np.abs(lse.cpu().numpy().reshape(B, new, nkv, group) - want_lse[None, :, None]).max()
+            assert off <= 2.0 ** -16 * (1 + want_lse.max())
     assert C.catq_device_status() == 0

@@ -24,3 +24,31 @@ def test_kernels_launched_beside_the_launch_ahead_load_coherently():
         code = re.sub(r"//[^\n]*", "", source(name))
         for load in ("__ldg(", "ldg_hint(", "ld.global.nc"):
             assert load not in code, f"{name}: {load}"
+
+
+def test_three_terms_of_a_weight():
+    """The attention's weights as three e5m2 terms, restated: every fp16 number up to 2^15.75 within 2^-9 of itself (with its own
+    rounding from fp32, 2^-11), or half of the last term's least step, and none of the terms behind the first leans to a side."""
+    import numpy as np
+    code = source("kv_attn_tc.cu")
+    units = [float(x) for x in re.search(r"kUnitM = ([0-9.]+)f, kUnitL = ([0-9.]+)f", code).groups()]
+    x = np.arange(0x7C00, dtype=np.uint16).view(np.float16)
+    exact = x.astype(float)
+    x, exact = x[exact <= 2.0 ** 15.75], exact[exact <= 2.0 ** 15.75]
+
+    def cut(v):
+        return (v.view(np.uint16) & 0xFF00).view(np.float16)
+
+    def rounded(v):
+        return cut((v.view(np.uint16) + np.uint16(0x80)).view(np.float16))
+
+    for (um, ul), floor in ((units, 2.0 ** -23), ((1.0, 1.0), 2.0 ** -17)):
+        h = rounded(x)
+        b = (x - h) * np.float16(1 / um)
+        c = (b - cut(b)) * np.float16(um / ul)
+        terms = [t.astype(float) * u for t, u in zip((h, cut(b), rounded(c)), (1.0, um, ul))]
+        assert all(np.isfinite(t).all() for t in terms)
+        assert (np.abs(sum(terms) - exact) <= np.maximum((2.0 ** -9 - 2.0 ** -11) * exact, floor)).all()
+        big = exact > 2.0 ** -6
+        for t in terms[1:]:
+            assert abs((t[big] / exact[big]).mean()) <= 2.0 ** -9
