@@ -689,7 +689,7 @@ size_t catq_kv_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, in
  *   O[r, h] = softmax(Q[r, h] K^T / sqrt(d)) V   over the sequence's tokens at positions up to the row's own.
  * Q, O [T rows of n_heads d] bf16, ldq and ldo elements apart, rows 16-byte aligned; O may be Q with ldo == ldq.
  * lse [T, n_heads] fp32 (nullable): the natural log-sum-exp of the scaled scores.  Queries enter the
- * products as two e4m3 terms, exactly but for 2^-19 of their row's largest element, the weights of the values (with the scale
+ * products as two e4m3 terms, exactly but for 2^-19 of their row's largest element (of 2^-118 in rows below that), the weights of the values (with the scale
  * of their page) as three e5m2 terms, within 2^-9 of themselves (bf16 ones would be within 2^-8) or within 2^-31 of the row's largest;
  * scores, softmax and sums are fp32.  The same call gives
  * the same bits on a given device; how a sequence's tokens are shared out depends on all lengths, so a row may round

@@ -59,6 +59,7 @@ constexpr int kGroup = 128;                  // threads of a softmax group
 constexpr float kNominal = 10.0f;            // log2 of a weight at the maximum taken
 constexpr float kOver = 15.75f;              // raise the maximum past this (2^15.75 < 57344)
 constexpr float kNoMax = -3e38f;             // maximum of a row that has seen nothing
+constexpr int kLeastExp = -126;              // of a query row's scale: both powers of two, 2^-126 and 2^126, are normal numbers
 constexpr float kLoUnit = 0.0625f;           // unit of a query's lo term
 constexpr float kUnitM = 0.125f, kUnitL = 0.015625f;  // units of a weight's second and third term
 constexpr int kScaleRing = 16;               // tiles whose scales are kept (see the TMA warp)
@@ -741,7 +742,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
 #pragma unroll
           for (int o = 1; o < kPerRow; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
           // 2^-e brings the largest element into (224, 448]; a row that is not finite has NaN as its factor
-          const int e = max(static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), -100);
+          const int e = max(static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), kLeastExp);
           const bool bad = top >= 0x7f800000u;
           const float by = bad ? 0.0f : __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
 #pragma unroll
@@ -1302,7 +1303,7 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
           return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));  // (as integers: NaN is the largest)
         }));
         // 2^-e brings the largest element into (224, 448]; a row that is not finite has NaN as its factor
-        const int e = max(static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), -100);
+        const int e = max(static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), kLeastExp);
         const bool bad = top >= 0x7f800000u;
         const float by = bad ? 0.0f : __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
         f = bad ? __uint_as_float(0x7fffffffu) : __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * p.a.scale_log2;

@@ -1,5 +1,5 @@
 """GPU tests of the decoding calls at the ends of their ranges, against the fp64 oracle: rows of more than 2^31 elements, launches
-that overlap, sines and cosines by themselves, weights far below a row's largest.
+that overlap, sines and cosines by themselves, weights far below a row's largest, tiny queries.
 
 Tolerances, from the arithmetic: a rotation is off by 2^-22 (|a| + |b|) (sine and cosine within 2^-22.5, two products and a
 sum in fp32) and half a step of the output's type."""
@@ -8,7 +8,7 @@ import pytest
 
 from oracle import kv_oracle as K
 from paper_2606_26650_gb300 import synthetic as syn
-from tests.test_gpu_kv import bf16, device, i32, rope_bound  # noqa: F401 (device: the fixture)
+from tests.test_gpu_kv import Paged, attend, bf16, check_attention, device, i32, rope_bound, starts  # noqa: F401 (a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -194,3 +194,19 @@ def test_the_tail_below_a_loud_token_counts(device, d, new, group, n, B, nkv, lo
             off = np.abs(lse.cpu().numpy().reshape(B, new, nkv, group) - want_lse[None, :, None]).max()
             assert off <= 2.0 ** -16 * (1 + want_lse.max())
     assert C.catq_device_status() == 0
+
+
+@pytest.mark.parametrize("d,new", [(128, 1), (64, 1), (128, 6), (64, 20), (128, 60)])
+def test_tiny_queries_against_huge_keys(device, d, new):  # noqa: F811
+    """Queries of 2^-117 and keys of 2^118: the scores are ordinary ones."""
+    r = syn.rng(24, f"tiny/{d}/{new}")
+    lens = [new + 150, new]
+
+    def huge(p):
+        p.scale[0] = p.scale[0] * 2.0 ** 119
+
+    paged = Paged(r, lens, 2, 32, d, device, kv=huge)
+    rs = starts([new, new])
+    q = r.standard_normal((rs[-1], 4, d)) * 2.0 ** -118
+    got, lse = attend(paged, rs, lens, q, 4, device)
+    check_attention(paged, rs, np.array(lens), q, 4, got, lse)
