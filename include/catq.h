@@ -688,11 +688,12 @@ size_t catq_kv_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, in
  * normally called just before) and query head h, which uses key/value head h / (n_heads / n_kv_heads):
  *   O[r, h] = softmax(Q[r, h] K^T / sqrt(d)) V   over the sequence's tokens at positions up to the row's own.
  * Q, O [T rows of n_heads d] bf16, ldq and ldo elements apart, rows 16-byte aligned; O may be Q with ldo == ldq.
- * lse [T, n_heads] fp32 (nullable): the natural log-sum-exp of the scaled scores.  Queries enter the
- * products as two e4m3 terms, exactly but for 2^-19 of their row's largest element (of 2^-118 in rows below that), the weights of the values (with the scale
- * of their page) as three e5m2 terms, within 2^-9 of themselves (bf16 ones would be within 2^-8) or within 2^-31 of the row's largest;
- * scores, softmax and sums are fp32.  The same call gives
- * the same bits on a given device; how a sequence's tokens are shared out depends on all lengths, so a row may round
+ * lse [T, n_heads] fp32 (nullable): the natural log-sum-exp of the scaled scores.  Queries enter the products as
+ * two e4m3 terms, exactly but for 2^-19 of their row's largest element (of 2^-118 in rows below that), the weights of the
+ * values, with the scale of their page, as three e5m2 terms, within 2^-9 of themselves (bf16 ones would be within 2^-8) or
+ * within 2^-31 of the row's largest; scores, softmax and sums are fp32.  (Value scales
+ * 2^100 and more below a sequence's largest, 0 counting as 2^-60, may lose their tokens' part of the sums.)  The same call
+ * gives the same bits on a given device; how a sequence's tokens are shared out depends on all lengths, so a row may round
  * differently beside other rows.  A row that sees no token (a negative position) gets 0 and lse -inf; rows outside every
  * sequence are left as they were.  Codes are never NaN (catq_kv_append writes none) in tokens of the sequence; what lies
  * behind its last token may be anything.  Scales are powers of two, 0 or NaN.  Out-of-range offsets and lengths as in

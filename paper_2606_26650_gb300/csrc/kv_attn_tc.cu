@@ -59,6 +59,7 @@ constexpr int kGroup = 128;                  // threads of a softmax group
 constexpr float kNominal = 10.0f;            // log2 of a weight at the maximum taken
 constexpr float kOver = 15.75f;              // raise the maximum past this (2^15.75 < 57344)
 constexpr float kNoMax = -3e38f;             // maximum of a row that has seen nothing
+constexpr uint32_t kLeastScale = (127u - 60u) << 23;  // 2^-60: stands for a scale of 0
 constexpr int kLeastExp = -126;              // of a query row's scale: both powers of two, 2^-126 and 2^126, are normal numbers
 constexpr float kLoUnit = 0.0625f;           // unit of a query's lo term
 constexpr float kUnitM = 0.125f, kUnitL = 0.015625f;  // units of a weight's second and third term
@@ -786,9 +787,9 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
         const float* const at_scale = scales + (gt % kScaleRing) * (2 * Y::kPages) + page_at;
         float ks = at_scale[0];
         uint32_t vb = __float_as_uint(at_scale[Y::kPages]);
-        // log2 and reciprocal of the values' scale; codes under a scale of 0 are zeros, any scale serves them; one that
-        // is not finite makes the scores of the rows that see the token NaN
-        if (vb == 0u) vb = (127u - 20u) << 23;
+        // log2 and reciprocal of the values' scale; codes under a scale of 0 are zeros, any scale serves them, and the least one that
+        // an append writes leaves the row's maximum to the pages that have values; one that is not finite makes the scores of the rows that see the token NaN
+        if (vb == 0u) vb = kLeastScale;
         if (vb >= 0x7f800000u) {
           ks = __uint_as_float(0x7fffffffu);
           vb = 127u << 23;
@@ -1341,7 +1342,7 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
           const int at_page = (W * c + 16 * i) >> page_shift;
           ks[i] = sc[at_page];
           uint32_t vb = __float_as_uint(sc[Y::kPages + at_page]);
-          if (vb == 0u) vb = (127u - 20u) << 23;
+          if (vb == 0u) vb = kLeastScale;
           if (vb >= 0x7f800000u) {
             ks[i] = __uint_as_float(0x7fffffffu);
             vb = 127u << 23;

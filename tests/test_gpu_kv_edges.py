@@ -1,5 +1,6 @@
 """GPU tests of the decoding calls at the ends of their ranges, against the fp64 oracle: rows of more than 2^31 elements, launches
-that overlap, sines and cosines by themselves, weights far below a row's largest, tiny queries.
+that overlap, sines and cosines by themselves, weights far below a row's largest, tiny queries,
+pages of zeros.
 
 Tolerances, from the arithmetic: a rotation is off by 2^-22 (|a| + |b|) (sine and cosine within 2^-22.5, two products and a
 sum in fp32) and half a step of the output's type."""
@@ -208,5 +209,26 @@ def test_tiny_queries_against_huge_keys(device, d, new):  # noqa: F811
     paged = Paged(r, lens, 2, 32, d, device, kv=huge)
     rs = starts([new, new])
     q = r.standard_normal((rs[-1], 4, d)) * 2.0 ** -118
+    got, lse = attend(paged, rs, lens, q, 4, device)
+    check_attention(paged, rs, np.array(lens), q, 4, got, lse)
+
+
+@pytest.mark.parametrize("d,new", [(128, 1), (64, 1), (128, 6), (64, 20), (128, 60)])
+@pytest.mark.parametrize("least", [-60, -20, 0, 30])
+def test_pages_of_zeros_beside_values_of_any_size(device, d, new, least):  # noqa: F811
+    """Pages whose values are all 0 (their scale is 0) beside pages of very small and of large values: their tokens count in the
+    divisor and hide no other."""
+    r = syn.rng(25, f"zeros/{d}/{new}/{least}")
+    lens = [new + 150, new + 300]
+
+    def some(p):
+        p.scale[1] = p.scale[1] * 2.0 ** (least + 9)
+        for b in range(2):
+            for pg in p.table[b][[0, 2]]:
+                p.codes[1][pg], p.scale[1][pg] = 0, 0.0
+
+    paged = Paged(r, lens, 2, 32, d, device, kv=some)
+    rs = starts([new, new])
+    q = r.standard_normal((rs[-1], 4, d)) * 2.0
     got, lse = attend(paged, rs, lens, q, 4, device)
     check_attention(paged, rs, np.array(lens), q, 4, got, lse)
