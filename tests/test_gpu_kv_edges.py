@@ -1,6 +1,6 @@
 """GPU tests of the decoding calls at the ends of their ranges, against the fp64 oracle: rows of more than 2^31 elements, launches
 that overlap, sines and cosines by themselves, weights far below a row's largest, tiny queries,
-pages of zeros.
+pages of zeros, rows before a sequence's first position.
 
 Tolerances, from the arithmetic: a rotation is off by 2^-22 (|a| + |b|) (sine and cosine within 2^-22.5, two products and a
 sum in fp32) and half a step of the output's type."""
@@ -232,3 +232,36 @@ def test_pages_of_zeros_beside_values_of_any_size(device, d, new, least):  # noq
     q = r.standard_normal((rs[-1], 4, d)) * 2.0
     got, lse = attend(paged, rs, lens, q, 4, device)
     check_attention(paged, rs, np.array(lens), q, 4, got, lse)
+
+
+@pytest.mark.parametrize("d,page", [(128, 64), (64, 16)])
+def test_rows_before_the_first_position_are_not_stored(device, d, page):  # noqa: F811
+    """An idle slot of length 0 with a row, a sequence shorter than its rows, and an ordinary one: rows at negative positions
+    leave the cache as it was, and their queries are rotated all the same."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(26, f"negative/{d}/{page}")
+    lens, news, nkv, nh = [0, 2, 40, 0], [1, 5, 3, 2], 2, 4
+    paged = Paged(r, lens, nkv, page, d, device)
+    rs, T = starts(news), sum(news)
+    k, v = (syn.round_bf16(r.standard_normal((T, nkv, d)).astype(np.float32)) for _ in range(2))
+    q = syn.round_bf16(r.standard_normal((T, nh, d)).astype(np.float32))
+    rope = C.Rope.create(d, 10000.0, device)
+    Q = bf16(q.reshape(T, -1), device)
+    C.catq_kv_append(paged.cache, i32(rs, device), i32(lens, device), bf16(k.reshape(T, -1), device),
+                     bf16(v.reshape(T, -1), device), Q=Q, Q_out=Q, n_heads=nh, rope=rope)
+    torch.cuda.synchronize()
+    assert C.catq_device_status() == 0
+    freq, _ = K.frequencies(d, 10000.0)
+    pos = np.concatenate([np.arange(n - m, n) for n, m in zip(lens, news)])
+    want = K.rope(q, pos, freq, False)
+    off = np.abs(Q.float().cpu().numpy().reshape(T, nh, d) - want)
+    assert (off <= rope_bound(q, freq, False, 1.0) + 2.0 ** -8 * np.abs(want)).all()
+    codes, scale = paged.host()
+    K.append(paged.codes[1], paged.scale[1], paged.table, page, rs, lens, v.astype(np.float64))
+    assert np.array_equal(scale[1], paged.scale[1]) and np.array_equal(K.E4M3[codes[1]], K.E4M3[paged.codes[1]])
+    asked = K.append(paged.codes[0], paged.scale[0], paged.table, page, rs, lens, K.rope(k, pos, freq, False))
+    kept = np.isnan(asked)
+    assert np.array_equal(scale[0], paged.scale[0]) and np.array_equal(K.E4M3[codes[0]][kept], K.E4M3[paged.codes[0]][kept])
+    assert kept.sum() == kept.size - 5 * nkv * d  # (2 and 3 tokens are new)
