@@ -110,12 +110,14 @@ __device__ __forceinline__ void rotate_heads(const E* x, E* y, int32_t h0, int32
   }
 }
 
-// Heads a thread takes at once: the longest run (fewest repeated angles) that still gives every SM a full set of
-// threads.  An append with queries (32 / 8 heads of 128), us by runs of 1 / 2 / 4 / 8: 64 tokens 3.5 / 3.4 / 3.4 / 4.3, 1024
-// tokens 9.5 / 7.6 / 6.6 / 7.1, 8192 tokens 62.7 / 49.7 / 41.1 / 40.5.
-int32_t heads_per_thread(int64_t tokens, int32_t nh, int32_t units) {
-  int32_t hpt = 8;
-  while (hpt > 1 && tokens * units * ((nh + hpt - 1) / hpt) < 152 * 2048) hpt /= 2;
+// Heads a thread takes at once: the longest run (fewest repeated angles) that still gives every SM six warps.  us by runs of 1 / 2 /
+// 4 / 8: 32 heads of 128 in bf16, 64 tokens 2.7 / 2.8 / 3.2 / 4.2, 256 3.6 / 3.0 / 3.3 / 4.3, 512 5.2 / 4.1 / 3.4 / 4.4, 2048 13.8 / 9.4 /
+// 7.1 / 6.2, 8192 47.6 / 31.9 / 26.0 / 24.5; 16 heads of 64, 1024 tokens 3.4 / 2.9 / 3.4 / 4.5; an append with queries (32 / 8 heads of 128),
+// 512 tokens 8.7 / 7.1 / 6.7 / 6.7, 4 x 2048 69.8 / 50.6 / 43.9 / 40.3.  fp32, of which only two heads are loaded ahead, in runs of 4 at
+// most: 4096 tokens 29.5 / 24.6 / 24.1 / 22.9, 8192 52.8 / 43.7 / 42.6 / 44.3.
+int32_t heads_per_thread(int64_t tokens, int32_t nh, int32_t units, int32_t most) {
+  int32_t hpt = most;
+  while (hpt > 1 && tokens * units * ((nh + hpt - 1) / hpt) < 152 * 192) hpt /= 2;
   return hpt;
 }
 
@@ -579,7 +581,7 @@ cudaError_t launch_rope_at(const void* x, int64_t ldx, void* y, int64_t ldy, boo
   const bool vec = d % 16 == 0 && rot.rot % 16 == 0 && ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y)) & 15u) == 0 &&
                    ldx * e % 16 == 0 && ldy * e % 16 == 0;
   if (vec) {
-    const int32_t hpt = heads_per_thread(T, nh, d / 16);
+    const int32_t hpt = heads_per_thread(T, nh, d / 16, f32 ? 4 : 8);
     const int32_t part = (d / 16) * ((nh + hpt - 1) / hpt);
     const int grid = grid_for(T * part);
     if (f32)
@@ -601,7 +603,10 @@ cudaError_t launch_kv_append(KvAppendArgs a, cudaStream_t st) {
   if (!launch_wait_ctl(&wc)) return cudaErrorInvalidDevice;
   a.status = wc.status_word;
   const int32_t units = a.cache.d / 16, heads = 2 * a.cache.nkv;
-  const int32_t hpt = a.q ? heads_per_thread(a.T, a.nh, units) : 1, runs = a.q ? (a.nh + hpt - 1) / hpt : 0;
+  // (no longer than a sequence's queries fill a chunk: 512 single tokens of 32 heads 14.5 us by runs of 1, 16.9 of 4)
+  int32_t hpt = a.q ? heads_per_thread(a.T, a.nh, units, 8) : 1;
+  while (hpt > 1 && (a.T + a.B - 1) / a.B * units * ((a.nh + hpt - 1) / hpt) < kThreads) hpt /= 2;
+  const int32_t runs = a.q ? (a.nh + hpt - 1) / hpt : 0;
   // Teams of a warp up to 8 tokens a sequence in the mean, of two above (32 / 8 heads of 128: 64 sequences of 1, 8, 12 and 16
   // tokens take 4.3, 8.0, 13.9 and 15.6 us by one warp, 5.7, 8.4, 10.2 and 12.4 by two; four prompts of 2048 in pages of 16
   // tokens 61.9 and 44.7).
