@@ -617,7 +617,7 @@ cudaError_t launch_kv_append(KvAppendArgs a, cudaStream_t st) {
   const int64_t team = a.T <= 8 * static_cast<int64_t>(a.B) ? 1 : 2, teams = kThreads / 32 / team;
   const int64_t singles = std::min<int64_t>(a.T, a.B), pages = (a.T - singles) / a.cache.page + (a.T > singles ? singles : 0);
   const int64_t kv = std::min<int64_t>((singles * heads + teams - 1) / teams + pages * heads, a.q ? 228 : 304);
-  const int64_t chunks = (a.T * runs * units + kThreads - 1) / kThreads + (a.q && a.T > singles ? singles : 0);
+  const int64_t chunks = a.q ? std::max((a.T * runs * units + kThreads - 1) / kThreads + (a.T > singles ? singles : 0), singles) : 0;
   const int64_t qs = std::min<int64_t>(std::max<int64_t>(chunks / 4, std::min<int64_t>(chunks, 304)), 1 << 20);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(kv + qs));
