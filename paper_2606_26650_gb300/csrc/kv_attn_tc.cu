@@ -31,10 +31,10 @@
 // the result does not depend on which one that is.
 //
 // Bound by the codes' way from HBM where sequences are long: 64 of 300 to 8192 tokens, 32 / 8 heads of 128, one row
-// each, take 91 us for 572 MB, 6.3 TB/s (7 while it streams); a build without the softmax's arithmetic takes as
+// each, take 92 us for 572 MB, 6.2 TB/s (7 while it streams); a build without the softmax's arithmetic takes as
 // long, the rest is the start (lengths, page numbers, first tile: 5 us) and the last runs' join.  One sequence of
-// 131,071 tokens: 50.5 us for 268 MB.  16 sequences of 1000 to 4500 tokens with 25 rows a head: 29 us for 94 MB, 21 without
-// the softmax's arithmetic.  128 sequences of 17 to 2001 tokens, 12 heads of 64: 55 us for 199 MB, 46 without, bound by the
+// 131,071 tokens: 50.3 us for 268 MB.  16 sequences of 1000 to 4500 tokens with 25 rows a head: 30 us for 94 MB, 22 without
+// the softmax's arithmetic.  128 sequences of 17 to 2001 tokens, 12 heads of 64: 54 us for 199 MB, 48 without, bound by the
 // beginnings and ends of 1536 row tiles.
 // Two CTAs an SM: with three (rings of 4 slots) the 64 sequences took 94 us and the long one 54.8, with one (12 slots) 108
 // and 51.5, with two 92.5 and 51.8.
@@ -72,8 +72,8 @@ struct KvLay {
   static constexpr int kR = R;                                       // rows of a row tile
   static constexpr int kTpr = 128 / HD;                              // tokens a shared-memory row
   static constexpr int kTok = kRows * kTpr;                          // cached tokens a tile
-  // What a row tile's beginning and end cost, in tiles (one GB300; no such cost: 32 us for drafted tokens, 66 for heads of
-  // 64, 53 for one long sequence; with it 29, 55 and 51; 4 for the heads of 64: 60, 1 for the drafted tokens: 32).
+  // What a row tile's beginning and end cost, in tiles (one GB300; no such cost: 34 us for drafted tokens, 65 for heads of
+  // 64, 53 for one long sequence; with it 30, 54 and 50; 4 for the heads of 64: 59, 1 for the drafted tokens: 33).
   static constexpr int kHead = R == 8 ? (HD == 64 ? 1 : 2) : 4;
   static constexpr int kPages = kTok / 16;                           // most pages a tile
   static constexpr int kCols = 2 * R;                                // N of the scores: two terms of the queries
@@ -401,8 +401,8 @@ struct KvTcArgs {
 };
 
 // The run of this CTA: every CTA adds up all sequences' tiles, a thread a stretch of them.  A run is at least a row tile of two
-// tiles, or of one where no sequence has more (prompts of 64 and 100 tokens, 32 / 8 heads of 128: 16.8 and 17.1 us with two,
-// 10.3 and 10.7 with one).  scan [warps], longest [warps] and start [4]: shared memory.  Every thread of the CTA comes here,
+// tiles, or of one where no sequence has more (prompts of 64 and 100 tokens, 32 / 8 heads of 128: 15.3 and 15.7 us with two,
+// 9.8 and 10.2 with one).  scan [warps], longest [warps] and start [4]: shared memory.  Every thread of the CTA comes here,
 // and what it wrote before is visible to all afterwards, tensor memory's address too.
 template <class Y>
 __device__ __forceinline__ KvWalk<Y> find_run(const KvTcArgs& p, int64_t* scan, int32_t* longest, int32_t* start, int64_t& run,
@@ -787,8 +787,9 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
         const float* const at_scale = scales + (gt % kScaleRing) * (2 * Y::kPages) + page_at;
         float ks = at_scale[0];
         uint32_t vb = __float_as_uint(at_scale[Y::kPages]);
-        // log2 and reciprocal of the values' scale; codes under a scale of 0 are zeros, any scale serves them, and the least one that
-        // an append writes leaves the row's maximum to the pages that have values; one that is not finite makes the scores of the rows that see the token NaN
+        // log2 and reciprocal of the values' scale; codes under a scale of 0 are zeros, any scale serves them, and the least
+        // that an append writes leaves the row's maximum to the pages that have values; one that is not finite makes the scores
+        // of the rows that see the token NaN
         if (vb == 0u) vb = kLeastScale;
         if (vb >= 0x7f800000u) {
           ks = __uint_as_float(0x7fffffffu);
@@ -1090,10 +1091,11 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
 // step, 2^-17, below: 2^-31 of the row's largest, which is 2^kNominalRows or more.
 // Thread (row, quarter c) has the row's tokens 32 c .. 32 c + 31 of a tile.  The four agree on the row's maximum through
 // shared memory; raising it is lazy, as there, row by row.
-// Two prompts' chunks of 1023 tokens on 6001 and 8191 (32 / 8 heads of 128, 213 GFLOP) take 257 us, 0.8 PFLOP/s, bound by
-// the softmax: without its arithmetic 167, the products' time (two terms of the queries and of the weights are twice the
-// multiply-adds).  Two threads a row: 284; the accumulators raised before the weights are made, and only those of the rows
-// that have to be: 266; rows read and written by their own lanes: 261.  The other kernel with tiles of 64 rows took 386.
+// Two prompts' chunks of 1023 tokens on 6001 and 8191 (32 / 8 heads of 128, 213 GFLOP) take 264 us, 0.8 PFLOP/s, bound by
+// the softmax's arithmetic.  The products by themselves, the softmax's threads only keeping pace, take 188: 1,280 cycles a tile
+// would be 115, the rest is that a tile's scores, its weights and their product follow one another.  In a form with two terms a
+// weight (257 us): two threads a row 284; the accumulators raised before the weights are made, and only those of the rows
+// that have to be, 266; rows read and written by their own lanes 261; the other kernel with tiles of 64 rows 386.
 constexpr float kNominalRows = 14.0f;
 struct KvMany {
   static constexpr int kHd = 128, kR = 128, kTpr = 1, kTok = kRows, kHead = 4, kPages = kTok / 16;
@@ -1617,11 +1619,11 @@ cudaError_t run_kv(void (*kern)(CUtensorMap, CUtensorMap, KvTcArgs), int ctas, c
 }
 
 // Rows of a tile: by what an average sequence has a key/value head (any number is right).  16 sequences of 4096 tokens, 8
-// key/value heads, us with tiles of 8 / 16 / 32 / 128 rows: heads of 128, 4 rows 29.2 / 29.0 / 31.4 / 47.9, 12 rows 33.7 /
-// 29.7 / 33.3 / 49, 24 rows 44.7 / 36.0 / 34.7 / 50, 64 rows 118 / 67 / 47 / 56, 128 rows 189 / 123 / 83 / 67; heads of 64, 4
-// rows 16.9 / 17.8 / 23, 16 rows 24 / 19 / 24, 128 rows 119 / 80 / 73.  The mean is a poor guide to a batch of single tokens
-// with a prompt among them: 128 single tokens on 2048 and a prompt of 512 (32 / 8 heads of 128) take 146 us in one call, 130
-// in two; 32 on 4096 and a prompt of 2048 183 and 150.
+// key/value heads, us with tiles of 8 / 16 / 32 / 128 rows: heads of 128, 4 rows 29.4 / 28.8 / 31.7 / 49.4, 12 rows 33.9 /
+// 29.4 / 33.4 / 50, 24 rows 44.8 / 36.8 / 35.2 / 52, 64 rows 117 / 68 / 51 / 56, 96 rows 144 / 104 / 71 / 61, 128 rows 191 / 125 / 90 /
+// 66; heads of 64, 4 rows 17.5 / 18.7 / 23.9, 16 rows 24.6 / 19.5 / 24.9, 32 rows 38 / 29 / 28, 128 rows 122 / 84 / 79.  The mean is a
+// poor guide to a batch of single tokens with a prompt among them: 128 single tokens on 2048 and a prompt of 512 (32 / 8 heads
+// of 128) take 155 us in one call, 129 in two; 32 on 4096 and a prompt of 2048 171 and 146.
 template <int HD, int R>
 cudaError_t run_few(const KvAttnArgs& a, cudaStream_t st) {
   return run_kv<KvLay<HD, R>>(kv_attn_kernel<HD, R>, KvLay<HD, R>::kCtas, a, st);

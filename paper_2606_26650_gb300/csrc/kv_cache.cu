@@ -110,11 +110,11 @@ __device__ __forceinline__ void rotate_heads(const E* x, E* y, int32_t h0, int32
   }
 }
 
-// Heads a thread takes at once: the longest run (fewest repeated angles) that still gives every SM six warps.  us by runs of 1 / 2 /
-// 4 / 8: 32 heads of 128 in bf16, 64 tokens 2.7 / 2.8 / 3.2 / 4.2, 256 3.6 / 3.0 / 3.3 / 4.3, 512 5.2 / 4.1 / 3.4 / 4.4, 2048 13.8 / 9.4 /
-// 7.1 / 6.2, 8192 47.6 / 31.9 / 26.0 / 24.5; 16 heads of 64, 1024 tokens 3.4 / 2.9 / 3.4 / 4.5; an append with queries (32 / 8 heads of 128),
-// 512 tokens 8.7 / 7.1 / 6.7 / 6.7, 4 x 2048 69.8 / 50.6 / 43.9 / 40.3.  fp32, of which only two heads are loaded ahead, in runs of 4 at
-// most: 4096 tokens 29.5 / 24.6 / 24.1 / 22.9, 8192 52.8 / 43.7 / 42.6 / 44.3.
+// Heads a thread takes at once: the longest run (fewest repeated angles) that still gives every SM six warps.  us by runs
+// of 1 / 2 / 4 / 8: 32 heads of 128 in bf16, 64 tokens 2.7 / 2.8 / 3.2 / 4.2, 256 3.6 / 3.0 / 3.3 / 4.3, 512 5.2 / 4.1 / 3.4 /
+// 4.4, 2048 13.8 / 9.4 / 7.1 / 6.2, 8192 47.6 / 31.9 / 26.0 / 24.5; 16 heads of 64, 1024 tokens 3.4 / 2.9 / 3.4 / 4.5; an append
+// with queries (32 / 8 heads of 128), 512 tokens 8.7 / 7.1 / 6.7 / 6.7, 4 x 2048 69.8 / 50.6 / 43.9 / 40.3.  fp32, of which only two
+// heads are loaded ahead, in runs of 4 at most: 4096 tokens 29.5 / 24.6 / 24.1 / 22.9, 8192 52.8 / 43.7 / 42.6 / 44.3.
 int32_t heads_per_thread(int64_t tokens, int32_t nh, int32_t units, int32_t most) {
   int32_t hpt = most;
   while (hpt > 1 && tokens * units * ((nh + hpt - 1) / hpt) < 152 * 192) hpt /= 2;
@@ -122,9 +122,9 @@ int32_t heads_per_thread(int64_t tokens, int32_t nh, int32_t units, int32_t most
 }
 
 // One thread per (token, unit, run of `hpt` heads); `part` items a token (below 2^31), a CTA's tokens side by side.
-// Bound by HBM: 8192 tokens of 32 heads of 128 in bf16 take 25 us for 134 MB, 5.3 TB/s (a copy of the same bytes 21.6), 4999
-// of 40 heads in fp32 38.5 us, 5.3 TB/s.  Two CTAs an SM with four heads' loads ahead: three with four or two ahead
-// (80 registers) 31 and 26 us, four with two 27, two with eight 30.
+// Bound by HBM: 8192 tokens of 32 heads of 128 in bf16 take 23.6 us for 134 MB, 5.7 TB/s (a copy of the same bytes 21.6), 4999
+// of 40 heads in fp32 39 us, 5.2 TB/s.  Two CTAs an SM with four heads' loads ahead (by runs of four heads 25 us): three with four
+// or two ahead (80 registers) 31 and 26 us, four with two 27, two with eight 30.
 template <typename E>
 __global__ void __launch_bounds__(kThreads, 2) rope_at_vec_kernel(const RopeAtArgs a, int32_t hpt, Divisor by_units,
                                                                      Divisor by_part, int32_t part) {
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kThreads, 2) rope_at_vec_kernel(const RopeAtAr
 }
 
 // Any even rot and d, rows of the type's alignment: one thread per pair, or per element behind the rotated
-// part (the 8192 tokens 97 us; 64 tokens 2.8 against 2.7).
+// part (the 8192 tokens 103 us; 64 tokens 2.8 like the vector kernel).
 template <typename E>
 __global__ void __launch_bounds__(kThreads) rope_at_kernel(const RopeAtArgs a) {
   const int32_t half = a.rot.rot / 2, per = half + (a.d - a.rot.rot);
@@ -220,8 +220,8 @@ __device__ __forceinline__ void latch_index_error(int32_t* status) { atomicCAS(s
 // one or two warps takes one head's keys or values of such a page), pages that get more (a CTA), and the queries in chunks
 // of kThreads units of 16 elements.  Lengths are read on the device and every CTA adds them up, so that a batch of single
 // tokens with a long prompt among them is shared out like any other: 128 single tokens and a prompt of 512 (32 / 8 heads of
-// 128, pages of 64) take 11 us, where a grid over sequences and shares of the mean one's pages took 97 to 135; single
-// tokens alone pay 0.7 us for it (64 sequences: 4.3 against 3.6).
+// 128, pages of 64) take 10 us, where a grid over sequences and shares of the mean one's pages took 97 to 135; single
+// tokens alone pay 0.7 us for it (64 sequences: 4.5).
 // Few tokens are 64 units a warp of the team, so that its lanes hold two.
 struct KvSpan {
   int64_t r0;
@@ -408,8 +408,8 @@ __device__ __forceinline__ void copy16(void* smem, const void* global) {
 
 // CTAs below ctas_kv take keys and values, a run of whole pages and heads each, the next one's elements on their way to
 // shared memory meanwhile (each thread copies what it will read itself), and the angles of a page's tokens kept there
-// from its first head on (without that 45 us for four prompts of 2048, with it 41); the others chunks of the queries.
-// Four prompts of 2048 (32 / 8 heads of 128) move 185 MB in 41 us, 4.5 TB/s, bound by the latency of an item (elements,
+// from its first head on (four us less for four prompts of 2048); the others chunks of the queries.
+// Four prompts of 2048 (32 / 8 heads of 128) move 185 MB in 40 us, 4.6 TB/s, bound by the latency of an item (elements,
 // maximum over the CTA, codes) and the arithmetic beside it; single tokens by a chain of loads: row offsets, page
 // number, scale.  kHeld kThreads units: a page and head at most.
 template <int D, int kTeam, int kHeld>
@@ -608,16 +608,17 @@ cudaError_t launch_kv_append(KvAppendArgs a, cudaStream_t st) {
   while (hpt > 1 && (a.T + a.B - 1) / a.B * units * ((a.nh + hpt - 1) / hpt) < kThreads) hpt /= 2;
   const int32_t runs = a.q ? (a.nh + hpt - 1) / hpt : 0;
   // Teams of a warp up to 8 tokens a sequence in the mean, of two above (32 / 8 heads of 128: 64 sequences of 1, 8, 12 and 16
-  // tokens take 4.3, 8.0, 13.9 and 15.6 us by one warp, 5.7, 8.4, 10.2 and 12.4 by two; four prompts of 2048 in pages of 16
-  // tokens 61.9 and 44.7).
+  // tokens take 4.5, 5.9, 11.0 and 11.1 us by one warp, 5.7, 7.5, 8.5 and 9.2 by two; four prompts of 2048 in pages of 16
+  // tokens 62.7 and 45.9).
   // CTAs for keys and values: as many as there can be work for (a sequence's pages: its rows' and two that it gets a part
-  // of), two an SM at most, with queries three for two SMs (32 heads of each, 4 x 1024 tokens: 59 us with one an SM, 47 with
-  // 228; 32 / 8 heads the same from one an SM on).  The queries' CTAs come behind them, for four chunks each where they are
-  // many (one each: 46 us instead of 41 for four prompts of 2048).  Any number is right.
+  // of), two an SM at most, with queries three for two SMs (32 heads of each, 4 x 1024 tokens: 64 us with one an SM, 45 with
+  // 228, 44 with two; 32 / 8 heads, 4 x 2048 tokens: 38, 40 and 40).  The queries' CTAs come behind them, one a chunk up to 304, then
+  // for up to four chunks each (the prompts take 40 to 42 us from one to eight).  Any number is right.
   const int64_t team = a.T <= 8 * static_cast<int64_t>(a.B) ? 1 : 2, teams = kThreads / 32 / team;
   const int64_t singles = std::min<int64_t>(a.T, a.B), pages = (a.T - singles) / a.cache.page + (a.T > singles ? singles : 0);
   const int64_t kv = std::min<int64_t>((singles * heads + teams - 1) / teams + pages * heads, a.q ? 228 : 304);
-  const int64_t chunks = a.q ? std::max((a.T * runs * units + kThreads - 1) / kThreads + (a.T > singles ? singles : 0), singles) : 0;
+  const int64_t chunks =
+      a.q ? std::max((a.T * runs * units + kThreads - 1) / kThreads + (a.T > singles ? singles : 0), singles) : 0;
   const int64_t qs = std::min<int64_t>(std::max<int64_t>(chunks / 4, std::min<int64_t>(chunks, 304)), 1 << 20);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(kv + qs));

@@ -34,11 +34,11 @@ __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 // cos and sin, times m, of pos * turn for two pairs.  The product wraps modulo 2^64, which is modulo one turn, so that
 // the angle of a far position is as exact as that of a near one (32-bit floats would lose 2^-24 of the whole angle: 0.008
 // rad at 131072).  Its upper 32 bits fall into the nearest half turn, which is a sign of both, and a rest of at most a
-// quarter as x + e: x the upper 24 of its bits in radians, rounded to fp32, e the rounding and the lower 8 bits.  sin x and cos x
-// are their Taylor series up to x^13 and x^14 (remainders x^15 / 15! and x^16 / 16! at pi / 2: 6.7e-10 and 6.6e-11), evaluated for
-// the two pairs at once, sin(x + e) = sin x + e cos x, cos(x + e) = cos x - e sin x.  Over all rests either is off by 2^-22.86 at most,
-// 2^-25.3 in the mean square: what is left is the series' own roundings near pi / 2, where x, of 1.5, is rounded to 2^-24; without e 2^-22.13
-// and 2^-24.85.  Quarter turns would save three terms and cost twice their instructions in exchanging sine and cosine.
+// quarter as x + e: x the upper 24 of its bits in radians, rounded to fp32, e the rounding and the lower 8 bits.  sin x
+// and cos x are their Taylor series up to x^13 and x^14 (remainders x^15 / 15! and x^16 / 16! at pi / 2: 6.7e-10 and 6.6e-11),
+// evaluated for the two pairs at once, sin(x + e) = sin x + e cos x, cos(x + e) = cos x - e sin x.  Over all rests either is
+// off by 2^-22.84 at most, 2^-25.3 in the mean square, by the series' own roundings near pi / 2; without e by 2^-22.09 and
+// 2^-24.85.  Quarter turns would save three terms and cost twice their instructions in exchanging sine and cosine.
 __device__ __forceinline__ uint32_t turn_of(int32_t pos, uint64_t turn) {
   const uint32_t lo = static_cast<uint32_t>(turn), hi = static_cast<uint32_t>(turn >> 32);
   return __umulhi(static_cast<uint32_t>(pos), lo) + static_cast<uint32_t>(pos) * hi - (pos < 0 ? lo : 0u);

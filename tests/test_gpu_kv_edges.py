@@ -172,8 +172,9 @@ class LoudAndTail:
 def test_the_tail_below_a_loud_token_counts(device, d, new, group, n, B, nkv, loud):  # noqa: F811
     """One token far above thousands of others, whose weights count by their sum: the output is the constant that all values are, or,
     where the loud token's value is nothing, what the others give.  A bound that does not grow with the number of tokens: half a
-    step of bf16 (2^-8), weights to 2^-11, what is below their range 2^-31 of the largest (2^-11 of a weight of 2^-20; of a
-    constant's 131,072 terms 2^-14), scores, exponentials and sums 2^-14: 2^-8 + 2^-9 of the output, all of whose terms have one sign.
+    step of bf16 (2^-8); the loud weight is a power of two and exact, the others' errors, 2^-9 at most and of either sign, come to
+    less than 2^-11 over thousands; what is below their range is 2^-31 of the largest (2^-11 of a weight of 2^-20; of a constant's
+    131,072 terms 2^-14); scores, exponentials and sums 2^-12: 2^-8 + 2^-9 of the output, all of whose terms have one sign.
     With 40 sequences on the same pages whole rows fall to one CTA; few sequences are cut, long ones in pieces."""
     import torch
 
