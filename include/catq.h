@@ -709,6 +709,89 @@ catq_status catq_kv_attention(const catq_kv_cache* cache, const int32_t* row_sta
                               const void* Q, int64_t ldq, int64_t T, int32_t n_heads, void* O, int64_t ldo, float* lse,
                               void* workspace, size_t ws_bytes, catq_stream stream);
 
+/* ------------------------------------------------------------------ trees of drafted tokens
+ * Decoding several drafted continuations of a sequence in one pass (this library's addition).  A sequence's new rows
+ * are the nodes of a tree: row 0 is the last token that is certain, every other row a drafted token that follows its
+ * parent.  A step: catq_tree_masks once; in every layer catq_rope_at (the masks' positions) on queries and keys,
+ * catq_kv_append without a rotation and catq_kv_tree_attention; then catq_sample for every row, catq_tree_accept, and
+ * catq_kv_compact for the caches of all layers.  Rows, lengths and errors as for the calls over the cache. */
+
+/* What each row of a tree sees of the rows, and where it stands.  parent [T] int32: the parent's place among the sequence's
+ * rows, less than the row's own; negative: none, the row follows the context (the root, or one of several).  seen [T, words]
+ * int32 words: bit j % 32 of word j / 32 of a row is set for the row itself and its ancestors, 0 for others.  positions [T]
+ * int32 (nullable): seq_len[b] - n + the number of ancestors, n = row_start[b+1] - row_start[b] (as if the row's branch alone
+ * followed the context).  1 <= words <= 8 (else CATQ_ERR_SHAPE).  A parent that is not less than its row counts as
+ * none, latching CATQ_ERR_INDEX; sequences with row offsets outside 0 .. T or decreasing, a negative length, or more than 32
+ * words rows are skipped, latching it.  Device pointers, 4-byte aligned.  0 <= B <= 65535, T < 2^31; T == 0 or B == 0 is a
+ * no-op. */
+catq_status catq_tree_masks(const int32_t* parent, const int32_t* row_start, const int32_t* seq_len, int32_t B, int64_t T,
+                            uint32_t* seen, int32_t words, int32_t* positions, catq_stream stream);
+
+/* catq_kv_attention with what a row sees of its sequence's new tokens given by bits: all tokens before the sequence's new
+ * ones, and of these, which the cache holds at positions seq_len[b] - n + j, the j-th if bit j % 32 of word j / 32 of the row's
+ * `words` words is set (bits at n and behind are ignored; any bits: a row may see later rows, or not itself).  A row that
+ * sees nothing gets 0 and lse -inf.  seen [T, words], 1 <= words <= 8, 4-byte aligned; a sequence with more than 32 words
+ * rows is left as it was, latching CATQ_ERR_INDEX.  All else as catq_kv_attention, the workspace too. */
+catq_status catq_kv_tree_attention(const catq_kv_cache* cache, const int32_t* row_start, const int32_t* seq_len, int32_t B,
+                                   const uint32_t* seen, int32_t words, const void* Q, int64_t ldq, int64_t T,
+                                   int32_t n_heads, void* O, int64_t ldo, float* lse, void* workspace, size_t ws_bytes,
+                                   catq_stream stream);
+
+/* A token for each row of logits [R rows of V, ld >= V elements apart] (dtype CATQ_BF16 or CATQ_F32) from a random number
+ * u [R] that the caller gives, 0 <= u < 1.  With x the row's logits and T its temperature, a token weighs
+ *   w_i = rint(2^40 exp((x_i - max x) / T))      (in units of 2^-40: below 2^-41 of the largest 0)
+ * and the tokens stand in the order of falling x, equal ones by rising index.  Kept is the longest first part of them that
+ *   has at most top_k tokens (top_k <= 0: any number),
+ *   has no token behind the first at which the cumulated weight reaches ceil(top_p S), S the weight of the first top_k
+ *     (top_p >= 1: any; at least one token is kept), and
+ *   has only tokens with w >= max(1, 2^40 min_p) (min_p <= 0: 1; above 1: 1 is taken).
+ * With Z its weight, the token is the first whose cumulated weight exceeds floor(u Z) (at most Z - 1, at least 0).  The products
+ * u Z and top_p S are taken in 64-bit floats, all else is exact: no result depends on an order of additions.
+ * temperature, top_p, min_p [R] fp32, top_k [R] int32, each nullable: 1, 1, 0, 0.  T == 0: the first token (no other filter).
+ * Temperatures from 2^-60 to 2^60; others above 0 count as the nearer of these.
+ * tokens [R] int32.  logprob [R] fp32 (nullable): ln(w / Z), the probability with which the token was drawn; 0 for T == 0.
+ * Logits of -inf are never drawn.  A row with NaN or +inf, without any finite logit, or with a temperature that is negative
+ * or NaN gets token -1 and logprob NaN.  A NaN among the other settings counts as its default (u: as 0).
+ * 1 <= V <= 2^20, R < 2^31, ld >= V (else CATQ_ERR_SHAPE); logits aligned to their type (16-byte aligned rows are faster),
+ * the vectors 4-byte.  R == 0 is a no-op. */
+catq_status catq_sample(const void* logits, int64_t ld, int32_t dtype, int64_t R, int64_t V, const float* temperature,
+                        const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* tokens,
+                        float* logprob, catq_stream stream);
+
+/* The branch of each sequence's tree that agrees with the tokens drawn.  drafted [T] int32: the rows' tokens (row 0's is not
+ * read); sampled [T] int32: the token drawn from each row's logits; parent as in catq_tree_masks.  From row 0 on: of the last
+ * kept row's children, the first (by its place) whose drafted token is the one drawn at the last kept row (and not
+ * negative) is kept, until there is none.
+ *   path [T] int32: the kept rows' places in their order, rising, then -1;
+ *   n_kept [B]: their number (0 without rows);  next [B]: the token drawn at the last of them, which the sequence goes on
+ *   with (-1 without rows);  new_len [B]: seq_len[b] - n + n_kept (may be seq_len itself; catq_kv_compact wants the old one).
+ * Sequences with row offsets outside 0 .. T or decreasing or a negative length count as without rows, latching CATQ_ERR_INDEX.
+ * Device pointers, 4-byte aligned.  0 <= B <= 65535, T < 2^31; B == 0 is a no-op. */
+catq_status catq_tree_accept(const int32_t* drafted, const int32_t* sampled, const int32_t* parent, const int32_t* row_start,
+                             const int32_t* seq_len, int32_t B, int64_t T, int32_t* path, int32_t* n_kept, int32_t* next,
+                             int32_t* new_len, catq_stream stream);
+
+/* Caches of one catq_kv_compact call at most. */
+int32_t catq_kv_compact_max_caches(void);
+
+/* Moves the kept rows' keys and values together behind the context, in n_caches caches (a HOST array, 1 <= n_caches <=
+ * catq_kv_compact_max_caches(), e.g. those of all layers; equal n_pages, n_kv_heads, page, d and max_pages, else
+ * CATQ_ERR_SHAPE): of every sequence and j < n_kept[b], the token at position seq_len[b] - n + path[row_start[b] + j] goes to
+ * position seq_len[b] - n + j.  path [T] and n_kept [B] as catq_tree_accept gives them, row_start and seq_len as they were at the
+ * append; the sequence's length afterwards is seq_len[b] - n + n_kept[b], and what lies behind it in its pages is
+ * unspecified.  For every page and head of keys or values into which a token with path != j goes:
+ *   want  = the least power of two, 2^-60 or more, with max |values that come| <= 448 want   (0 when all are 0)
+ *   scale = max(scale, want);  codes of the page: multiplied by old scale / scale and rounded again (to nearest, ties to
+ *           even; exact but for e4m3's subnormals);  codes that come = e4m3(value / scale), likewise
+ * (inside one page that is a copy).  A scale that is NaN, of this page or of one that a token comes from, makes the page's NaN.
+ * Tokens whose new position is negative are dropped.
+ * Sequences with row offsets outside 0 .. T or decreasing, a length outside 0 .. max_pages page, n_kept outside 0 .. n, or a
+ * path that does not rise strictly below n are left as they were, latching CATQ_ERR_INDEX; so are pages with numbers outside
+ * 0 .. n_pages - 1 (as a source they count as zeros).  No two sequences may have tokens in one page that either moves, and no
+ * two caches of a call may share codes or scales.  Limits as for catq_kv_append.  T == 0 or B == 0 is a no-op. */
+catq_status catq_kv_compact(const catq_kv_cache* caches, int32_t n_caches, const int32_t* row_start, const int32_t* seq_len,
+                            int32_t B, const int32_t* path, const int32_t* n_kept, int64_t T, catq_stream stream);
+
 /* Self-test of the device-side failure detection (no counterpart in the paper): launches
  * one thread that waits, through the library's bounded mbarrier wait, on a barrier nothing
  * arrives on.  After timeout_ns (1 us .. 1 s) the wait gives up, latches CATQ_ERR_TIMEOUT

@@ -149,6 +149,12 @@ def lib() -> ctypes.CDLL:
         "catq_kv_append": (I32, [KP, P, P, I32, P, I64, P, I64, I64, P, I64, P, I64, I32, RP, P]),
         "catq_kv_attention_workspace_bytes": (S, [I32, I32, I32]),
         "catq_kv_attention": (I32, [KP, P, P, I32, P, I64, I64, I32, P, I64, P, P, S, P]),
+        "catq_tree_masks": (I32, [P, P, P, I32, I64, P, I32, P, P]),
+        "catq_kv_tree_attention": (I32, [KP, P, P, I32, P, I32, P, I64, I64, I32, P, I64, P, P, S, P]),
+        "catq_sample": (I32, [P, I64, I32, I64, I64, P, P, P, P, P, P, P, P]),
+        "catq_tree_accept": (I32, [P, P, P, P, P, I32, I64, P, P, P, P, P]),
+        "catq_kv_compact_max_caches": (I32, []),
+        "catq_kv_compact": (I32, [KP, I32, P, P, I32, P, P, I64, P]),
         "catq_grouped_soft_ternary_linear_fwd_loss": (I32, [GP, catq_schedule, P, P, I32, P, I32, P, P, P, P, S, P]),
     }
     for name, (res, args) in sig.items():
@@ -922,3 +928,78 @@ def catq_kv_attention(cache: KVCache, row_start, seq_len, Q, O, n_heads: int, wo
     ws, ws_bytes = _ws(workspace, w)
     _check(lib().catq_kv_attention(cache._struct, rs, sl, B, q, ldq, T, n_heads, o, ldo,
                                    _f32(lse, "lse", 4 * T * n_heads, w), ws, ws_bytes, _stream(stream)), w)
+
+
+# ------------------------------------------------------------------ trees of drafted tokens
+# int32 vectors on the GPU: row_start [B + 1], seq_len [B], and one entry a row [T] (parents, tokens, paths).
+
+def catq_tree_masks(parent, row_start, seq_len, seen, positions=None, stream=None):
+    """seen [T, words] (int32 bits, words = ceil(largest tree / 32)) and positions [T] of the trees' rows from their
+    parents [T] (places among the sequence's rows, -1 for a root)."""
+    w, T = "catq_tree_masks", parent.shape[0]
+    B = seq_len.shape[0]
+    if seen.dim() != 2 or seen.shape[0] != T:
+        raise ValueError(f"{w}: seen has shape {tuple(seen.shape)}, the call needs [{T}, words]")
+    words = seen.shape[1]
+    _check(lib().catq_tree_masks(_i32(parent, "parent", T, w), _i32(row_start, "row_start", B + 1, w),
+                                 _i32(seq_len, "seq_len", B, w), B, T, _i32(seen, "seen", T * words, w), words,
+                                 None if positions is None else _i32(positions, "positions", T, w), _stream(stream)), w)
+
+
+def catq_kv_tree_attention(cache: KVCache, row_start, seq_len, seen, Q, O, n_heads: int, workspace, lse=None, stream=None):
+    """catq_kv_attention whose rows see, of their sequence's new tokens, those of their bits in seen [T, words]."""
+    w = "catq_kv_tree_attention"
+    B, T, width = cache.B, Q.shape[0], n_heads * cache.d
+    rs, sl = _i32(row_start, "row_start", B + 1, w), _i32(seq_len, "seq_len", B, w)
+    if seen.dim() != 2 or seen.shape[0] != T:
+        raise ValueError(f"{w}: seen has shape {tuple(seen.shape)}, the call needs [{T}, words]")
+    words = seen.shape[1]
+    bits = _i32(seen, "seen", T * words, w)
+    q, ldq = _bf16_rows(Q, "Q", T, width, w)
+    o, ldo = _bf16_rows(O, "O", T, width, w)
+    ws, ws_bytes = _ws(workspace, w)
+    _check(lib().catq_kv_tree_attention(cache._struct, rs, sl, B, bits, words, q, ldq, T, n_heads, o, ldo,
+                                        _f32(lse, "lse", 4 * T * n_heads, w), ws, ws_bytes, _stream(stream)), w)
+
+
+def catq_sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, stream=None):
+    """tokens [R] int32 drawn from logits [R, V] (bf16 or fp32, rows may lie apart) by the random numbers u [R] (fp32);
+    settings a row: temperature, top_p, min_p [R] fp32, top_k [R] int32; logprob [R] fp32 (optional)."""
+    w = "catq_sample"
+    if logits.dim() != 2:
+        raise ValueError(f"{w}: logits have shape {tuple(logits.shape)}, the call needs [R, V]")
+    R, V = logits.shape
+    x, ld = _rows(logits, "logits", R, V, w)
+    _check(lib().catq_sample(x, ld, _dtype_code(logits), R, V, _f32(temperature, "temperature", 4 * R, w),
+                             None if top_k is None else _i32(top_k, "top_k", R, w), _f32(top_p, "top_p", 4 * R, w),
+                             _f32(min_p, "min_p", 4 * R, w), _f32(u, "u", 4 * R, w), _i32(tokens, "tokens", R, w),
+                             _f32(logprob, "logprob", 4 * R, w), _stream(stream)), w)
+
+
+def catq_tree_accept(drafted, sampled, parent, row_start, seq_len, path, n_kept, next_token, new_len, stream=None):
+    """The branch of each tree that agrees with the tokens drawn: path [T], n_kept, next_token and new_len [B]."""
+    w, T = "catq_tree_accept", parent.shape[0]
+    B = seq_len.shape[0]
+    _check(lib().catq_tree_accept(
+        _i32(drafted, "drafted", T, w), _i32(sampled, "sampled", T, w), _i32(parent, "parent", T, w),
+        _i32(row_start, "row_start", B + 1, w), _i32(seq_len, "seq_len", B, w), B, T, _i32(path, "path", T, w),
+        _i32(n_kept, "n_kept", B, w), _i32(next_token, "next_token", B, w), _i32(new_len, "new_len", B, w),
+        _stream(stream)), w)
+
+
+def catq_kv_compact_max_caches() -> int:
+    return int(lib().catq_kv_compact_max_caches())
+
+
+def catq_kv_compact(caches, row_start, seq_len, path, n_kept, stream=None):
+    """Moves the kept rows' tokens (path [T], n_kept [B] of catq_tree_accept) behind the context in every cache of the
+    list (the layers', of one geometry); row_start and seq_len as at the append."""
+    w, T = "catq_kv_compact", path.shape[0]
+    if not caches:
+        raise ValueError(f"{w}: no caches")
+    B = caches[0].B
+    if any(c.B != B for c in caches):
+        raise ValueError(f"{w}: every cache needs a table of the same sequences ({B})")
+    arr = (catq_kv_cache * len(caches)).from_buffer_copy(b"".join([c._struct for c in caches]))
+    _check(lib().catq_kv_compact(arr, len(caches), _i32(row_start, "row_start", B + 1, w), _i32(seq_len, "seq_len", B, w),
+                                 B, _i32(path, "path", T, w), _i32(n_kept, "n_kept", B, w), T, _stream(stream)), w)

@@ -1109,9 +1109,14 @@ size_t catq_kv_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, in
   return kv_attention_ws_bytes(n_heads, n_kv_heads, d);
 }
 
-catq_status catq_kv_attention(const catq_kv_cache* cache, const int32_t* row_start, const int32_t* seq_len, int32_t B,
-                              const void* Q, int64_t ldq, int64_t T, int32_t n_heads, void* O, int64_t ldo, float* lse,
-                              void* workspace, size_t ws_bytes, catq_stream stream) {
+}  // extern "C"
+
+namespace {
+
+// seen: NULL for rows that see the new tokens up to their own.
+catq_status kv_attention(const catq_kv_cache* cache, const int32_t* row_start, const int32_t* seq_len, int32_t B,
+                         const uint32_t* seen, int32_t words, const void* Q, int64_t ldq, int64_t T, int32_t n_heads, void* O,
+                         int64_t ldo, float* lse, void* workspace, size_t ws_bytes, catq_stream stream) {
   catq_status st = check_kv(cache, row_start, seq_len, B, T);
   if (st != CATQ_OK) return st;
   const int32_t nkv = cache->n_kv_heads, d = cache->d;
@@ -1138,8 +1143,105 @@ catq_status catq_kv_attention(const catq_kv_cache* cache, const int32_t* row_sta
   a.nh = n_heads;
   a.scale_log2 = 1.4426950408889634f / std::sqrt(static_cast<float>(d));
   a.lse = lse;
+  a.seen = seen;
+  a.words = words;
   a.workspace = workspace;
   return cuda_status(launch_kv_attention(a, as_stream(stream)));
+}
+
+bool sequences_ok(int32_t B, int64_t T) { return B >= 0 && B <= 65535 && T >= 0 && T <= 0x7fffffff; }
+
+}  // namespace
+
+extern "C" {
+
+catq_status catq_kv_attention(const catq_kv_cache* cache, const int32_t* row_start, const int32_t* seq_len, int32_t B,
+                              const void* Q, int64_t ldq, int64_t T, int32_t n_heads, void* O, int64_t ldo, float* lse,
+                              void* workspace, size_t ws_bytes, catq_stream stream) {
+  return kv_attention(cache, row_start, seq_len, B, nullptr, 0, Q, ldq, T, n_heads, O, ldo, lse, workspace, ws_bytes, stream);
+}
+
+// ------------------------------------------------------------------ trees of drafted tokens
+
+catq_status catq_tree_masks(const int32_t* parent, const int32_t* row_start, const int32_t* seq_len, int32_t B, int64_t T,
+                            uint32_t* seen, int32_t words, int32_t* positions, catq_stream stream) {
+  if (!sequences_ok(B, T) || words < 1 || words > 8) return CATQ_ERR_SHAPE;
+  if (T == 0 || B == 0) return CATQ_OK;
+  if (!parent || !row_start || !seq_len || !seen) return CATQ_ERR_INVALID_ARG;
+  if (!aligned4(parent) || !aligned4(row_start) || !aligned4(seq_len) || !aligned4(seen) || !aligned4(positions))
+    return CATQ_ERR_ALIGN;
+  return cuda_status(launch_tree_masks(parent, row_start, seq_len, B, T, seen, words, positions, as_stream(stream)));
+}
+
+catq_status catq_kv_tree_attention(const catq_kv_cache* cache, const int32_t* row_start, const int32_t* seq_len, int32_t B,
+                                   const uint32_t* seen, int32_t words, const void* Q, int64_t ldq, int64_t T,
+                                   int32_t n_heads, void* O, int64_t ldo, float* lse, void* workspace, size_t ws_bytes,
+                                   catq_stream stream) {
+  if (words < 1 || words > 8) return CATQ_ERR_SHAPE;
+  if (!seen && T != 0 && B != 0) return CATQ_ERR_INVALID_ARG;
+  if (!aligned4(seen)) return CATQ_ERR_ALIGN;
+  return kv_attention(cache, row_start, seq_len, B, seen, words, Q, ldq, T, n_heads, O, ldo, lse, workspace, ws_bytes, stream);
+}
+
+catq_status catq_sample(const void* logits, int64_t ld, int32_t dtype, int64_t R, int64_t V, const float* temperature,
+                        const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* tokens,
+                        float* logprob, catq_stream stream) {
+  if (dtype != CATQ_BF16 && dtype != CATQ_F32) return CATQ_ERR_DTYPE;
+  if (R < 0 || R > 0x7fffffff || V < 1 || V > (1 << 20) || ld < V) return CATQ_ERR_SHAPE;
+  if (R == 0) return CATQ_OK;
+  if (!logits || !u || !tokens) return CATQ_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(logits) & (dtype == CATQ_F32 ? 3u : 1u)) || !aligned4(temperature) || !aligned4(top_k) ||
+      !aligned4(top_p) || !aligned4(min_p) || !aligned4(u) || !aligned4(tokens) || !aligned4(logprob))
+    return CATQ_ERR_ALIGN;
+  const SampleArgs a{logits, ld, R, static_cast<int32_t>(V), temperature, top_k, top_p, min_p, u, tokens, logprob};
+  return cuda_status(launch_sample(a, dtype == CATQ_F32, as_stream(stream)));
+}
+
+catq_status catq_tree_accept(const int32_t* drafted, const int32_t* sampled, const int32_t* parent, const int32_t* row_start,
+                             const int32_t* seq_len, int32_t B, int64_t T, int32_t* path, int32_t* n_kept, int32_t* next,
+                             int32_t* new_len, catq_stream stream) {
+  if (!sequences_ok(B, T)) return CATQ_ERR_SHAPE;
+  if (B == 0) return CATQ_OK;
+  if (!row_start || !seq_len || !n_kept || !next || !new_len || (T != 0 && (!drafted || !sampled || !parent || !path)))
+    return CATQ_ERR_INVALID_ARG;
+  if (!aligned4(drafted) || !aligned4(sampled) || !aligned4(parent) || !aligned4(row_start) || !aligned4(seq_len) ||
+      !aligned4(path) || !aligned4(n_kept) || !aligned4(next) || !aligned4(new_len))
+    return CATQ_ERR_ALIGN;
+  const TreeAcceptArgs a{drafted, sampled, parent, row_start, seq_len, B, T, path, n_kept, next, new_len, nullptr};
+  return cuda_status(launch_tree_accept(a, as_stream(stream)));
+}
+
+int32_t catq_kv_compact_max_caches(void) { return kCompactCaches; }
+
+catq_status catq_kv_compact(const catq_kv_cache* caches, int32_t n_caches, const int32_t* row_start, const int32_t* seq_len,
+                            int32_t B, const int32_t* path, const int32_t* n_kept, int64_t T, catq_stream stream) {
+  if (!caches || n_caches < 1 || n_caches > kCompactCaches) return CATQ_ERR_INVALID_ARG;
+  KvCompactArgs a{};
+  for (int32_t i = 0; i < n_caches; ++i) {
+    const catq_kv_cache& c = caches[i];
+    const catq_status st = check_kv(&c, row_start, seq_len, B, T);
+    if (st != CATQ_OK) return st;
+    if (c.n_pages != caches->n_pages || c.n_kv_heads != caches->n_kv_heads || c.page != caches->page || c.d != caches->d ||
+        c.max_pages != caches->max_pages)
+      return CATQ_ERR_SHAPE;
+    a.cache[i] = {static_cast<uint8_t*>(c.k_codes), static_cast<uint8_t*>(c.v_codes), c.k_scale, c.v_scale, c.table};
+  }
+  if (T == 0 || B == 0) return CATQ_OK;
+  if (!path || !n_kept) return CATQ_ERR_INVALID_ARG;
+  if (!aligned4(path) || !aligned4(n_kept)) return CATQ_ERR_ALIGN;
+  a.n_caches = n_caches;
+  a.n_pages = caches->n_pages;
+  a.nkv = caches->n_kv_heads;
+  a.page = caches->page;
+  a.d = caches->d;
+  a.max_pages = caches->max_pages;
+  a.row_start = row_start;
+  a.seq_len = seq_len;
+  a.path = path;
+  a.n_kept = n_kept;
+  a.B = B;
+  a.T = T;
+  return cuda_status(launch_kv_compact(a, as_stream(stream)));
 }
 
 }  // extern "C"

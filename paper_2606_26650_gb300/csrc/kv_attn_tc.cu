@@ -64,11 +64,14 @@ constexpr int kLeastExp = -126;              // of a query row's scale: both pow
 constexpr float kLoUnit = 0.0625f;           // unit of a query's lo term
 constexpr float kUnitM = 0.125f, kUnitL = 0.015625f;  // units of a weight's second and third term
 constexpr int kScaleRing = 16;               // tiles whose scales are kept (see the TMA warp)
+constexpr int kSeenWords = 8;                // words of a row's bits, at most
 constexpr int kRows = 128;                   // shared-memory rows of a tile of codes, 128 bytes each
 
-template <int HD, int R>
+// TREE: what a row sees of the new tokens is given by bits (catq_kv_tree_attention), else those up to its own.
+template <int HD, int R, bool TREE>
 struct KvLay {
   static constexpr int kHd = HD;
+  static constexpr bool kTree = TREE;
   static constexpr int kR = R;                                       // rows of a row tile
   static constexpr int kTpr = 128 / HD;                              // tokens a shared-memory row
   static constexpr int kTok = kRows * kTpr;                          // cached tokens a tile
@@ -94,7 +97,8 @@ struct KvLay {
   static constexpr uint32_t kOffScale = 640, kOffF = kOffScale + kScaleRing * 8 * kPages, kOffM = kOffF + 4 * R,
                             kOffFac = kOffM + 4 * R, kOffLim = kOffFac + 4 * R, kOffRow = kOffLim + 4 * R,
                             kOffZero = kOffRow + 8 * R, kOffRed = kOffZero + 4 * R,
-                            kOffQ = (kOffRed + 16 * R + 127) / 128 * 128, kOffP = kOffQ + kQ,
+                            kOffSeen = kOffRed + 16 * R,                // [R][kSeenWords]
+                            kOffQ = (kOffSeen + (TREE ? 4 * R * kSeenWords : 0) + 127) / 128 * 128, kOffP = kOffQ + kQ,
                             kOffRing = (kOffP + 2 * kP + 1023) / 1024 * 1024;
   static constexpr uint32_t kBudget = (kCtas == 2 ? 112 : 224) * 1024;
   static constexpr int kSlots0 = (kBudget - 1024 - kOffRing) / kTile;
@@ -116,15 +120,17 @@ struct KvGeom {
   const int32_t *row_start, *seq_len;
   int32_t B, group, nkv;
   uint32_t group_inv;  // ceil(2^32 / group): rows below 2^26 are divided by one product
+  int32_t most;        // rows of a sequence at most
   int64_t T, max_len;
   __device__ __forceinline__ int32_t token_of(int32_t row) const {
     return group == 1 ? row : static_cast<int32_t>(__umulhi(static_cast<uint32_t>(row), group_inv));
   }
 };
 
-// Tokens that the row tile `q` of a sequence can see.
+// Tokens that the row tile `q` of a sequence can see, counted to the last of them.
 template <class Y>
 __device__ __forceinline__ int32_t visible(const KvGeom& g, const KvSeq& s, int32_t q) {
+  if constexpr (Y::kTree) return s.len;
   return max(s.len - s.n + g.token_of(min((q + 1) * Y::kR, s.n * g.group) - 1) + 1, 0);
 }
 template <class Y>
@@ -143,7 +149,7 @@ __device__ __forceinline__ KvSeq load_seq(const KvGeom& g, int32_t b, int32_t* s
   s.len = g.seq_len[b];
   s.n = r1 - s.r0;
   s.per_head = 0;
-  if (s.r0 < 0 || r1 < s.r0 || r1 > g.T || s.len < 0 || s.len > g.max_len) {
+  if (s.r0 < 0 || r1 < s.r0 || r1 > g.T || s.len < 0 || s.len > g.max_len || (Y::kTree && s.n > g.most)) {
     if (status) atomicCAS(status, 0, 10 /* CATQ_ERR_INDEX */);
     s.n = 0;
     return s;
@@ -562,10 +568,10 @@ __device__ __forceinline__ void copy_tiles(const CUtensorMap& tmk, const CUtenso
   for (int t = max(0, loads - NS); t < loads; ++t) drain(full0 + 8u * (t % NS), (t / NS) & 1);
 }
 
-template <int HD, int R>
-__global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
+template <int HD, int R, bool TREE>
+__global__ void __launch_bounds__(KvLay<HD, R, TREE>::kThreads, KvLay<HD, R, TREE>::kCtas)
     kv_attn_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const KvTcArgs p) {
-  using Y = KvLay<HD, R>;
+  using Y = KvLay<HD, R, TREE>;
   constexpr int NC = Y::kCols, PC = Y::kPCols, CH = Y::kChunk, NS = Y::kSlots, kThreads = Y::kThreads, kSoft = Y::kSoft,
                 kTok = Y::kTok, TPR = Y::kTpr;
   extern __shared__ uint8_t smem_raw[];
@@ -591,6 +597,7 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
   int64_t* const row_at = reinterpret_cast<int64_t*>(gbase + Y::kOffRow);
   float* const row_zero = reinterpret_cast<float*>(gbase + Y::kOffZero);
   float* const red = reinterpret_cast<float*>(gbase + Y::kOffRed);          // [groups][4][CH]
+  uint32_t* const row_seen = reinterpret_cast<uint32_t*>(gbase + Y::kOffSeen);
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < NS; ++i) {
@@ -725,8 +732,16 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
           const int32_t tk = g.token_of(row);
           row_m[r0 + tid] = kNoMax;
           row_zero[r0 + tid] = 0.0f;
-          row_lim[r0 + tid] = r0 + tid < rows ? w.len - w.rows_n + tk : -1;
+          row_lim[r0 + tid] = r0 + tid < rows ? w.len - w.rows_n + tk : -1;  // (TREE: not read)
           row_at[r0 + tid] = (w.r0 + tk) * p.a.ldo + (w.sh * g.group + row - tk * g.group) * HD;
+        }
+        if constexpr (TREE) {
+          for (int k = tid; k < CH * p.a.words; k += kGroup) {
+            const int r = k / p.a.words, row = w.sq * R + r0 + r;
+            uint32_t bits = 0;
+            if (r0 + r < rows) bits = p.a.seen[static_cast<int64_t>(w.r0 + g.token_of(row)) * p.a.words + k - r * p.a.words];
+            row_seen[(r0 + r) * kSeenWords + k - r * p.a.words] = bits;
+          }
         }
 #pragma unroll
         for (int k = 0; k < kPasses; ++k) {
@@ -767,8 +782,8 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
       ahead = w;
       more = ahead.next(g);
       if (kAhead && more) ask(ahead);
-      // tokens that the group's first row sees (the others at least as many)
-      const int32_t sees_all = active ? row_lim[r0] + 1 : 0;
+      // tokens that the group's first row sees (the others at least as many); TREE: the context
+      const int32_t sees_all = !active ? 0 : TREE ? w.len - w.rows_n : row_lim[r0] + 1;
       float l[CH];
 #pragma unroll
       for (int i = 0; i < CH; ++i) l[i] = 0.0f;
@@ -835,11 +850,23 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
             }
           }
           if (masked) {
+            if constexpr (TREE) {
 #pragma unroll
-            for (int i = 0; i < CH; ++i)
+              for (int e = 0; e < TPR; ++e) {
+                const int at = tok + e - (w.len - w.rows_n);  // the token's place among the new ones
+                if (at < 0) continue;
+                const uint32_t bit = tok + e < w.len ? 1u << (at & 31) : 0u;
 #pragma unroll
-              for (int e = 0; e < TPR; ++e)
-                if (tok + e > row_lim[r0 + i]) y[e * CH + i] = -INFINITY;
+                for (int i = 0; i < CH; ++i)
+                  if (!(row_seen[(r0 + i) * kSeenWords + (bit ? at >> 5 : 0)] & bit)) y[e * CH + i] = -INFINITY;
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int e = 0; e < TPR; ++e)
+                  if (tok + e > row_lim[r0 + i]) y[e * CH + i] = -INFINITY;
+            }
           }
         };
         // Scored under the maxima so far (a segment's first tile has none); where they do not serve this tile, without any, for
@@ -1097,7 +1124,9 @@ __global__ void __launch_bounds__(KvLay<HD, R>::kThreads, KvLay<HD, R>::kCtas)
 // weight (257 us): two threads a row 284; the accumulators raised before the weights are made, and only those of the rows
 // that have to be, 266; rows read and written by their own lanes 261; the other kernel with tiles of 64 rows 386.
 constexpr float kNominalRows = 14.0f;
+template <bool TREE>
 struct KvMany {
+  static constexpr bool kTree = TREE;
   static constexpr int kHd = 128, kR = 128, kTpr = 1, kTok = kRows, kHead = 4, kPages = kTok / 16;
   static constexpr int kShare = 4;  // threads a row
   static constexpr int kSoft = 128 * kShare, kTmaWarp = 4 * kShare, kMmaWarp = kTmaWarp + 1, kThreads = kSoft + 64, kSlots = 12;
@@ -1153,9 +1182,10 @@ __device__ __forceinline__ void exchange4(uint4 (&r)[4], int lane) {
   swap(r[1], r[3], 2);
 }
 
-__global__ void __launch_bounds__(KvMany::kThreads, 1)
+template <bool TREE>
+__global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
     kv_attn_rows_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const KvTcArgs p) {
-  using Y = KvMany;
+  using Y = KvMany<TREE>;
   constexpr int NS = Y::kSlots, HD = 128, R = Y::kR, kTok = Y::kTok, C = Y::kShare, W = 128 / C;  // W columns a thread
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -1294,7 +1324,8 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
       const int32_t at = w.sq * R + row, tk = g.token_of(at), head = w.sh * g.group + at - tk * g.group;
       const bool mine = at < w.rows_n * g.group;
       const int32_t lim = mine ? w.len - w.rows_n + tk : -1;
-      const int32_t sees_all = w.len - w.rows_n + g.token_of(w.sq * R) + 1;  // (the first row's, the others' at least that)
+      // (the first row's, the others' at least that)
+      const int32_t sees_all = w.len - w.rows_n + (TREE ? 0 : g.token_of(w.sq * R) + 1);
       float f;
       {
         uint4 q[W / 8];
@@ -1359,6 +1390,21 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
           lsv[i] = static_cast<float>(static_cast<int>(vb >> 23) - 127);
           inv[i] = __uint_as_float((254u - (vb >> 23)) << 23);
         }
+        // TREE: which of the thread's tokens its row sees
+        uint32_t sees_bits = 0xffffffffu;
+        if (TREE && tile + kTok > sees_all) {
+          const int32_t at = tile + W * c - sees_all;  // the first token's place among the new ones
+          auto word = [&](int32_t k) -> uint32_t {
+            const int32_t left = w.rows_n - 32 * k;
+            if (!mine || left <= 0) return 0u;
+            const uint32_t bits = p.a.seen[static_cast<int64_t>(w.r0 + tk) * p.a.words + k];
+            return left < 32 ? bits & ((1u << left) - 1u) : bits;
+          };
+          if (at >= 0)
+            sees_bits = __funnelshift_r(word(at >> 5), word((at >> 5) + 1), at & 31);
+          else if (at > -32)
+            sees_bits = (1u << -at) - 1u | word(0) << -at;
+        }
         ok = mbar_wait_warp(s_full0 + 8u * buf, (gt >> 1) & 1, p.wc) && ok;
         tc_fence_after();
         if (c == 0 && tile + kTok > w.vis) {
@@ -1382,7 +1428,13 @@ __global__ void __launch_bounds__(KvMany::kThreads, 1)
           x[i] = t.x;
           x[i + 1] = t.y;
         }
-        if (tile + kTok > sees_all) {
+        if (TREE) {
+          if (sees_bits != 0xffffffffu) {
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+              if (!(sees_bits >> i & 1u)) x[i] = -INFINITY;
+          }
+        } else if (tile + kTok > sees_all) {
           const int32_t sees = lim - tile - W * c;  // the thread's last visible token
 #pragma unroll
           for (int i = 0; i < W; ++i)
@@ -1590,7 +1642,7 @@ cudaError_t run_kv(void (*kern)(CUtensorMap, CUtensorMap, KvTcArgs), int ctas, c
   if (!launch_wait_ctl(&p.wc)) return cudaErrorInvalidDevice;
   p.a.status = p.wc.status_word;
   p.g = KvGeom{a.row_start, a.seq_len, a.B, a.nh / a.cache.nkv, a.cache.nkv,
-               static_cast<uint32_t>(((uint64_t(1) << 32) + a.nh / a.cache.nkv - 1) / (a.nh / a.cache.nkv)), a.T,
+               static_cast<uint32_t>(((uint64_t(1) << 32) + a.nh / a.cache.nkv - 1) / (a.nh / a.cache.nkv)), 32 * a.words, a.T,
                static_cast<int64_t>(a.cache.max_pages) * a.cache.page};
   p.counters = static_cast<uint32_t*>(a.workspace);
   p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + kCounterBytes);
@@ -1624,17 +1676,19 @@ cudaError_t run_kv(void (*kern)(CUtensorMap, CUtensorMap, KvTcArgs), int ctas, c
 // 66; heads of 64, 4 rows 17.5 / 18.7 / 23.9, 16 rows 24.6 / 19.5 / 24.9, 32 rows 38 / 29 / 28, 128 rows 122 / 84 / 79.  The mean is a
 // poor guide to a batch of single tokens with a prompt among them: 128 single tokens on 2048 and a prompt of 512 (32 / 8 heads
 // of 128) take 155 us in one call, 129 in two; 32 on 4096 and a prompt of 2048 171 and 146.
-template <int HD, int R>
+template <int HD, int R, bool TREE>
 cudaError_t run_few(const KvAttnArgs& a, cudaStream_t st) {
-  return run_kv<KvLay<HD, R>>(kv_attn_kernel<HD, R>, KvLay<HD, R>::kCtas, a, st);
+  using Y = KvLay<HD, R, TREE>;
+  static_assert(Y::kSlots >= KvLay<HD, R, false>::kSlots - 1, "the bits cost a slot at most");
+  return run_kv<Y>(kv_attn_kernel<HD, R, TREE>, Y::kCtas, a, st);
 }
-template <int HD>
+template <int HD, bool TREE>
 cudaError_t run_kv_rows(const KvAttnArgs& a, cudaStream_t st) {
   const int64_t rows = (a.T + a.B - 1) / a.B * (a.nh / a.cache.nkv);
-  if (rows <= 8) return run_few<HD, 8>(a, st);
-  if (rows <= 16) return run_few<HD, 16>(a, st);
-  if (rows <= 64 || HD == 64) return run_few<HD, 32>(a, st);
-  return run_kv<KvMany>(kv_attn_rows_kernel, 1, a, st);
+  if (rows <= 8) return run_few<HD, 8, TREE>(a, st);
+  if (rows <= 16) return run_few<HD, 16, TREE>(a, st);
+  if (rows <= 64 || HD == 64) return run_few<HD, 32, TREE>(a, st);
+  return run_kv<KvMany<TREE>>(kv_attn_rows_kernel<TREE>, 1, a, st);
 }
 
 }  // namespace
@@ -1646,7 +1700,8 @@ size_t kv_attention_ws_bytes(int32_t, int32_t, int32_t d) {
 }
 
 cudaError_t launch_kv_attention(KvAttnArgs a, cudaStream_t st) {
-  return a.cache.d == 128 ? run_kv_rows<128>(a, st) : run_kv_rows<64>(a, st);
+  if (a.seen) return a.cache.d == 128 ? run_kv_rows<128, true>(a, st) : run_kv_rows<64, true>(a, st);
+  return a.cache.d == 128 ? run_kv_rows<128, false>(a, st) : run_kv_rows<64, false>(a, st);
 }
 
 }  // namespace catq

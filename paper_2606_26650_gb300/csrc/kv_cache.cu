@@ -568,6 +568,148 @@ __global__ void __launch_bounds__(kThreads, 2) kv_append_kernel(const KvAppendAr
   }
 }
 
+// ---------------------------------------------------------------- compaction
+constexpr int kCompactWarps = 8;
+
+// The float of one e4m3 code.
+__device__ __forceinline__ float of_code(uint32_t c) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(c)));
+  return __low2float(*reinterpret_cast<const __half2*>(&h));
+}
+
+// Four codes times a power of two, rounded to codes again (no product passes 448).  In fp32: the power may be any.
+__device__ __forceinline__ uint32_t move4(uint32_t codes, float by) {
+  uint32_t out = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(codes >> (16 * i))));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    out |= static_cast<uint32_t>(e4m3x2(f.x * by, f.y * by)) << (16 * i);
+  }
+  return out;
+}
+
+// A warp takes the keys or values of one head, sequence and cache, page by page.  A token moves to an earlier slot and a later
+// token's slot is never written before it has been read: sources rise strictly, so the j-th kept token's is j or more behind
+// the context.  A page that has to grow is rounded again before what moves inside it moves.
+template <int D>
+__global__ void __launch_bounds__(32 * kCompactWarps) kv_compact_kernel(const __grid_constant__ KvCompactArgs a, Divisor by_page,
+                                                                        Divisor by_heads) {
+  constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes, kDeep = 4;  // lanes a token, tokens a pass, passes under way
+  const int lane = threadIdx.x & 31, sub = lane / kLanes, word = lane % kLanes;
+  const int32_t heads = 2 * a.nkv, page = a.page;
+  const int64_t items = static_cast<int64_t>(a.n_caches) * a.B * heads;
+#pragma unroll 1
+  for (int64_t e = blockIdx.x * static_cast<int64_t>(kCompactWarps) + (threadIdx.x >> 5); e < items;
+       e += static_cast<int64_t>(gridDim.x) * kCompactWarps) {
+    const int64_t lb = e < 0x7fffffff ? by_heads.of(static_cast<int32_t>(e)) : e / heads;
+    const int32_t hv = static_cast<int32_t>(e - lb * heads), l = static_cast<int32_t>(lb / a.B);
+    const int32_t b = static_cast<int32_t>(lb - static_cast<int64_t>(l) * a.B), h = hv >= a.nkv ? hv - a.nkv : hv;
+    const int32_t r0 = a.row_start[b], r1 = a.row_start[b + 1], len = a.seq_len[b], m = a.n_kept[b], n = r1 - r0;
+    bool bad = r0 < 0 || r1 < r0 || r1 > a.T || len < 0 || len > static_cast<int64_t>(a.max_pages) * page || m < 0 || m > n;
+    // the kept rows rise strictly; the first that is not in its place, all behind it are not either
+    int32_t from = m;
+    if (!bad) {
+#pragma unroll 1
+      for (int32_t c = 0; c < m; c += 32) {
+        const int32_t j = c + lane;
+        int32_t i = j;
+        if (j < m) {
+          i = a.path[r0 + j];
+          bad |= i >= n || i <= (j > 0 ? a.path[r0 + j - 1] : -1);
+        }
+        const uint32_t moved = __ballot_sync(0xffffffffu, i != j);
+        if (moved && from == m) from = c + __ffs(moved) - 1;
+      }
+    }
+    if (__any_sync(0xffffffffu, bad)) {
+      if (lane == 0) latch_index_error(a.status);
+      continue;
+    }
+    const KvCompactArgs::Cache& kv = a.cache[l];
+    uint8_t* const codes = hv >= a.nkv ? kv.v_codes : kv.k_codes;
+    float* const scales = hv >= a.nkv ? kv.v_scale : kv.k_scale;
+    const int32_t* const table = kv.table + static_cast<int64_t>(b) * a.max_pages;
+    const int32_t first = len - n;
+    from = max(from, -first);  // (slots before the first are not stored)
+    auto block_of = [&](int32_t pg) -> int32_t {
+      const int32_t id = table[pg];
+      if (id >= 0 && id < a.n_pages) return id * a.nkv + h;
+      latch_index_error(a.status);
+      return -1;
+    };
+#pragma unroll 1
+    for (int32_t j0 = from; j0 < m;) {
+      const int32_t pg = by_page.of(first + j0), j1 = min(m, (pg + 1) * page - first);
+      const int32_t block = block_of(pg);
+      uint8_t* const dst = codes + static_cast<int64_t>(max(block, 0)) * page * D;
+      const float old = block >= 0 ? scales[block] : 0.0f;
+      // a lane's word of a token's codes where they lie, its page's scale and whether that is another page
+      auto source = [&](int32_t j, uint32_t& w, float& scale) -> bool {
+        const int32_t at = first + a.path[r0 + j], sp = by_page.of(at);
+        const int32_t sb = sp == pg ? block : block_of(sp);
+        w = 0;
+        scale = old;
+        if (sb < 0) return true;
+        w = *reinterpret_cast<const uint32_t*>(codes + (static_cast<int64_t>(sb) * page + at - sp * page) * D + 4 * word);
+        if (sp != pg) scale = scales[sb];
+        return sp != pg;
+      };
+      float top = 0.0f;
+#pragma unroll kDeep
+      for (int32_t j = j0 + sub; j < j1; j += kAtOnce) {
+        uint32_t w;
+        float scale;
+        if (!source(j, w, scale)) continue;
+        w &= 0x7f7f7f7fu;
+        w = __vmaxu4(w, w >> 16);
+        const float v = of_code(max(w & 0xffu, w >> 8 & 0xffu)) * scale;
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(top), "f"(v));
+      }
+      const float want = scale_of(__reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu));
+      const bool nan = !(want == want) || !(old == old);
+      const float now = nan ? __uint_as_float(0x7fffffffu) : fmaxf(old, want);
+      if (block >= 0) {
+        if (lane == 0) scales[block] = now;
+        if (!nan && old > 0.0f && now > old) {
+          const __half2 by = __float2half2_rn(fmaxf(old / now, 5.9604645e-8f));
+#pragma unroll 1
+          for (int32_t k = lane; k < page * D / 16; k += 32) {
+            uint4 w = reinterpret_cast<const uint4*>(dst)[k];
+            w.x = rescale4(w.x, by);
+            w.y = rescale4(w.y, by);
+            w.z = rescale4(w.z, by);
+            w.w = rescale4(w.w, by);
+            reinterpret_cast<uint4*>(dst)[k] = w;
+          }
+        }
+        __syncwarp();
+#pragma unroll 1
+        for (int32_t c = j0; c < j1; c += kDeep * kAtOnce) {
+          uint32_t w[kDeep];
+#pragma unroll
+          for (int k = 0; k < kDeep; ++k) {
+            const int32_t j = c + k * kAtOnce + sub;
+            if (j >= j1) continue;
+            float scale;
+            if (source(j, w[k], scale)) w[k] = nan ? 0u : move4(w[k], now > 0.0f ? scale / now : 1.0f);
+          }
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < kDeep; ++k) {
+            const int32_t j = c + k * kAtOnce + sub;
+            if (j < j1) *reinterpret_cast<uint32_t*>(dst + (first + j - pg * page) * D + 4 * word) = w[k];
+          }
+          __syncwarp();
+        }
+      }
+      j0 = j1;
+    }
+  }
+}
+
 int grid_for(int64_t n) {
   return static_cast<int>(std::min<int64_t>(std::max<int64_t>((n + kThreads - 1) / kThreads, 1), 152 * 16));
 }
@@ -653,6 +795,19 @@ cudaError_t launch_kv_append(KvAppendArgs a, cudaStream_t st) {
   if (a.cache.d == 64) return team == 1 ? go(c64, c1, c2) : go(c64, c2, c2);
   if (a.cache.page <= 64) return team == 1 ? go(c128, c1, c2) : go(c128, c2, c2);
   return team == 1 ? go(c128, c1, c4) : go(c128, c2, c4);  // pages of 128 tokens of 128 elements
+}
+
+cudaError_t launch_kv_compact(KvCompactArgs& a, cudaStream_t st) {
+  WaitCtl wc;
+  if (!launch_wait_ctl(&wc)) return cudaErrorInvalidDevice;
+  a.status = wc.status_word;
+  const int64_t items = static_cast<int64_t>(a.n_caches) * a.B * 2 * a.nkv;
+  const unsigned grid = static_cast<unsigned>(std::min<int64_t>((items + kCompactWarps - 1) / kCompactWarps, 152 * 64));
+  if (a.d == 64)
+    kv_compact_kernel<64><<<grid, 32 * kCompactWarps, 0, st>>>(a, divisor(a.page), divisor(2 * a.nkv));
+  else
+    kv_compact_kernel<128><<<grid, 32 * kCompactWarps, 0, st>>>(a, divisor(a.page), divisor(2 * a.nkv));
+  return cudaGetLastError();
 }
 
 }  // namespace catq

@@ -228,6 +228,21 @@ struct KvAppendArgs {
   int32_t* status;  // set by the launcher
 };
 cudaError_t launch_kv_append(KvAppendArgs a, cudaStream_t st);
+// The kept branches' tokens moved behind the context in up to kCompactCaches caches of one geometry.
+constexpr int kCompactCaches = 64;
+struct KvCompactArgs {
+  struct Cache {
+    uint8_t *k_codes, *v_codes;
+    float *k_scale, *v_scale;
+    const int32_t* table;
+  } cache[kCompactCaches];
+  int32_t n_caches, n_pages, nkv, page, d, max_pages;
+  const int32_t *row_start, *seq_len, *path, *n_kept;
+  int32_t B;
+  int64_t T;
+  int32_t* status;  // set by the launcher
+};
+cudaError_t launch_kv_compact(KvCompactArgs& a, cudaStream_t st);
 
 // kv_attn_tc.cu
 struct KvAttnArgs {
@@ -241,11 +256,40 @@ struct KvAttnArgs {
   int32_t nh;
   float scale_log2;  // log2(e) / sqrt(d)
   float* lse;        // [T, nh], nullable
+  const uint32_t* seen;  // [T, words]: which new tokens of its sequence a row sees; NULL: those up to its own
+  int32_t words;
   void* workspace;
   int32_t* status;   // set by the launcher
 };
 size_t kv_attention_ws_bytes(int32_t nh, int32_t nkv, int32_t d);
 cudaError_t launch_kv_attention(KvAttnArgs a, cudaStream_t st);
+
+// tree.cu
+// Bits and positions of trees of up to 32 words rows a sequence (1 <= words <= 8).
+cudaError_t launch_tree_masks(const int32_t* parent, const int32_t* row_start, const int32_t* seq_len, int32_t B,
+                              int64_t T, uint32_t* seen, int32_t words, int32_t* positions, cudaStream_t st);
+struct TreeAcceptArgs {
+  const int32_t *drafted, *sampled, *parent, *row_start, *seq_len;
+  int32_t B;
+  int64_t T;
+  int32_t *path, *n_kept, *next, *new_len;
+  int32_t* status;  // set by the launcher
+};
+cudaError_t launch_tree_accept(TreeAcceptArgs a, cudaStream_t st);
+
+// sample.cu
+struct SampleArgs {
+  const void* logits;
+  int64_t ld, R;
+  int32_t V;
+  const float* temperature;  // [R] each, nullable
+  const int32_t* top_k;
+  const float *top_p, *min_p;
+  const float* u;
+  int32_t* tokens;
+  float* logprob;  // nullable
+};
+cudaError_t launch_sample(const SampleArgs& a, bool f32, cudaStream_t st);
 
 // Status word latched by device-side bounded waits (0 = none); read-and-clear.
 cudaError_t read_and_clear_device_status(int32_t* out);

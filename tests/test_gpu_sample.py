@@ -1,0 +1,178 @@
+"""GPU parity of catq_sample with the oracle.  Tokens are the oracle's: weights are whole numbers on both sides, a weight differs
+from the oracle's by one at most (2^-44 of its size before it is rounded), and no case draws its u so near a border (the odds
+are about V 2^-39 a row).  ln of the probability: two roundings of 64-bit sums to fp32, a division and a logarithm, 2^-21."""
+import numpy as np
+import pytest
+
+from oracle import tree_oracle as O
+from paper_2606_26650_gb300 import synthetic as syn
+from tests.test_gpu_kv import i32
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def device():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    return torch.device("cuda:0")
+
+
+def logits(r, R, V, kind):
+    x = r.standard_normal((R, V))
+    if kind == "lm":
+        x = 2.2 * x + np.where(r.random((R, V)) < 30 / V, r.uniform(4, 15, (R, V)), 0)
+    elif kind == "flat":
+        x = 1.5 * x
+    elif kind == "ties":
+        x = np.round(2 * x)
+    elif kind == "equal":
+        x = np.zeros((R, V)) + 3.5
+    elif kind == "few":
+        x = np.where(r.random((R, V)) < 5 / V, x, -np.inf)
+        x[:, V // 3] = 0.5
+    elif kind == "rising":
+        x = np.sort(3 * x, axis=1)
+    elif kind == "zeros":
+        x = np.where(r.random((R, V)) < 0.5, -0.0, 0.0)
+        x[:, ::7] = -1e-30
+    elif kind == "wide":
+        x = 3e38 * np.tanh(x)
+    return x
+
+
+def run(device, x, dtype="f32", gap=0, **kw):
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    x = np.asarray(x, np.float32)
+    R, V = x.shape
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    whole = torch.full((R, V + gap), float("nan"), dtype=dt, device=device)
+    X = whole[:, :V]
+    X.copy_(torch.from_numpy(x).to(device))
+    tokens = torch.full((R + 1,), 77, dtype=torch.int32, device=device)
+    lp = torch.full((R + 1,), 77.0, device=device)
+    on = {k: None if v is None else (i32(v, device) if k == "top_k" else
+                                     torch.tensor(np.asarray(v, np.float32), device=device)) for k, v in kw.items()}
+    C.catq_sample(X, on.pop("u"), tokens[:R], logprob=lp[:R], **on)
+    torch.cuda.synchronize()
+    assert C.catq_device_status() == 0
+    assert tokens[R] == 77 and lp[R] == 77
+    return X.float().cpu().numpy(), tokens[:R].cpu().numpy(), lp[:R].cpu().numpy()
+
+
+def check(device, x, dtype="f32", gap=0, **kw):
+    read, tokens, lp = run(device, x, dtype, gap, **kw)
+    for r in range(len(read)):
+        one = {k: np.float32(v[r]) if k != "top_k" else int(v[r]) for k, v in kw.items() if v is not None}
+        want, ln = O.sample(read[r], **one)
+        assert tokens[r] == want, (r, tokens[r], want, one)
+        assert np.isnan(lp[r]) and np.isnan(ln) or abs(lp[r] - ln) <= 2.0 ** -21 * (1e-6 + abs(ln)), (r, lp[r], ln)
+
+
+def settings(r, R):
+    return dict(temperature=np.where(r.random(R) < 0.15, 0, r.uniform(0.3, 1.5, R)),
+                top_k=r.choice([0, 1, 2, 20, 1000, 10 ** 6], R), top_p=r.choice([0.0, 0.3, 0.9, 0.95, 1.0], R),
+                min_p=r.choice([0.0, 0.0, 0.02, 0.3, 1.0], R))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["lm", "flat", "ties", "equal", "few", "rising", "zeros"])
+@pytest.mark.parametrize("R,V,gap", [(1, 1, 0), (3, 2, 1), (4, 7, 0), (5, 33, 3), (9, 1000, 0), (6, 4099, 5), (3, 50001, 0)])
+def test_tokens_match_oracle(device, dtype, kind, R, V, gap):
+    r = syn.rng(60, f"sample/{kind}/{R}/{V}")
+    x = logits(r, R, V, kind)
+    check(device, x, dtype, gap, u=r.random(R))
+    check(device, x, dtype, gap, u=r.random(R), **settings(r, R))
+    for name, value in settings(r, R).items():
+        check(device, x, dtype, gap, u=r.random(R), **{name: value})
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_rows_of_many_settings(device, dtype):
+    r = syn.rng(61, "many")
+    for kind, R, V in (("lm", 300, 700), ("flat", 40, 9000), ("ties", 200, 300), ("lm", 20, 32000)):
+        check(device, logits(r, R, V, kind), dtype, 1, u=r.random(R), **settings(r, R))
+
+
+def test_borders(device):
+    """u at both ends, running sums that meet p and u exactly, p of the first token alone."""
+    x = np.zeros((8, 16))
+    u = np.array([0.0, 1 / 16, 0.5, 15 / 16, 1 - 2.0 ** -24, 1.0, 2.0, -1.0])
+    check(device, x, u=u)
+    assert run(device, x, u=u)[1].tolist() == [0, 1, 8, 15, 15, 15, 15, 0]
+    p = np.array([1 / 16, 0.5, 0.5 + 2.0 ** -20, 1e-30, -1.0, 15 / 16, 1 - 2.0 ** -24, 1.0])
+    check(device, x, u=np.full(8, 1 - 2.0 ** -24), top_p=p)
+    assert run(device, x, u=np.full(8, 0.9999999), top_p=p)[1].tolist() == [0, 7, 8, 0, 0, 14, 15, 15]
+    nan = np.full(8, np.nan)
+    check(device, x, u=np.full(8, 0.7), top_p=np.ones(8), min_p=np.zeros(8))
+    assert run(device, x, u=np.full(8, 0.7), top_p=nan, min_p=nan)[1].tolist() == [11] * 8
+    assert run(device, x, u=nan)[1].tolist() == [0] * 8
+
+
+def test_temperatures(device):
+    r = syn.rng(62, "temperature")
+    T = np.array([0.0, 2.0 ** -70, 1e-9, 1e-3, 0.1, 1.0, 30.0, 1e6, 1e30, np.inf])
+    check(device, logits(r, 10, 999, "lm"), u=r.random(10), temperature=T)
+    check(device, logits(r, 10, 999, "wide"), u=r.random(10), temperature=T)
+    check(device, logits(r, 10, 999, "wide"), u=r.random(10), temperature=np.full(10, 3e37))
+    # nearby logits at a temperature that tells them apart
+    x = 20.0 + np.arange(64)[None] * 2.0 ** -19
+    check(device, np.repeat(x, 10, 0), u=r.random(10), temperature=np.full(10, 2.0 ** -15))
+
+
+def test_rows_from_which_nothing_can_be_drawn(device):
+    r = syn.rng(63, "bad")
+    for V in (5, 1000, 20000):
+        x = logits(r, 7, V, "lm")
+        x[0] = -np.inf
+        x[1, V - 1] = np.nan
+        x[2, 0] = np.inf
+        x[3, V // 2] = -np.nan
+        t = np.ones(7)
+        t[4], t[5] = -1.0, np.nan
+        for dtype in ("f32", "bf16"):
+            _, tokens, lp = run(device, x, dtype, u=r.random(7), temperature=t)
+            assert (tokens[:6] == -1).all() and np.isnan(lp[:6]).all() and tokens[6] >= 0 and lp[6] <= 0
+            check(device, x, dtype, u=r.random(7), temperature=t)
+
+
+def test_frequencies(device):
+    """Drawn with evenly spread u, each token comes as often as its probability says, within one."""
+    R = 4096
+    p = np.array([0.35, 0.05, 0.3, 0.2, 0.1])
+    x = np.repeat(np.log(p)[None], R, 0)
+    _, tokens, _ = run(device, x, u=(np.arange(R) + 0.5) / R)
+    assert np.abs(np.bincount(tokens, minlength=5) - R * p).max() <= 1
+    _, tokens, _ = run(device, x, u=(np.arange(R) + 0.5) / R, top_k=np.full(R, 3))
+    assert np.abs(np.bincount(tokens, minlength=5) - R * np.array([0.35, 0, 0.3, 0.2, 0]) / 0.85).max() <= 1
+
+
+def test_streams_graphs_and_repeats(device):
+    """The same bits each time, on another stream, and replayed with new numbers."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(64, "graph")
+    R, V = 33, 30000
+    x = torch.tensor(logits(r, R, V, "flat"), dtype=torch.bfloat16, device=device)
+    u = torch.tensor(r.random(R), dtype=torch.float32, device=device)
+    p = torch.full((R,), 0.9, device=device)
+    out = [torch.empty(R, dtype=torch.int32, device=device) for _ in range(3)]
+    C.catq_sample(x, u, out[0], top_p=p)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    C.catq_sample(x, u, out[1], top_p=p, stream=stream)
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], out[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        C.catq_sample(x, u, out[2], top_p=p)
+    for _ in range(3):
+        u.copy_(torch.tensor(r.random(R), dtype=torch.float32))
+        graph.replay()
+        C.catq_sample(x, u, out[0], top_p=p)
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], out[2])
