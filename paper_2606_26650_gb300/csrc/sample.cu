@@ -7,20 +7,22 @@
 // the first whose cumulated weight passes floor(u Z).  Nothing is sorted: a first part's end is found by a histogram of
 // counts and weights over the range of keys (x's bits as a number that rises as x falls) that have any weight, then
 // inside one of its bins: by ranks where it has few tokens, by a finer histogram where it has many.
-#include <cuda_bf16.h>
+#include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
 #include <atomic>
 
 #include "launch.h"
+#include "ptx_sm100.cuh"
 
 namespace catq {
 namespace {
 
-constexpr int kThreads = 1024, kWarps = kThreads / 32;
-constexpr int kBinBits = 12, kBins = 1 << kBinBits;
-constexpr int kList = 1024;  // tokens whose ranks are found one against all others
+namespace cg = cooperative_groups;
+
+constexpr float kLowest = -3.402823466e38f;
+constexpr int kUndecided = -2;  // a row's token where the first kernel leaves it to the second
 
 // ---------------------------------------------------------------- weights
 // 2^(-i / 64) in units of 2^-63.
@@ -48,6 +50,19 @@ constexpr uint64_t kOne = uint64_t(1) << kOneBits;
 // up to 63 bits (max - x as an fp32 number and its rounding, both exact), and C = 2^(120 - k) log2(e) / T.  t is its whole part,
 // its next six bits (a table) and a rest below 2^-6, whose exponential is its series up to y^5 / 5!, y < 2^-6.5 (remainder
 // 2^-48.6).  What is cut off in C (53 bits) and the products leaves a weight within 2^-44 of itself before it is rounded.
+// 2^-f of the fraction f of t (units of 2^-56), in units of 2^-63.
+__device__ __forceinline__ uint64_t exp2_fraction(uint64_t t, const uint64_t* pow2) {
+  const uint64_t p = pow2[(t >> 50) & 63];
+  const uint64_t y = __umul64hi(t << 14, 0xb17217f7d1cf79acull);  // ln 2 of the rest: 64 y
+  const uint32_t h = static_cast<uint32_t>(y >> 32);
+  // (1 - e^-y) / y = 1 - y/2 (1 - y/3 (1 - y/4 (1 - y/5)))
+  uint32_t q = 0xffffffffu - __umulhi(h, 0x00cccccdu);
+  q = 0xffffffffu - (__umulhi(h, q) >> 8);
+  q = 0xffffffffu - __umulhi(__umulhi(h, q), 0x01555555u);
+  const uint64_t s = ~(__umul64hi(y, static_cast<uint64_t>(q) << 32) >> 7);
+  return p - __umul64hi(p, __umul64hi(y, s) >> 6);
+}
+
 struct Weigher {
   float max, cut, scale;  // max - x at and above cut weighs nothing
   uint64_t c;
@@ -60,32 +75,45 @@ struct Weigher {
     const uint64_t t = __umul64hi(big, c);
     const int n = static_cast<int>(t >> 56);
     if (n > kOneBits) return 0;
-    const uint64_t p = pow2[(t >> 50) & 63];
-    const uint64_t y = __umul64hi(t << 14, 0xb17217f7d1cf79acull);  // ln 2 of the rest: 64 y
-    const uint32_t h = static_cast<uint32_t>(y >> 32);
-    // (1 - e^-y) / y = 1 - y/2 (1 - y/3 (1 - y/4 (1 - y/5)))
-    uint32_t q = 0xffffffffu - __umulhi(h, 0x00cccccdu);
-    q = 0xffffffffu - (__umulhi(h, q) >> 8);
-    q = 0xffffffffu - __umulhi(__umulhi(h, q), 0x01555555u);
-    const uint64_t s = ~(__umul64hi(y, static_cast<uint64_t>(q) << 32) >> 7);
-    const uint64_t e = p - __umul64hi(p, __umul64hi(y, s) >> 6);
     const int down = 63 - kOneBits + n;
-    return (e + (uint64_t(1) << (down - 1))) >> down;
+    return (exp2_fraction(t, pow2) + (uint64_t(1) << (down - 1))) >> down;
   }
 };
 
 // The weights of a row with largest logit `max` at temperature t > 0.
 __device__ __forceinline__ Weigher weigher(float max, float t, const uint64_t* pow2) {
-  const double rate = 1.4426950408889634 / fmin(fmax(static_cast<double>(t), 0x1p-60), 0x1p60);
-  int e;
-  frexp(41.5 / rate, &e);
+  const float held = fminf(fmaxf(t, 0x1p-60f), 0x1p60f);
+  const double wide = static_cast<double>(held), rate = 1.4426950408889634 / wide;
+  // e: 41.5 / rate = 28.7655 t is below 2^e, by a factor of two at most
+  const uint32_t most = __float_as_uint(28.7655830f * held);
+  const int e = static_cast<int>(most >> 23) - 126 + ((most & 0x7fffffu) >= 0x7ffff0u ? 1 : 0);
   Weigher w;
   w.max = max;
-  w.cut = static_cast<float>(41.2 / rate);
-  w.scale = static_cast<float>(ldexp(1.0, 63 - e));
-  w.c = static_cast<uint64_t>(ldexp(rate, 57 + e));
+  w.cut = 28.5576391f * held;  // 41.2 / rate
+  w.scale = __uint_as_float(static_cast<uint32_t>(127 + 63 - e) << 23);
+  w.c = static_cast<uint64_t>(__longlong_as_double(__double_as_longlong(rate) + (static_cast<int64_t>(57 + e) << 52)));
   w.pow2 = pow2;
   return w;
+}
+
+// The running weight at which p of the whole is reached: ceil(p whole), from 1 to whole.
+__device__ __forceinline__ uint64_t reaches(float p, uint64_t whole) {
+  const double part = ceil(static_cast<double>(p) * static_cast<double>(whole));
+  return part < 1.0 ? 1 : part < static_cast<double>(whole) ? static_cast<uint64_t>(part) : whole;
+}
+// The least weight that min-p keeps.
+__device__ __forceinline__ uint64_t least_of(float min_p) {
+  return static_cast<uint64_t>(ceil(static_cast<double>(fminf(min_p, 1.0f)) * static_cast<double>(kOne)));
+}
+// The running weight that the token has to reach: floor(u whole) + 1, from 1 to whole.
+__device__ __forceinline__ uint64_t passes(float u, uint64_t whole) {
+  const double part = floor(static_cast<double>(u) * static_cast<double>(whole));
+  return (!(part > 0.0) ? 0 : part < static_cast<double>(whole - 1) ? static_cast<uint64_t>(part) : whole - 1) + 1;
+}
+// ln(w / whole); where w is most of it, by what is left.
+__device__ __forceinline__ float ln_of(uint64_t w, uint64_t whole) {
+  const float rest = static_cast<float>(whole - w) / static_cast<float>(whole);
+  return rest < 0.5f ? log1pf(-rest) : logf(static_cast<float>(w) / static_cast<float>(whole));
 }
 
 // ---------------------------------------------------------------- logits
@@ -129,67 +157,71 @@ struct Logit<uint16_t> {
   }
 };
 
-// A row: elements up to the first 16-byte boundary, vectors, elements behind the last one.
+// A row: elements up to the first 16-byte boundary, vectors, elements behind the last one.  In parts: part i of n has the
+// vectors v0 .. v1 - 1, the first part the elements ahead of them, the last those behind.
 template <typename E>
 struct Row {
   const E* p;
-  int32_t V, head, vecs;
-  __device__ __forceinline__ Row(const E* row, int32_t n) : p(row), V(n) {
+  int32_t V, head, vecs, v0, v1;
+  bool first, last;
+  __device__ __forceinline__ Row(const E* row, int32_t n, int part, int parts) : p(row), V(n) {
     head = min(V, static_cast<int32_t>((16u - (reinterpret_cast<uintptr_t>(row) & 15u)) % 16u / sizeof(E)));
     vecs = (V - head) / Logit<E>::kVec;
+    v0 = static_cast<int32_t>(static_cast<int64_t>(vecs) * part / parts);
+    v1 = static_cast<int32_t>(static_cast<int64_t>(vecs) * (part + 1) / parts);
+    first = part == 0;
+    last = part == parts - 1;
   }
-  __device__ __forceinline__ const uint4* vec() const { return reinterpret_cast<const uint4*>(p + head); }
+  __device__ __forceinline__ uint4 vec(int32_t v) const { return reinterpret_cast<const uint4*>(p + head)[v]; }
   __device__ __forceinline__ int32_t tail() const { return head + vecs * Logit<E>::kVec; }
-  // f(x, index) of every element, by the CTA's threads.
-  template <class F>
+  // Elements of the part.
+  __device__ __forceinline__ int32_t count() const {
+    return (v1 - v0) * Logit<E>::kVec + (first ? head : 0) + (last ? V - tail() : 0);
+  }
+  // f(x, index) of every element of the part, by kThreads threads.
+  template <int kThreads, class F>
   __device__ __forceinline__ void each(F f) const {
     constexpr int VEC = Logit<E>::kVec;
     const int32_t t = threadIdx.x;
-    if (t < head) f(Logit<E>::get(p + t), t);
-    for (int32_t v = t; v < vecs; v += kThreads) {
+    if (first && t < head) f(Logit<E>::get(p + t), t);
+#pragma unroll 2
+    for (int32_t v = v0 + t; v < v1; v += kThreads) {
       float x[VEC];
-      Logit<E>::get(vec()[v], x);
+      Logit<E>::get(vec(v), x);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) f(x[i], head + v * VEC + i);
     }
-    if (tail() + t < V) f(Logit<E>::get(p + tail() + t), tail() + t);
+    if (last && tail() + t < V) f(Logit<E>::get(p + tail() + t), tail() + t);
   }
 };
 
-// ---------------------------------------------------------------- histograms
-// Counts and weights by bins; after sum_up those of a bin and all before it.
-struct Bins {
-  uint32_t count[kBins], lo[kBins], hi[kBins];
-  __device__ __forceinline__ void clear() {
-    for (int i = threadIdx.x; i < kBins; i += kThreads) count[i] = lo[i] = hi[i] = 0;
-  }
-  __device__ __forceinline__ void add(int bin, uint64_t w) {
-    atomicAdd(&count[bin], 1u);
-    const uint32_t low = static_cast<uint32_t>(w), old = atomicAdd(&lo[bin], low);
-    const uint32_t high = static_cast<uint32_t>(w >> 32) + (old + low < old ? 1u : 0u);
-    if (high) atomicAdd(&hi[bin], high);
-  }
-  __device__ __forceinline__ uint64_t weight(int bin) const { return static_cast<uint64_t>(hi[bin]) << 32 | lo[bin]; }
-};
+// ---------------------------------------------------------------- any row
+// The second kernel: the rows that the first left, a cluster of kPeers CTAs each, in one of two forms.  Both make running sums of
+// the tokens' counts and weights over steps of the order that all CTAs of the cluster see alike, so that they take the same
+// way, and find inside a step what is asked for.
+constexpr int kPeers = 8;
 
-struct Shared {
-  Bins bins[2];
+// What both forms keep.
+template <int T>
+struct Common {
   uint64_t pow2[64];
-  uint64_t list_w[kList];
-  uint32_t list_key[kList];
-  int32_t list_at[kList];
-  uint64_t red_w[kWarps];
-  uint32_t red_c[kWarps];
-  uint32_t n;
-  // a place in the order
-  uint32_t key, before;      // its key and how many are ahead of it
-  uint64_t w, w_before;      // its weight and theirs
-  int32_t at;                // its index, where it was asked for
+  uint64_t red_w[T / 32];
+  uint32_t red_c[T / 32];
+  uint32_t rows[T / 32];  // bits of the rows to do
+  uint32_t best, bad, had_c, n;
+  uint64_t had_w, target;
+  int32_t at;  // the token's index, -1 where another CTA has it
   Weigher weigh;
 };
+// A place in the order: its key, which of the tokens that have it, how many are ahead and what they weigh, and its own weight.
+struct Place {
+  uint32_t key, nth, before;
+  uint64_t w_before, w;
+};
 
-// Sums over the CTA (in every thread), counts and weights.
-__device__ __forceinline__ void block_sums(Shared& s, uint32_t& c, uint64_t& w) {
+// Sums over the CTA, in every thread.
+template <int T>
+__device__ __forceinline__ void block_sums(Common<T>& s, uint32_t& c, uint64_t& w) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     c += __shfl_xor_sync(0xffffffffu, c, o);
@@ -203,99 +235,88 @@ __device__ __forceinline__ void block_sums(Shared& s, uint32_t& c, uint64_t& w) 
   __syncthreads();
   c = 0;
   w = 0;
-  for (int i = 0; i < kWarps; ++i) {
+  for (int i = 0; i < T / 32; ++i) {
     c += s.red_c[i];
     w += s.red_w[i];
   }
 }
-
-// Bins to running sums, on top of what came before them.
-__device__ __forceinline__ void sum_up(Shared& s, Bins& b, uint32_t c0, uint64_t w0) {
-  constexpr int kPer = kBins / kThreads;
+// c and w become the sums over the threads ahead; all_c and all_w over all.
+template <int T>
+__device__ __forceinline__ void block_scan(Common<T>& s, uint32_t& c, uint64_t& w, uint32_t& all_c, uint64_t& all_w) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint32_t c[kPer];
-  uint64_t w[kPer];
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int at = threadIdx.x * kPer + i;
-    c[i] = b.count[at] + (i ? c[i - 1] : 0u);
-    w[i] = b.weight(at) + (i ? w[i - 1] : 0u);
-  }
-  uint32_t cs = c[kPer - 1];
-  uint64_t ws = w[kPer - 1];
+  const uint32_t own_c = c;
+  const uint64_t own_w = w;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t x = __shfl_up_sync(0xffffffffu, cs, o);
-    const uint64_t y = __shfl_up_sync(0xffffffffu, ws, o);
+    const uint32_t x = __shfl_up_sync(0xffffffffu, c, o);
+    const uint64_t y = __shfl_up_sync(0xffffffffu, w, o);
     if (lane >= o) {
-      cs += x;
-      ws += y;
+      c += x;
+      w += y;
     }
   }
+  __syncthreads();
   if (lane == 31) {
-    s.red_c[warp] = cs;
-    s.red_w[warp] = ws;
+    s.red_c[warp] = c;
+    s.red_w[warp] = w;
   }
   __syncthreads();
-  uint32_t cb = c0 + cs - c[kPer - 1];
-  uint64_t wb = w0 + ws - w[kPer - 1];
-  for (int i = 0; i < warp; ++i) {
-    cb += s.red_c[i];
-    wb += s.red_w[i];
+  c -= own_c;
+  w -= own_w;
+  all_c = 0;
+  all_w = 0;
+  for (int i = 0; i < T / 32; ++i) {
+    if (i == warp) {
+      c += all_c;
+      w += all_w;
+    }
+    all_c += s.red_c[i];
+    all_w += s.red_w[i];
   }
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int at = threadIdx.x * kPer + i;
-    const uint64_t v = wb + w[i];
-    b.count[at] = cb + c[i];
-    b.lo[at] = static_cast<uint32_t>(v);
-    b.hi[at] = static_cast<uint32_t>(v >> 32);
-  }
+}
+
+// The row's largest logit, from every CTA's least key; false (token -1 written) where nothing can be drawn.
+template <typename E, int T, class S>
+__device__ __forceinline__ bool largest(S& s, const cg::cluster_group& cluster, const SampleArgs& a, int64_t r, uint32_t& best,
+                                        uint32_t bad, float t) {
+  best = __reduce_min_sync(0xffffffffu, best);
+  bad = __syncthreads_or(bad);
+  if ((threadIdx.x & 31) == 0) s.red_c[threadIdx.x >> 5] = best;
   __syncthreads();
-}
-
-// The first bin whose running sum reaches target >= 1.
-__device__ __forceinline__ int first_bin(const Bins& b, bool by_weight, uint64_t target) {
-  int lo = 0, hi = kBins - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if ((by_weight ? b.weight(mid) : b.count[mid]) >= target)
-      hi = mid;
-    else
-      lo = mid + 1;
+  for (int i = 0; i < T / 32; ++i) best = min(best, s.red_c[i]);
+  if (threadIdx.x == 0) {
+    s.best = best;
+    s.bad = bad;
   }
-  return lo;
+  cluster.sync();
+  for (int i = 0; i < kPeers; ++i) {
+    const S& p = *cluster.map_shared_rank(&s, i);
+    best = min(best, p.best);
+    bad |= p.bad;
+  }
+  if (!bad && Logit<E>::of_key(best) > -INFINITY && t >= 0.0f) return true;
+  if (cluster.block_rank() == 0 && threadIdx.x == 0) {
+    a.tokens[r] = -1;
+    if (a.logprob) a.logprob[r] = __uint_as_float(0x7fffffffu);
+  }
+  return false;
 }
 
-// ---------------------------------------------------------------- a place in the order
-// The j-th element of a row (from 0) that has the key, in the order of the indexes, into s.at.
-template <typename E>
-__device__ __forceinline__ void nth_of(Shared& s, const Row<E>& row, uint32_t key, uint32_t j) {
+// The index of the part's j-th element (from 0) that has the key, in the order of the indexes, into s.at.
+template <typename E, int T>
+__device__ __forceinline__ void nth_of(Common<T>& s, const Row<E>& row, uint32_t key, uint32_t j) {
   constexpr int VEC = Logit<E>::kVec;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t seen = 0;
   // x: n consecutive elements of the thread from index `at` on, the threads' in order
   auto step = [&](const float* x, int n, int32_t at) {
-    uint32_t mine = 0;
+    uint32_t before = 0, all;
+    uint64_t none = 0, none2;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) mine += i < n && Logit<E>::key(x[i]) == key ? 1u : 0u;
-    uint32_t upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += v;
-    }
-    __syncthreads();
-    if (lane == 31) s.red_c[warp] = upto;
-    __syncthreads();
-    uint32_t base = seen;
-    for (int i = 0; i < kWarps; ++i) {
-      if (i == warp) upto += base;
-      base += s.red_c[i];
-    }
-    uint32_t before = upto - mine;
-    if (before <= j && j < upto) {
+    for (int i = 0; i < VEC; ++i) before += i < n && Logit<E>::key(x[i]) == key ? 1u : 0u;
+    const uint32_t own = before;
+    block_scan<T>(s, before, none, all, none2);
+    before += seen;
+    if (before <= j && j < before + own) {
 #pragma unroll
       for (int i = 0; i < VEC; ++i)
         if (i < n && Logit<E>::key(x[i]) == key) {
@@ -303,221 +324,985 @@ __device__ __forceinline__ void nth_of(Shared& s, const Row<E>& row, uint32_t ke
           ++before;
         }
     }
-    seen = base;
+    seen += all;
   };
+  const int32_t t = threadIdx.x;
   float x[VEC];
-  x[0] = static_cast<int>(threadIdx.x) < row.head ? Logit<E>::get(row.p + threadIdx.x) : 0.0f;
-  step(x, static_cast<int>(threadIdx.x) < row.head ? 1 : 0, threadIdx.x);
-  for (int32_t v0 = 0; v0 < row.vecs && seen <= j; v0 += kThreads) {
-    const int32_t v = v0 + threadIdx.x;
-    if (v < row.vecs) Logit<E>::get(row.vec()[v], x);
-    step(x, v < row.vecs ? VEC : 0, row.head + v * VEC);
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) x[i] = 0.0f;
+  if (row.first) {
+    if (t < row.head) x[0] = Logit<E>::get(row.p + t);
+    step(x, t < row.head ? 1 : 0, t);
   }
-  if (seen <= j) {
-    const int32_t at = row.tail() + threadIdx.x;
+  for (int32_t v0 = row.v0; v0 < row.v1 && seen <= j; v0 += T) {
+    const int32_t v = v0 + t;
+    if (v < row.v1) Logit<E>::get(row.vec(v), x);
+    step(x, v < row.v1 ? VEC : 0, row.head + v * VEC);
+  }
+  if (row.last && seen <= j) {
+    const int32_t at = row.tail() + t;
     if (at < row.V) x[0] = Logit<E>::get(row.p + at);
     step(x, at < row.V ? 1 : 0, at);
   }
   __syncthreads();
 }
 
-// The first place at which the running count or weight reaches target >= 1, which the row has.  first: the key of the
-// largest logit, shift: bins[0] holds the running sums over bins of 2^shift keys from there on.
-template <typename E>
-__device__ __forceinline__ void find(Shared& s, const Row<E>& row, uint32_t first, int shift, bool by_weight, uint64_t target,
-                                     bool want_at) {
-  uint32_t lo = 0, c0 = 0, n;
-  uint64_t w0 = 0;
-  const Bins* b = &s.bins[0];
-  for (;;) {
-    const int bin = first_bin(*b, by_weight, target);
-    if (bin > 0) {
-      c0 = b->count[bin - 1];
-      w0 = b->weight(bin - 1);
+// The token of a row from a form's running sums.  live, total: the number and weight of all tokens that weigh anything;
+// find(by_weight, target): the first place at which the running count or weight reaches target; heavy(w0, c, sum): the number
+// and weight of the tokens of w0 and more; where(place): its index, into s.at.
+template <class S, class Find, class Heavy, class Where>
+__device__ __forceinline__ void draw(const SampleArgs& a, int64_t r, S& s, bool greedy, uint32_t live, uint64_t total, Find find,
+                                     Heavy heavy, Where where) {
+  // what is kept: the first `kept` tokens, weighing `total` together
+  uint32_t kept = live;
+  auto limit = [&](uint32_t count, uint64_t weight) {
+    if (count < kept) {
+      kept = count;
+      total = weight;
     }
-    n = b->count[bin] - c0;
-    lo += static_cast<uint32_t>(bin) << shift;
+  };
+  auto ask = [&](auto f) {  // (64-bit floats: one thread's work)
     __syncthreads();
-    if (shift == 0) {
-      const uint64_t w = s.weigh(Logit<E>::of_key(first + lo));
-      const uint32_t j = static_cast<uint32_t>(by_weight ? (target - w0 - 1) / w : target - c0 - 1);
-      if (threadIdx.x == 0) {
-        s.key = first + lo;
-        s.before = c0 + j;
-        s.w = w;
-        s.w_before = w0 + j * w;
-      }
-      if (want_at) nth_of(s, row, first + lo, j);
-      __syncthreads();
-      return;
-    }
-    if (n <= kList) break;
-    const int finer = max(shift - kBinBits, 0);
-    s.bins[1].clear();
+    if (threadIdx.x == 0) s.target = f();
     __syncthreads();
-    row.each([&](float x, int32_t) {
-      const uint32_t rel = Logit<E>::key(x) - first - lo;
-      if (rel >> shift) return;
-      const uint64_t w = s.weigh(x);
-      if (w) s.bins[1].add(rel >> finer, w);
-    });
-    sum_up(s, s.bins[1], c0, w0);
-    shift = finer;
-    b = &s.bins[1];
+    return s.target;
+  };
+  const int32_t k = greedy ? 1 : a.top_k ? a.top_k[r] : 0;
+  if (k > 0 && static_cast<uint32_t>(k) < live) {
+    const Place p = find(false, k);
+    limit(p.before + 1, p.w_before + p.w);
   }
-  if (threadIdx.x == 0) s.n = 0;
-  __syncthreads();
-  row.each([&](float x, int32_t at) {
-    const uint32_t k = Logit<E>::key(x);
-    if ((k - first - lo) >> shift) return;
-    const uint64_t w = s.weigh(x);
-    if (!w) return;
-    const uint32_t i = atomicAdd(&s.n, 1u);
-    if (i >= kList) return;
-    s.list_key[i] = k;
-    s.list_at[i] = at;
-    s.list_w[i] = w;
-  });
-  __syncthreads();
-  const uint32_t m = min(s.n, static_cast<uint32_t>(kList));
-  for (uint32_t e = threadIdx.x; e < m; e += kThreads) {
-    const uint32_t k = s.list_key[e];
-    const int32_t at = s.list_at[e];
-    uint32_t c = c0;
-    uint64_t w = w0;
-    for (uint32_t i = 0; i < m; ++i) {
-      const uint32_t ki = s.list_key[i];
-      if (ki < k || (ki == k && s.list_at[i] < at)) {
-        ++c;
-        w += s.list_w[i];
+  const float top_p = a.top_p && !greedy ? a.top_p[r] : 1.0f;
+  if (top_p < 1.0f) {
+    const Place p = find(true, ask([&] { return reaches(top_p, total); }));
+    limit(p.before + 1, p.w_before + p.w);
+  }
+  const float least = a.min_p && !greedy ? a.min_p[r] : 0.0f;
+  if (least > 0.0f) {
+    uint32_t c = 0;
+    uint64_t sum = 0;
+    heavy(ask([&] { return least_of(least); }), c, sum);
+    limit(c, sum);
+  }
+  const Place p = find(true, ask([&] { return passes(a.u[r], total); }));
+  where(p);
+  if (threadIdx.x == 0 && s.at >= 0) {
+    a.tokens[r] = s.at;
+    if (a.logprob) a.logprob[r] = ln_of(p.w, total);
+  }
+}
+
+// f(row) of the rows that are left, clusters taking them in turn: which are left is read before any of them is written.
+template <int T, class S, class F>
+__device__ __forceinline__ void left_rows(const SampleArgs& a, S& s, const cg::cluster_group& cluster, F f) {
+  const int64_t clusters = gridDim.x / kPeers, id = blockIdx.x / kPeers;
+  for (int64_t r0 = id; r0 < a.R; r0 += clusters * T) {
+    const int64_t mine = r0 + threadIdx.x * clusters;
+    const uint32_t left = __ballot_sync(0xffffffffu, mine < a.R && a.tokens[mine] == kUndecided);
+    if ((threadIdx.x & 31) == 0) s.rows[threadIdx.x >> 5] = left;
+    if (!__syncthreads_or(left)) continue;
+    cluster.sync();
+    for (int i = 0; i < T / 32; ++i)
+      for (uint32_t bits = s.rows[i]; bits; bits &= bits - 1) {
+        f(r0 + (32 * i + __ffs(bits) - 1) * clusters);
+        cluster.sync();  // (what one CTA reads of another's is not overwritten)
       }
+  }
+}
+
+// ---- 16-bit logits: how often each key comes is all there is to know.  A CTA counts its part's keys in 16 bits each; of the
+// keys that weigh anything each CTA adds up a share over all parts, a thread some of them in order.
+constexpr int kCountThreads = 1024, kKeys = 65536, kShare = kKeys / kPeers;
+constexpr int32_t kMostCounted = 500000;  // a part's count of one key stays below 2^16
+
+struct Counts : Common<kCountThreads> {
+  alignas(16) uint32_t half[kKeys / 2];  // two keys' counts a word (cleared 16 bytes at a time)
+  uint32_t whole[kShare];      // the row's counts of the CTA's share of the keys
+  uint64_t upto_w[kCountThreads];  // ahead of a thread's keys, in the share
+  uint32_t upto_c[kCountThreads];
+  uint32_t all_c;
+  uint64_t all_w;
+  Place place[2];
+  __device__ __forceinline__ uint32_t count(uint32_t key) const { return half[key >> 1] >> (16 * (key & 1)) & 0xffffu; }
+};
+
+__global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const SampleArgs a) {
+  using E = uint16_t;
+  constexpr int T = kCountThreads;
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  Counts& s = *reinterpret_cast<Counts*>(smem_raw);
+  const cg::cluster_group cluster = cg::this_cluster();
+  const int rank = cluster.block_rank(), tid = threadIdx.x;
+  if (tid < 64) s.pow2[tid] = kPow2[tid];
+  grid_dependency_wait();
+  left_rows<T>(a, s, cluster, [&](int64_t r) {
+    const Row<E> row(static_cast<const E*>(a.logits) + r * a.ld, a.V, rank, kPeers);
+    const float t = a.temperature ? a.temperature[r] : 1.0f;
+    const bool greedy = t == 0.0f;
+    for (int i = tid; i < kKeys / 8; i += T) reinterpret_cast<uint4*>(s.half)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (tid == T - 1) s.weigh = weigher(0.0f, greedy ? 1.0f : t, s.pow2);
+    __syncthreads();
+    uint32_t best = 0xffffffffu, bad = 0;
+    row.template each<T>([&](float x, int32_t) {
+      const uint32_t k = Logit<E>::key(x);
+      bad |= x < INFINITY ? 0u : 1u;
+      best = min(best, k);
+      atomicAdd(&s.half[k >> 1], 1u << (16 * (k & 1)));
+    });
+    if (!largest<E, T>(s, cluster, a, r, best, bad, t)) return;
+    Weigher weigh = s.weigh;
+    weigh.max = Logit<E>::of_key(best);
+
+    // the share's keys over all parts, a thread's side by side
+    const uint32_t range = Logit<E>::key(fmaxf(__fsub_rd(weigh.max, 1.001f * weigh.cut), kLowest)) - best + 1;
+    const uint32_t share = (range + kPeers - 1) / kPeers, k0 = best + rank * share;
+    const uint32_t mine = k0 < best + range ? min(share, best + range - k0) : 0;
+    for (uint32_t i = tid; i < mine; i += T) {
+      uint32_t c = 0;
+#pragma unroll
+      for (int e = 0; e < kPeers; ++e) c += cluster.map_shared_rank(&s, e)->count(k0 + i);
+      s.whole[i] = c;
     }
-    const uint64_t mine = by_weight ? w : c, with = mine + (by_weight ? s.list_w[e] : 1u);
-    if (mine < target && target <= with) {
-      s.key = k;
-      s.before = c;
-      s.w = s.list_w[e];
-      s.w_before = w;
-      s.at = at;
+    __syncthreads();
+    const uint32_t per = (share + T - 1) / T, i0 = min(tid * per, mine), i1 = min(i0 + per, mine);
+    auto walk = [&](auto f) {  // f(key, tokens, weight of one) of the thread's keys that weigh anything
+      for (uint32_t i = i0; i < i1; ++i) {
+        const uint32_t c = s.whole[i];
+        const uint64_t w = c ? weigh(Logit<E>::of_key(k0 + i)) : 0;
+        if (w && f(k0 + i, c, w)) return;
+      }
+    };
+    uint32_t own_c = 0, all_c;
+    uint64_t own_w = 0, all_w;
+    walk([&](uint32_t, uint32_t c, uint64_t w) {
+      own_c += c;
+      own_w += c * w;
+      return false;
+    });
+    uint32_t c0 = own_c;
+    uint64_t w0 = own_w;
+    block_scan<T>(s, c0, w0, all_c, all_w);
+    if (tid == 0) {
+      s.all_c = all_c;
+      s.all_w = all_w;
     }
+    cluster.sync();
+    all_c = 0;
+    all_w = 0;
+    for (int i = 0; i < kPeers; ++i) {
+      const Counts& p = *cluster.map_shared_rank(&s, i);
+      if (i == rank) {
+        c0 += all_c;
+        w0 += all_w;
+      }
+      all_c += p.all_c;
+      all_w += p.all_w;
+    }
+    int turn = 0;
+    auto find = [&](bool by_weight, uint64_t target) {
+      Place& to = s.place[turn];  // (the other may still be read)
+      turn ^= 1;
+      if (by_weight ? w0 < target && target <= w0 + own_w : c0 < target && target <= c0 + own_c) {
+        Place p{0, 0, c0, w0, 0};
+        walk([&](uint32_t key, uint32_t c, uint64_t w) {
+          const uint64_t left = (by_weight ? (target - p.w_before - 1) / w : target - p.before - 1);
+          const uint32_t j = static_cast<uint32_t>(left < c ? left : c);
+          p.before += j;
+          p.w_before += j * w;
+          p.key = key;
+          p.nth = j;
+          p.w = w;
+          return j < c;
+        });
+        for (int i = 0; i < kPeers; ++i) *cluster.map_shared_rank(&to, i) = p;
+      }
+      cluster.sync();
+      return to;
+    };
+    auto heavy = [&](uint64_t least, uint32_t& c, uint64_t& sum) {
+      walk([&](uint32_t, uint32_t n, uint64_t w) {
+        if (w < least) return true;
+        c += n;
+        sum += n * w;
+        return false;
+      });
+      block_sums<T>(s, c, sum);
+      if (tid == 0) {
+        s.had_c = c;
+        s.had_w = sum;
+      }
+      cluster.sync();
+      c = 0;
+      sum = 0;
+      for (int i = 0; i < kPeers; ++i) {
+        c += cluster.map_shared_rank(&s, i)->had_c;
+        sum += cluster.map_shared_rank(&s, i)->had_w;
+      }
+    };
+    auto where = [&](const Place& p) {
+      uint32_t seen = 0;
+      for (int i = 0; i < rank; ++i) seen += cluster.map_shared_rank(&s, i)->count(p.key);
+      if (tid == 0) s.at = -1;
+      __syncthreads();
+      if (seen <= p.nth && p.nth < seen + s.count(p.key)) nth_of<E, T>(s, row, p.key, p.nth - seen);
+    };
+    draw(a, r, s, greedy, all_c, all_w, find, heavy, where);
+  });
+}
+
+// ---- any logits: a histogram of counts and weights by max - x; in one of its bins, by ranks where it has few tokens, by keys
+// (and finer ones) where it has many.
+constexpr int kThreads = 512;
+constexpr int kBinBits = 11, kBins = 1 << kBinBits, kBinShare = kBins / kPeers;
+constexpr int kList = 256;  // tokens whose ranks are found one against all others
+
+struct Sums {  // of a bin and all before it
+  uint64_t weight[kBins];
+  uint32_t count[kBins];
+};
+struct Tokens {
+  uint64_t w[kList];
+  uint32_t key[kList];
+  int32_t at[kList];
+};
+struct Binned : Common<kThreads> {
+  uint32_t count[kBins], lo[kBins], hi[kBins];  // the CTA's part of the row
+  Sums sums[2];
+  Tokens own, all;
+  uint64_t share_w[kBinShare];  // the whole row's, a share of the bins a CTA
+  uint32_t share_c[kBinShare];
+  Place place;
+  __device__ __forceinline__ void clear() {
+    for (int i = threadIdx.x; i < kBins; i += kThreads) count[i] = lo[i] = hi[i] = 0;
+    __syncthreads();
+  }
+  __device__ __forceinline__ void add(int bin, uint64_t weight) {
+    atomicAdd(&count[bin], 1u);
+    const uint32_t low = static_cast<uint32_t>(weight), old = atomicAdd(&lo[bin], low);
+    const uint32_t high = static_cast<uint32_t>(weight >> 32) + (old + low < old ? 1u : 0u);
+    if (high) atomicAdd(&hi[bin], high);
+  }
+};
+
+// The histograms of all CTAs to running sums, on top of what came before them.
+__device__ __forceinline__ void sum_up(Binned& s, const cg::cluster_group& cluster, Sums& to, uint32_t c0, uint64_t w0) {
+  constexpr int kPer = kBins / kThreads;
+  const int rank = cluster.block_rank();
+  cluster.sync();
+  if (threadIdx.x < kBinShare) {
+    const int bin = rank * kBinShare + threadIdx.x;
+    uint32_t c = 0;
+    uint64_t w = 0;
+#pragma unroll
+    for (int i = 0; i < kPeers; ++i) {
+      const Binned& p = *cluster.map_shared_rank(&s, i);
+      c += p.count[bin];
+      w += (static_cast<uint64_t>(p.hi[bin]) << 32) + p.lo[bin];
+    }
+    s.share_c[threadIdx.x] = c;
+    s.share_w[threadIdx.x] = w;
+  }
+  cluster.sync();
+  uint32_t c[kPer], ca = 0, all_c;
+  uint64_t w[kPer], wa = 0, all_w;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int bin = threadIdx.x * kPer + i;
+    const Binned& p = *cluster.map_shared_rank(&s, bin / kBinShare);
+    c[i] = ca += p.share_c[bin % kBinShare];
+    w[i] = wa += p.share_w[bin % kBinShare];
+  }
+  block_scan<kThreads>(s, ca, wa, all_c, all_w);
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    to.count[threadIdx.x * kPer + i] = c0 + ca + c[i];
+    to.weight[threadIdx.x * kPer + i] = w0 + wa + w[i];
   }
   __syncthreads();
 }
 
-// One CTA a row.
-template <typename E>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
-  extern __shared__ uint8_t smem_raw[];
-  Shared& s = *reinterpret_cast<Shared*>(smem_raw);
-  const int64_t r = blockIdx.x;
-  const Row<E> row(static_cast<const E*>(a.logits) + r * a.ld, a.V);
-  if (threadIdx.x < 64) s.pow2[threadIdx.x] = kPow2[threadIdx.x];
-  s.bins[0].clear();
+// The first bin whose running sum reaches target >= 1.
+__device__ __forceinline__ int first_bin(const Sums& b, bool by_weight, uint64_t target) {
+  int lo = 0, hi = kBins - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if ((by_weight ? b.weight[mid] : b.count[mid]) >= target)
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  return lo;
+}
 
-  // the largest logit, as the least key; not a number, or +inf, is worse than any
+template <typename E>
+__device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, Binned& s, const cg::cluster_group& cluster) {
+  constexpr int T = kThreads;
+  const int rank = cluster.block_rank(), tid = threadIdx.x;
+  const Row<E> row(static_cast<const E*>(a.logits) + r * a.ld, a.V, rank, kPeers);
+  const float t = a.temperature ? a.temperature[r] : 1.0f;
+  const bool greedy = t == 0.0f;
+  if (tid == T - 1) s.weigh = weigher(0.0f, greedy ? 1.0f : t, s.pow2);
+  s.clear();
   uint32_t best = 0xffffffffu, bad = 0;
-  row.each([&](float x, int32_t) {
+  row.template each<T>([&](float x, int32_t) {
     bad |= x < INFINITY ? 0u : 1u;
     best = min(best, Logit<E>::key(x));
   });
-  best = __reduce_min_sync(0xffffffffu, best);
-  bad = __syncthreads_or(bad);
-  if ((threadIdx.x & 31) == 0) s.red_c[threadIdx.x >> 5] = best;
-  __syncthreads();
-  for (int i = 0; i < kWarps; ++i) best = min(best, s.red_c[i]);
-  const float max = Logit<E>::of_key(best);
-  const float t = a.temperature ? a.temperature[r] : 1.0f;
-  if (bad || max == -INFINITY || !(t >= 0.0f)) {  // nothing can be drawn
-    if (threadIdx.x == 0) {
-      a.tokens[r] = -1;
-      if (a.logprob) a.logprob[r] = __uint_as_float(0x7fffffffu);
-    }
-    return;
-  }
-  const bool greedy = t == 0.0f;
-  if (threadIdx.x == 0) s.weigh = weigher(max, greedy ? 1.0f : t, s.pow2);
-  __syncthreads();
+  if (!largest<E, T>(s, cluster, a, r, best, bad, t)) return;
+  Weigher weigh = s.weigh;
+  weigh.max = Logit<E>::of_key(best);
 
   // all tokens that weigh anything
-  const uint32_t range = Logit<E>::key(fmaxf(__fsub_rd(max, 1.001f * s.weigh.cut), -3.402823466e38f)) - best;
-  int shift = 0;
-  while (range >> shift >= kBins) ++shift;
-  row.each([&](float x, int32_t) {
-    const uint64_t w = s.weigh(x);
-    if (w) s.bins[0].add(min((Logit<E>::key(x) - best) >> shift, kBins - 1u), w);
+  const float wide = weigh.cut * (1.0f / kBins), by = 1.0f / wide;
+  auto bin_of = [&](float x) { return min(static_cast<int>((weigh.max - x) * by), kBins - 1); };
+  row.template each<T>([&](float x, int32_t) {
+    const uint64_t w = weigh(x);
+    if (w) s.add(bin_of(x), w);
   });
-  sum_up(s, s.bins[0], 0, 0);
-  const uint32_t live = s.bins[0].count[kBins - 1];
+  sum_up(s, cluster, s.sums[0], 0, 0);
 
-  // what is kept: the first `kept` tokens, weighing `total` together
-  uint32_t kept = live;
-  uint64_t total = s.bins[0].weight(kBins - 1);
-  auto limit = [&] {  // up to the place found, with it
-    if (s.before + 1 < kept) {
-      kept = s.before + 1;
-      total = s.w_before + s.w;
+  auto find = [&](bool by_weight, uint64_t target) {
+    const int bin = first_bin(s.sums[0], by_weight, target);
+    uint32_t c0 = bin ? s.sums[0].count[bin - 1] : 0, n = s.sums[0].count[bin] - c0;
+    uint64_t w0 = bin ? s.sums[0].weight[bin - 1] : 0;
+    // the keys from `lo` on that a token of the bin can have (limits a little wide)
+    uint32_t lo = max(Logit<E>::key(fminf(weigh.max - wide * bin * 0.99999f, weigh.max)), best);
+    const float low_x = bin == kBins - 1 ? kLowest : fmaxf(weigh.max - wide * (bin + 1) * 1.00001f, kLowest);
+    int shift = 0;
+    while ((Logit<E>::key(low_x) - lo) >> shift >= kBins) ++shift;
+    shift += kBinBits;
+    auto each_in = [&](auto f) {
+      row.template each<T>([&](float x, int32_t at) {
+        if (!(weigh.max - x < weigh.cut) || bin_of(x) != bin) return;
+        const uint32_t k = Logit<E>::key(x);
+        if (static_cast<uint64_t>(k - lo) >> shift) return;
+        const uint64_t w = weigh(x);
+        if (w) f(k, at, w);
+      });
+    };
+    while (n > kList && shift > 0) {
+      const int finer = max(shift - kBinBits, 0);
+      __syncthreads();
+      s.clear();
+      each_in([&](uint32_t k, int32_t, uint64_t w) { s.add(min((k - lo) >> finer, kBins - 1u), w); });
+      sum_up(s, cluster, s.sums[1], c0, w0);
+      const int at = first_bin(s.sums[1], by_weight, target);
+      if (at) {
+        c0 = s.sums[1].count[at - 1];
+        w0 = s.sums[1].weight[at - 1];
+      }
+      n = s.sums[1].count[at] - c0;
+      lo += static_cast<uint32_t>(at) << finer;
+      shift = finer;
     }
     __syncthreads();
+    if (n > kList) {  // one key
+      Place p;
+      p.key = lo;
+      p.w = weigh(Logit<E>::of_key(lo));
+      p.nth = static_cast<uint32_t>(by_weight ? (target - w0 - 1) / p.w : target - c0 - 1);
+      p.before = c0 + p.nth;
+      p.w_before = w0 + p.nth * p.w;
+      if (tid == 0) s.at = -2;  // (which of them, nth_of says)
+      __syncthreads();
+      return p;
+    }
+    if (tid == 0) s.n = 0;
+    __syncthreads();
+    each_in([&](uint32_t k, int32_t at, uint64_t w) {
+      const uint32_t i = atomicAdd(&s.n, 1u);
+      if (i >= kList) return;
+      s.own.key[i] = k;
+      s.own.at[i] = at;
+      s.own.w[i] = w;
+    });
+    cluster.sync();
+    uint32_t m = 0;
+    for (int i = 0; i < kPeers; ++i) {
+      const Binned& p = *cluster.map_shared_rank(&s, i);
+      const uint32_t more = min(p.n, kList - m);
+      for (uint32_t e = tid; e < more; e += T) {
+        s.all.key[m + e] = p.own.key[e];
+        s.all.at[m + e] = p.own.at[e];
+        s.all.w[m + e] = p.own.w[e];
+      }
+      m += more;
+    }
+    cluster.sync();
+    if (static_cast<uint32_t>(tid) < m) {
+      const uint32_t k = s.all.key[tid];
+      const int32_t at = s.all.at[tid];
+      uint32_t c = c0;
+      uint64_t w = w0;
+      for (uint32_t i = 0; i < m; ++i) {
+        const uint32_t ki = s.all.key[i];
+        if (ki < k || (ki == k && s.all.at[i] < at)) {
+          ++c;
+          w += s.all.w[i];
+        }
+      }
+      const uint64_t mine = by_weight ? w : c, with = mine + (by_weight ? s.all.w[tid] : 1u);
+      if (mine < target && target <= with) {
+        s.place = Place{k, 0, c, w, s.all.w[tid]};
+        s.at = rank == 0 ? at : -1;
+      }
+    }
+    __syncthreads();
+    return s.place;
   };
-  const int32_t k = greedy ? 1 : a.top_k ? a.top_k[r] : 0;
-  if (k > 0 && static_cast<uint32_t>(k) < live) {
-    find(s, row, best, shift, false, k, false);
-    limit();
-  }
-  const float p = a.top_p && !greedy ? a.top_p[r] : 1.0f;
-  const float least = a.min_p && !greedy ? a.min_p[r] : 0.0f;
-  if (p < 1.0f) {
-    const double part = ceil(static_cast<double>(p) * static_cast<double>(total));
-    const uint64_t need = part < 1.0 ? 1u : part < static_cast<double>(total) ? static_cast<uint64_t>(part) : total;
-    find(s, row, best, shift, true, need, false);
-    limit();
-  }
-  if (least > 0.0f) {
-    const uint64_t w0 = static_cast<uint64_t>(ceil(static_cast<double>(fminf(least, 1.0f)) * static_cast<double>(kOne)));
-    uint32_t c = 0;
-    uint64_t sum = 0;
-    row.each([&](float x, int32_t) {
-      const uint64_t w = s.weigh(x);
-      if (w >= w0) {
+  auto heavy = [&](uint64_t least, uint32_t& c, uint64_t& sum) {
+    row.template each<T>([&](float x, int32_t) {
+      const uint64_t w = weigh(x);
+      if (w >= least) {
         ++c;
         sum += w;
       }
     });
-    block_sums(s, c, sum);
-    if (c < kept) {
-      kept = c;
-      total = sum;
+    block_sums<T>(s, c, sum);
+    if (tid == 0) {
+      s.had_c = c;
+      s.had_w = sum;
     }
-    __syncthreads();
+    cluster.sync();
+    c = 0;
+    sum = 0;
+    for (int i = 0; i < kPeers; ++i) {
+      c += cluster.map_shared_rank(&s, i)->had_c;
+      sum += cluster.map_shared_rank(&s, i)->had_w;
+    }
+  };
+  auto where = [&](const Place& p) {
+    if (s.at != -2) return;
+    uint32_t mine = 0, seen = 0;
+    uint64_t none = 0;
+    row.template each<T>([&](float x, int32_t) { mine += Logit<E>::key(x) == p.key ? 1u : 0u; });
+    block_sums<T>(s, mine, none);
+    if (tid == 0) {
+      s.n = mine;
+      s.at = -1;
+    }
+    cluster.sync();
+    for (int i = 0; i < rank; ++i) seen += cluster.map_shared_rank(&s, i)->n;
+    if (seen <= p.nth && p.nth < seen + mine) nth_of<E, T>(s, row, p.key, p.nth - seen);
+  };
+  draw(a, r, s, greedy, s.sums[0].count[kBins - 1], s.sums[0].weight[kBins - 1], find, heavy, where);
+}
+
+template <typename E>
+__global__ void __launch_bounds__(kThreads, 2) sample_binned_kernel(const SampleArgs a) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  Binned& s = *reinterpret_cast<Binned*>(smem_raw);
+  const cg::cluster_group cluster = cg::this_cluster();
+  if (threadIdx.x < 64) s.pow2[threadIdx.x] = kPow2[threadIdx.x];
+  grid_dependency_wait();
+  left_rows<kThreads>(a, s, cluster, [&](int64_t r) { sample_binned<E>(a, r, s, cluster); });
+}
+
+// ---------------------------------------------------------------- rows that their largest tokens decide
+// The first kernel: a cluster a row, one pass over it.  From a sample of the row, spread over it, comes a bound that about as many
+// of its tokens pass as are wanted.  Tokens at the bound and above go into a list; the others' weights are only summed, in
+// fp32 with an error that is bounded.  The cluster's first CTA puts the list in order and sums its weights up exactly.  Where
+// what is kept ends inside the list, or the token is inside it for the least and the largest sum that the others can have, this
+// is the result; a row of which neither holds, or whose list overflows, is left to the second kernel.
+constexpr int kHeadThreads = 512, kHeadWarps = kHeadThreads / 32;
+constexpr int kCap = 4096;       // tokens of a list
+constexpr int kWhole = 2048;     // rows of up to so many are taken whole
+constexpr float kWant = 500.0f, kMostWanted = 2600.0f;  // tokens that the list is to have
+constexpr int kSpread = 1024;    // bins of the list's order
+constexpr uint32_t kSame = 512;  // tokens of one of them at most
+constexpr int kMostCtas = 8;     // of a cluster
+
+struct Head {
+  float x[kCap];     // the list, then in order
+  int32_t at[kCap];
+  union {
+    struct {
+      float x2[kCap];  // by bins
+      int32_t at2[kCap];
+    };
+    uint64_t sum[kCap];  // running weights
+  };
+  uint32_t upto[kSpread];
+  uint64_t pow2[64];
+  uint64_t red_w[kHeadWarps], red_low[kHeadWarps];
+  int32_t red[kHeadWarps];
+  float sample[kHeadThreads];
+  int32_t reach[kHeadWarps];
+  // of every CTA of the cluster: its bound, the others' weights in units of 2^-28 2^(their reference), that, and their number
+  float bound[kMostCtas], ref[kMostCtas];
+  uint64_t rest[kMostCtas];
+  uint32_t others[kMostCtas];
+  uint32_t n, bad;
+  int32_t place;
+  Weigher weigh;
+  uint64_t rest_low, rest_high;  // limits of the others' weight
+  uint64_t asked[2], low_w;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// Floats as integers in the same order.
+__device__ __forceinline__ int32_t in_order(float x) {
+  const int32_t i = __float_as_int(x);
+  return i ^ (i >> 31 & 0x7fffffff);
+}
+__device__ __forceinline__ float from_order(int32_t i) { return __int_as_float(i ^ (i >> 31 & 0x7fffffff)); }
+
+// The largest of a vector's elements, NaN if any is.
+__device__ __forceinline__ float most_of(const uint4& q, const float*, const uint16_t*) {
+  uint32_t a, b;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(q.x), "r"(q.y));
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(q.z), "r"(q.w));
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(a << 16)), "f"(__uint_as_float(a & 0xffff0000u)));
+  return r;
+}
+__device__ __forceinline__ float most_of(const uint4&, const float* x, const float*) {
+  float a, b;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(x[0]), "f"(x[1]));
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(x[2]), "f"(x[3]));
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(a), "f"(b));
+  return a;
+}
+
+// The first of the n tokens in order whose running weight reaches target, n - 1 if none.
+__device__ __forceinline__ int32_t first_place(const Head& s, int32_t n, uint64_t target) {
+  int32_t lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int32_t mid = (lo + hi) / 2;
+    if (s.sum[mid] >= target)
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  return lo;
+}
+// The first of them that weighs less than w, n if none (the first weighs as much as any may be asked).
+__device__ __forceinline__ int32_t first_light(const Head& s, int32_t n, uint64_t w) {
+  int32_t lo = 1, hi = n;
+  while (lo < hi) {
+    const int32_t mid = (lo + hi) / 2;
+    if (s.sum[mid] - s.sum[mid - 1] < w)
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  return lo;
+}
+// f of the weight of what is kept, or of the least and the largest that it can be, in every thread (f is in 64-bit floats, of
+// which an SM has few: two threads compute it).
+template <class F>
+__device__ __forceinline__ void ask(Head& s, uint64_t (&out)[2], uint64_t least, uint64_t most, F f) {
+  if ((threadIdx.x & ~32u) == 0) s.asked[threadIdx.x >> 5] = f(threadIdx.x ? most : least);
+  __syncthreads();
+  out[0] = s.asked[0];
+  out[1] = s.asked[1];
+  __syncthreads();
+}
+
+template <typename E>
+__global__ void __launch_bounds__(kHeadThreads, 3) sample_head_kernel(const SampleArgs a) {
+  constexpr int VEC = Logit<E>::kVec, kDeep = 4, kPicks = 8 / VEC;
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  Head& s = *reinterpret_cast<Head*>(smem_raw);
+  const cg::cluster_group cluster = cg::this_cluster();
+  const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int64_t r = blockIdx.x / ctas;
+  const Row<E> row(static_cast<const E*>(a.logits) + r * a.ld, a.V, rank, ctas);
+  const int32_t v0 = row.v0, v1 = row.v1;
+  if (tid < 64) s.pow2[tid] = kPow2[tid];
+  if (tid == 0) s.n = s.bad = 0;
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const float t = a.temperature ? a.temperature[r] : 1.0f;
+  const int32_t k = a.top_k ? a.top_k[r] : 0;
+  const bool greedy = t == 0.0f, plain = greedy || (t >= 0x1p-10f && t <= 0x1p10f);
+  if (!(t >= 0.0f) || !plain) {  // (one for all CTAs of the cluster)
+    if (rank == 0 && tid == 0) a.tokens[r] = kUndecided;
+    return;
+  }
+  // c = log2(e) / T as a float and a positive rest (with which -inf stays -inf)
+  float c_hi, c_lo;
+  {
+    const float by = greedy ? 1.0f : t;
+    c_hi = __fdiv_rn(1.44269504f, by);
+    c_lo = __fdiv_rn(fmaf(-c_hi, by, 1.44269504f) + 1.925963e-8f, by);
+    if (!(c_lo > 0.0f)) {
+      c_hi = __uint_as_float(__float_as_uint(c_hi) - 1u);
+      c_lo = __fdiv_rn(fmaf(-c_hi, by, 1.44269504f) + 1.925963e-8f, by);
+    }
   }
 
-  // the first whose running weight passes u of the whole
-  const double part = floor(static_cast<double>(a.u[r]) * static_cast<double>(total));
-  const uint64_t pass = !(part > 0.0) ? 0u : part < static_cast<double>(total - 1) ? static_cast<uint64_t>(part) : total - 1;
-  find(s, row, best, shift, true, pass + 1, true);
-  if (threadIdx.x == 0) {
-    a.tokens[r] = s.at;
-    if (a.logprob) {  // ln(w / total), where w is most of it from what is left
-      const float rest = static_cast<float>(total - s.w) / static_cast<float>(total);
-      a.logprob[r] = rest < 0.5f ? log1pf(-rest) : logf(static_cast<float>(s.w) / static_cast<float>(total));
+  // The bound: of the sample, the largest of 8 elements a thread; of a share q of the row, one of 8 is in it with
+  // 1 - (1 - q)^8.  In two rounds each warp counts how many of the threads reach one of 16 values between the largest of all and
+  // the least that can matter.
+  float bound = kLowest;
+  if (a.V > kWhole && v1 > v0) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kPicks; ++i) {
+      const uint4 q = row.vec(v0 + static_cast<int32_t>(static_cast<int64_t>(tid * kPicks + i) * (v1 - v0) / (kHeadThreads * kPicks)));
+      float x[VEC];
+      Logit<E>::get(q, x);
+      top = fmaxf(top, most_of(q, x, static_cast<const E*>(nullptr)));
+    }
+    s.sample[tid] = top;
+    const int32_t highest = __reduce_max_sync(0xffffffffu, in_order(top));
+    if (lane == 0) s.red[warp] = highest;
+    const float want = greedy ? 64.0f : k > 0 ? fminf(fmaxf(1.25f * k + 100.0f, kWant), kMostWanted) : kWant;
+    const float miss = fmaxf(1.0f - want / a.V, 0.0f), miss2 = miss * miss, miss4 = miss2 * miss2;
+    const int32_t reach = max(static_cast<int32_t>(kHeadThreads * (1.0f - miss4 * miss4)), 4);
+    __syncthreads();
+    int32_t most = s.red[0];
+#pragma unroll
+    for (int i = 1; i < kHeadWarps; ++i) most = max(most, s.red[i]);
+    const float hi = from_order(most);
+    float lo = fmaxf(hi - 32.0f * (greedy ? 1.0f : t), kLowest), step = (hi - lo) * (1.0f / 17.0f);
+    if (hi > -INFINITY && hi < INFINITY) {
+      float mine[kHeadThreads / 32];
+#pragma unroll
+      for (int i = 0; i < kHeadThreads / 32; ++i) mine[i] = s.sample[32 * i + lane];
+      bound = lo;
+#pragma unroll
+      for (int round = 0; round < 2; ++round) {
+        const float at = bound + step * (warp + 1);
+        int32_t has = 0;
+#pragma unroll
+        for (int i = 0; i < kHeadThreads / 32; ++i) has += mine[i] >= at ? 1 : 0;
+        has = __reduce_add_sync(0xffffffffu, has);
+        if (lane == 0) s.reach[warp] = has;
+        __syncthreads();
+        int32_t up = 0;
+#pragma unroll
+        for (int i = 0; i < kHeadWarps; ++i) up += s.reach[i] >= reach ? 1 : 0;
+        bound += step * up;
+        step *= 1.0f / 17.0f;
+        __syncthreads();
+      }
     }
   }
+  const float ref = bound > -1e30f ? bound * c_hi : 0.0f;
+  // (constants of the exact weights: 64-bit floats, beside the pass)
+  if (tid == kHeadThreads - 1) s.weigh = weigher(0.0f, greedy ? 1.0f : t, s.pow2);
+
+  // the pass over the row
+  uint64_t rest = 0;
+  auto one = [&](float x, int32_t at) -> float {  // a weight, or a token of the list
+    if (x < bound) return ex2(fmaf(x, c_lo, fmaf(x, c_hi, -ref)));
+    if (!(x < INFINITY)) s.bad = 1;
+    const uint32_t i = atomicAdd(&s.n, 1u);
+    if (i < kCap) {
+      s.x[i] = x;
+      s.at[i] = at;
+    }
+    return 0.0f;
+  };
+  auto vec = [&](const uint4& q, int32_t v) {
+    float x[VEC], w[VEC];
+    Logit<E>::get(q, x);
+    if (!(most_of(q, x, static_cast<const E*>(nullptr)) < bound)) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) w[e] = one(x[e], row.head + v * VEC + e);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) w[e] = ex2(fmaf(x[e], c_lo, fmaf(x[e], c_hi, -ref)));
+    }
+#pragma unroll
+    for (int o = VEC / 2; o > 0; o >>= 1)
+#pragma unroll
+      for (int e = 0; e < o; ++e) w[e] += w[e + o];
+    rest += __float2uint_rn(w[0] * 0x1p28f);
+  };
+  int32_t v = v0 + tid;
+#pragma unroll 1
+  for (; v + (kDeep - 1) * kHeadThreads < v1; v += kDeep * kHeadThreads) {
+    uint4 q[kDeep];
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) q[i] = row.vec(v + i * kHeadThreads);
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) vec(q[i], v + i * kHeadThreads);
+  }
+#pragma unroll 1
+  for (; v < v1; v += kHeadThreads) vec(row.vec(v), v);
+  if (row.first && tid < row.head) rest += __float2uint_rn(one(Logit<E>::get(row.p + tid), tid) * 0x1p28f);
+  if (row.last && row.tail() + tid < row.V)
+    rest += __float2uint_rn(one(Logit<E>::get(row.p + row.tail() + tid), row.tail() + tid) * 0x1p28f);
+
+  // everything to the first CTA
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
+  if (lane == 0) s.red_w[warp] = rest;
+  __syncthreads();
+  const uint32_t mine = s.n;
+  if (ctas > 1) cluster.sync();  // (the first CTA's counters are set, and its own tokens counted)
+  Head& f = *cluster.map_shared_rank(&s, 0);
+  {
+    if (tid == 0) {
+      rest = 0;
+      for (int i = 0; i < kHeadWarps; ++i) rest += s.red_w[i];
+      f.rest[rank] = rest;
+      f.bound[rank] = bound;
+      f.ref[rank] = ref;
+      f.others[rank] = static_cast<uint32_t>(row.count()) - mine;
+      if (rank > 0) {
+        if (s.bad) f.bad = 1;
+        s.place = static_cast<int32_t>(atomicAdd(&f.n, mine));
+      }
+    }
+    __syncthreads();
+    if (rank > 0) {
+      const uint32_t from = s.place;
+      if (mine <= kCap && from + mine <= kCap)
+        for (uint32_t i = tid; i < mine; i += kHeadThreads) {
+          f.x[from + i] = s.x[i];
+          f.at[from + i] = s.at[i];
+        }
+    }
+  }
+  if (ctas > 1) cluster.sync();
+  if (rank > 0) return;
+
+  // ---- the list in order
+  const uint32_t n_all = s.n;
+  const bool bad = s.bad || n_all == 0;
+  if (bad || n_all > kCap) {
+    if (tid == 0) {
+      a.tokens[r] = bad ? -1 : kUndecided;
+      if (a.logprob && bad) a.logprob[r] = __uint_as_float(0x7fffffffu);
+    }
+    return;
+  }
+  float floor_ = kLowest;
+  for (int i = 0; i < ctas; ++i) floor_ = fmaxf(floor_, s.bound[i]);
+  int32_t top = in_order(-INFINITY);
+  for (uint32_t i = tid; i < n_all; i += kHeadThreads) top = max(top, in_order(s.x[i]));
+  top = __reduce_max_sync(0xffffffffu, top);
+  if (lane == 0) s.red[warp] = top;
+  for (int i = tid; i < kSpread; i += kHeadThreads) s.upto[i] = 0;
+  __syncthreads();
+  for (int i = 0; i < kHeadWarps; ++i) top = max(top, s.red[i]);
+  const float max_x = from_order(top);
+  Weigher weigh = s.weigh;
+  weigh.max = max_x;
+  // Tokens below every CTA's bound, or without weight, are not put in order; the former's weights are summed.
+  const float cut = weigh.cut, span = fminf(max_x - floor_, cut);
+  const float scale = span > 0.0f && span < 1e37f ? (kSpread - 1) / span : 0.0f;
+  auto bin_of = [&](float x) { return min(static_cast<int>((max_x - x) * scale), kSpread - 1); };
+  for (uint32_t i = tid; i < n_all; i += kHeadThreads) {
+    const float x = s.x[i];
+    if (x >= floor_ && max_x - x < cut) atomicAdd(&s.upto[bin_of(x)], 1u);
+  }
+  __syncthreads();
+  {  // counts to first places
+    constexpr int kPer = kSpread / kHeadThreads;
+    uint32_t c[kPer], sum = 0;
+    bool full = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      c[i] = sum;
+      const uint32_t here = s.upto[tid * kPer + i];
+      full |= here > kSame;
+      sum += here;
+    }
+    if (__syncthreads_or(full)) {
+      if (tid == 0) a.tokens[r] = kUndecided;
+      return;
+    }
+    uint32_t upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    if (lane == 31) s.red[warp] = upto;
+    __syncthreads();
+    uint32_t base = upto - sum;
+    for (int i = 0; i < warp; ++i) base += s.red[i];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) s.upto[tid * kPer + i] = base + c[i];
+  }
+  __syncthreads();
+  uint64_t low = 0;
+  for (uint32_t i = tid; i < n_all; i += kHeadThreads) {
+    const float x = s.x[i];
+    if (x >= floor_ && max_x - x < cut) {
+      const uint32_t j = atomicAdd(&s.upto[bin_of(x)], 1u);  // (afterwards: the next bin's first place)
+      s.x2[j] = x;
+      s.at2[j] = s.at[i];
+    } else {
+      low += weigh(x);
+    }
+  }
+  __syncthreads();
+  const int32_t n = s.upto[kSpread - 1];
+  for (int32_t i = tid; i < n; i += kHeadThreads) {
+    const float x = s.x2[i];
+    const int32_t at = s.at2[i], b = bin_of(x), from = b ? s.upto[b - 1] : 0, to = s.upto[b];
+    int32_t j = from;
+    for (int32_t e = from; e < to; ++e) {
+      const float y = s.x2[e];
+      j += y > x || (y == x && s.at2[e] < at) ? 1 : 0;
+    }
+    s.x[j] = x;
+    s.at[j] = at;
+  }
+  __syncthreads();
+  {  // running weights
+    constexpr int kEach = kCap / kHeadThreads;
+    const int32_t per = (n + kHeadThreads - 1) / kHeadThreads, i0 = tid * per;
+    uint64_t own[kEach], upto = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (i < per) {
+        if (i0 + i < n) upto += weigh(s.x[i0 + i]);
+        own[i] = upto;
+      }
+    const uint64_t mine_w = upto;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint64_t y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) low += __shfl_xor_sync(0xffffffffu, low, o);
+    if (lane == 31) s.red_w[warp] = upto;
+    if (lane == 0) s.red_low[warp] = low;
+    __syncthreads();
+    uint64_t run = upto - mine_w;
+#pragma unroll
+    for (int i = 0; i < kHeadWarps - 1; ++i) run += i < warp ? s.red_w[i] : 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (i < per && i0 + i < n) s.sum[i0 + i] = run + own[i];
+  }
+
+  // ---- the weight of the whole row, between low_all and high_all
+  bool known = !(max_x - floor_ < cut);  // what is kept ends in the list: here, as all else weighs nothing
+  if (!known && warp == 0) {
+    uint64_t rest_sum = lane < kHeadWarps ? s.red_low[lane] : 0, off = 0;
+    if (lane < ctas) {
+      const double down = fmax(static_cast<double>(max_x) * c_hi + static_cast<double>(max_x) * c_lo - s.ref[lane], 0.0);
+      if (down < 60.0) {  // (else it weighs nothing)
+        const uint64_t tq = static_cast<uint64_t>(down * 0x1p56);
+        const uint64_t w = __umul64hi(s.rest[lane] << 15, exp2_fraction(tq, s.pow2)) >> (2 + static_cast<int>(tq >> 56));
+        // Each weight is off by 2^-22 (ex2), its argument's two roundings, |t| 2^-24 with |t| 2^t at most 0.53 of the bound's
+        // weight, three additions, and half a unit when it is rounded to one.
+        rest_sum += w;
+        off = (w >> 20) + (s.others[lane] * weigh(s.bound[lane]) >> 24) + s.others[lane] / 2 + 2;
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      rest_sum += __shfl_xor_sync(0xffffffffu, rest_sum, o);
+      off += __shfl_xor_sync(0xffffffffu, off, o);
+    }
+    if (lane == 0) {
+      s.rest_low = rest_sum > off ? rest_sum - off : 0;
+      s.rest_high = rest_sum + off;
+    }
+  }
+  __syncthreads();
+  const uint64_t head = s.sum[n - 1];
+  uint64_t low_all = head, high_all = head, total = head;
+  if (!known) {
+    low_all += s.rest_low;
+    high_all += s.rest_high;
+  }
+  int32_t kept = n;
+  bool decided = true;
+  if (greedy || (k > 0 && k <= n)) {
+    kept = greedy ? 1 : k;
+    total = s.sum[kept - 1];
+    known = true;
+  } else if (k > 0 && !known) {
+    decided = false;
+  }
+  const float p = a.top_p && !greedy ? a.top_p[r] : 1.0f;
+  const float least = a.min_p && !greedy ? a.min_p[r] : 0.0f;
+  if (decided && p < 1.0f) {
+    uint64_t need[2];
+    ask(s, need, known ? total : low_all, known ? total : high_all, [&](uint64_t whole) { return reaches(p, whole); });
+    const int32_t m = first_place(s, n, need[0]);
+    decided = need[1] <= head && s.sum[m] >= need[1];
+    if (decided && m + 1 <= kept) {
+      kept = m + 1;
+      total = s.sum[m];
+    }
+    known = true;
+  }
+  if (decided && least > 0.0f) {
+    if (tid == 0) s.low_w = least_of(least);
+    __syncthreads();
+    const int32_t m = first_light(s, n, s.low_w);
+    if (m < kept) {
+      kept = m;
+      total = s.sum[m - 1];
+      known = true;
+    } else if (m == n && !known) {
+      decided = false;
+    }
+  }
+  if (decided) {
+    uint64_t pass[2];
+    const float u = a.u[r];
+    ask(s, pass, known ? total : low_all, known ? total : high_all, [&](uint64_t whole) { return passes(u, whole); });
+    const int32_t m = first_place(s, n, pass[0]);
+    if (pass[1] <= head && s.sum[m] >= pass[1]) {
+      if (tid == 0) {
+        a.tokens[r] = s.at[m];
+        if (a.logprob)
+          a.logprob[r] = ln_of(s.sum[m] - (m ? s.sum[m - 1] : 0), known ? total : low_all + (high_all - low_all) / 2);
+      }
+      return;
+    }
+  }
+  if (tid == 0) a.tokens[r] = kUndecided;
+}
+
+// A kernel whose launch may begin beside the end of the one ahead (it waits by itself), in clusters of `ctas`.
+template <class S>
+cudaError_t go(void (*kern)(SampleArgs), const SampleArgs& a, int64_t rows, int ctas, int threads, std::atomic<uint64_t>& ready,
+               cudaStream_t st) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = uint64_t(1) << (dev & 63);  // ready: devices on which the kernel may use its shared memory
+  if (!(ready.load(std::memory_order_relaxed) & bit)) {
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(S)));
+    if (e != cudaSuccess) return e;
+    ready.fetch_or(bit, std::memory_order_relaxed);
+  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(rows * ctas));
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = sizeof(S);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ctas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
 template <typename E>
 cudaError_t run_sample(const SampleArgs& a, cudaStream_t st) {
-  static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
+  static std::atomic<uint64_t> ready[3];
+  // CTAs a row: as many as there are SMs for, with two vectors a thread or more
+  int ctas = 1;
+  while (ctas < kMostCtas && a.R * ctas * 2 <= 304 && a.V / Logit<E>::kVec >= 2 * kHeadThreads * ctas * 2) ctas *= 2;
+  const cudaError_t e = go<Head>(sample_head_kernel<E>, a, a.R, ctas, kHeadThreads, ready[0], st);
   if (e != cudaSuccess) return e;
-  const uint64_t bit = uint64_t(1) << (dev & 63);
-  if (!(ready.load(std::memory_order_relaxed) & bit)) {
-    e = cudaFuncSetAttribute(sample_kernel<E>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(Shared)));
-    if (e != cudaSuccess) return e;
-    ready.fetch_or(bit, std::memory_order_relaxed);
-  }
-  sample_kernel<E><<<static_cast<unsigned>(a.R), kThreads, sizeof(Shared), st>>>(a);
-  return cudaGetLastError();
+  if (sizeof(E) == 2 && a.V <= kMostCounted)
+    return go<Counts>(sample_counts_kernel, a, std::min<int64_t>(a.R, 152 / kPeers), kPeers, kCountThreads, ready[1], st);
+  return go<Binned>(sample_binned_kernel<E>, a, std::min<int64_t>(a.R, 304 / kPeers), kPeers, kThreads, ready[2], st);
 }
 
 }  // namespace
