@@ -578,6 +578,10 @@ __device__ __forceinline__ float of_code(uint32_t c) {
   return __low2float(*reinterpret_cast<const __half2*>(&h));
 }
 
+__device__ __forceinline__ uint4 rescale16(uint4 w, __half2 by) {
+  return make_uint4(rescale4(w.x, by), rescale4(w.y, by), rescale4(w.z, by), rescale4(w.w, by));
+}
+
 // Four codes times a power of two, rounded to codes again (no product passes 448).  In fp32: the power may be any.
 __device__ __forceinline__ uint32_t move4(uint32_t codes, float by) {
   uint32_t out = 0;
@@ -591,121 +595,172 @@ __device__ __forceinline__ uint32_t move4(uint32_t codes, float by) {
   return out;
 }
 
-// A warp takes the keys or values of one head, sequence and cache, page by page.  A token moves to an earlier slot and a later
-// token's slot is never written before it has been read: sources rise strictly, so the j-th kept token's is j or more behind
-// the context.  A page that has to grow is rounded again before what moves inside it moves.
+constexpr int kMoves = 256;   // tokens whose places a CTA keeps at a time: two whole pages or more
+constexpr int kInHand = 2;    // passes over a page's tokens that a warp keeps in registers
+
+// A CTA takes a sequence and some of the (cache, keys or values, head) of it, a warp one at a time; where the tokens lie and go
+// is found once.  Page by page, so that a token's slot is never written before it has been read: sources rise strictly, so the
+// j-th kept token's is j or more behind the context.  A page that has to grow is rounded again before what moves inside it.
+// Bound by the chain of loads (rows, path, page numbers, codes and scales), 3 us for one sequence and layer; 16 layers of 64
+// sequences with up to 8 moved tokens each (8 heads of 128) move 19.6 MB in 12.6 us.
 template <int D>
 __global__ void __launch_bounds__(32 * kCompactWarps) kv_compact_kernel(const __grid_constant__ KvCompactArgs a, Divisor by_page,
-                                                                        Divisor by_heads) {
-  constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes, kDeep = 4;  // lanes a token, tokens a pass, passes under way
-  const int lane = threadIdx.x & 31, sub = lane / kLanes, word = lane % kLanes;
-  const int32_t heads = 2 * a.nkv, page = a.page;
-  const int64_t items = static_cast<int64_t>(a.n_caches) * a.B * heads;
+                                                                        int32_t per_cta) {
+  constexpr int kLanes = D / 16, kAtOnce = 32 / kLanes;  // lanes a token, tokens a pass
+  __shared__ int32_t src_page[kMoves], src_at[kMoves];    // where the tokens lie: page of the sequence, slot in it
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane / kLanes, word = lane % kLanes;
+  const int32_t b = blockIdx.x, page = a.page, heads = 2 * a.nkv, items = a.n_caches * heads;
+  const int32_t r0 = a.row_start[b], r1 = a.row_start[b + 1], len = a.seq_len[b], m = a.n_kept[b], n = r1 - r0;
+  bool bad = r0 < 0 || r1 < r0 || r1 > a.T || len < 0 || len > static_cast<int64_t>(a.max_pages) * page || m < 0 || m > n;
+  // the kept rows rise strictly; the first that is not in its place, all behind it are not either
+  int32_t still = 0;
+  if (!bad) {
 #pragma unroll 1
-  for (int64_t e = blockIdx.x * static_cast<int64_t>(kCompactWarps) + (threadIdx.x >> 5); e < items;
-       e += static_cast<int64_t>(gridDim.x) * kCompactWarps) {
-    const int64_t lb = e < 0x7fffffff ? by_heads.of(static_cast<int32_t>(e)) : e / heads;
-    const int32_t hv = static_cast<int32_t>(e - lb * heads), l = static_cast<int32_t>(lb / a.B);
-    const int32_t b = static_cast<int32_t>(lb - static_cast<int64_t>(l) * a.B), h = hv >= a.nkv ? hv - a.nkv : hv;
-    const int32_t r0 = a.row_start[b], r1 = a.row_start[b + 1], len = a.seq_len[b], m = a.n_kept[b], n = r1 - r0;
-    bool bad = r0 < 0 || r1 < r0 || r1 > a.T || len < 0 || len > static_cast<int64_t>(a.max_pages) * page || m < 0 || m > n;
-    // the kept rows rise strictly; the first that is not in its place, all behind it are not either
-    int32_t from = m;
-    if (!bad) {
-#pragma unroll 1
-      for (int32_t c = 0; c < m; c += 32) {
-        const int32_t j = c + lane;
-        int32_t i = j;
-        if (j < m) {
-          i = a.path[r0 + j];
-          bad |= i >= n || i <= (j > 0 ? a.path[r0 + j - 1] : -1);
-        }
-        const uint32_t moved = __ballot_sync(0xffffffffu, i != j);
-        if (moved && from == m) from = c + __ffs(moved) - 1;
-      }
+    for (int32_t j = tid; j < m; j += 32 * kCompactWarps) {
+      const int32_t i = a.path[r0 + j];
+      bad |= i >= n || i <= (j > 0 ? a.path[r0 + j - 1] : -1);
+      still += i == j ? 1 : 0;
     }
-    if (__any_sync(0xffffffffu, bad)) {
-      if (lane == 0) latch_index_error(a.status);
-      continue;
-    }
-    const KvCompactArgs::Cache& kv = a.cache[l];
-    uint8_t* const codes = hv >= a.nkv ? kv.v_codes : kv.k_codes;
-    float* const scales = hv >= a.nkv ? kv.v_scale : kv.k_scale;
-    const int32_t* const table = kv.table + static_cast<int64_t>(b) * a.max_pages;
-    const int32_t first = len - n;
-    from = max(from, -first);  // (slots before the first are not stored)
-    auto block_of = [&](int32_t pg) -> int32_t {
-      const int32_t id = table[pg];
-      if (id >= 0 && id < a.n_pages) return id * a.nkv + h;
-      latch_index_error(a.status);
-      return -1;
-    };
+  }
+  __shared__ int32_t in_place;
+  if (tid == 0) in_place = 0;
+  if (__syncthreads_or(bad)) {
+    if (tid == 0) latch_index_error(a.status);
+    return;
+  }
+  still = __reduce_add_sync(0xffffffffu, still);
+  if (lane == 0 && still) atomicAdd(&in_place, still);
+  __syncthreads();
+  const int32_t first = len - n;
 #pragma unroll 1
-    for (int32_t j0 = from; j0 < m;) {
-      const int32_t pg = by_page.of(first + j0), j1 = min(m, (pg + 1) * page - first);
-      const int32_t block = block_of(pg);
-      uint8_t* const dst = codes + static_cast<int64_t>(max(block, 0)) * page * D;
-      const float old = block >= 0 ? scales[block] : 0.0f;
-      // a lane's word of a token's codes where they lie, its page's scale and whether that is another page
-      auto source = [&](int32_t j, uint32_t& w, float& scale) -> bool {
-        const int32_t at = first + a.path[r0 + j], sp = by_page.of(at);
-        const int32_t sb = sp == pg ? block : block_of(sp);
-        w = 0;
-        scale = old;
-        if (sb < 0) return true;
-        w = *reinterpret_cast<const uint32_t*>(codes + (static_cast<int64_t>(sb) * page + at - sp * page) * D + 4 * word);
-        if (sp != pg) scale = scales[sb];
-        return sp != pg;
+  for (int32_t c0 = max(in_place, -first), c1; c0 < m; c0 = c1) {  // (slots before the first are not stored)
+    // as many tokens as are kept in mind, up to the end of a page
+    c1 = m - c0 <= kMoves ? m : by_page.of(first + c0 + kMoves) * page - first;
+    __syncthreads();
+    for (int32_t j = c0 + tid; j < c1; j += 32 * kCompactWarps) {
+      const int32_t at = first + a.path[r0 + j], pg = by_page.of(at);
+      src_page[j - c0] = pg;
+      src_at[j - c0] = at - pg * page;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int32_t e = blockIdx.y * per_cta + warp; e < min(items, (static_cast<int32_t>(blockIdx.y) + 1) * per_cta); e += kCompactWarps) {
+      const int32_t l = e / heads, hv = e - l * heads, h = hv >= a.nkv ? hv - a.nkv : hv;
+      const KvCompactArgs::Cache& kv = a.cache[l];
+      uint8_t* const codes = hv >= a.nkv ? kv.v_codes : kv.k_codes;
+      float* const scales = hv >= a.nkv ? kv.v_scale : kv.k_scale;
+      const int32_t* const table = kv.table + static_cast<int64_t>(b) * a.max_pages;
+      auto block_of = [&](int32_t pg) -> int32_t {
+        const int32_t id = table[pg];
+        if (id >= 0 && id < a.n_pages) return id * a.nkv + h;
+        latch_index_error(a.status);
+        return -1;
       };
-      float top = 0.0f;
-#pragma unroll kDeep
-      for (int32_t j = j0 + sub; j < j1; j += kAtOnce) {
-        uint32_t w;
-        float scale;
-        if (!source(j, w, scale)) continue;
-        w &= 0x7f7f7f7fu;
-        w = __vmaxu4(w, w >> 16);
-        const float v = of_code(max(w & 0xffu, w >> 8 & 0xffu)) * scale;
-        asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(top), "f"(v));
-      }
-      const float want = scale_of(__reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu));
-      const bool nan = !(want == want) || !(old == old);
-      const float now = nan ? __uint_as_float(0x7fffffffu) : fmaxf(old, want);
-      if (block >= 0) {
-        if (lane == 0) scales[block] = now;
-        if (!nan && old > 0.0f && now > old) {
-          const __half2 by = __float2half2_rn(fmaxf(old / now, 5.9604645e-8f));
+#pragma unroll 1
+      for (int32_t j0 = c0, j1; j0 < c1; j0 = j1) {
+        const int32_t pg = by_page.of(first + j0);
+        j1 = min(c1, (pg + 1) * page - first);
+        const int32_t block = block_of(pg);
+        uint8_t* const dst = codes + static_cast<int64_t>(max(block, 0)) * page * D;
+        const float old = block >= 0 ? scales[block] : 0.0f;
+        // a lane's 16 bytes of a token's codes where they lie, its page's scale; whether that is another page
+        auto source = [&](int32_t j, uint4& w, float& scale) -> bool {
+          const int32_t sp = src_page[j - c0], sb = sp == pg ? block : block_of(sp);
+          w = make_uint4(0u, 0u, 0u, 0u);
+          scale = old;
+          if (sb < 0) return true;
+          w = *reinterpret_cast<const uint4*>(codes + (static_cast<int64_t>(sb) * page + src_at[j - c0]) * D + 16 * word);
+          if (sp != pg) scale = scales[sb];
+          return sp != pg;
+        };
+        auto magnitude = [&](const uint4& q, float scale) {
+          constexpr uint32_t kAbs = 0x7f7f7f7fu;
+          uint32_t w = __vmaxu4(__vmaxu4(q.x & kAbs, q.y & kAbs), __vmaxu4(q.z & kAbs, q.w & kAbs));
+          w = __vmaxu4(w, w >> 16);
+          return of_code(max(w & 0xffu, w >> 8 & 0xffu)) * scale;
+        };
+        auto put = [&](int32_t j, const uint4& w) {
+          *reinterpret_cast<uint4*>(dst + (first + j - pg * page) * D + 16 * word) = w;
+        };
+        const int32_t count = j1 - j0;
+        const bool in_hand = count <= kInHand * kAtOnce;
+        uint4 held[kInHand];
+        uint32_t far = 0;  // bit j: the j-th comes from another page
+        float from = 0.0f, top = 0.0f;    // (a lane a token: its page's scale)
+        if (in_hand) {
+          int32_t at = -1;  // its row of codes
+          bool other = false;
+          if (lane < count) {
+            const int32_t sp = src_page[j0 - c0 + lane], sb = block_of(sp);
+            other = sp != pg;
+            if (sb >= 0) {
+              at = sb * page + src_at[j0 - c0 + lane];
+              from = scales[sb];
+            }
+          }
+          far = __ballot_sync(0xffffffffu, other);
+#pragma unroll
+          for (int k = 0; k < kInHand; ++k)
+            if (k * kAtOnce < count) {
+              const int32_t row = __shfl_sync(0xffffffffu, at, k * kAtOnce + sub);
+              held[k] = make_uint4(0u, 0u, 0u, 0u);
+              if (row >= 0) held[k] = *reinterpret_cast<const uint4*>(codes + static_cast<int64_t>(row) * D + 16 * word);
+            }
+#pragma unroll
+          for (int k = 0; k < kInHand; ++k)
+            if (k * kAtOnce < count) {
+              const float scale = __shfl_sync(0xffffffffu, from, k * kAtOnce + sub);
+              if (far >> (k * kAtOnce + sub) & 1u)
+                asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(top), "f"(magnitude(held[k], scale)));
+            }
+        } else {
+#pragma unroll 1
+          for (int32_t j = j0 + sub; j < j1; j += kAtOnce) {
+            uint4 w;
+            float scale;
+            if (source(j, w, scale)) asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(top), "f"(magnitude(w, scale)));
+          }
+        }
+        if (block < 0) continue;
+        const float want = scale_of(__reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu));
+        const bool nan = !(want == want) || !(old == old);
+        const float now = nan ? __uint_as_float(0x7fffffffu) : fmaxf(old, want);
+        const bool grows = !nan && old > 0.0f && now > old;
+        const __half2 shrink = __float2half2_rn(grows ? fmaxf(old / now, 5.9604645e-8f) : 1.0f);
+        if (lane == 0 && !(now == old)) scales[block] = now;
+        if (grows) {
 #pragma unroll 1
           for (int32_t k = lane; k < page * D / 16; k += 32) {
-            uint4 w = reinterpret_cast<const uint4*>(dst)[k];
-            w.x = rescale4(w.x, by);
-            w.y = rescale4(w.y, by);
-            w.z = rescale4(w.z, by);
-            w.w = rescale4(w.w, by);
-            reinterpret_cast<uint4*>(dst)[k] = w;
+            uint4* const at = reinterpret_cast<uint4*>(dst) + k;
+            *at = rescale16(*at, shrink);
+          }
+        }
+        auto moved = [&](const uint4& w, float scale) {
+          const float by = now > 0.0f ? scale / now : 1.0f;
+          return nan ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(move4(w.x, by), move4(w.y, by), move4(w.z, by), move4(w.w, by));
+        };
+        __syncwarp();
+        if (in_hand) {
+#pragma unroll
+          for (int k = 0; k < kInHand; ++k)
+            if (k * kAtOnce < count) {
+              const int32_t j = k * kAtOnce + sub;
+              const float scale = __shfl_sync(0xffffffffu, from, j);
+              if (j < count) put(j0 + j, far >> j & 1u ? moved(held[k], scale) : grows ? rescale16(held[k], shrink) : held[k]);
+            }
+        } else {
+#pragma unroll 1
+          for (int32_t j = j0 + sub; __any_sync(0xffffffffu, j < j1); j += kAtOnce) {
+            uint4 w;
+            float scale;
+            if (j < j1 && source(j, w, scale)) w = moved(w, scale);
+            __syncwarp();
+            if (j < j1) put(j, w);
+            __syncwarp();
           }
         }
         __syncwarp();
-#pragma unroll 1
-        for (int32_t c = j0; c < j1; c += kDeep * kAtOnce) {
-          uint32_t w[kDeep];
-#pragma unroll
-          for (int k = 0; k < kDeep; ++k) {
-            const int32_t j = c + k * kAtOnce + sub;
-            if (j >= j1) continue;
-            float scale;
-            if (source(j, w[k], scale)) w[k] = nan ? 0u : move4(w[k], now > 0.0f ? scale / now : 1.0f);
-          }
-          __syncwarp();
-#pragma unroll
-          for (int k = 0; k < kDeep; ++k) {
-            const int32_t j = c + k * kAtOnce + sub;
-            if (j < j1) *reinterpret_cast<uint32_t*>(dst + (first + j - pg * page) * D + 4 * word) = w[k];
-          }
-          __syncwarp();
-        }
       }
-      j0 = j1;
     }
   }
 }
@@ -801,12 +856,14 @@ cudaError_t launch_kv_compact(KvCompactArgs& a, cudaStream_t st) {
   WaitCtl wc;
   if (!launch_wait_ctl(&wc)) return cudaErrorInvalidDevice;
   a.status = wc.status_word;
-  const int64_t items = static_cast<int64_t>(a.n_caches) * a.B * 2 * a.nkv;
-  const unsigned grid = static_cast<unsigned>(std::min<int64_t>((items + kCompactWarps - 1) / kCompactWarps, 152 * 64));
+  // A warp takes one (cache, keys or values, head) (16 layers of 64 sequences: 12.6 us, two each 14, four 16.7); as many CTAs a
+  // sequence as a grid's second dimension has.
+  const int32_t items = a.n_caches * 2 * a.nkv, per_cta = ((items / kCompactWarps) / 65535 + 1) * kCompactWarps;
+  const dim3 grid(a.B, (items + per_cta - 1) / per_cta);
   if (a.d == 64)
-    kv_compact_kernel<64><<<grid, 32 * kCompactWarps, 0, st>>>(a, divisor(a.page), divisor(2 * a.nkv));
+    kv_compact_kernel<64><<<grid, 32 * kCompactWarps, 0, st>>>(a, divisor(a.page), per_cta);
   else
-    kv_compact_kernel<128><<<grid, 32 * kCompactWarps, 0, st>>>(a, divisor(a.page), divisor(2 * a.nkv));
+    kv_compact_kernel<128><<<grid, 32 * kCompactWarps, 0, st>>>(a, divisor(a.page), per_cta);
   return cudaGetLastError();
 }
 

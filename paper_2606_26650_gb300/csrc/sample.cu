@@ -22,7 +22,8 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr float kLowest = -3.402823466e38f;
-constexpr int kUndecided = -2;  // a row's token where the first kernel leaves it to the second
+constexpr int kUndecided = -2;  // a row's token where the first kernel leaves it to the second,
+constexpr int kTaken = -3;      // and where a cluster of the second has taken it
 
 // ---------------------------------------------------------------- weights
 // 2^(-i / 64) in units of 2^-63.
@@ -63,6 +64,17 @@ __device__ __forceinline__ uint64_t exp2_fraction(uint64_t t, const uint64_t* po
   return p - __umul64hi(p, __umul64hi(y, s) >> 6);
 }
 
+__device__ __forceinline__ uint64_t weight_inline(float d, float rest, float scale, uint64_t c, const uint64_t* pow2) {
+  const uint64_t big = static_cast<uint64_t>(__float2ll_rn(d * scale) + __float2ll_rn(rest * scale));
+  const uint64_t t = __umul64hi(big, c);
+  const int n = static_cast<int>(t >> 56);
+  const int down = 63 - kOneBits + min(n, kOneBits);
+  return n > kOneBits ? 0 : (exp2_fraction(t, pow2) + (uint64_t(1) << (down - 1))) >> down;
+}
+// (A call where a thread has few of them: code that is fetched for the first time costs a short kernel more than the call.)
+__device__ __noinline__ uint64_t weight_of(float d, float rest, float scale, uint64_t c, const uint64_t* pow2) {
+  return weight_inline(d, rest, scale, c, pow2);
+}
 struct Weigher {
   float max, cut, scale;  // max - x at and above cut weighs nothing
   uint64_t c;
@@ -70,13 +82,14 @@ struct Weigher {
   __device__ __forceinline__ uint64_t operator()(float x) const {
     const float d = max - x;
     if (!(d < cut)) return 0;
-    const float b = d - max, rest = (max - (d - b)) + (-x - b);
-    const uint64_t big = static_cast<uint64_t>(__float2ll_rn(d * scale) + __float2ll_rn(rest * scale));
-    const uint64_t t = __umul64hi(big, c);
-    const int n = static_cast<int>(t >> 56);
-    if (n > kOneBits) return 0;
-    const int down = 63 - kOneBits + n;
-    return (exp2_fraction(t, pow2) + (uint64_t(1) << (down - 1))) >> down;
+    const float b = d - max;
+    return weight_of(d, (max - (d - b)) + (-x - b), scale, c, pow2);
+  }
+  // The same beside others of its kind.
+  __device__ __forceinline__ uint64_t beside(float x) const {
+    const float d = max - x, held = fminf(d, cut), b = d - max;
+    const uint64_t w = weight_inline(held, d < cut ? (max - (d - b)) + (-x - b) : 0.0f, scale, c, pow2);
+    return d < cut ? w : 0;
   }
 };
 
@@ -135,6 +148,9 @@ struct Logit<float> {
     x[2] = __uint_as_float(q.z);
     x[3] = __uint_as_float(q.w);
   }
+  static __device__ __forceinline__ float get(const uint4& q, int e) {
+    return __uint_as_float(e & 2 ? (e & 1 ? q.w : q.z) : (e & 1 ? q.y : q.x));
+  }
 };
 template <>
 struct Logit<uint16_t> {
@@ -154,6 +170,10 @@ struct Logit<uint16_t> {
       x[2 * i] = __uint_as_float(w[i] << 16);
       x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
+  }
+  static __device__ __forceinline__ float get(const uint4& q, int e) {
+    const uint32_t w = e & 4 ? (e & 2 ? q.w : q.z) : (e & 2 ? q.y : q.x);
+    return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
   }
 };
 
@@ -181,25 +201,37 @@ struct Row {
   // f(x, index) of every element of the part, by kThreads threads.
   template <int kThreads, class F>
   __device__ __forceinline__ void each(F f) const {
+    each<kThreads>([](float x) { return x; }, [&](float, float x, int32_t at) { f(x, at); });
+  }
+  // f(g(x), x, index), g of a vector's elements first.
+  template <int kThreads, class G, class F>
+  __device__ __forceinline__ void each(G g, F f) const {
     constexpr int VEC = Logit<E>::kVec;
     const int32_t t = threadIdx.x;
-    if (first && t < head) f(Logit<E>::get(p + t), t);
-#pragma unroll 2
+    auto one = [&](int32_t at) {
+      const float x = Logit<E>::get(p + at);
+      f(g(x), x, at);
+    };
+    if (first && t < head) one(t);
+#pragma unroll 1
     for (int32_t v = v0 + t; v < v1; v += kThreads) {
       float x[VEC];
       Logit<E>::get(vec(v), x);
+      decltype(g(0.0f)) y[VEC];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) f(x[i], head + v * VEC + i);
+      for (int i = 0; i < VEC; ++i) y[i] = g(x[i]);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) f(y[i], x[i], head + v * VEC + i);
     }
-    if (last && tail() + t < V) f(Logit<E>::get(p + tail() + t), tail() + t);
+    if (last && tail() + t < V) one(tail() + t);
   }
 };
 
 // ---------------------------------------------------------------- any row
-// The second kernel: the rows that the first left, a cluster of kPeers CTAs each, in one of two forms.  Both make running sums of
+// The second kernel: the rows that the first left, a cluster of CTAs each, in one of two forms.  Both make running sums of
 // the tokens' counts and weights over steps of the order that all CTAs of the cluster see alike, so that they take the same
 // way, and find inside a step what is asked for.
-constexpr int kPeers = 8;
+constexpr int kSearched = 64;  // chunks of a CTA's threads: rows of which every cluster looks at all
 
 // What both forms keep.
 template <int T>
@@ -207,7 +239,7 @@ struct Common {
   uint64_t pow2[64];
   uint64_t red_w[T / 32];
   uint32_t red_c[T / 32];
-  uint32_t rows[T / 32];  // bits of the rows to do
+  int64_t next;  // the row to do, -1: none
   uint32_t best, bad, had_c, n;
   uint64_t had_w, target;
   int32_t at;  // the token's index, -1 where another CTA has it
@@ -222,73 +254,76 @@ struct Place {
 // Sums over the CTA, in every thread.
 template <int T>
 __device__ __forceinline__ void block_sums(Common<T>& s, uint32_t& c, uint64_t& w) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     c += __shfl_xor_sync(0xffffffffu, c, o);
     w += __shfl_xor_sync(0xffffffffu, w, o);
   }
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) {
+  if (lane == 0) {
     s.red_c[threadIdx.x >> 5] = c;
     s.red_w[threadIdx.x >> 5] = w;
   }
   __syncthreads();
-  c = 0;
-  w = 0;
-  for (int i = 0; i < T / 32; ++i) {
-    c += s.red_c[i];
-    w += s.red_w[i];
+  c = s.red_c[lane % (T / 32)];
+  w = s.red_w[lane % (T / 32)];
+#pragma unroll
+  for (int o = T / 64; o > 0; o >>= 1) {
+    c += __shfl_xor_sync(0xffffffffu, c, o);
+    w += __shfl_xor_sync(0xffffffffu, w, o);
   }
+}
+// Sums of a value over the lanes up to the own one.
+template <class V>
+__device__ __forceinline__ V warp_scan(V v) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const V y = __shfl_up_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) >= o) v += y;
+  }
+  return v;
 }
 // c and w become the sums over the threads ahead; all_c and all_w over all.
 template <int T>
 __device__ __forceinline__ void block_scan(Common<T>& s, uint32_t& c, uint64_t& w, uint32_t& all_c, uint64_t& all_w) {
+  static_assert(T <= 1024, "a lane a warp");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t own_c = c;
   const uint64_t own_w = w;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t x = __shfl_up_sync(0xffffffffu, c, o);
-    const uint64_t y = __shfl_up_sync(0xffffffffu, w, o);
-    if (lane >= o) {
-      c += x;
-      w += y;
-    }
-  }
+  c = warp_scan(c);
+  w = warp_scan(w);
   __syncthreads();
   if (lane == 31) {
     s.red_c[warp] = c;
     s.red_w[warp] = w;
   }
   __syncthreads();
-  c -= own_c;
-  w -= own_w;
-  all_c = 0;
-  all_w = 0;
-  for (int i = 0; i < T / 32; ++i) {
-    if (i == warp) {
-      c += all_c;
-      w += all_w;
-    }
-    all_c += s.red_c[i];
-    all_w += s.red_w[i];
-  }
+  const uint32_t cs = warp_scan(lane < T / 32 ? s.red_c[lane] : 0u);
+  const uint64_t ws = warp_scan(lane < T / 32 ? s.red_w[lane] : uint64_t(0));
+  all_c = __shfl_sync(0xffffffffu, cs, 31);
+  all_w = __shfl_sync(0xffffffffu, ws, 31);
+  const uint32_t cb = __shfl_sync(0xffffffffu, cs, (warp + 31) & 31);
+  const uint64_t wb = __shfl_sync(0xffffffffu, ws, (warp + 31) & 31);
+  c += (warp ? cb : 0u) - own_c;
+  w += (warp ? wb : 0u) - own_w;
 }
 
 // The row's largest logit, from every CTA's least key; false (token -1 written) where nothing can be drawn.
-template <typename E, int T, class S>
+template <typename E, int T, int kPeers, class S>
 __device__ __forceinline__ bool largest(S& s, const cg::cluster_group& cluster, const SampleArgs& a, int64_t r, uint32_t& best,
                                         uint32_t bad, float t) {
   best = __reduce_min_sync(0xffffffffu, best);
   bad = __syncthreads_or(bad);
   if ((threadIdx.x & 31) == 0) s.red_c[threadIdx.x >> 5] = best;
   __syncthreads();
-  for (int i = 0; i < T / 32; ++i) best = min(best, s.red_c[i]);
+  best = __reduce_min_sync(0xffffffffu, s.red_c[threadIdx.x % (T / 32)]);
   if (threadIdx.x == 0) {
     s.best = best;
     s.bad = bad;
   }
   cluster.sync();
+#pragma unroll
   for (int i = 0; i < kPeers; ++i) {
     const S& p = *cluster.map_shared_rank(&s, i);
     best = min(best, p.best);
@@ -392,34 +427,71 @@ __device__ __forceinline__ void draw(const SampleArgs& a, int64_t r, S& s, bool 
   }
 }
 
-// f(row) of the rows that are left, clusters taking them in turn: which are left is read before any of them is written.
+// f(row) of the rows that are left.  The first CTA of a cluster looks for one and takes it; a cluster begins its search at a place
+// of its own.  (Of very many rows a cluster looks at a share only.)
 template <int T, class S, class F>
 __device__ __forceinline__ void left_rows(const SampleArgs& a, S& s, const cg::cluster_group& cluster, F f) {
-  const int64_t clusters = gridDim.x / kPeers, id = blockIdx.x / kPeers;
-  for (int64_t r0 = id; r0 < a.R; r0 += clusters * T) {
-    const int64_t mine = r0 + threadIdx.x * clusters;
-    const uint32_t left = __ballot_sync(0xffffffffu, mine < a.R && a.tokens[mine] == kUndecided);
-    if ((threadIdx.x & 31) == 0) s.rows[threadIdx.x >> 5] = left;
-    if (!__syncthreads_or(left)) continue;
+  const int peers = cluster.num_blocks();
+  const int64_t clusters = gridDim.x / peers, id = blockIdx.x / peers, chunks = (a.R + T - 1) / T;
+  if (a.R <= clusters) {  // a row each: no other cluster writes it, and none of this one before all have come
+    if (__syncthreads_or(a.tokens[id] == kUndecided)) f(id);
     cluster.sync();
-    for (int i = 0; i < T / 32; ++i)
-      for (uint32_t bits = s.rows[i]; bits; bits &= bits - 1) {
-        f(r0 + (32 * i + __ffs(bits) - 1) * clusters);
-        cluster.sync();  // (what one CTA reads of another's is not overwritten)
+    return;
+  }
+  const bool share = chunks > kSearched;
+  const int64_t todo = share ? (chunks + clusters - 1 - id) / clusters : chunks;
+  auto row_of = [&](int64_t i, int t) {  // thread t's of the i-th chunk
+    if (share) return (id + i * clusters) * T + t;
+    const int64_t r = i * T + t + id * a.R / clusters;
+    return i * T + t < a.R ? (r < a.R ? r : r - a.R) : a.R;
+  };
+  int64_t i = 0;
+  uint32_t left = 0;
+  bool looked = false;
+  cluster.sync();  // (every CTA of it is there)
+  for (;;) {
+    if (cluster.block_rank() == 0) {
+      int64_t found = -1;
+      while (found < 0 && i < todo) {
+        const int64_t mine = row_of(i, threadIdx.x);
+        if (!looked) left = mine < a.R && *static_cast<volatile int32_t*>(a.tokens + mine) == kUndecided ? 1 : 0;
+        looked = true;
+        if (!__syncthreads_or(left)) {
+          ++i;
+          looked = false;
+          continue;
+        }
+        // the first thread that still has one
+        const uint32_t bits = __ballot_sync(0xffffffffu, left);
+        if ((threadIdx.x & 31) == 0) s.red_c[threadIdx.x >> 5] = bits;
+        __syncthreads();
+        int w = 0;
+        while (!s.red_c[w]) ++w;
+        if (static_cast<int>(threadIdx.x) == 32 * w + __ffs(s.red_c[w]) - 1) {
+          left = 0;
+          s.next = atomicCAS(a.tokens + mine, kUndecided, kTaken) == kUndecided ? mine : -1;
+        }
+        __syncthreads();
+        found = s.next;
+        __syncthreads();
       }
+      if (static_cast<int>(threadIdx.x) < peers) cluster.map_shared_rank(&s, threadIdx.x)->next = found;
+    }
+    cluster.sync();
+    const int64_t r = s.next;
+    if (r < 0) return;
+    f(r);
+    cluster.sync();  // (what one CTA reads of another's is not overwritten)
   }
 }
-
 // ---- 16-bit logits: how often each key comes is all there is to know.  A CTA counts its part's keys in 16 bits each; of the
 // keys that weigh anything each CTA adds up a share over all parts, a thread some of them in order.
-constexpr int kCountThreads = 1024, kKeys = 65536, kShare = kKeys / kPeers;
+constexpr int kCountPeers = 8, kCountThreads = 1024, kKeys = 65536, kShare = kKeys / kCountPeers;
 constexpr int32_t kMostCounted = 500000;  // a part's count of one key stays below 2^16
 
 struct Counts : Common<kCountThreads> {
   alignas(16) uint32_t half[kKeys / 2];  // two keys' counts a word (cleared 16 bytes at a time)
-  uint32_t whole[kShare];      // the row's counts of the CTA's share of the keys
-  uint64_t upto_w[kCountThreads];  // ahead of a thread's keys, in the share
-  uint32_t upto_c[kCountThreads];
+  alignas(8) uint32_t whole[kShare];     // the row's counts of the CTA's share of the keys
   uint32_t all_c;
   uint64_t all_w;
   Place place[2];
@@ -428,7 +500,7 @@ struct Counts : Common<kCountThreads> {
 
 __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const SampleArgs a) {
   using E = uint16_t;
-  constexpr int T = kCountThreads;
+  constexpr int T = kCountThreads, kPeers = kCountPeers;
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Counts& s = *reinterpret_cast<Counts*>(smem_raw);
   const cg::cluster_group cluster = cg::this_cluster();
@@ -449,19 +521,25 @@ __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const S
       best = min(best, k);
       atomicAdd(&s.half[k >> 1], 1u << (16 * (k & 1)));
     });
-    if (!largest<E, T>(s, cluster, a, r, best, bad, t)) return;
+    if (!largest<E, T, kPeers>(s, cluster, a, r, best, bad, t)) return;
     Weigher weigh = s.weigh;
     weigh.max = Logit<E>::of_key(best);
 
     // the share's keys over all parts, a thread's side by side
     const uint32_t range = Logit<E>::key(fmaxf(__fsub_rd(weigh.max, 1.001f * weigh.cut), kLowest)) - best + 1;
-    const uint32_t share = (range + kPeers - 1) / kPeers, k0 = best + rank * share;
-    const uint32_t mine = k0 < best + range ? min(share, best + range - k0) : 0;
-    for (uint32_t i = tid; i < mine; i += T) {
-      uint32_t c = 0;
+    const uint32_t even = best & ~1u, words = (best + range + 1 - even) / 2, share = (words + kPeers - 1) / kPeers * 2;
+    const uint32_t k0 = even + rank * share, mine = 2 * min(share / 2, words - min(words, rank * share / 2));
+    for (uint32_t i = tid; i < mine / 2; i += T) {
+      uint32_t c[kPeers];
 #pragma unroll
-      for (int e = 0; e < kPeers; ++e) c += cluster.map_shared_rank(&s, e)->count(k0 + i);
-      s.whole[i] = c;
+      for (int e = 0; e < kPeers; ++e) c[e] = cluster.map_shared_rank(&s, e)->half[k0 / 2 + i];
+      uint2 sum = make_uint2(0u, 0u);
+#pragma unroll
+      for (int e = 0; e < kPeers; ++e) {
+        sum.x += c[e] & 0xffffu;
+        sum.y += c[e] >> 16;
+      }
+      reinterpret_cast<uint2*>(s.whole)[i] = sum;
     }
     __syncthreads();
     const uint32_t per = (share + T - 1) / T, i0 = min(tid * per, mine), i1 = min(i0 + per, mine);
@@ -489,6 +567,7 @@ __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const S
     cluster.sync();
     all_c = 0;
     all_w = 0;
+#pragma unroll
     for (int i = 0; i < kPeers; ++i) {
       const Counts& p = *cluster.map_shared_rank(&s, i);
       if (i == rank) {
@@ -514,6 +593,7 @@ __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const S
           p.w = w;
           return j < c;
         });
+#pragma unroll
         for (int i = 0; i < kPeers; ++i) *cluster.map_shared_rank(&to, i) = p;
       }
       cluster.sync();
@@ -534,14 +614,15 @@ __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const S
       cluster.sync();
       c = 0;
       sum = 0;
+#pragma unroll
       for (int i = 0; i < kPeers; ++i) {
         c += cluster.map_shared_rank(&s, i)->had_c;
         sum += cluster.map_shared_rank(&s, i)->had_w;
       }
     };
     auto where = [&](const Place& p) {
-      uint32_t seen = 0;
-      for (int i = 0; i < rank; ++i) seen += cluster.map_shared_rank(&s, i)->count(p.key);
+      const uint32_t seen =
+          __reduce_add_sync(0xffffffffu, (tid & 31) < rank ? cluster.map_shared_rank(&s, tid & 31)->count(p.key) : 0u);
       if (tid == 0) s.at = -1;
       __syncthreads();
       if (seen <= p.nth && p.nth < seen + s.count(p.key)) nth_of<E, T>(s, row, p.key, p.nth - seen);
@@ -552,9 +633,10 @@ __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const S
 
 // ---- any logits: a histogram of counts and weights by max - x; in one of its bins, by ranks where it has few tokens, by keys
 // (and finer ones) where it has many.
-constexpr int kThreads = 512;
+constexpr int kThreads = 1024;
+constexpr int kPeers = 8;  // CTAs of a cluster
 constexpr int kBinBits = 11, kBins = 1 << kBinBits, kBinShare = kBins / kPeers;
-constexpr int kList = 256;  // tokens whose ranks are found one against all others
+constexpr int kList = 512;  // tokens whose ranks are found one against all others
 
 struct Sums {  // of a bin and all before it
   uint64_t weight[kBins];
@@ -569,8 +651,6 @@ struct Binned : Common<kThreads> {
   uint32_t count[kBins], lo[kBins], hi[kBins];  // the CTA's part of the row
   Sums sums[2];
   Tokens own, all;
-  uint64_t share_w[kBinShare];  // the whole row's, a share of the bins a CTA
-  uint32_t share_c[kBinShare];
   Place place;
   __device__ __forceinline__ void clear() {
     for (int i = threadIdx.x; i < kBins; i += kThreads) count[i] = lo[i] = hi[i] = 0;
@@ -599,18 +679,20 @@ __device__ __forceinline__ void sum_up(Binned& s, const cg::cluster_group& clust
       c += p.count[bin];
       w += (static_cast<uint64_t>(p.hi[bin]) << 32) + p.lo[bin];
     }
-    s.share_c[threadIdx.x] = c;
-    s.share_w[threadIdx.x] = w;
+#pragma unroll
+    for (int i = 0; i < kPeers; ++i) {
+      Sums& p = *cluster.map_shared_rank(&to, i);
+      p.count[bin] = c;
+      p.weight[bin] = w;
+    }
   }
   cluster.sync();
   uint32_t c[kPer], ca = 0, all_c;
   uint64_t w[kPer], wa = 0, all_w;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const int bin = threadIdx.x * kPer + i;
-    const Binned& p = *cluster.map_shared_rank(&s, bin / kBinShare);
-    c[i] = ca += p.share_c[bin % kBinShare];
-    w[i] = wa += p.share_w[bin % kBinShare];
+    c[i] = ca += to.count[threadIdx.x * kPer + i];
+    w[i] = wa += to.weight[threadIdx.x * kPer + i];
   }
   block_scan<kThreads>(s, ca, wa, all_c, all_w);
 #pragma unroll
@@ -648,15 +730,14 @@ __device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, Bi
     bad |= x < INFINITY ? 0u : 1u;
     best = min(best, Logit<E>::key(x));
   });
-  if (!largest<E, T>(s, cluster, a, r, best, bad, t)) return;
+  if (!largest<E, T, kPeers>(s, cluster, a, r, best, bad, t)) return;
   Weigher weigh = s.weigh;
   weigh.max = Logit<E>::of_key(best);
 
   // all tokens that weigh anything
   const float wide = weigh.cut * (1.0f / kBins), by = 1.0f / wide;
   auto bin_of = [&](float x) { return min(static_cast<int>((weigh.max - x) * by), kBins - 1); };
-  row.template each<T>([&](float x, int32_t) {
-    const uint64_t w = weigh(x);
+  row.template each<T>([&](float x) { return weigh.beside(x); }, [&](uint64_t w, float x, int32_t) {
     if (w) s.add(bin_of(x), w);
   });
   sum_up(s, cluster, s.sums[0], 0, 0);
@@ -717,16 +798,18 @@ __device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, Bi
       s.own.w[i] = w;
     });
     cluster.sync();
-    uint32_t m = 0;
-    for (int i = 0; i < kPeers; ++i) {
-      const Binned& p = *cluster.map_shared_rank(&s, i);
-      const uint32_t more = min(p.n, kList - m);
-      for (uint32_t e = tid; e < more; e += T) {
-        s.all.key[m + e] = p.own.key[e];
-        s.all.at[m + e] = p.own.at[e];
-        s.all.w[m + e] = p.own.w[e];
+    const int lane = tid & 31, warp = tid >> 5;
+    const uint32_t upto = warp_scan(lane < kPeers ? cluster.map_shared_rank(&s, lane)->n : 0u);
+    const uint32_t m = min(__shfl_sync(0xffffffffu, upto, 31), static_cast<uint32_t>(kList));
+    static_assert(kPeers <= T / 32, "a warp a CTA of the cluster");
+    if (warp < kPeers) {
+      const Binned& p = *cluster.map_shared_rank(&s, warp);
+      const uint32_t end = min(__shfl_sync(0xffffffffu, upto, warp), m), from = end - min(p.n, end);
+      for (uint32_t e = lane; e < end - from; e += 32) {
+        s.all.key[from + e] = p.own.key[e];
+        s.all.at[from + e] = p.own.at[e];
+        s.all.w[from + e] = p.own.w[e];
       }
-      m += more;
     }
     cluster.sync();
     if (static_cast<uint32_t>(tid) < m) {
@@ -734,12 +817,12 @@ __device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, Bi
       const int32_t at = s.all.at[tid];
       uint32_t c = c0;
       uint64_t w = w0;
+#pragma unroll 4
       for (uint32_t i = 0; i < m; ++i) {
         const uint32_t ki = s.all.key[i];
-        if (ki < k || (ki == k && s.all.at[i] < at)) {
-          ++c;
-          w += s.all.w[i];
-        }
+        const bool ahead = ki < k || (ki == k && s.all.at[i] < at);
+        c += ahead ? 1u : 0u;
+        w += ahead ? s.all.w[i] : 0u;
       }
       const uint64_t mine = by_weight ? w : c, with = mine + (by_weight ? s.all.w[tid] : 1u);
       if (mine < target && target <= with) {
@@ -782,14 +865,14 @@ __device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, Bi
       s.at = -1;
     }
     cluster.sync();
-    for (int i = 0; i < rank; ++i) seen += cluster.map_shared_rank(&s, i)->n;
+    seen = __reduce_add_sync(0xffffffffu, (tid & 31) < rank ? cluster.map_shared_rank(&s, tid & 31)->n : 0u);
     if (seen <= p.nth && p.nth < seen + mine) nth_of<E, T>(s, row, p.key, p.nth - seen);
   };
   draw(a, r, s, greedy, s.sums[0].count[kBins - 1], s.sums[0].weight[kBins - 1], find, heavy, where);
 }
 
 template <typename E>
-__global__ void __launch_bounds__(kThreads, 2) sample_binned_kernel(const SampleArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) sample_binned_kernel(const SampleArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Binned& s = *reinterpret_cast<Binned*>(smem_raw);
   const cg::cluster_group cluster = cg::this_cluster();
@@ -805,23 +888,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_binned_kernel(const Sample
 // what is kept ends inside the list, or the token is inside it for the least and the largest sum that the others can have, this
 // is the result; a row of which neither holds, or whose list overflows, is left to the second kernel.
 constexpr int kHeadThreads = 512, kHeadWarps = kHeadThreads / 32;
-constexpr int kCap = 4096;       // tokens of a list
+constexpr int kCap = 2560;       // tokens of a list
 constexpr int kWhole = 2048;     // rows of up to so many are taken whole
-constexpr float kWant = 500.0f, kMostWanted = 2600.0f;  // tokens that the list is to have
+constexpr float kWant = 500.0f, kMostWanted = 1700.0f;  // tokens that the list is to have
 constexpr int kSpread = 1024;    // bins of the list's order
 constexpr uint32_t kSame = 512;  // tokens of one of them at most
 constexpr int kMostCtas = 8;     // of a cluster
 
 struct Head {
-  float x[kCap];     // the list, then in order
-  int32_t at[kCap];
-  union {
-    struct {
-      float x2[kCap];  // by bins
-      int32_t at2[kCap];
-    };
-    uint64_t sum[kCap];  // running weights
-  };
+  uint64_t packed[kCap];  // the list by bins: a token's key and index
+  uint64_t sum[kCap];     // the weights in order, then their running sums
+  float x[kCap];          // the list
+  int32_t at[kCap];       // its indexes, then in order
   uint32_t upto[kSpread];
   uint64_t pow2[64];
   uint64_t red_w[kHeadWarps], red_low[kHeadWarps];
@@ -905,7 +983,7 @@ __device__ __forceinline__ void ask(Head& s, uint64_t (&out)[2], uint64_t least,
 }
 
 template <typename E>
-__global__ void __launch_bounds__(kHeadThreads, 3) sample_head_kernel(const SampleArgs a) {
+__global__ void __launch_bounds__(kHeadThreads, 2) sample_head_kernel(const SampleArgs a) {
   constexpr int VEC = Logit<E>::kVec, kDeep = 4, kPicks = 8 / VEC;
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Head& s = *reinterpret_cast<Head*>(smem_raw);
@@ -991,25 +1069,35 @@ __global__ void __launch_bounds__(kHeadThreads, 3) sample_head_kernel(const Samp
 
   // the pass over the row
   uint64_t rest = 0;
-  auto one = [&](float x, int32_t at) -> float {  // a weight, or a token of the list
-    if (x < bound) return ex2(fmaf(x, c_lo, fmaf(x, c_hi, -ref)));
+  auto keep = [&](float x, int32_t at) {  // a token of the list
     if (!(x < INFINITY)) s.bad = 1;
     const uint32_t i = atomicAdd(&s.n, 1u);
     if (i < kCap) {
       s.x[i] = x;
       s.at[i] = at;
     }
-    return 0.0f;
+  };
+  auto one = [&](int32_t at) {
+    const float x = Logit<E>::get(row.p + at);
+    if (x < bound)
+      rest += __float2uint_rn(ex2(fmaf(x, c_lo, fmaf(x, c_hi, -ref))) * 0x1p28f);
+    else
+      keep(x, at);
   };
   auto vec = [&](const uint4& q, int32_t v) {
     float x[VEC], w[VEC];
     Logit<E>::get(q, x);
-    if (!(most_of(q, x, static_cast<const E*>(nullptr)) < bound)) {
+    uint32_t high = 0;  // bit e: the e-th is at the bound or above
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) w[e] = one(x[e], row.head + v * VEC + e);
-    } else {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) w[e] = ex2(fmaf(x[e], c_lo, fmaf(x[e], c_hi, -ref)));
+    for (int e = 0; e < VEC; ++e) {
+      const bool below = x[e] < bound;
+      w[e] = below ? ex2(fmaf(x[e], c_lo, fmaf(x[e], c_hi, -ref))) : 0.0f;
+      high |= below ? 0u : 1u << e;
+    }
+#pragma unroll 1
+    for (; high; high &= high - 1) {
+      const int e = __ffs(high) - 1;
+      keep(Logit<E>::get(q, e), row.head + v * VEC + e);
     }
 #pragma unroll
     for (int o = VEC / 2; o > 0; o >>= 1)
@@ -1017,20 +1105,26 @@ __global__ void __launch_bounds__(kHeadThreads, 3) sample_head_kernel(const Samp
       for (int e = 0; e < o; ++e) w[e] += w[e + o];
     rest += __float2uint_rn(w[0] * 0x1p28f);
   };
-  int32_t v = v0 + tid;
+  // (the next vectors are on their way while these are looked at)
+  uint4 q[kDeep];
+  auto load = [&](int32_t v) {
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i)
+      if (v + i * kHeadThreads < v1) q[i] = row.vec(v + i * kHeadThreads);
+  };
+  load(v0 + tid);
 #pragma unroll 1
-  for (; v + (kDeep - 1) * kHeadThreads < v1; v += kDeep * kHeadThreads) {
-    uint4 q[kDeep];
+  for (int32_t v = v0 + tid; v < v1; v += kDeep * kHeadThreads) {
+    uint4 now[kDeep];
 #pragma unroll
-    for (int i = 0; i < kDeep; ++i) q[i] = row.vec(v + i * kHeadThreads);
+    for (int i = 0; i < kDeep; ++i) now[i] = q[i];
+    load(v + kDeep * kHeadThreads);
 #pragma unroll
-    for (int i = 0; i < kDeep; ++i) vec(q[i], v + i * kHeadThreads);
+    for (int i = 0; i < kDeep; ++i)
+      if (v + i * kHeadThreads < v1) vec(now[i], v + i * kHeadThreads);
   }
-#pragma unroll 1
-  for (; v < v1; v += kHeadThreads) vec(row.vec(v), v);
-  if (row.first && tid < row.head) rest += __float2uint_rn(one(Logit<E>::get(row.p + tid), tid) * 0x1p28f);
-  if (row.last && row.tail() + tid < row.V)
-    rest += __float2uint_rn(one(Logit<E>::get(row.p + row.tail() + tid), row.tail() + tid) * 0x1p28f);
+  if (row.first && tid < row.head) one(tid);
+  if (row.last && row.tail() + tid < row.V) one(row.tail() + tid);
 
   // everything to the first CTA
 #pragma unroll
@@ -1131,8 +1225,7 @@ __global__ void __launch_bounds__(kHeadThreads, 3) sample_head_kernel(const Samp
     const float x = s.x[i];
     if (x >= floor_ && max_x - x < cut) {
       const uint32_t j = atomicAdd(&s.upto[bin_of(x)], 1u);  // (afterwards: the next bin's first place)
-      s.x2[j] = x;
-      s.at2[j] = s.at[i];
+      s.packed[j] = static_cast<uint64_t>(~static_cast<uint32_t>(in_order(x + 0.0f)) ^ 0x80000000u) << 32 | static_cast<uint32_t>(s.at[i]);
     } else {
       low += weigh(x);
     }
@@ -1140,15 +1233,15 @@ __global__ void __launch_bounds__(kHeadThreads, 3) sample_head_kernel(const Samp
   __syncthreads();
   const int32_t n = s.upto[kSpread - 1];
   for (int32_t i = tid; i < n; i += kHeadThreads) {
-    const float x = s.x2[i];
-    const int32_t at = s.at2[i], b = bin_of(x), from = b ? s.upto[b - 1] : 0, to = s.upto[b];
+    const uint64_t mine = s.packed[i];
+    const float x = from_order(static_cast<int32_t>(~static_cast<uint32_t>(mine >> 32) ^ 0x80000000u));
+    const int32_t b = bin_of(x), from = b ? s.upto[b - 1] : 0, to = s.upto[b];
+    const uint64_t w = weigh(x);
     int32_t j = from;
-    for (int32_t e = from; e < to; ++e) {
-      const float y = s.x2[e];
-      j += y > x || (y == x && s.at2[e] < at) ? 1 : 0;
-    }
-    s.x[j] = x;
-    s.at[j] = at;
+#pragma unroll 4
+    for (int32_t e = from; e < to; ++e) j += s.packed[e] < mine ? 1 : 0;
+    s.at[j] = static_cast<int32_t>(static_cast<uint32_t>(mine));
+    s.sum[j] = w;
   }
   __syncthreads();
   {  // running weights
@@ -1156,17 +1249,12 @@ __global__ void __launch_bounds__(kHeadThreads, 3) sample_head_kernel(const Samp
     const int32_t per = (n + kHeadThreads - 1) / kHeadThreads, i0 = tid * per;
     uint64_t own[kEach], upto = 0;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      if (i < per) {
-        if (i0 + i < n) upto += weigh(s.x[i0 + i]);
-        own[i] = upto;
-      }
-    const uint64_t mine_w = upto;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint64_t y = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += y;
+    for (int i = 0; i < kEach; ++i) {
+      if (i < per && i0 + i < n) upto += s.sum[i0 + i];
+      own[i] = upto;
     }
+    const uint64_t mine_w = upto;
+    upto = warp_scan(upto);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) low += __shfl_xor_sync(0xffffffffu, low, o);
     if (lane == 31) s.red_w[warp] = upto;
@@ -1301,8 +1389,8 @@ cudaError_t run_sample(const SampleArgs& a, cudaStream_t st) {
   const cudaError_t e = go<Head>(sample_head_kernel<E>, a, a.R, ctas, kHeadThreads, ready[0], st);
   if (e != cudaSuccess) return e;
   if (sizeof(E) == 2 && a.V <= kMostCounted)
-    return go<Counts>(sample_counts_kernel, a, std::min<int64_t>(a.R, 152 / kPeers), kPeers, kCountThreads, ready[1], st);
-  return go<Binned>(sample_binned_kernel<E>, a, std::min<int64_t>(a.R, 304 / kPeers), kPeers, kThreads, ready[2], st);
+    return go<Counts>(sample_counts_kernel, a, std::min<int64_t>(a.R, 152 / kCountPeers), kCountPeers, kCountThreads, ready[1], st);
+  return go<Binned>(sample_binned_kernel<E>, a, std::min<int64_t>(a.R, 152 / kPeers), kPeers, kThreads, ready[2], st);
 }
 
 }  // namespace
