@@ -298,6 +298,11 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
                : "memory");
 }
 
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t (&r)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
+               : "memory");
+}
+
 // N rows' products (8 where R is, else 16) from their hi columns at `base` and their lo columns R behind: hi + lo / 16, by
 // pairs.
 template <int R, int N>
@@ -1124,14 +1129,17 @@ __global__ void __launch_bounds__(KvLay<HD, R, TREE>::kThreads, KvLay<HD, R, TRE
 // weight (257 us): two threads a row 284; the accumulators raised before the weights are made, and only those of the rows
 // that have to be, 266; rows read and written by their own lanes 261; the other kernel with tiles of 64 rows 386.
 constexpr float kNominalRows = 14.0f;
-template <bool TREE>
+// Heads of 64 (TREE): a shared-memory row has two tokens, a tile of 128 tokens 64 of them; the scores' columns are the first tokens
+// of all rows, then the second ones.
+template <int HD, bool TREE>
 struct KvMany {
   static constexpr bool kTree = TREE;
-  static constexpr int kHd = 128, kR = 128, kTpr = 1, kTok = kRows, kHead = 4, kPages = kTok / 16;
+  static constexpr int kHd = HD, kR = 128, kTpr = 128 / HD, kTok = 128, kHead = 4, kPages = kTok / 16;
+  static constexpr int kSmemRows = kTok / kTpr;
   static constexpr int kShare = 4;  // threads a row
   static constexpr int kSoft = 128 * kShare, kTmaWarp = 4 * kShare, kMmaWarp = kTmaWarp + 1, kThreads = kSoft + 64, kSlots = 12;
-  static constexpr uint32_t kTile = kRows * 128, kTmem = 512;
-  static constexpr uint32_t kColO = 256, kColQ = 384;  // scores twice, accumulators, queries (32 columns hi, 32 lo)
+  static constexpr uint32_t kTile = kSmemRows * 128, kTmem = 512;
+  static constexpr uint32_t kColO = 256, kColQ = 384;  // scores twice, accumulators, queries (HD / 4 columns hi, as many lo)
   static constexpr uint32_t kBarFull = 0, kBarEmpty = 8 * kSlots, kBarScale = 16 * kSlots, kBarRest = kBarScale + 8 * kScaleRing;
   static constexpr uint32_t kOffScale = 640, kOffEx = kOffScale + kScaleRing * 8 * kPages, kOffRing = 7 * 1024;
   static constexpr uint32_t kSmem = kOffRing + kSlots * kTile + 1024;
@@ -1182,11 +1190,12 @@ __device__ __forceinline__ void exchange4(uint4 (&r)[4], int lane) {
   swap(r[1], r[3], 2);
 }
 
-template <bool TREE>
-__global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
+template <int HD, bool TREE>
+__global__ void __launch_bounds__(KvMany<HD, TREE>::kThreads, 1)
     kv_attn_rows_kernel(const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv, const KvTcArgs p) {
-  using Y = KvMany<TREE>;
-  constexpr int NS = Y::kSlots, HD = 128, R = Y::kR, kTok = Y::kTok, C = Y::kShare, W = 128 / C;  // W columns a thread
+  using Y = KvMany<HD, TREE>;
+  constexpr int NS = Y::kSlots, R = Y::kR, kTok = Y::kTok, C = Y::kShare, W = 128 / C;  // W columns of scores a thread
+  constexpr int WO = HD / C, TPR = Y::kTpr;                                             // of the head; tokens a shared-memory row
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
@@ -1237,7 +1246,7 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
   if (warp == Y::kTmaWarp) {
     copy_tiles<Y>(tmk, tmv, p, w, base, scales);
   } else if (warp == Y::kMmaWarp) {
-    constexpr uint32_t idesc_s = idesc_f8(R, kTok, false, false), idesc_o = idesc_f8(R, HD, false, true, true);
+    constexpr uint32_t idesc_s = idesc_f8(R, kTok / TPR, false, false), idesc_o = idesc_f8(R, HD, false, true, true);
     constexpr uint32_t kHi = desc_hi(1024, 2);
     const bool issuer = elect_one();
     int slot = 0;
@@ -1250,9 +1259,13 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
       tc_fence_after();
       if (issuer) {
         const uint32_t bd = desc_lo(base + Y::kOffRing + slot * Y::kTile, 16);
+        constexpr int kSteps = HD / 32;  // of 32 bytes of a token
 #pragma unroll
-        for (int k = 0; k < 8; ++k)  // hi, then lo
-          umma_f8_ts(tmem + 128 * buf, tmem + Y::kColQ + 8 * k, bd + 2 * (k % 4), kHi, idesc_s, k > 0 ? 1u : 0u);
+        for (int e = 0; e < TPR; ++e)
+#pragma unroll
+          for (int k = 0; k < 2 * kSteps; ++k)  // hi, then lo
+            umma_f8_ts(tmem + 128 * buf + 64 * e, tmem + Y::kColQ + 8 * k, bd + 4 * e + 2 * (k % kSteps), kHi, idesc_s,
+                       k > 0 ? 1u : 0u);
         umma_commit<1>(s_full0 + 8u * buf);
         umma_commit<1>(empty0 + 8u * slot);
       }
@@ -1276,8 +1289,8 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
           const uint32_t bd = desc_lo(base + Y::kOffRing + slot * Y::kTile, 16);
 #pragma unroll
           for (int k = 0; k < 12; ++k)  // 32 tokens at a time, whose words lie over their scores: 8 columns a term
-            umma_f8_ts(tmem + Y::kColO, tmem + 128 * buf + 32 * (k % 4) + 8 * (k / 4), bd + 256 * (k % 4), kHi, idesc_o,
-                       (j > 0 || k > 0) ? 1u : 0u);
+            umma_f8_ts(tmem + Y::kColO, tmem + 128 * buf + 32 * (k % 4) + 8 * (k / 4),
+                       bd + (TPR == 1 ? 256 * (k % 4) : 256 * (k % 2) + 4 * (k % 4 / 2)), kHi, idesc_o, (j > 0 || k > 0) ? 1u : 0u);
           umma_commit<1>(pv_done0 + 8u * buf);
           umma_commit<1>(empty0 + 8u * slot);
         }
@@ -1301,6 +1314,8 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
     };
     const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
     uint32_t gt = 0, ring = 0;
+    // Vector i of the thread's columns in a part: a warp's rows side by side.
+    auto vec_of = [&](float* part, int i) { return reinterpret_cast<float4*>(part + 2 * R) + (WO / 4 * c + i) * R + row; };
     // (see the other kernel's)
     auto wait_pv = [&](uint32_t t) { return mbar_wait_warp(pv_done0 + 8u * (t & 1), (t >> 1) & 1, p.wc); };
     // Rows come and go four at a time, 64 bytes of each by the four lanes whose rows they are (by the row's own
@@ -1311,7 +1326,7 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
       return at < v.rows_n * g.group ? (v.r0 + tk) * ld + (v.sh * g.group + at - tk * g.group) * HD + W * c + 8 * (lane & 3) : -1;
     };
     static_assert(W == 32, "four vectors a row");
-    auto ask = [&](const KvWalk<Y>& v, uint4 (&q)[W / 8]) {
+    auto ask = [&](const KvWalk<Y>& v, auto& q) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int64_t from = place(v, i, p.a.ldq);
@@ -1328,12 +1343,20 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
       const int32_t sees_all = w.len - w.rows_n + (TREE ? 0 : g.token_of(w.sq * R) + 1);
       float f;
       {
-        uint4 q[W / 8];
-        ask(w, q);
-        exchange4(q, lane);
+        uint4 q[WO / 8];
+        if constexpr (HD == 128) {
+          ask(w, q);
+          exchange4(q, lane);
+        } else {  // (two vectors a row and thread)
+#pragma unroll
+          for (int k = 0; k < WO / 8; ++k) {
+            q[k] = make_uint4(0u, 0u, 0u, 0u);
+            if (mine) q[k] = *reinterpret_cast<const uint4*>(p.a.q + (w.r0 + tk) * p.a.ldq + head * HD + WO * c + 8 * k);
+          }
+        }
         uint32_t top = 0;
 #pragma unroll
-        for (int k = 0; k < W / 8; ++k) {
+        for (int k = 0; k < WO / 8; ++k) {
           const uint32_t u[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
 #pragma unroll
           for (int e = 0; e < 4; ++e) top = max(top, max(u[e] << 16 & 0x7fffffffu, u[e] & 0x7fff0000u));
@@ -1348,9 +1371,9 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
         const bool bad = top >= 0x7f800000u;
         const float by = bad ? 0.0f : __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
         f = bad ? __uint_as_float(0x7fffffffu) : __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * p.a.scale_log2;
-        uint32_t hi[W / 4], lo[W / 4];
+        uint32_t hi[WO / 4], lo[WO / 4];
 #pragma unroll
-        for (int k = 0; k < W / 8; ++k) {
+        for (int k = 0; k < WO / 8; ++k) {
           const uint32_t u[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
           float x[8];
 #pragma unroll
@@ -1361,8 +1384,13 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
           split4(x, hi[2 * k], lo[2 * k]);
           split4(x + 4, hi[2 * k + 1], lo[2 * k + 1]);
         }
-        tmem_st8(lanes + Y::kColQ + W / 4 * c, hi);
-        tmem_st8(lanes + Y::kColQ + 32 + W / 4 * c, lo);
+        if constexpr (HD == 128) {
+          tmem_st8(lanes + Y::kColQ + 8 * c, hi);
+          tmem_st8(lanes + Y::kColQ + 32 + 8 * c, lo);
+        } else {
+          tmem_st4(lanes + Y::kColQ + 4 * c, hi);
+          tmem_st4(lanes + Y::kColQ + 16 + 4 * c, lo);
+        }
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -1376,10 +1404,11 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
         const int32_t tile = (w.t0 + j) * kTok;
         ok = mbar_wait_warp(scale_full0 + 8u * (gt % kScaleRing), (gt / kScaleRing) & 1, p.wc) && ok;
         const float* const sc = scales + (gt % kScaleRing) * (2 * Y::kPages);
-        float ks[W / 16], lsv[W / 16], inv[W / 16];  // of 16 tokens each (see the other kernel)
+        constexpr int G = 16 / TPR;                   // columns of 16 tokens
+        float ks[W / G], lsv[W / G], inv[W / G];  // of 16 tokens each (see the other kernel)
 #pragma unroll
-        for (int i = 0; i < W / 16; ++i) {
-          const int at_page = (W * c + 16 * i) >> page_shift;
+        for (int i = 0; i < W / G; ++i) {
+          const int at_page = (TPR == 1 ? W * c + 16 * i : 64 * (c & 1) + 16 * i) >> page_shift;
           ks[i] = sc[at_page];
           uint32_t vb = __float_as_uint(sc[Y::kPages + at_page]);
           if (vb == 0u) vb = kLeastScale;
@@ -1390,20 +1419,26 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
           lsv[i] = static_cast<float>(static_cast<int>(vb >> 23) - 127);
           inv[i] = __uint_as_float((254u - (vb >> 23)) << 23);
         }
-        // TREE: which of the thread's tokens its row sees
-        uint32_t sees_bits = 0xffffffffu;
+        // TREE: which of the thread's tokens its row sees, a word of 32 tokens
+        uint32_t sees_bits[TPR];
+#pragma unroll
+        for (int e = 0; e < TPR; ++e) sees_bits[e] = 0xffffffffu;
         if (TREE && tile + kTok > sees_all) {
-          const int32_t at = tile + W * c - sees_all;  // the first token's place among the new ones
           auto word = [&](int32_t k) -> uint32_t {
             const int32_t left = w.rows_n - 32 * k;
             if (!mine || left <= 0) return 0u;
             const uint32_t bits = p.a.seen[static_cast<int64_t>(w.r0 + tk) * p.a.words + k];
             return left < 32 ? bits & ((1u << left) - 1u) : bits;
           };
-          if (at >= 0)
-            sees_bits = __funnelshift_r(word(at >> 5), word((at >> 5) + 1), at & 31);
-          else if (at > -32)
-            sees_bits = (1u << -at) - 1u | word(0) << -at;
+#pragma unroll
+          for (int e = 0; e < TPR; ++e) {
+            // the first token's place among the new ones
+            const int32_t at = tile + (TPR == 1 ? W * c : 64 * (c & 1) + (c >> 1) + 32 * e) - sees_all;
+            if (at >= 0)
+              sees_bits[e] = __funnelshift_r(word(at >> 5), word((at >> 5) + 1), at & 31);
+            else if (at > -32)
+              sees_bits[e] = (1u << -at) - 1u | word(0) << -at;
+          }
         }
         ok = mbar_wait_warp(s_full0 + 8u * buf, (gt >> 1) & 1, p.wc) && ok;
         tc_fence_after();
@@ -1413,7 +1448,8 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
           ok = mbar_wait_warp(full0 + 8u * sl, (vat / NS) & 1, p.wc) && ok;
           uint4* const v = reinterpret_cast<uint4*>(gbase + Y::kOffRing + sl * Y::kTile);
 #pragma unroll 1
-          for (int32_t i = max(w.vis - tile, 0) * 8 + row; i < kRows * 8; i += 128) v[i] = make_uint4(0u, 0u, 0u, 0u);
+          for (int32_t i = max(w.vis - tile, 0) / TPR * 8 + row; i < Y::kSmemRows * 8; i += 128)  // (chunks of a row are swizzled)
+            if (TPR == 1 || tile + TPR * (i / 8) + ((i ^ (i / 8)) & 7) / (HD / 16) >= w.vis) v[i] = make_uint4(0u, 0u, 0u, 0u);
           fence_proxy_async_smem();
         }
         uint32_t v[32];
@@ -1424,15 +1460,17 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
 #pragma unroll
         for (int i = 0; i < W; i += 2) {
           const float2 t = fma2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])),
-                                both(f * ks[i / 16]), both(lsv[i / 16]));
+                                both(f * ks[i / G]), both(lsv[i / G]));
           x[i] = t.x;
           x[i + 1] = t.y;
         }
         if (TREE) {
-          if (sees_bits != 0xffffffffu) {
+          uint32_t all = sees_bits[0];
+          if (TPR > 1) all &= sees_bits[TPR - 1];
+          if (all != 0xffffffffu) {
 #pragma unroll
             for (int i = 0; i < W; ++i)
-              if (!(sees_bits >> i & 1u)) x[i] = -INFINITY;
+              if (!(sees_bits[TPR * i / 32] >> (TPR * i % 32) & 1u)) x[i] = -INFINITY;
           }
         } else if (tile + kTok > sees_all) {
           const int32_t sees = lim - tile - W * c;  // the thread's last visible token
@@ -1456,18 +1494,18 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
         }
         uint32_t t[3][W / 4];
 #pragma unroll
-        for (int i = 0; i < W; i += 16) {
+        for (int i = 0; i < W; i += G) {
           float2 sum = both(0.0f);
 #pragma unroll
-          for (int e = 0; e < 16; e += 2) {
+          for (int e = 0; e < G; e += 2) {
             const float2 y = fma2(both(m), both(-1.0f), make_float2(x[i + e], x[i + e + 1]));
             x[i + e] = fast_exp2(y.x);
             x[i + e + 1] = fast_exp2(y.y);
             sum = fma2(make_float2(x[i + e], x[i + e + 1]), both(1.0f), sum);
           }
-          l = fmaf(sum.x + sum.y, inv[i / 16], l);
+          l = fmaf(sum.x + sum.y, inv[i / G], l);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) split3<false>(x + i + 4 * e, t[0][i / 4 + e], t[1][i / 4 + e], t[2][i / 4 + e]);
+          for (int e = 0; e < G / 4; ++e) split3<false>(x + i + 4 * e, t[0][i / 4 + e], t[1][i / 4 + e], t[2][i / 4 + e]);
         }
 #pragma unroll
         for (int k = 0; k < 3; ++k) tmem_st8(sbuf + 8 * k, t[k]);
@@ -1476,7 +1514,7 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
           tc_fence_after();
           const float2 f4[4] = {both(fac), both(fac), both(fac), both(fac)};
 #pragma unroll 1
-          for (int i = 0; i < W; i += 8) scale_cols8<1>(lanes + Y::kColO + W * c + i, 0, f4);
+          for (int i = 0; i < WO; i += 8) scale_cols8<1>(lanes + Y::kColO + WO * c + i, 0, f4);
         }
         tmem_st_wait();
         tc_fence_before();
@@ -1486,7 +1524,7 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
       ring += 2 * w.n;
       const bool whole = w.n == w.all;
       float* const part = p.parts + (2 * static_cast<int64_t>(blockIdx.x) + (w.begin >= first ? 1 : 0)) * Y::kPartFloats;
-      uint16_t* const out = p.a.o + (w.r0 + tk) * p.a.ldo + head * HD + W * c;
+      uint16_t* const out = p.a.o + (w.r0 + tk) * p.a.ldo + head * HD + WO * c;
       const int64_t lse_at = static_cast<int64_t>(w.r0 + tk) * p.a.nh + head;
       if (!failed) {
         // (the exchange of the tile before last is free: the row's threads have met since)
@@ -1508,11 +1546,11 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
         ok = wait_pv(gt - 1) && ok;
         tc_fence_after();
         if (whole) {
-          uint4 two[W / 8];
+          uint4 two[WO / 8];
 #pragma unroll
-          for (int i = 0; i < W; i += 16) {
+          for (int i = 0; i < WO; i += 16) {
             uint32_t o[16], u[8];
-            tmem_ld16(lanes + Y::kColO + W * c + i, o);
+            tmem_ld16(lanes + Y::kColO + WO * c + i, o);
             tmem_ld_wait();
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -1523,31 +1561,107 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
             two[i / 8] = make_uint4(u[0], u[1], u[2], u[3]);
             two[i / 8 + 1] = make_uint4(u[4], u[5], u[6], u[7]);
           }
-          exchange4(two, lane);
+          if constexpr (HD == 128) {
+            exchange4(two, lane);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int64_t to = place(w, i, p.a.ldo);
-            if (ok && to >= 0) *reinterpret_cast<uint4*>(p.a.o + to) = two[i];
+            for (int i = 0; i < 4; ++i) {
+              const int64_t to = place(w, i, p.a.ldo);
+              if (ok && to >= 0) *reinterpret_cast<uint4*>(p.a.o + to) = two[i];
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < WO / 8; ++i)
+              if (ok && mine) *reinterpret_cast<uint4*>(out + 8 * i) = two[i];
           }
         } else {
 #pragma unroll 1
-          for (int i = 0; i < W; i += 16) {
+          for (int i = 0; i < WO; i += 16) {
             uint32_t o[16];
-            tmem_ld16(lanes + Y::kColO + W * c + i, o);
+            tmem_ld16(lanes + Y::kColO + WO * c + i, o);
             tmem_ld_wait();
             if (!mine || !ok) continue;
-            uint4* const to = reinterpret_cast<uint4*>(part + 2 * R + row * HD + W * c + i);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) to[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            for (int e = 0; e < 4; ++e)
+              *reinterpret_cast<uint4*>(vec_of(part, i / 4 + e)) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
           }
         }
         tc_fence_before();
       }
       ok = ok && !failed;
       if (whole) continue;
-      // the last of the row tile's runs joins their parts, a thread its quarter of its row
       if (!bar_all(kEvery, Y::kSoft, ok)) { ok = false; break; }
       const int32_t c0 = static_cast<int32_t>(w.begin / run), c1 = static_cast<int32_t>((w.begin + w.all - 1) / run);
+      auto slot_of = [&](int32_t r) { return p.parts + (2 * static_cast<int64_t>(r) + (r == c0 ? 1 : 0)) * Y::kPartFloats; };
+      if constexpr (TREE) {
+        // The parts are joined by twos, each pair by the run that comes second to it (a counter for each, which it leaves at zero):
+        // one run's join of 152 parts of 128 rows took 350 us, of 19 100.
+        const int32_t parts = c1 - c0 + 1;
+        int32_t from = static_cast<int32_t>(blockIdx.x) - c0;
+#pragma unroll 1
+        for (int32_t width = 1; width < parts; width *= 2) {
+          const int32_t other = from ^ width, low = min(from, other), high = max(from, other);
+          if (high >= parts) continue;
+          if (threadIdx.x == 0) {
+            uint32_t old;
+            asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(old) : "l"(p.counters + c0 + high), "r"(1u) : "memory");
+            *merge_flag = old == 1;
+          }
+          bar_sync(kEvery, Y::kSoft);
+          const bool second = *merge_flag;
+          bar_sync(kEvery, Y::kSoft);  // (everyone has read it)
+          if (!second) break;
+          const bool final = 2 * width >= parts;
+          float* const a = slot_of(c0 + low);
+          float* const b = slot_of(c0 + high);
+          float to = 0.0f, sum = 0.0f;
+          if (mine) {
+            const float am = __ldcg(a + row), bm = __ldcg(b + row);
+            to = fmaxf(am, bm);
+            const float fa = fast_exp2(am - to), fb = fast_exp2(bm - to);
+            sum = __ldcg(a + R + row) * fa + __ldcg(b + R + row) * fb;
+            const float by = !final ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+            for (int i0 = 0; i0 < WO / 4; i0 += 4) {
+              float4 x[4], y[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                x[i] = __ldcg(vec_of(a, i0 + i));
+                y[i] = __ldcg(vec_of(b, i0 + i));
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                x[i].x = by == 0.0f ? 0.0f : (x[i].x * fa + y[i].x * fb) * by;
+                x[i].y = by == 0.0f ? 0.0f : (x[i].y * fa + y[i].y * fb) * by;
+                x[i].z = by == 0.0f ? 0.0f : (x[i].z * fa + y[i].z * fb) * by;
+                x[i].w = by == 0.0f ? 0.0f : (x[i].w * fa + y[i].w * fb) * by;
+                if (!final) *vec_of(a, i0 + i) = x[i];
+              }
+#pragma unroll
+              for (int i = 0; i < 4; i += 2) {
+                uint4 two;
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(two.x) : "f"(x[i].y), "f"(x[i].x));
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(two.y) : "f"(x[i].w), "f"(x[i].z));
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(two.z) : "f"(x[i + 1].y), "f"(x[i + 1].x));
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(two.w) : "f"(x[i + 1].w), "f"(x[i + 1].z));
+                if (final) *reinterpret_cast<uint4*>(out + 4 * (i0 + i)) = two;
+              }
+            }
+          }
+          bar_sync(kEvery, Y::kSoft);  // (the threads of a row have read its maximum and sum before one of them writes)
+          if (mine && c == 0) {
+            if (!final) {
+              a[row] = to;
+              a[R + row] = sum;
+            } else if (p.a.lse) {
+              p.a.lse[lse_at] = sum == 0.0f ? -INFINITY : (to + log2f(sum)) * 0.6931471805599453f;
+            }
+          }
+          from = low;
+          bar_sync(kEvery, Y::kSoft);
+        }
+        continue;
+      }
+      // the last of the row tile's runs joins their parts, a thread its quarter of its row
       if (threadIdx.x == 0) {
         const uint32_t last = static_cast<uint32_t>(c1 - c0);
         uint32_t old;
@@ -1556,21 +1670,21 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
       }
       bar_sync(kEvery, Y::kSoft);
       if (*merge_flag && mine) {
-        float top = kNoMax, sum = 0.0f, acc[W];
+        float top = kNoMax, sum = 0.0f, acc[WO];
 #pragma unroll
-        for (int i = 0; i < W; ++i) acc[i] = 0.0f;
+        for (int i = 0; i < WO; ++i) acc[i] = 0.0f;
 #pragma unroll 1
         for (int32_t r = c0; r <= c1; ++r) {
-          const float* const q = p.parts + (2 * static_cast<int64_t>(r) + (r == c0 ? 1 : 0)) * Y::kPartFloats;
-          float4 v[W / 4];
+          float* const q = p.parts + (2 * static_cast<int64_t>(r) + (r == c0 ? 1 : 0)) * Y::kPartFloats;
+          float4 v[WO / 4];
 #pragma unroll
-          for (int i = 0; i < W / 4; ++i) v[i] = __ldcg(reinterpret_cast<const float4*>(q + 2 * R + row * HD + W * c) + i);
+          for (int i = 0; i < WO / 4; ++i) v[i] = __ldcg(vec_of(q, i));
           const float pm = __ldcg(q + row), pl = __ldcg(q + R + row), to = fmaxf(top, pm);
           const float fa = fast_exp2(top - to), fb = fast_exp2(pm - to);
           sum = sum * fa + pl * fb;
           top = to;
 #pragma unroll
-          for (int i = 0; i < W / 4; ++i) {
+          for (int i = 0; i < WO / 4; ++i) {
             acc[4 * i] = acc[4 * i] * fa + v[i].x * fb;
             acc[4 * i + 1] = acc[4 * i + 1] * fa + v[i].y * fb;
             acc[4 * i + 2] = acc[4 * i + 2] * fa + v[i].z * fb;
@@ -1580,7 +1694,7 @@ __global__ void __launch_bounds__(KvMany<TREE>::kThreads, 1)
         const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
         if (p.a.lse && c == 0) p.a.lse[lse_at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 #pragma unroll
-        for (int i = 0; i < W; i += 8) {
+        for (int i = 0; i < WO; i += 8) {
           uint32_t two[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -1676,6 +1790,7 @@ cudaError_t run_kv(void (*kern)(CUtensorMap, CUtensorMap, KvTcArgs), int ctas, c
 // 66; heads of 64, 4 rows 17.5 / 18.7 / 23.9, 16 rows 24.6 / 19.5 / 24.9, 32 rows 38 / 29 / 28, 128 rows 122 / 84 / 79.  The mean is a
 // poor guide to a batch of single tokens with a prompt among them: 128 single tokens on 2048 and a prompt of 512 (32 / 8 heads
 // of 128) take 155 us in one call, 129 in two; 32 on 4096 and a prompt of 2048 171 and 146.
+constexpr int kTreeFew = 32;
 template <int HD, int R, bool TREE>
 cudaError_t run_few(const KvAttnArgs& a, cudaStream_t st) {
   using Y = KvLay<HD, R, TREE>;
@@ -1687,15 +1802,20 @@ cudaError_t run_kv_rows(const KvAttnArgs& a, cudaStream_t st) {
   const int64_t rows = (a.T + a.B - 1) / a.B * (a.nh / a.cache.nkv);
   if (rows <= 8) return run_few<HD, 8, TREE>(a, st);
   if (rows <= 16) return run_few<HD, 16, TREE>(a, st);
-  if (rows <= 64 || HD == 64) return run_few<HD, 32, TREE>(a, st);
-  return run_kv<KvMany<TREE>>(kv_attn_rows_kernel<TREE>, 1, a, st);
+  if constexpr (TREE) {
+    if (rows <= kTreeFew) return run_few<HD, 32, TREE>(a, st);
+    return run_kv<KvMany<HD, TREE>>(kv_attn_rows_kernel<HD, TREE>, 1, a, st);
+  } else {
+    if (rows <= 64 || HD == 64) return run_few<HD, 32, TREE>(a, st);
+    return run_kv<KvMany<128, TREE>>(kv_attn_rows_kernel<128, TREE>, 1, a, st);
+  }
 }
 
 }  // namespace
 
 size_t kv_attention_ws_bytes(int32_t, int32_t, int32_t d) {
-  // two parts for each CTA: two CTAs an SM with tiles of up to 32 rows, one of 128 (heads of 64: of 32)
-  const size_t parts = static_cast<size_t>(sm_count()) * 2 * (d == 128 ? 128 : 64) * (static_cast<size_t>(d) + 2) * sizeof(float);
+  // two parts for each CTA: two CTAs an SM with tiles of up to 32 rows, one of 128
+  const size_t parts = static_cast<size_t>(sm_count()) * 2 * 128 * (static_cast<size_t>(d) + 2) * sizeof(float);
   return (kCounterBytes + parts + 255) / 256 * 256;
 }
 

@@ -446,31 +446,25 @@ __device__ __forceinline__ void left_rows(const SampleArgs& a, S& s, const cg::c
     return i * T + t < a.R ? (r < a.R ? r : r - a.R) : a.R;
   };
   int64_t i = 0;
-  uint32_t left = 0;
-  bool looked = false;
   cluster.sync();  // (every CTA of it is there)
   for (;;) {
     if (cluster.block_rank() == 0) {
       int64_t found = -1;
       while (found < 0 && i < todo) {
         const int64_t mine = row_of(i, threadIdx.x);
-        if (!looked) left = mine < a.R && *static_cast<volatile int32_t*>(a.tokens + mine) == kUndecided ? 1 : 0;
-        looked = true;
+        const uint32_t left = mine < a.R && *static_cast<volatile int32_t*>(a.tokens + mine) == kUndecided ? 1 : 0;
         if (!__syncthreads_or(left)) {
           ++i;
-          looked = false;
           continue;
         }
-        // the first thread that still has one
+        // the first thread that sees one tries to take it
         const uint32_t bits = __ballot_sync(0xffffffffu, left);
         if ((threadIdx.x & 31) == 0) s.red_c[threadIdx.x >> 5] = bits;
         __syncthreads();
         int w = 0;
         while (!s.red_c[w]) ++w;
-        if (static_cast<int>(threadIdx.x) == 32 * w + __ffs(s.red_c[w]) - 1) {
-          left = 0;
+        if (static_cast<int>(threadIdx.x) == 32 * w + __ffs(s.red_c[w]) - 1)
           s.next = atomicCAS(a.tokens + mine, kUndecided, kTaken) == kUndecided ? mine : -1;
-        }
         __syncthreads();
         found = s.next;
         __syncthreads();

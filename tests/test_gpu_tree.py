@@ -143,6 +143,10 @@ def check(paged, row_start, seq_len, seen, q, nh, got, lse):
     (64, 8, 1, 64, [600, 90], [64, 90]),
     (64, 3, 3, 128, [300], [256]),
     (64, 2, 1, 16, [9, 40], [3, 4]),
+    (128, 4, 1, 64, [9000], [30]),                    # one row tile in as many parts as there are CTAs
+    (128, 4, 2, 16, [2500, 1400], [70, 33]),          # parts of several row tiles, an odd number of them
+    (64, 4, 1, 128, [8000, 50], [33, 40]),
+    (64, 4, 2, 16, [2500, 1400], [70, 33]),
 ])
 @pytest.mark.parametrize("kind", ["tree", "any"])
 def test_attention_matches_oracle(device, d, nh, nkv, page, lens, news, kind):
