@@ -749,7 +749,8 @@ catq_status catq_kv_tree_attention(const catq_kv_cache* cache, const int32_t* ro
  * u Z and top_p S are taken in 64-bit floats, all else is exact: no result depends on an order of additions.
  * temperature, top_p, min_p [R] fp32, top_k [R] int32, each nullable: 1, 1, 0, 0.  T == 0: the first token (no other filter).
  * Temperatures from 2^-60 to 2^60; others above 0 count as the nearer of these.
- * tokens [R] int32.  logprob [R] fp32 (nullable): ln(w / Z), the probability with which the token was drawn; 0 for T == 0.
+ * tokens [R] int32, overlapping no input (it holds the kernels' marks in between).  logprob [R] fp32 (nullable): ln(w / Z), the
+ * probability with which the token was drawn, with Z to 2^-16 of itself at least; 0 for T == 0.
  * Logits of -inf are never drawn.  A row with NaN or +inf, without any finite logit, or with a temperature that is negative
  * or NaN gets token -1 and logprob NaN.  A NaN among the other settings counts as its default (u: as 0).
  * 1 <= V <= 2^20, R < 2^31, ld >= V (else CATQ_ERR_SHAPE); logits aligned to their type (16-byte aligned rows are faster),

@@ -596,6 +596,7 @@ __device__ __forceinline__ uint32_t move4(uint32_t codes, float by) {
 }
 
 constexpr int kMoves = 256;   // tokens whose places a CTA keeps at a time: two whole pages or more
+constexpr float kLeastScale = 0x1p-60f;
 constexpr int kInHand = 2;    // passes over a page's tokens that a warp keeps in registers
 
 // A CTA takes a sequence and some of the (cache, keys or values, head) of it, a warp one at a time; where the tokens lie and go
@@ -673,11 +674,13 @@ __global__ void __launch_bounds__(32 * kCompactWarps) kv_compact_kernel(const __
           if (sp != pg) scale = scales[sb];
           return sp != pg;
         };
-        auto magnitude = [&](const uint4& q, float scale) {
+        // the scale that a lane's codes under theirs ask for (by the code's and the scale's: their product may pass fp32's range)
+        auto wanted = [&](const uint4& q, float scale) {
           constexpr uint32_t kAbs = 0x7f7f7f7fu;
           uint32_t w = __vmaxu4(__vmaxu4(q.x & kAbs, q.y & kAbs), __vmaxu4(q.z & kAbs, q.w & kAbs));
           w = __vmaxu4(w, w >> 16);
-          return of_code(max(w & 0xffu, w >> 8 & 0xffu)) * scale;
+          const float s = scale_of(__float_as_uint(of_code(max(w & 0xffu, w >> 8 & 0xffu)))) * scale;
+          return s > 0.0f && s < kLeastScale ? kLeastScale : s;
         };
         auto put = [&](int32_t j, const uint4& w) {
           *reinterpret_cast<uint4*>(dst + (first + j - pg * page) * D + 16 * word) = w;
@@ -711,18 +714,18 @@ __global__ void __launch_bounds__(32 * kCompactWarps) kv_compact_kernel(const __
             if (k * kAtOnce < count) {
               const float scale = __shfl_sync(0xffffffffu, from, k * kAtOnce + sub);
               if (far >> (k * kAtOnce + sub) & 1u)
-                asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(top), "f"(magnitude(held[k], scale)));
+                asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(top), "f"(wanted(held[k], scale)));
             }
         } else {
 #pragma unroll 1
           for (int32_t j = j0 + sub; j < j1; j += kAtOnce) {
             uint4 w;
             float scale;
-            if (source(j, w, scale)) asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(top), "f"(magnitude(w, scale)));
+            if (source(j, w, scale)) asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(top), "f"(wanted(w, scale)));
           }
         }
         if (block < 0) continue;
-        const float want = scale_of(__reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu));
+        const float want = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu));
         const bool nan = !(want == want) || !(old == old);
         const float now = nan ? __uint_as_float(0x7fffffffu) : fmaxf(old, want);
         const bool grows = !nan && old > 0.0f && now > old;

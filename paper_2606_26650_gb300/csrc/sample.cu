@@ -485,12 +485,14 @@ constexpr int32_t kMostCounted = 500000;  // a part's count of one key stays bel
 
 struct Counts : Common<kCountThreads> {
   alignas(16) uint32_t half[kKeys / 2];  // two keys' counts a word (cleared 16 bytes at a time)
-  alignas(8) uint32_t whole[kShare];     // the row's counts of the CTA's share of the keys
+  uint64_t weight[kShare];               // of the keys of the CTA's share, 0 for those that no token has
+  alignas(8) uint32_t whole[kShare];     // the row's counts of them
   uint32_t all_c;
   uint64_t all_w;
   Place place[2];
   __device__ __forceinline__ uint32_t count(uint32_t key) const { return half[key >> 1] >> (16 * (key & 1)) & 0xffffu; }
 };
+static_assert(sizeof(Counts) <= 227 * 1024, "a CTA's shared memory");
 
 __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const SampleArgs a) {
   using E = uint16_t;
@@ -536,12 +538,13 @@ __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const S
       reinterpret_cast<uint2*>(s.whole)[i] = sum;
     }
     __syncthreads();
+    for (uint32_t i = tid; i < mine; i += T) s.weight[i] = s.whole[i] ? weigh(Logit<E>::of_key(k0 + i)) : 0;
+    __syncthreads();
     const uint32_t per = (share + T - 1) / T, i0 = min(tid * per, mine), i1 = min(i0 + per, mine);
     auto walk = [&](auto f) {  // f(key, tokens, weight of one) of the thread's keys that weigh anything
       for (uint32_t i = i0; i < i1; ++i) {
-        const uint32_t c = s.whole[i];
-        const uint64_t w = c ? weigh(Logit<E>::of_key(k0 + i)) : 0;
-        if (w && f(k0 + i, c, w)) return;
+        const uint64_t w = s.weight[i];
+        if (w && f(k0 + i, s.whole[i], w)) return;
       }
     };
     uint32_t own_c = 0, all_c;
@@ -1333,7 +1336,9 @@ __global__ void __launch_bounds__(kHeadThreads, 2) sample_head_kernel(const Samp
     const float u = a.u[r];
     ask(s, pass, known ? total : low_all, known ? total : high_all, [&](uint64_t whole) { return passes(u, whole); });
     const int32_t m = first_place(s, n, pass[0]);
-    if (pass[1] <= head && s.sum[m] >= pass[1]) {
+    // (with a probability wanted, the weight that it is a part of has to be known to 2^-16)
+    const bool near = known || !a.logprob || high_all - low_all <= low_all >> 15;
+    if (near && pass[1] <= head && s.sum[m] >= pass[1]) {
       if (tid == 0) {
         a.tokens[r] = s.at[m];
         if (a.logprob)

@@ -112,11 +112,18 @@ def test_borders(device):
     assert run(device, x, u=nan)[1].tolist() == [0] * 8
 
 
-def test_temperatures(device):
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [999, 5000])
+def test_temperatures(device, dtype, V):
     r = syn.rng(62, "temperature")
     T = np.array([0.0, 2.0 ** -70, 1e-9, 1e-3, 0.1, 1.0, 30.0, 1e6, 1e30, np.inf])
-    check(device, logits(r, 10, 999, "lm"), u=r.random(10), temperature=T)
-    check(device, logits(r, 10, 999, "wide"), u=r.random(10), temperature=T)
+    for kind in ("lm", "wide", "few"):
+        check(device, logits(r, 10, V, kind), dtype, u=r.random(10), temperature=T)
+        check(device, logits(r, 10, V, kind), dtype, u=r.random(10), temperature=T, top_p=np.full(10, 0.8), top_k=np.full(10, 300))
+
+
+def test_temperatures_near_the_limits(device):
+    r = syn.rng(62, "temperature")
     check(device, logits(r, 10, 999, "wide"), u=r.random(10), temperature=np.full(10, 3e37))
     # nearby logits at a temperature that tells them apart
     x = 20.0 + np.arange(64)[None] * 2.0 ** -19
@@ -148,6 +155,48 @@ def test_frequencies(device):
     assert np.abs(np.bincount(tokens, minlength=5) - R * p).max() <= 1
     _, tokens, _ = run(device, x, u=(np.arange(R) + 0.5) / R, top_k=np.full(R, 3))
     assert np.abs(np.bincount(tokens, minlength=5) - R * np.array([0.35, 0, 0.3, 0.2, 0]) / 0.85).max() <= 1
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_vocabularies(device, dtype):
+    """More tokens than 16-bit counts hold, all with one logit, and undecided rows of them."""
+    r = syn.rng(65, "large")
+    V = 600001
+    check(device, logits(r, 2, V, "flat"), dtype, 3, u=r.random(2))
+    check(device, logits(r, 2, V, "equal"), dtype, 3, u=r.random(2), top_k=np.array([0, 599000]))
+    check(device, logits(r, 1, V, "ties"), dtype, 0, u=r.random(1), top_p=np.array([0.7]), min_p=np.array([1e-4]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R", [70, 3000, 70000])
+def test_many_rows_that_need_every_logit(device, dtype, R):
+    """Rows of 600 equal logits: u of the way through them, each row its own."""
+    u = syn.rng(66, "equal").random(R).astype(np.float32)
+    _, tokens, lp = run(device, np.full((R, 600), -7.0), dtype, 1, u=u)
+    assert np.array_equal(tokens, np.floor(u.astype(np.float64) * 600).astype(np.int64))
+    assert np.abs(lp + np.log(600)).max() <= 2.0 ** -21 * np.log(600)
+
+
+def test_calls_at_once(device):
+    """Two streams' calls, which share nothing, give what they give one after the other."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(67, "two")
+    x = [torch.tensor(logits(r, 40, 20000, kind), dtype=torch.bfloat16, device=device) for kind in ("lm", "flat")]
+    u = torch.tensor(r.random(40), dtype=torch.float32, device=device)
+    p = torch.full((40,), 0.95, device=device)
+    want = [torch.empty(40, dtype=torch.int32, device=device) for _ in x]
+    got = [torch.empty(40, dtype=torch.int32, device=device) for _ in x]
+    for a, b in zip(x, want):
+        C.catq_sample(a, u, b, top_p=p)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in x]
+    for _ in range(20):
+        for a, b, st in zip(x, got, streams):
+            C.catq_sample(a, u, b, top_p=p, stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
 def test_streams_graphs_and_repeats(device):

@@ -299,6 +299,8 @@ def branches(r, news, most, moved=True):
     (64, 1, 128, [300, 129], [200, 3]),
     (128, 4, 32, [65] * 40, [13] * 40),
     (64, 2, 64, [6], [9]),                                 # a first position below 0
+    (64, 2, 16, [700], [600]),                             # more moved tokens than are kept in mind at once
+    (128, 1, 128, [600], [500]),
 ])
 @pytest.mark.parametrize("kind", ["alike", "growing", "shrinking", "still"])
 @pytest.mark.parametrize("layers", [1, 3])
@@ -392,7 +394,63 @@ def test_compact_of_pages_that_are_not_finite(device):
     assert np.isnan(scale[0][paged.table[0, 1]]).all() and np.isfinite(scale[0][paged.table[1, 1]]).all()
 
 
+def test_compact_behind_the_first_4_gb(device):
+    """Pages whose codes lie behind 2^32 bytes."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    n_pages, page, d = 300000, 128, 128
+    table = i32([[n_pages - 2, n_pages - 1]], device)
+    codes = [torch.empty(n_pages, 1, page, d, dtype=torch.uint8, device=device) for _ in range(2)]
+    scales = [torch.ones(n_pages, 1, device=device) for _ in range(2)]
+    for x in codes:
+        x[-2:] = (torch.arange(2 * page, device=device) % 100).to(torch.uint8).view(2, 1, page, 1)
+    cache = C.KVCache(*(x.view(torch.float8_e4m3fn) for x in codes), *scales, table)
+    C.catq_kv_compact([cache], i32([0, 8], device), i32([132], device), i32([0, 2, 6, 7, -1, -1, -1, -1], device), i32([4], device))
+    assert done() == 0
+    for x in codes:
+        got = x[-2:].view(2 * page, d)
+        for slot, token in zip(range(124, 128), (124, 126, 130, 131)):
+            assert (got[slot] == token % 100).all()
+        assert (got[:124, 0].cpu() == torch.arange(124) % 100).all()
+
+
 # ------------------------------------------------------------------ together
+
+def test_two_captured_graphs_at_once(device):
+    """Two graphs with workspaces of their own, replayed on two streams, give what they give alone."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(51, "graphs")
+    graphs, outs, want = [], [], []
+    for d, nh, nkv, lens, news in ((128, 8, 1, [3000, 900], [24, 31]), (64, 8, 2, [2000, 100], [40, 7])):
+        paged = Paged(r, lens, nkv, 16, d, device)
+        rs = starts(news)
+        seen, _ = O.masks(trees(r, news), rs, lens, 2)
+        T = int(rs[-1])
+        q, out = bf16(r.standard_normal((T, nh * d)), device), torch.empty(T, nh * d, dtype=torch.bfloat16, device=device)
+        args = (paged.cache, i32(rs, device), i32(lens, device), torch.from_numpy(seen.view(np.int32)).to(device), q, out, nh,
+                C.kv_attention_workspace(paged.cache, nh))
+        C.catq_kv_tree_attention(*args)
+        torch.cuda.synchronize()
+        want.append(out.clone())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            C.catq_kv_tree_attention(*args)
+        graphs.append((g, args))
+        outs.append(out)
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(10):
+        for out in outs:
+            out.zero_()
+        torch.cuda.synchronize()
+        for (g, _), st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+        assert done() == 0
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
 
 def step_tensors(device, B, T, nh, nkv, d, V, words):
     import torch
