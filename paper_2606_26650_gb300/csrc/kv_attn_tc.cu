@@ -1123,8 +1123,8 @@ __global__ void __launch_bounds__(KvLay<HD, R, TREE>::kThreads, KvLay<HD, R, TRE
 // step, 2^-17, below: 2^-31 of the row's largest, which is 2^kNominalRows or more.
 // Thread (row, quarter c) has the row's tokens 32 c .. 32 c + 31 of a tile.  The four agree on the row's maximum through
 // shared memory; raising it is lazy, as there, row by row.
-// Two prompts' chunks of 1023 tokens on 6001 and 8191 (32 / 8 heads of 128, 213 GFLOP) take 264 us, 0.8 PFLOP/s, bound by
-// the softmax's arithmetic.  The products by themselves, the softmax's threads only keeping pace, take 188: 1,280 cycles a tile
+// Two prompts' chunks of 1023 tokens on 6001 and 8191 (32 / 8 heads of 128, 213 GFLOP) take 254 us, 0.84 PFLOP/s, bound by
+// the softmax's arithmetic (265 with the parts of a cut row tile row by row, whose 16 bytes a lane are 32 lines an instruction).  The products by themselves, the softmax's threads only keeping pace, take 188: 1,280 cycles a tile
 // would be 115, the rest is that a tile's scores, its weights and their product follow one another.  In a form with two terms a
 // weight (257 us): two threads a row 284; the accumulators raised before the weights are made, and only those of the rows
 // that have to be, 266; rows read and written by their own lanes 261; the other kernel with tiles of 64 rows 386.
@@ -1593,8 +1593,8 @@ __global__ void __launch_bounds__(KvMany<HD, TREE>::kThreads, 1)
       const int32_t c0 = static_cast<int32_t>(w.begin / run), c1 = static_cast<int32_t>((w.begin + w.all - 1) / run);
       auto slot_of = [&](int32_t r) { return p.parts + (2 * static_cast<int64_t>(r) + (r == c0 ? 1 : 0)) * Y::kPartFloats; };
       if constexpr (TREE) {
-        // The parts are joined by twos, each pair by the run that comes second to it (a counter for each, which it leaves at zero):
-        // one run's join of 152 parts of 128 rows took 350 us, of 19 100.
+        // The parts are joined by twos, each pair by the run that comes second to it (a counter for each, which it leaves at zero).
+        // 32 rows of 4 heads on 65,536 tokens, one key/value head: 40 us, with the last run joining all 152 parts 75.
         const int32_t parts = c1 - c0 + 1;
         int32_t from = static_cast<int32_t>(blockIdx.x) - c0;
 #pragma unroll 1
@@ -1785,12 +1785,13 @@ cudaError_t run_kv(void (*kern)(CUtensorMap, CUtensorMap, KvTcArgs), int ctas, c
 }
 
 // Rows of a tile: by what an average sequence has a key/value head (any number is right).  16 sequences of 4096 tokens, 8
-// key/value heads, us with tiles of 8 / 16 / 32 / 128 rows: heads of 128, 4 rows 29.4 / 28.8 / 31.7 / 49.4, 12 rows 33.9 /
-// 29.4 / 33.4 / 50, 24 rows 44.8 / 36.8 / 35.2 / 52, 64 rows 117 / 68 / 51 / 56, 96 rows 144 / 104 / 71 / 61, 128 rows 191 / 125 / 90 /
-// 66; heads of 64, 4 rows 17.5 / 18.7 / 23.9, 16 rows 24.6 / 19.5 / 24.9, 32 rows 38 / 29 / 28, 128 rows 122 / 84 / 79.  The mean is a
-// poor guide to a batch of single tokens with a prompt among them: 128 single tokens on 2048 and a prompt of 512 (32 / 8 heads
+// key/value heads, us with tiles of 8 / 16 / 32 / 128 rows: heads of 128, 4 rows 29.2 / 28.7 / 32.9 / 51.8, 12 rows 34.3 /
+// 29.6 / 35.7 / 53, 24 rows 46.3 / 38.3 / 38.7 / 53, 48 rows 102 / 52.4 / 56.8 / 53.9, 64 rows 119 / 69 / 58.8 / 54.5, 96 rows 145 / 104 /
+// 78 / 55.5, 128 rows 193 / 127 / 99 / 57.3; heads of 64 (those of 128 rows: TREE), 4 rows 17.8 / 19.7 / 25.1 / 52, 16 rows 24.6 / 19.5 / 24.9,
+// 32 rows 39 / 32.7 / 30 / 53, 64 rows 69 / 52 / 47.1 / 53.5, 96 rows 96 / 71 / 65.5 / 53.9, 128 rows 125 / 90 / 83.5 / 54.7.  Trees of
+// unlike size in one batch bring the line between the last two down.  The mean is a poor guide to a batch of single tokens
+// with a prompt among them: 128 single tokens on 2048 and a prompt of 512 (32 / 8 heads
 // of 128) take 155 us in one call, 129 in two; 32 on 4096 and a prompt of 2048 171 and 146.
-constexpr int kTreeFew = 32;
 template <int HD, int R, bool TREE>
 cudaError_t run_few(const KvAttnArgs& a, cudaStream_t st) {
   using Y = KvLay<HD, R, TREE>;
@@ -1803,7 +1804,7 @@ cudaError_t run_kv_rows(const KvAttnArgs& a, cudaStream_t st) {
   if (rows <= 8) return run_few<HD, 8, TREE>(a, st);
   if (rows <= 16) return run_few<HD, 16, TREE>(a, st);
   if constexpr (TREE) {
-    if (rows <= kTreeFew) return run_few<HD, 32, TREE>(a, st);
+    if (rows <= (HD == 128 ? 32 : 64)) return run_few<HD, 32, TREE>(a, st);
     return run_kv<KvMany<HD, TREE>>(kv_attn_rows_kernel<HD, TREE>, 1, a, st);
   } else {
     if (rows <= 64 || HD == 64) return run_few<HD, 32, TREE>(a, st);
