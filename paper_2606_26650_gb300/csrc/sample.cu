@@ -1059,6 +1059,8 @@ __global__ void __launch_bounds__(kHeadThreads, 2) sample_head_kernel(const Samp
         __syncthreads();
       }
     }
+  } else {
+    __syncthreads();  // (the list's counters are set)
   }
   const float ref = bound > -1e30f ? bound * c_hi : 0.0f;
   // (constants of the exact weights: 64-bit floats, beside the pass)

@@ -177,6 +177,16 @@ def test_many_rows_that_need_every_logit(device, dtype, R):
     assert np.abs(lp + np.log(600)).max() <= 2.0 ** -21 * np.log(600)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 40, 513, 2048])
+def test_rows_that_are_taken_whole(device, dtype, V):
+    """Rows without a pass for a bound: no token is lost between a block's first threads and its others, in any call."""
+    u = syn.rng(68, "whole").random(20000).astype(np.float32)
+    want = np.floor(u.astype(np.float64) * V).astype(np.int64)
+    for _ in range(4):
+        assert np.array_equal(run(device, np.full((20000, V), 3.0), dtype, 1, u=u)[1], want)
+
+
 def test_calls_at_once(device):
     """Two streams' calls, which share nothing, give what they give one after the other."""
     import torch
