@@ -22,8 +22,11 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr float kLowest = -3.402823466e38f;
-constexpr int kUndecided = -2;  // a row's token where the first kernel leaves it to the second,
-constexpr int kTaken = -3;      // and where a cluster of the second has taken it
+constexpr int32_t kTaken = -2;      // a row's token where a cluster of the second kernel has taken it,
+constexpr int32_t kUndecided = -3;  // where the first kernel leaves it to the second, and below that where
+// the first kernel leaves it and knows that its tokens can be drawn and which is the largest.
+__device__ __forceinline__ int32_t left_with(int32_t at) { return at <= 0x7ffffffc ? kUndecided - 1 - at : kUndecided; }
+__device__ __forceinline__ int32_t largest_of(int32_t left) { return kUndecided - 1 - left; }  // -1: not known
 
 // ---------------------------------------------------------------- weights
 // 2^(-i / 64) in units of 2^-63.
@@ -240,6 +243,7 @@ struct Common {
   uint64_t red_w[T / 32];
   uint32_t red_c[T / 32];
   int64_t next;  // the row to do, -1: none
+  int32_t left;  // and what the first kernel left of it
   uint32_t best, bad, had_c, n;
   uint64_t had_w, target;
   int32_t at;  // the token's index, -1 where another CTA has it
@@ -427,14 +431,15 @@ __device__ __forceinline__ void draw(const SampleArgs& a, int64_t r, S& s, bool 
   }
 }
 
-// f(row) of the rows that are left.  The first CTA of a cluster looks for one and takes it; a cluster begins its search at a place
+// f(row, what its token says) of the rows that are left.  The first CTA of a cluster looks for one and takes it; a cluster begins its search at a place
 // of its own.  (Of very many rows a cluster looks at a share only.)
 template <int T, class S, class F>
 __device__ __forceinline__ void left_rows(const SampleArgs& a, S& s, const cg::cluster_group& cluster, F f) {
   const int peers = cluster.num_blocks();
   const int64_t clusters = gridDim.x / peers, id = blockIdx.x / peers, chunks = (a.R + T - 1) / T;
   if (a.R <= clusters) {  // a row each: no other cluster writes it, and none of this one before all have come
-    if (__syncthreads_or(a.tokens[id] == kUndecided)) f(id);
+    const int32_t left = a.tokens[id];
+    if (__syncthreads_or(left <= kUndecided)) f(id, left);
     cluster.sync();
     return;
   }
@@ -452,29 +457,35 @@ __device__ __forceinline__ void left_rows(const SampleArgs& a, S& s, const cg::c
       int64_t found = -1;
       while (found < 0 && i < todo) {
         const int64_t mine = row_of(i, threadIdx.x);
-        const uint32_t left = mine < a.R && *static_cast<volatile int32_t*>(a.tokens + mine) == kUndecided ? 1 : 0;
-        if (!__syncthreads_or(left)) {
+        const int32_t left = mine < a.R ? *static_cast<volatile int32_t*>(a.tokens + mine) : 0;
+        if (!__syncthreads_or(left <= kUndecided)) {
           ++i;
           continue;
         }
         // the first thread that sees one tries to take it
-        const uint32_t bits = __ballot_sync(0xffffffffu, left);
+        const uint32_t bits = __ballot_sync(0xffffffffu, left <= kUndecided);
         if ((threadIdx.x & 31) == 0) s.red_c[threadIdx.x >> 5] = bits;
         __syncthreads();
         int w = 0;
         while (!s.red_c[w]) ++w;
-        if (static_cast<int>(threadIdx.x) == 32 * w + __ffs(s.red_c[w]) - 1)
-          s.next = atomicCAS(a.tokens + mine, kUndecided, kTaken) == kUndecided ? mine : -1;
+        if (static_cast<int>(threadIdx.x) == 32 * w + __ffs(s.red_c[w]) - 1) {
+          s.next = atomicCAS(a.tokens + mine, left, kTaken) == left ? mine : -1;
+          s.left = left;
+        }
         __syncthreads();
         found = s.next;
         __syncthreads();
       }
-      if (static_cast<int>(threadIdx.x) < peers) cluster.map_shared_rank(&s, threadIdx.x)->next = found;
+      if (static_cast<int>(threadIdx.x) < peers) {
+        S& to = *cluster.map_shared_rank(&s, threadIdx.x);
+        to.next = found;
+        to.left = s.left;
+      }
     }
     cluster.sync();
     const int64_t r = s.next;
     if (r < 0) return;
-    f(r);
+    f(r, s.left);
     cluster.sync();  // (what one CTA reads of another's is not overwritten)
   }
 }
@@ -503,7 +514,7 @@ __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const S
   const int rank = cluster.block_rank(), tid = threadIdx.x;
   if (tid < 64) s.pow2[tid] = kPow2[tid];
   grid_dependency_wait();
-  left_rows<T>(a, s, cluster, [&](int64_t r) {
+  left_rows<T>(a, s, cluster, [&](int64_t r, int32_t left) {
     const Row<E> row(static_cast<const E*>(a.logits) + r * a.ld, a.V, rank, kPeers);
     const float t = a.temperature ? a.temperature[r] : 1.0f;
     const bool greedy = t == 0.0f;
@@ -517,7 +528,12 @@ __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const S
       best = min(best, k);
       atomicAdd(&s.half[k >> 1], 1u << (16 * (k & 1)));
     });
-    if (!largest<E, T, kPeers>(s, cluster, a, r, best, bad, t)) return;
+    if (largest_of(left) >= 0) {
+      best = Logit<E>::key(Logit<E>::get(row.p + largest_of(left)));
+      cluster.sync();
+    } else if (!largest<E, T, kPeers>(s, cluster, a, r, best, bad, t)) {
+      return;
+    }
     Weigher weigh = s.weigh;
     weigh.max = Logit<E>::of_key(best);
 
@@ -714,7 +730,8 @@ __device__ __forceinline__ int first_bin(const Sums& b, bool by_weight, uint64_t
 }
 
 template <typename E>
-__device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, Binned& s, const cg::cluster_group& cluster) {
+__device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, int32_t left, Binned& s,
+                                              const cg::cluster_group& cluster) {
   constexpr int T = kThreads;
   const int rank = cluster.block_rank(), tid = threadIdx.x;
   const Row<E> row(static_cast<const E*>(a.logits) + r * a.ld, a.V, rank, kPeers);
@@ -723,11 +740,15 @@ __device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, Bi
   if (tid == T - 1) s.weigh = weigher(0.0f, greedy ? 1.0f : t, s.pow2);
   s.clear();
   uint32_t best = 0xffffffffu, bad = 0;
-  row.template each<T>([&](float x, int32_t) {
-    bad |= x < INFINITY ? 0u : 1u;
-    best = min(best, Logit<E>::key(x));
-  });
-  if (!largest<E, T, kPeers>(s, cluster, a, r, best, bad, t)) return;
+  if (largest_of(left) >= 0) {
+    best = Logit<E>::key(Logit<E>::get(row.p + largest_of(left)));
+  } else {
+    row.template each<T>([&](float x, int32_t) {
+      bad |= x < INFINITY ? 0u : 1u;
+      best = min(best, Logit<E>::key(x));
+    });
+    if (!largest<E, T, kPeers>(s, cluster, a, r, best, bad, t)) return;
+  }
   Weigher weigh = s.weigh;
   weigh.max = Logit<E>::of_key(best);
 
@@ -875,7 +896,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_binned_kernel(const Sample
   const cg::cluster_group cluster = cg::this_cluster();
   if (threadIdx.x < 64) s.pow2[threadIdx.x] = kPow2[threadIdx.x];
   grid_dependency_wait();
-  left_rows<kThreads>(a, s, cluster, [&](int64_t r) { sample_binned<E>(a, r, s, cluster); });
+  left_rows<kThreads>(a, s, cluster, [&](int64_t r, int32_t left) { sample_binned<E>(a, r, left, s, cluster); });
 }
 
 // ---------------------------------------------------------------- rows that their largest tokens decide
@@ -1349,7 +1370,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) sample_head_kernel(const Samp
       return;
     }
   }
-  if (tid == 0) a.tokens[r] = kUndecided;
+  if (tid == 0) a.tokens[r] = left_with(s.at[0]);
 }
 
 // A kernel whose launch may begin beside the end of the one ahead (it waits by itself), in clusters of `ctas`.
