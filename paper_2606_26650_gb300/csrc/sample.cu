@@ -820,6 +820,7 @@ __device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, in
     const uint32_t upto = warp_scan(lane < kPeers ? cluster.map_shared_rank(&s, lane)->n : 0u);
     const uint32_t m = min(__shfl_sync(0xffffffffu, upto, 31), static_cast<uint32_t>(kList));
     static_assert(kPeers <= T / 32, "a warp a CTA of the cluster");
+    const uint32_t own1 = min(__shfl_sync(0xffffffffu, upto, rank), m), own0 = own1 - min(s.n, own1);
     if (warp < kPeers) {
       const Binned& p = *cluster.map_shared_rank(&s, warp);
       const uint32_t end = min(__shfl_sync(0xffffffffu, upto, warp), m), from = end - min(p.n, end);
@@ -829,26 +830,37 @@ __device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, in
         s.all.w[from + e] = p.own.w[e];
       }
     }
-    cluster.sync();
-    if (static_cast<uint32_t>(tid) < m) {
-      const uint32_t k = s.all.key[tid];
-      const int32_t at = s.all.at[tid];
-      uint32_t c = c0;
-      uint64_t w = w0;
+    __syncthreads();
+    // (a CTA looks at its own tokens, a group of lanes at one of them)
+    constexpr uint32_t kGroup = 16;
+    for (uint32_t e = own0; e < own1; e += T / kGroup) {
+      const uint32_t mine = e + tid / kGroup, me = min(mine, own1 - 1), k = s.all.key[me];
+      const int32_t at = s.all.at[me];
+      uint32_t c = 0;
+      uint64_t w = 0;
 #pragma unroll 4
-      for (uint32_t i = 0; i < m; ++i) {
+      for (uint32_t i = tid % kGroup; i < m; i += kGroup) {
         const uint32_t ki = s.all.key[i];
         const bool ahead = ki < k || (ki == k && s.all.at[i] < at);
         c += ahead ? 1u : 0u;
         w += ahead ? s.all.w[i] : 0u;
       }
-      const uint64_t mine = by_weight ? w : c, with = mine + (by_weight ? s.all.w[tid] : 1u);
-      if (mine < target && target <= with) {
-        s.place = Place{k, 0, c, w, s.all.w[tid]};
-        s.at = rank == 0 ? at : -1;
+#pragma unroll
+      for (uint32_t o = kGroup / 2; o > 0; o >>= 1) {
+        c += __shfl_xor_sync(0xffffffffu, c, o);
+        w += __shfl_xor_sync(0xffffffffu, w, o);
+      }
+      c += c0;
+      w += w0;
+      const uint64_t from = by_weight ? w : c, with = from + (by_weight ? s.all.w[me] : 1u);
+      const uint32_t to = tid % kGroup;  // (a lane tells a CTA)
+      if (mine < own1 && from < target && target <= with && to < kPeers) {
+        Binned& p = *cluster.map_shared_rank(&s, to);
+        p.place = Place{k, 0, c, w, s.all.w[me]};
+        p.at = to == 0 ? at : -1;
       }
     }
-    __syncthreads();
+    cluster.sync();
     return s.place;
   };
   auto heavy = [&](uint64_t least, uint32_t& c, uint64_t& sum) {
