@@ -490,14 +490,19 @@ __device__ __forceinline__ void left_rows(const SampleArgs& a, S& s, const cg::c
   }
 }
 // ---- 16-bit logits: how often each key comes is all there is to know.  A CTA counts its part's keys in 16 bits each; of the
-// keys that weigh anything each CTA adds up a share over all parts, a thread some of them in order.
+// keys that weigh anything each CTA adds up a share over all parts, a thread some of them in order.  Most keys are of numbers
+// next to 0, which no token has: the shares are of the blocks of 32 keys that any CTA has met.
 constexpr int kCountPeers = 8, kCountThreads = 1024, kKeys = 65536, kShare = kKeys / kCountPeers;
+constexpr int kBlockKeys = 32, kBlocks = kKeys / kBlockKeys;
 constexpr int32_t kMostCounted = 500000;  // a part's count of one key stays below 2^16
 
 struct Counts : Common<kCountThreads> {
   alignas(16) uint32_t half[kKeys / 2];  // two keys' counts a word (cleared 16 bytes at a time)
   uint64_t weight[kShare];               // of the keys of the CTA's share, 0 for those that no token has
   alignas(8) uint32_t whole[kShare];     // the row's counts of them
+  uint32_t met[kBlocks / 32];            // bits of the blocks that the CTA has met
+  uint32_t any[kBlocks / 32], ahead[kBlocks / 32];  // that any CTA has, and how many such lie ahead of the word's
+  uint16_t block[kShare / kBlockKeys];   // the share's
   uint32_t all_c;
   uint64_t all_w;
   Place place[2];
@@ -528,6 +533,22 @@ __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const S
       best = min(best, k);
       atomicAdd(&s.half[k >> 1], 1u << (16 * (k & 1)));
     });
+    __syncthreads();
+    {  // 64 blocks a warp, 8 at a time
+      uint32_t met[2] = {0u, 0u};
+      const uint4* const at = reinterpret_cast<const uint4*>(s.half) + (tid >> 5) * 256 + (tid & 31);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint4 c = at[32 * i];
+        uint32_t bits = __ballot_sync(0xffffffffu, (c.x | c.y | c.z | c.w) != 0u);
+        bits |= bits >> 1;
+        bits = (bits | bits >> 2) & 0x11111111u;  // of four lanes a block
+        bits = (bits | bits >> 3) & 0x03030303u;
+        bits = (bits | bits >> 6) & 0x000f000fu;
+        met[i / 4] |= ((bits | bits >> 12) & 0xffu) << (8 * (i % 4));
+      }
+      if ((tid & 31) < 2) s.met[tid >> 5 << 1 | (tid & 31)] = tid & 1 ? met[1] : met[0];
+    }
     if (largest_of(left) >= 0) {
       best = Logit<E>::key(Logit<E>::get(row.p + largest_of(left)));
       cluster.sync();
@@ -538,13 +559,35 @@ __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const S
     weigh.max = Logit<E>::of_key(best);
 
     // the share's keys over all parts, a thread's side by side
-    const uint32_t range = Logit<E>::key(fmaxf(__fsub_rd(weigh.max, 1.001f * weigh.cut), kLowest)) - best + 1;
-    const uint32_t even = best & ~1u, words = (best + range + 1 - even) / 2, share = (words + kPeers - 1) / kPeers * 2;
-    const uint32_t k0 = even + rank * share, mine = 2 * min(share / 2, words - min(words, rank * share / 2));
+    const uint32_t last = Logit<E>::key(fmaxf(__fsub_rd(weigh.max, 1.001f * weigh.cut), kLowest)) / kBlockKeys;
+    if (tid < kBlocks / 32) {
+      uint32_t any = 0;
+#pragma unroll
+      for (int e = 0; e < kPeers; ++e) any |= cluster.map_shared_rank(&s, e)->met[tid];
+      const int below = static_cast<int>(last) + 1 - 32 * tid;  // (blocks behind the last weigh nothing)
+      s.any[tid] = below >= 32 ? any : below > 0 ? any & ((1u << below) - 1u) : 0u;
+    }
+    __syncthreads();
+    if (tid < 32) {
+      const uint32_t n0 = __popc(s.any[2 * tid]), n1 = __popc(s.any[2 * tid + 1]), upto = warp_scan(n0 + n1);
+      s.ahead[2 * tid] = upto - n0 - n1;
+      s.ahead[2 * tid + 1] = upto - n1;
+    }
+    __syncthreads();
+    const uint32_t met = s.ahead[kBlocks / 32 - 1] + __popc(s.any[kBlocks / 32 - 1]), share = (met + kPeers - 1) / kPeers;
+    const uint32_t first = min(rank * share, met), mine = kBlockKeys * (min(first + share, met) - first);
+#pragma unroll
+    for (int i = tid; i < kBlocks; i += T) {
+      const uint32_t bits = s.any[i / 32], at = s.ahead[i / 32] + __popc(bits & ((1u << (i % 32)) - 1u)) - first;
+      if ((bits >> (i % 32) & 1u) && at < mine / kBlockKeys) s.block[at] = static_cast<uint16_t>(i);
+    }
+    __syncthreads();
+    auto key_of = [&](uint32_t i) { return kBlockKeys * s.block[i / kBlockKeys] + i % kBlockKeys; };
     for (uint32_t i = tid; i < mine / 2; i += T) {
+      const uint32_t word = key_of(2 * i) / 2;
       uint32_t c[kPeers];
 #pragma unroll
-      for (int e = 0; e < kPeers; ++e) c[e] = cluster.map_shared_rank(&s, e)->half[k0 / 2 + i];
+      for (int e = 0; e < kPeers; ++e) c[e] = cluster.map_shared_rank(&s, e)->half[word];
       uint2 sum = make_uint2(0u, 0u);
 #pragma unroll
       for (int e = 0; e < kPeers; ++e) {
@@ -554,13 +597,13 @@ __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const S
       reinterpret_cast<uint2*>(s.whole)[i] = sum;
     }
     __syncthreads();
-    for (uint32_t i = tid; i < mine; i += T) s.weight[i] = s.whole[i] ? weigh(Logit<E>::of_key(k0 + i)) : 0;
+    for (uint32_t i = tid; i < mine; i += T) s.weight[i] = s.whole[i] ? weigh(Logit<E>::of_key(key_of(i))) : 0;
     __syncthreads();
-    const uint32_t per = (share + T - 1) / T, i0 = min(tid * per, mine), i1 = min(i0 + per, mine);
+    const uint32_t per = (share * kBlockKeys + T - 1) / T, i0 = min(tid * per, mine), i1 = min(i0 + per, mine);
     auto walk = [&](auto f) {  // f(key, tokens, weight of one) of the thread's keys that weigh anything
       for (uint32_t i = i0; i < i1; ++i) {
         const uint64_t w = s.weight[i];
-        if (w && f(k0 + i, s.whole[i], w)) return;
+        if (w && f(key_of(i), s.whole[i], w)) return;
       }
     };
     uint32_t own_c = 0, all_c;
@@ -927,8 +970,10 @@ constexpr int kMostCtas = 8;     // of a cluster
 
 struct Head {
   uint64_t packed[kCap];  // the list by bins: a token's key and index
-  uint64_t sum[kCap];     // the weights in order, then their running sums
-  float x[kCap];          // the list
+  union {
+    float x[kCap];        // the list, then (in order)
+    uint64_t sum[kCap];   // the weights, then their running sums
+  };
   int32_t at[kCap];       // its indexes, then in order
   uint32_t upto[kSpread];
   uint64_t pow2[64];
@@ -936,7 +981,7 @@ struct Head {
   int32_t red[kHeadWarps];
   float sample[kHeadThreads];
   int32_t reach[kHeadWarps];
-  // of every CTA of the cluster: its bound, the others' weights in units of 2^-28 2^(their reference), that, and their number
+  // of every CTA of the cluster: its bound, the others' weights in units of 2^-26 2^(their reference), that, and their number
   float bound[kMostCtas], ref[kMostCtas];
   uint64_t rest[kMostCtas];
   uint32_t others[kMostCtas];
@@ -1014,7 +1059,7 @@ __device__ __forceinline__ void ask(Head& s, uint64_t (&out)[2], uint64_t least,
 
 template <typename E>
 __global__ void __launch_bounds__(kHeadThreads, 2) sample_head_kernel(const SampleArgs a) {
-  constexpr int VEC = Logit<E>::kVec, kDeep = 4, kPicks = 8 / VEC;
+  constexpr int VEC = Logit<E>::kVec, kDeep = 4;
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Head& s = *reinterpret_cast<Head*>(smem_raw);
   const cg::cluster_group cluster = cg::this_cluster();
@@ -1033,37 +1078,48 @@ __global__ void __launch_bounds__(kHeadThreads, 2) sample_head_kernel(const Samp
     if (rank == 0 && tid == 0) a.tokens[r] = kUndecided;
     return;
   }
-  // c = log2(e) / T as a float and a positive rest (with which -inf stays -inf)
+  // c = log2(e) / T as a float and a rest (the pass over the row does without it: c_hi (x - bound) is what it needs)
   float c_hi, c_lo;
   {
     const float by = greedy ? 1.0f : t;
     c_hi = __fdiv_rn(1.44269504f, by);
     c_lo = __fdiv_rn(fmaf(-c_hi, by, 1.44269504f) + 1.925963e-8f, by);
-    if (!(c_lo > 0.0f)) {
-      c_hi = __uint_as_float(__float_as_uint(c_hi) - 1u);
-      c_lo = __fdiv_rn(fmaf(-c_hi, by, 1.44269504f) + 1.925963e-8f, by);
-    }
   }
 
-  // The bound: of the sample, the largest of 8 elements a thread; of a share q of the row, one of 8 is in it with
-  // 1 - (1 - q)^8.  In two rounds each warp counts how many of the threads reach one of 16 values between the largest of all and
+  // The part's vectors, 32 at a time, in as many streams as a step of the pass takes, side by side in the row: a step's i-th
+  // vectors of the thread.  The first step's are the sample, too.
+  const int32_t groups = (v1 - v0 + 31) / 32, per = max((groups + kDeep * kHeadWarps - 1) / (kDeep * kHeadWarps), 1);
+  auto spot = [&](int i, int32_t step) { return v0 + 32 * ((i * kHeadWarps + warp) * per + step) + lane; };
+  uint4 q[kDeep];
+  auto load = [&](int32_t step) {
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i)
+      if (spot(i, step) < v1) q[i] = row.vec(spot(i, step));
+  };
+  load(0);
+
+  // The bound: of the sample, the largest of a thread's elements; of a share q of the row, one of m is in it with
+  // 1 - (1 - q)^m.  In two rounds each warp counts how many of the threads reach one of 16 values between the largest of all and
   // the least that can matter.
   float bound = kLowest;
   if (a.V > kWhole && v1 > v0) {
     float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kPicks; ++i) {
-      const uint4 q = row.vec(v0 + static_cast<int32_t>(static_cast<int64_t>(tid * kPicks + i) * (v1 - v0) / (kHeadThreads * kPicks)));
-      float x[VEC];
-      Logit<E>::get(q, x);
-      top = fmaxf(top, most_of(q, x, static_cast<const E*>(nullptr)));
-    }
+    for (int i = 0; i < kDeep; ++i)
+      if (spot(i, 0) < v1) {
+        float x[VEC];
+        Logit<E>::get(q[i], x);
+        top = fmaxf(top, most_of(q[i], x, static_cast<const E*>(nullptr)));
+      }
     s.sample[tid] = top;
     const int32_t highest = __reduce_max_sync(0xffffffffu, in_order(top));
     if (lane == 0) s.red[warp] = highest;
     const float want = greedy ? 64.0f : k > 0 ? fminf(fmaxf(1.25f * k + 100.0f, kWant), kMostWanted) : kWant;
-    const float miss = fmaxf(1.0f - want / a.V, 0.0f), miss2 = miss * miss, miss4 = miss2 * miss2;
-    const int32_t reach = max(static_cast<int32_t>(kHeadThreads * (1.0f - miss4 * miss4)), 4);
+    // (some warps have a vector a thread more than the others)
+    const int32_t streams = (groups + per - 1) / per, full = streams / kHeadWarps;
+    const float miss = log2f(fmaxf(1.0f - want / a.V, 0.0f)) * VEC, none = full > 0 ? ex2(miss * full) : 1.0f;
+    const float more = ex2(miss * (full + 1)), share = static_cast<float>(streams % kHeadWarps) / kHeadWarps;
+    const int32_t reach = max(static_cast<int32_t>(kHeadThreads * (1.0f - share * more - (1.0f - share) * none)), 4);
     __syncthreads();
     int32_t most = s.red[0];
 #pragma unroll
@@ -1112,7 +1168,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) sample_head_kernel(const Samp
   auto one = [&](int32_t at) {
     const float x = Logit<E>::get(row.p + at);
     if (x < bound)
-      rest += __float2uint_rn(ex2(fmaf(x, c_lo, fmaf(x, c_hi, -ref))) * 0x1p28f);
+      rest += __float2uint_rn(ex2(fmaf(x, c_hi, -ref)) * 0x1p26f);
     else
       keep(x, at);
   };
@@ -1123,7 +1179,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) sample_head_kernel(const Samp
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       const bool below = x[e] < bound;
-      w[e] = below ? ex2(fmaf(x[e], c_lo, fmaf(x[e], c_hi, -ref))) : 0.0f;
+      w[e] = below ? ex2(fmaf(x[e], c_hi, -ref)) : 0.0f;
       high |= below ? 0u : 1u << e;
     }
 #pragma unroll 1
@@ -1135,25 +1191,20 @@ __global__ void __launch_bounds__(kHeadThreads, 2) sample_head_kernel(const Samp
     for (int o = VEC / 2; o > 0; o >>= 1)
 #pragma unroll
       for (int e = 0; e < o; ++e) w[e] += w[e + o];
-    rest += __float2uint_rn(w[0] * 0x1p28f);
+    return w[0];
   };
-  // (the next vectors are on their way while these are looked at)
-  uint4 q[kDeep];
-  auto load = [&](int32_t v) {
-#pragma unroll
-    for (int i = 0; i < kDeep; ++i)
-      if (v + i * kHeadThreads < v1) q[i] = row.vec(v + i * kHeadThreads);
-  };
-  load(v0 + tid);
+  // (the next step's vectors are on their way while these are looked at)
 #pragma unroll 1
-  for (int32_t v = v0 + tid; v < v1; v += kDeep * kHeadThreads) {
+  for (int32_t step = 0; step < per; ++step) {
     uint4 now[kDeep];
 #pragma unroll
     for (int i = 0; i < kDeep; ++i) now[i] = q[i];
-    load(v + kDeep * kHeadThreads);
+    if (step + 1 < per) load(step + 1);
+    float sum = 0.0f;  // (below 2^5)
 #pragma unroll
     for (int i = 0; i < kDeep; ++i)
-      if (v + i * kHeadThreads < v1) vec(now[i], v + i * kHeadThreads);
+      if (spot(i, step) < v1) sum += vec(now[i], spot(i, step));
+    rest += __float2uint_rn(sum * 0x1p26f);
   }
   if (row.first && tid < row.head) one(tid);
   if (row.last && row.tail() + tid < row.V) one(row.tail() + tid);
@@ -1305,12 +1356,13 @@ __global__ void __launch_bounds__(kHeadThreads, 2) sample_head_kernel(const Samp
   if (!known && warp == 0) {
     uint64_t rest_sum = lane < kHeadWarps ? s.red_low[lane] : 0, off = 0;
     if (lane < ctas) {
-      const double down = fmax(static_cast<double>(max_x) * c_hi + static_cast<double>(max_x) * c_lo - s.ref[lane], 0.0);
+      const double at = s.bound[lane], up = static_cast<double>(max_x) - at;
+      const double down = fmax(up * c_hi + up * c_lo + (at * c_hi - s.ref[lane]), 0.0);
       if (down < 60.0) {  // (else it weighs nothing)
         const uint64_t tq = static_cast<uint64_t>(down * 0x1p56);
-        const uint64_t w = __umul64hi(s.rest[lane] << 15, exp2_fraction(tq, s.pow2)) >> (2 + static_cast<int>(tq >> 56));
-        // Each weight is off by 2^-22 (ex2), its argument's two roundings, |t| 2^-24 with |t| 2^t at most 0.53 of the bound's
-        // weight, three additions, and half a unit when it is rounded to one.
+        const uint64_t w = __umul64hi(s.rest[lane] << 17, exp2_fraction(tq, s.pow2)) >> (2 + static_cast<int>(tq >> 56));
+        // Each weight is off by 2^-22 (ex2), seven additions, its argument's rounding and that of c, |t| (2^-24 + 2^-25) with
+        // |t| 2^t at most 0.53 of the bound's weight, the sum's rounding to 2^-26 of that, and half a unit when it is rounded to one.
         rest_sum += w;
         off = (w >> 20) + (s.others[lane] * weigh(s.bound[lane]) >> 24) + s.others[lane] / 2 + 2;
       }
