@@ -48,7 +48,6 @@ __device__ const uint64_t kPow2[64] = {
     0x45cae0f1f545eb73ull, 0x450a6abaa4b77ecdull, 0x444c0740496d4294ull, 0x438fb0cb4f468808ull,
     0x42d561b3e6243d8aull, 0x421d1461d66f2023ull, 0x4166c34c5615d0ecull, 0x40b268f9de0183baull};
 constexpr int kOneBits = 40;                     // the largest weight is 2^40
-constexpr uint64_t kOne = uint64_t(1) << kOneBits;
 
 // Weights of a row: exp(-(max - x) / T) as 2^-t in integers, t = D C / 2^64 in units of 2^-56 with D = (max - x) 2^k, which has
 // up to 63 bits (max - x as an fp32 number and its rounding, both exact), and C = 2^(120 - k) log2(e) / T.  t is its whole part,
@@ -119,7 +118,7 @@ __device__ __forceinline__ uint64_t reaches(float p, uint64_t whole) {
 }
 // The least weight that min-p keeps.
 __device__ __forceinline__ uint64_t least_of(float min_p) {
-  return static_cast<uint64_t>(ceil(static_cast<double>(fminf(min_p, 1.0f)) * static_cast<double>(kOne)));
+  return __float2ull_ru(fminf(min_p, 1.0f) * 0x1p40f);  // (an exact product)
 }
 // The running weight that the token has to reach: floor(u whole) + 1, from 1 to whole.
 __device__ __forceinline__ uint64_t passes(float u, uint64_t whole) {
@@ -1022,29 +1021,21 @@ __device__ __forceinline__ float most_of(const uint4&, const float* x, const flo
   return a;
 }
 
+// How many of the n tokens in order f(token) holds for, in every thread.
+template <class F>
+__device__ __forceinline__ int32_t count_of(int32_t n, F f) {
+  int32_t c = 0;
+#pragma unroll 1
+  for (int32_t i = threadIdx.x; i - static_cast<int32_t>(threadIdx.x) < n; i += kHeadThreads) c += __syncthreads_count(i < n && f(i));
+  return c;
+}
 // The first of the n tokens in order whose running weight reaches target, n - 1 if none.
 __device__ __forceinline__ int32_t first_place(const Head& s, int32_t n, uint64_t target) {
-  int32_t lo = 0, hi = n - 1;
-  while (lo < hi) {
-    const int32_t mid = (lo + hi) / 2;
-    if (s.sum[mid] >= target)
-      hi = mid;
-    else
-      lo = mid + 1;
-  }
-  return lo;
+  return min(count_of(n, [&](int32_t i) { return s.sum[i] < target; }), n - 1);
 }
 // The first of them that weighs less than w, n if none (the first weighs as much as any may be asked).
 __device__ __forceinline__ int32_t first_light(const Head& s, int32_t n, uint64_t w) {
-  int32_t lo = 1, hi = n;
-  while (lo < hi) {
-    const int32_t mid = (lo + hi) / 2;
-    if (s.sum[mid] - s.sum[mid - 1] < w)
-      hi = mid;
-    else
-      lo = mid + 1;
-  }
-  return lo;
+  return max(count_of(n, [&](int32_t i) { return s.sum[i] - (i ? s.sum[i - 1] : 0) >= w; }), 1);
 }
 // f of the weight of what is kept, or of the least and the largest that it can be, in every thread (f is in 64-bit floats, of
 // which an SM has few: two threads compute it).
@@ -1469,9 +1460,12 @@ cudaError_t go(void (*kern)(SampleArgs), const SampleArgs& a, int64_t rows, int 
 template <typename E>
 cudaError_t run_sample(const SampleArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> ready[3];
-  // CTAs a row: as many as there are SMs for, with two vectors a thread or more
+  // CTAs a row.  Rows that one takes in a step of its pass have one (8,000 logits: 13.6 us, 14.2 by two).  Others as many as leave
+  // the SMs a CTA each: 131,072 bf16 logits, 64 rows: 28.6 us by one, 25.2 by two, 26.6 by four; 100 rows: 29.4, 31.5, 35.6;
+  // 16 rows: 25.6, 21.7, 19.0 and 19.6 by eight; 4 rows 16.9 by four, 15.6 by eight.
   int ctas = 1;
-  while (ctas < kMostCtas && a.R * ctas * 2 <= 304 && a.V / Logit<E>::kVec >= 2 * kHeadThreads * ctas * 2) ctas *= 2;
+  if (a.V / Logit<E>::kVec >= 4 * kHeadThreads)
+    while (ctas < kMostCtas && a.R * ctas * 2 <= (ctas == 4 ? 64 : 128)) ctas *= 2;
   const cudaError_t e = go<Head>(sample_head_kernel<E>, a, a.R, ctas, kHeadThreads, ready[0], st);
   if (e != cudaSuccess) return e;
   if (sizeof(E) == 2 && a.V <= kMostCounted)
