@@ -184,6 +184,7 @@ struct Logit<uint16_t> {
 template <typename E>
 struct Row {
   const E* p;
+  const uint4* held;  // the part's vectors, from the first on
   int32_t V, head, vecs, v0, v1;
   bool first, last;
   __device__ __forceinline__ Row(const E* row, int32_t n, int part, int parts) : p(row), V(n) {
@@ -191,10 +192,11 @@ struct Row {
     vecs = (V - head) / Logit<E>::kVec;
     v0 = static_cast<int32_t>(static_cast<int64_t>(vecs) * part / parts);
     v1 = static_cast<int32_t>(static_cast<int64_t>(vecs) * (part + 1) / parts);
+    held = reinterpret_cast<const uint4*>(p + head) + v0;
     first = part == 0;
     last = part == parts - 1;
   }
-  __device__ __forceinline__ uint4 vec(int32_t v) const { return reinterpret_cast<const uint4*>(p + head)[v]; }
+  __device__ __forceinline__ uint4 vec(int32_t v) const { return held[v - v0]; }
   __device__ __forceinline__ int32_t tail() const { return head + vecs * Logit<E>::kVec; }
   // Elements of the part.
   __device__ __forceinline__ int32_t count() const {
@@ -205,9 +207,10 @@ struct Row {
   __device__ __forceinline__ void each(F f) const {
     each<kThreads>([](float x) { return x; }, [&](float, float x, int32_t at) { f(x, at); });
   }
-  // f(g(x), x, index), g of a vector's elements first.
+  // f(g(x), x, index), g of a vector's elements first.  The vectors go into `keep` too, where that is given; every thread finds
+  // its own there.
   template <int kThreads, class G, class F>
-  __device__ __forceinline__ void each(G g, F f) const {
+  __device__ __forceinline__ void each(G g, F f, uint4* keep = nullptr) const {
     constexpr int VEC = Logit<E>::kVec;
     const int32_t t = threadIdx.x;
     auto one = [&](int32_t at) {
@@ -218,7 +221,9 @@ struct Row {
 #pragma unroll 1
     for (int32_t v = v0 + t; v < v1; v += kThreads) {
       float x[VEC];
-      Logit<E>::get(vec(v), x);
+      const uint4 q = vec(v);
+      if (keep) keep[v - v0] = q;
+      Logit<E>::get(q, x);
       decltype(g(0.0f)) y[VEC];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) y[i] = g(x[i]);
@@ -692,6 +697,7 @@ constexpr int kThreads = 1024;
 constexpr int kPeers = 8;  // CTAs of a cluster
 constexpr int kBinBits = 11, kBins = 1 << kBinBits, kBinShare = kBins / kPeers;
 constexpr int kList = 512;  // tokens whose ranks are found one against all others
+constexpr int kHeld = 4096;  // vectors of its part that a CTA keeps (131,072 fp32 logits)
 
 struct Sums {  // of a bin and all before it
   uint64_t weight[kBins];
@@ -707,6 +713,7 @@ struct Binned : Common<kThreads> {
   Sums sums[2];
   Tokens own, all;
   Place place;
+  uint4 held[kHeld];
   __device__ __forceinline__ void clear() {
     for (int i = threadIdx.x; i < kBins; i += kThreads) count[i] = lo[i] = hi[i] = 0;
     __syncthreads();
@@ -724,19 +731,34 @@ __device__ __forceinline__ void sum_up(Binned& s, const cg::cluster_group& clust
   constexpr int kPer = kBins / kThreads;
   const int rank = cluster.block_rank();
   cluster.sync();
-  if (threadIdx.x < kBinShare) {
-    const int bin = rank * kBinShare + threadIdx.x;
+  {  // some threads a bin, each for some of the CTAs, a warp's bins side by side
+    constexpr int kShare = kThreads / kBinShare, kEach = kPeers / kShare;
+    static_assert(kShare * kBinShare == kThreads && kEach * kShare == kPeers && kThreads == 2 * kList, "all threads, all CTAs");
+    const int at = threadIdx.x % kBinShare, bin = rank * kBinShare + at, peer = threadIdx.x / kBinShare * kEach;
     uint32_t c = 0;
     uint64_t w = 0;
 #pragma unroll
-    for (int i = 0; i < kPeers; ++i) {
-      const Binned& p = *cluster.map_shared_rank(&s, i);
+    for (int i = 0; i < kEach; ++i) {
+      const Binned& p = *cluster.map_shared_rank(&s, peer + i);
       c += p.count[bin];
       w += (static_cast<uint64_t>(p.hi[bin]) << 32) + p.lo[bin];
     }
+    Tokens& mine = threadIdx.x < kList ? s.own : s.all;
+    mine.key[threadIdx.x % kList] = c;
+    mine.w[threadIdx.x % kList] = w;
+    __syncthreads();
+    c = 0;
+    w = 0;
 #pragma unroll
-    for (int i = 0; i < kPeers; ++i) {
-      Sums& p = *cluster.map_shared_rank(&to, i);
+    for (int i = 0; i < kShare; ++i) {
+      const int t = i * kBinShare + at;
+      const Tokens& of = t < kList ? s.own : s.all;
+      c += of.key[t % kList];
+      w += of.w[t % kList];
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      Sums& p = *cluster.map_shared_rank(&to, peer + i);
       p.count[bin] = c;
       p.weight[bin] = w;
     }
@@ -776,7 +798,7 @@ __device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, in
                                               const cg::cluster_group& cluster) {
   constexpr int T = kThreads;
   const int rank = cluster.block_rank(), tid = threadIdx.x;
-  const Row<E> row(static_cast<const E*>(a.logits) + r * a.ld, a.V, rank, kPeers);
+  Row<E> row(static_cast<const E*>(a.logits) + r * a.ld, a.V, rank, kPeers);
   const float t = a.temperature ? a.temperature[r] : 1.0f;
   const bool greedy = t == 0.0f;
   if (tid == T - 1) s.weigh = weigher(0.0f, greedy ? 1.0f : t, s.pow2);
@@ -799,7 +821,8 @@ __device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, in
   auto bin_of = [&](float x) { return min(static_cast<int>((weigh.max - x) * by), kBins - 1); };
   row.template each<T>([&](float x) { return weigh.beside(x); }, [&](uint64_t w, float x, int32_t) {
     if (w) s.add(bin_of(x), w);
-  });
+  }, row.v1 - row.v0 <= kHeld ? s.held : nullptr);
+  if (row.v1 - row.v0 <= kHeld) row.held = s.held;
   sum_up(s, cluster, s.sums[0], 0, 0);
 
   auto find = [&](bool by_weight, uint64_t target) {
