@@ -495,7 +495,9 @@ __device__ __forceinline__ void left_rows(const SampleArgs& a, S& s, const cg::c
 }
 // ---- 16-bit logits: how often each key comes is all there is to know.  A CTA counts its part's keys in 16 bits each; of the
 // keys that weigh anything each CTA adds up a share over all parts, a thread some of them in order.  Most keys are of numbers
-// next to 0, which no token has: the shares are of the blocks of 32 keys that any CTA has met.
+// next to 0, which no token has: the shares are of the blocks of 32 keys that any CTA has met (64 undecided rows of 131,072: 90 us
+// for both kernels, 102 with shares of all keys).  A row is 11 us of exchanges and barriers: counting 3, the keys' sums and
+// weights 3, running sums 3, a place 2 for each filter and the token.
 constexpr int kCountPeers = 8, kCountThreads = 1024, kKeys = 65536, kShare = kKeys / kCountPeers;
 constexpr int kBlockKeys = 32, kBlocks = kKeys / kBlockKeys;
 constexpr int32_t kMostCounted = 500000;  // a part's count of one key stays below 2^16
@@ -692,7 +694,8 @@ __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const S
 }
 
 // ---- any logits: a histogram of counts and weights by max - x; in one of its bins, by ranks where it has few tokens, by keys
-// (and finer ones) where it has many.
+// (and finer ones) where it has many.  A row of 100,003 fp32 logits takes 28 us: 12 for all weights and their three atomics a
+// token, 5 for the bins' sums over the CTAs, 10 for a place.
 constexpr int kThreads = 1024;
 constexpr int kPeers = 8;  // CTAs of a cluster
 constexpr int kBinBits = 11, kBins = 1 << kBinBits, kBinShare = kBins / kPeers;
@@ -982,6 +985,11 @@ __global__ void __launch_bounds__(kThreads, 1) sample_binned_kernel(const Sample
 // fp32 with an error that is bounded.  The cluster's first CTA puts the list in order and sums its weights up exactly.  Where
 // what is kept ends inside the list, or the token is inside it for the least and the largest sum that the others can have, this
 // is the result; a row of which neither holds, or whose list overflows, is left to the second kernel.
+// 64 rows of 131,072 bf16 logits (16.8 MB) take 18 us here, 384 of 100,003 in fp32 (153.6 MB) 53, 2.9 TB/s.  The pass itself runs
+// at 6 TB/s with two CTAs an SM; bounds are the last wave of CTAs (384 on 304 places) and some 16,000 cycles of a CTA behind
+// its pass in which the SM loads little: the exchange, the list's order, exact weights, and sums and decisions with a barrier
+// after each.  Three CTAs an SM (40 registers) 3 % slower; elements at the bound and above looked for in a second look at their
+// vectors 6 to 20 %; stretches of 2 KB a warp and step 2 % faster for long rows and 9 % slower for parts of one step.
 constexpr int kHeadThreads = 512, kHeadWarps = kHeadThreads / 32;
 constexpr int kCap = 2560;       // tokens of a list
 constexpr int kWhole = 2048;     // rows of up to so many are taken whole
