@@ -443,8 +443,10 @@ __device__ __forceinline__ void left_rows(const SampleArgs& a, S& s, const cg::c
   const int64_t clusters = gridDim.x / peers, id = blockIdx.x / peers, chunks = (a.R + T - 1) / T;
   if (a.R <= clusters) {  // a row each: no other cluster writes it, and none of this one before all have come
     const int32_t left = a.tokens[id];
-    if (__syncthreads_or(left <= kUndecided)) f(id, left);
-    cluster.sync();
+    if (__syncthreads_or(left <= kUndecided)) {
+      f(id, left);
+      cluster.sync();  // (what one CTA reads of another's is there until it has)
+    }
     return;
   }
   const bool share = chunks > kSearched;
