@@ -699,8 +699,7 @@ __global__ void __launch_bounds__(kCountThreads, 1) sample_counts_kernel(const S
 // (and finer ones) where it has many.  A row of 100,003 fp32 logits takes 28 us: 12 for all weights and their three atomics a
 // token, 5 for the bins' sums over the CTAs, 10 for a place.
 constexpr int kThreads = 1024;
-constexpr int kPeers = 8;  // CTAs of a cluster
-constexpr int kBinBits = 11, kBins = 1 << kBinBits, kBinShare = kBins / kPeers;
+constexpr int kBinBits = 11, kBins = 1 << kBinBits;
 constexpr int kList = 512;  // tokens whose ranks are found one against all others
 constexpr int kHeld = 4096;  // vectors of its part that a CTA keeps (131,072 fp32 logits)
 
@@ -732,12 +731,20 @@ struct Binned : Common<kThreads> {
 };
 
 // The histograms of all CTAs to running sums, on top of what came before them.
+template <int kPeers>
 __device__ __forceinline__ void sum_up(Binned& s, const cg::cluster_group& cluster, Sums& to, uint32_t c0, uint64_t w0) {
   constexpr int kPer = kBins / kThreads;
   const int rank = cluster.block_rank();
-  cluster.sync();
-  {  // some threads a bin, each for some of the CTAs, a warp's bins side by side
-    constexpr int kShare = kThreads / kBinShare, kEach = kPeers / kShare;
+  if constexpr (kPeers == 1) {
+    __syncthreads();
+    for (int bin = threadIdx.x; bin < kBins; bin += kThreads) {
+      to.count[bin] = s.count[bin];
+      to.weight[bin] = (static_cast<uint64_t>(s.hi[bin]) << 32) + s.lo[bin];
+    }
+    __syncthreads();
+  } else {  // some threads a bin, each for some of the CTAs, a warp's bins side by side
+    cluster.sync();
+    constexpr int kBinShare = kBins / kPeers, kShare = kThreads / kBinShare, kEach = kPeers / kShare;
     static_assert(kShare * kBinShare == kThreads && kEach * kShare == kPeers && kThreads == 2 * kList, "all threads, all CTAs");
     const int at = threadIdx.x % kBinShare, bin = rank * kBinShare + at, peer = threadIdx.x / kBinShare * kEach;
     uint32_t c = 0;
@@ -767,8 +774,8 @@ __device__ __forceinline__ void sum_up(Binned& s, const cg::cluster_group& clust
       p.count[bin] = c;
       p.weight[bin] = w;
     }
+    cluster.sync();
   }
-  cluster.sync();
   uint32_t c[kPer], ca = 0, all_c;
   uint64_t w[kPer], wa = 0, all_w;
 #pragma unroll
@@ -798,7 +805,7 @@ __device__ __forceinline__ int first_bin(const Sums& b, bool by_weight, uint64_t
   return lo;
 }
 
-template <typename E>
+template <typename E, int kPeers>
 __device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, int32_t left, Binned& s,
                                               const cg::cluster_group& cluster) {
   constexpr int T = kThreads;
@@ -828,7 +835,7 @@ __device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, in
     if (w) s.add(bin_of(x), w);
   }, row.v1 - row.v0 <= kHeld ? s.held : nullptr);
   if (row.v1 - row.v0 <= kHeld) row.held = s.held;
-  sum_up(s, cluster, s.sums[0], 0, 0);
+  sum_up<kPeers>(s, cluster, s.sums[0], 0, 0);
 
   auto find = [&](bool by_weight, uint64_t target) {
     const int bin = first_bin(s.sums[0], by_weight, target);
@@ -854,7 +861,7 @@ __device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, in
       __syncthreads();
       s.clear();
       each_in([&](uint32_t k, int32_t, uint64_t w) { s.add(min((k - lo) >> finer, kBins - 1u), w); });
-      sum_up(s, cluster, s.sums[1], c0, w0);
+      sum_up<kPeers>(s, cluster, s.sums[1], c0, w0);
       const int at = first_bin(s.sums[1], by_weight, target);
       if (at) {
         c0 = s.sums[1].count[at - 1];
@@ -971,14 +978,14 @@ __device__ __forceinline__ void sample_binned(const SampleArgs& a, int64_t r, in
   draw(a, r, s, greedy, s.sums[0].count[kBins - 1], s.sums[0].weight[kBins - 1], find, heavy, where);
 }
 
-template <typename E>
+template <typename E, int kPeers>
 __global__ void __launch_bounds__(kThreads, 1) sample_binned_kernel(const SampleArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Binned& s = *reinterpret_cast<Binned*>(smem_raw);
   const cg::cluster_group cluster = cg::this_cluster();
   if (threadIdx.x < 64) s.pow2[threadIdx.x] = kPow2[threadIdx.x];
   grid_dependency_wait();
-  left_rows<kThreads>(a, s, cluster, [&](int64_t r, int32_t left) { sample_binned<E>(a, r, left, s, cluster); });
+  left_rows<kThreads>(a, s, cluster, [&](int64_t r, int32_t left) { sample_binned<E, kPeers>(a, r, left, s, cluster); });
 }
 
 // ---------------------------------------------------------------- rows that their largest tokens decide
@@ -1492,7 +1499,7 @@ cudaError_t go(void (*kern)(SampleArgs), const SampleArgs& a, int64_t rows, int 
 
 template <typename E>
 cudaError_t run_sample(const SampleArgs& a, cudaStream_t st) {
-  static std::atomic<uint64_t> ready[3];
+  static std::atomic<uint64_t> ready[4];
   // CTAs a row.  Rows that one takes in a step of its pass have one (8,000 logits: 13.6 us, 14.2 by two).  Others as many as leave
   // the SMs a CTA each: 131,072 bf16 logits, 64 rows: 28.6 us by one, 25.2 by two, 26.6 by four; 100 rows: 29.4, 31.5, 35.6;
   // 16 rows: 25.6, 21.7, 19.0 and 19.6 by eight; 4 rows 16.9 by four, 15.6 by eight.
@@ -1501,9 +1508,14 @@ cudaError_t run_sample(const SampleArgs& a, cudaStream_t st) {
     while (ctas < kMostCtas && a.R * ctas * 2 <= (ctas == 4 ? 64 : 128)) ctas *= 2;
   const cudaError_t e = go<Head>(sample_head_kernel<E>, a, a.R, ctas, kHeadThreads, ready[0], st);
   if (e != cudaSuccess) return e;
+  // Rows that are left: a cluster each, or, of many short rows, of which many may be, a CTA (300 flat rows of 3,000, 6,000, 12,000
+  // and 24,000 bf16 logits: 46, 49, 63 and 86 us by CTAs, 138, 95, 115 and 124 by clusters; 300 of which none to two are left,
+  // of 6,000, 12,000 and 24,000: 22, 30 and 52 against 24, 29 and 38; 30 flat rows of 12,000: 51 against 36).
+  if (a.V <= 12288 && a.R >= 64)
+    return go<Binned>(sample_binned_kernel<E, 1>, a, std::min<int64_t>(a.R, 152), 1, kThreads, ready[3], st);
   if (sizeof(E) == 2 && a.V <= kMostCounted)
     return go<Counts>(sample_counts_kernel, a, std::min<int64_t>(a.R, 152 / kCountPeers), kCountPeers, kCountThreads, ready[1], st);
-  return go<Binned>(sample_binned_kernel<E>, a, std::min<int64_t>(a.R, 152 / kPeers), kPeers, kThreads, ready[2], st);
+  return go<Binned>(sample_binned_kernel<E, 8>, a, std::min<int64_t>(a.R, 152 / 8), 8, kThreads, ready[2], st);
 }
 
 }  // namespace

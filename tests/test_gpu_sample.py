@@ -235,3 +235,27 @@ def test_streams_graphs_and_repeats(device):
         C.catq_sample(x, u, out[0], top_p=p)
         torch.cuda.synchronize()
         assert torch.equal(out[0], out[2])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["flat", "ties", "equal", "rising"])
+@pytest.mark.parametrize("R,V,gap", [(64, 12288, 0), (200, 2049, 1), (170, 5003, 0), (63, 4096, 3)])
+def test_many_short_rows(device, dtype, kind, R, V, gap):
+    r = syn.rng(69, f"short/{kind}/{R}/{V}")
+    check(device, logits(r, R, V, kind), dtype, gap, u=r.random(R), **settings(r, R))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R", [40, 1100, 70000])
+def test_many_longer_rows_that_need_every_logit(device, dtype, R):
+    """As the 600 equal logits, in rows that a cluster takes each."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+
+    V = 12300
+    u = syn.rng(70, "longer").random(R).astype(np.float32)
+    x = torch.full((R, V), 2.5, dtype=torch.float32 if dtype == "f32" else torch.bfloat16, device=device)
+    tokens = torch.full((R,), -9, dtype=torch.int32, device=device)
+    C.catq_sample(x, torch.from_numpy(u).to(device), tokens)
+    assert np.array_equal(tokens.cpu().numpy(), np.floor(u.astype(np.float64) * V).astype(np.int64))
