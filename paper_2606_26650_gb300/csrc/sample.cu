@@ -435,8 +435,8 @@ __device__ __forceinline__ void draw(const SampleArgs& a, int64_t r, S& s, bool 
   }
 }
 
-// f(row, what its token says) of the rows that are left.  The first CTA of a cluster looks for one and takes it; a cluster begins its search at a place
-// of its own.  (Of very many rows a cluster looks at a share only.)
+// f(row, what its token says) of the rows that are left.  The first CTA of a cluster looks for one and takes it; a cluster begins
+// its search at a place of its own.  (Of very many rows a cluster looks at a share only.)
 template <int T, class S, class F>
 __device__ __forceinline__ void left_rows(const SampleArgs& a, S& s, const cg::cluster_group& cluster, F f) {
   const int peers = cluster.num_blocks();
