@@ -1387,13 +1387,22 @@ __global__ void __launch_bounds__(kHeadThreads, 2) sample_head_kernel(const Samp
   if (!known && warp == 0) {
     uint64_t rest_sum = lane < kHeadWarps ? s.red_low[lane] : 0, off = 0;
     if (lane < ctas) {
-      const double at = s.bound[lane], up = static_cast<double>(max_x) - at;
-      const double down = fmax(up * c_hi + up * c_lo + (at * c_hi - s.ref[lane]), 0.0);
-      if (down < 60.0) {  // (else it weighs nothing)
-        const uint64_t tq = static_cast<uint64_t>(down * 0x1p56);
-        const uint64_t w = __umul64hi(s.rest[lane] << 17, exp2_fraction(tq, s.pow2)) >> (2 + static_cast<int>(tq >> 56));
+      // How far the bound lies below the largest, and the reference that the others were summed under, in octaves.  The reference is
+      // the bound's product with c, rounded: `above` it by part of an octave or more where logits are large against T, or below.
+      const double at = s.bound[lane], up = static_cast<double>(max_x) - at, above = s.ref[lane] - at * c_hi;
+      const double fall = up * c_hi + up * c_lo, down = fall - above;
+      if (fall < 60.0 && above > 0.125) {
+        // The others were summed too coarsely: all that is taken of them is that each weighs no more than the bound.
+        off = s.others[lane] * (weigh(s.bound[lane]) + 1);
+      } else if (fall < 60.0 && down < 60.0) {  // (else they weigh nothing)
+        const bool rises = down < 0.0;  // (by an eighth at most: an octave more, and back)
+        const uint64_t tq = static_cast<uint64_t>((rises ? down + 1.0 : down) * 0x1p56);
+        const uint64_t w =
+            __umul64hi(s.rest[lane] << 17, exp2_fraction(tq, s.pow2)) >> ((rises ? 1 : 2) + static_cast<int>(tq >> 56));
         // Each weight is off by 2^-22 (ex2), seven additions, its argument's rounding and that of c, |t| (2^-24 + 2^-25) with
-        // |t| 2^t at most 0.53 of the bound's weight, the sum's rounding to 2^-26 of that, and half a unit when it is rounded to one.
+        // |t| 2^t at most 0.53 of the bound's weight and |t| up to an eighth larger for the reference, the sum's rounding to 2^-26
+        // of 2^(1/8) of that weight (but for the first two, 2^-24 (ln 2 (0.53 1.5 + 1/8) + 2^(1/8) / 8) < 2^-24 of the bound's weight a
+        // token), and half a unit when it is rounded to one.
         rest_sum += w;
         off = (w >> 20) + (s.others[lane] * weigh(s.bound[lane]) >> 24) + s.others[lane] / 2 + 2;
       }

@@ -259,3 +259,31 @@ def test_many_longer_rows_that_need_every_logit(device, dtype, R):
     tokens = torch.full((R,), -9, dtype=torch.int32, device=device)
     C.catq_sample(x, torch.from_numpy(u).to(device), tokens)
     assert np.array_equal(tokens.cpu().numpy(), np.floor(u.astype(np.float64) * V).astype(np.int64))
+
+
+# In rows whose kept weight Z is only known between limits, Z is taken in their middle, 2^-16 of itself at most from either
+# one: ln(w / Z) is off by 2^-16 (1 + 2^-16) beside the roundings named above.
+def near(lp, ln):
+    return abs(lp - ln) <= 2.0 ** -16 * (1 + 2.0 ** -15) + 2.0 ** -21 * abs(ln)
+
+
+@pytest.mark.parametrize("base,T", [(4.337e6, 1.0), (5.57e6, 1.0), (6.392e6, 1.0), (7.625e6, 1.0), (-7.625e6, 1.0), (1.21e7, 1.0),
+                                    (3.1e7, 1.0), (6.7e7, 4.0), (6.392e4, 2.0 ** -7), (9.1e8, 100.0), (1e3, 1.0)])
+@pytest.mark.parametrize("V,ties", [(4096, 508), (4099, 300), (40000, 480)])
+def test_logits_far_from_zero(device, V, ties, base, T):
+    """Logits of a few units in the last place around a number that is large against T: a product of the number with log2(e) / T
+    is rounded by a good part of 1, up or down.  About 300 to 508 tokens share the largest."""
+    r = syn.rng(71, f"far/{V}/{ties}")
+    top = np.float32(base)
+    x = np.full(V, top) - np.spacing(np.abs(top)) * r.integers(1, 9, V).astype(np.float32)
+    x[r.permutation(V)[:ties]] = top
+    order = np.lexsort((np.arange(V), -x))
+    w = np.rint(2.0 ** 40 * np.exp((x[order].astype(np.float64) - float(top)) / T)).astype(np.int64)
+    upto, share = np.cumsum(w), w[:ties].sum() / w.sum()
+    u = np.concatenate([r.random(24) * share, r.random(8)]).astype(np.float32)
+    read, tokens, lp = run(device, np.repeat(x[None], 32, 0), u=u, temperature=np.full(32, T))
+    assert np.array_equal(read[0], x)
+    for i in range(32):
+        at = int(np.searchsorted(upto, int(np.floor(np.float64(u[i]) * np.float64(upto[-1]))), side="right"))
+        assert tokens[i] == order[at], (i, u[i], at)
+        assert near(lp[i], np.log(w[at] / upto[-1])), (i, lp[i], np.log(w[at] / upto[-1]))
