@@ -681,7 +681,7 @@ catq_status catq_kv_append(const catq_kv_cache* cache, const int32_t* row_start,
                            void* Q_out, int64_t ldq_out, int32_t n_heads, const catq_rotation* rotation,
                            catq_stream stream);
 
-/* Workspace bytes of catq_kv_attention on the current device. */
+/* Workspace bytes of catq_kv_attention and catq_kv_tree_attention on the current device. */
 size_t catq_kv_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, int32_t d);
 
 /* Attention of the new tokens over the cache: row r of sequence b (rows, lengths and positions as in catq_kv_append,
@@ -701,7 +701,8 @@ size_t catq_kv_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, in
  * Sequences of very different numbers of rows (single tokens with a prompt among them) give their result in one call,
  * but take less time in one call a kind: sequences b0 .. b1 - 1 of a batch are row_start + b0, seq_len + b0, the table from
  * its row b0 on, B = b1 - b0 and T = the end of the last one's rows (short ones first: T / B is taken as their mean).
- * workspace: >= catq_kv_attention_workspace_bytes(), 256-byte aligned, zero before the first call; a call leaves the
+ * workspace: >= catq_kv_attention_workspace_bytes() (of heads of 64, whose larger tiles are for trees alone, this call takes
+ * half of what is above 4096 bytes, too), 256-byte aligned, zero before the first call; a call leaves the
  * part that has to be zero as zero (one that latched CATQ_ERR_TIMEOUT may not).  Calls that may run at the same time
  * (other streams, other graphs) need workspaces of their own.
  * n_heads % n_kv_heads == 0, n_heads / n_kv_heads <= 64, T n_heads / n_kv_heads <= 2^26; other limits as for catq_kv_append. */
@@ -731,7 +732,7 @@ catq_status catq_tree_masks(const int32_t* parent, const int32_t* row_start, con
  * ones, and of these, which the cache holds at positions seq_len[b] - n + j, the j-th if bit j % 32 of word j / 32 of the row's
  * `words` words is set (bits at n and behind are ignored; any bits: a row may see later rows, or not itself).  A row that
  * sees nothing gets 0 and lse -inf.  seen [T, words], 1 <= words <= 8, 4-byte aligned; a sequence with more than 32 words
- * rows is left as it was, latching CATQ_ERR_INDEX.  All else as catq_kv_attention, the workspace too. */
+ * rows is left as it was, latching CATQ_ERR_INDEX.  All else as catq_kv_attention, the workspace too (of the whole size). */
 catq_status catq_kv_tree_attention(const catq_kv_cache* cache, const int32_t* row_start, const int32_t* seq_len, int32_t B,
                                    const uint32_t* seen, int32_t words, const void* Q, int64_t ldq, int64_t T,
                                    int32_t n_heads, void* O, int64_t ldo, float* lse, void* workspace, size_t ws_bytes,

@@ -911,7 +911,7 @@ def catq_kv_attention_workspace_bytes(n_heads: int, n_kv_heads: int, d: int) -> 
 
 
 def kv_attention_workspace(cache: KVCache, n_heads: int):
-    """A zeroed workspace for catq_kv_attention over this cache."""
+    """A zeroed workspace for catq_kv_attention and catq_kv_tree_attention over this cache."""
     import torch
     return torch.zeros(catq_kv_attention_workspace_bytes(n_heads, cache.n_kv_heads, cache.d), dtype=torch.uint8,
                        device=cache.k_codes.device)

@@ -1106,7 +1106,7 @@ catq_status catq_kv_append(const catq_kv_cache* cache, const int32_t* row_start,
 
 size_t catq_kv_attention_workspace_bytes(int32_t n_heads, int32_t n_kv_heads, int32_t d) {
   if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || (d != 64 && d != 128)) return 0;
-  return kv_attention_ws_bytes(n_heads, n_kv_heads, d);
+  return kv_attention_ws_bytes(n_heads, n_kv_heads, d, true);  // (enough for either call)
 }
 
 }  // extern "C"
@@ -1127,7 +1127,7 @@ catq_status kv_attention(const catq_kv_cache* cache, const int32_t* row_start, c
   if (T == 0 || B == 0) return CATQ_OK;
   if (!Q || !O || (Q == O && ldq != ldo)) return CATQ_ERR_INVALID_ARG;
   if (!rows_ok(Q, ldq) || !rows_ok(O, ldo) || (lse && !aligned4(lse))) return CATQ_ERR_ALIGN;
-  if (!workspace || ws_bytes < kv_attention_ws_bytes(n_heads, nkv, d)) return CATQ_ERR_WORKSPACE;
+  if (!workspace || ws_bytes < kv_attention_ws_bytes(n_heads, nkv, d, seen != nullptr)) return CATQ_ERR_WORKSPACE;
   if (!aligned256(workspace)) return CATQ_ERR_ALIGN;
   if ((st = check_tensor_core_device()) != CATQ_OK) return st;
   KvAttnArgs a{};

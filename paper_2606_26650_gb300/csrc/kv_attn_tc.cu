@@ -1814,9 +1814,9 @@ cudaError_t run_kv_rows(const KvAttnArgs& a, cudaStream_t st) {
 
 }  // namespace
 
-size_t kv_attention_ws_bytes(int32_t, int32_t, int32_t d) {
-  // two parts for each CTA: two CTAs an SM with tiles of up to 32 rows, one of 128
-  const size_t parts = static_cast<size_t>(sm_count()) * 2 * 128 * (static_cast<size_t>(d) + 2) * sizeof(float);
+size_t kv_attention_ws_bytes(int32_t, int32_t, int32_t d, bool tree) {
+  // two parts for each CTA: two CTAs an SM with tiles of up to 32 rows, one of 128 (heads of 64: for trees alone)
+  const size_t parts = static_cast<size_t>(sm_count()) * 2 * (d == 128 || tree ? 128 : 64) * (static_cast<size_t>(d) + 2) * sizeof(float);
   return (kCounterBytes + parts + 255) / 256 * 256;
 }
 

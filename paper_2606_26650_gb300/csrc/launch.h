@@ -261,7 +261,8 @@ struct KvAttnArgs {
   void* workspace;
   int32_t* status;   // set by the launcher
 };
-size_t kv_attention_ws_bytes(int32_t nh, int32_t nkv, int32_t d);
+// tree: with `seen`, whose tiles may be larger.
+size_t kv_attention_ws_bytes(int32_t nh, int32_t nkv, int32_t d, bool tree);
 cudaError_t launch_kv_attention(KvAttnArgs a, cudaStream_t st);
 
 // tree.cu

@@ -266,3 +266,27 @@ def test_rows_before_the_first_position_are_not_stored(device, d, page):  # noqa
     kept = np.isnan(asked)
     assert np.array_equal(scale[0], paged.scale[0]) and np.array_equal(K.E4M3[codes[0]][kept], K.E4M3[paged.codes[0]][kept])
     assert kept.sum() == kept.size - 5 * nkv * d  # (2 and 3 tokens are new)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 9, 30])
+def test_heads_of_64_stay_within_the_workspace_of_tiles_of_32_rows(device, rows):
+    """Half of the parts' bytes are enough for this call, and what lies behind them is left as it was."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(90, f"half/{rows}")
+    lens, news, nh = [9000, 1700], [rows, max(1, rows // 2)], 8
+    paged = Paged(r, lens, 2, 64, 64, device)
+    T = sum(news)
+    q = bf16(r.standard_normal((T, nh * 64)), device)
+    args = (paged.cache, i32(starts(news), device), i32(lens, device), q)
+    out = [torch.empty(T, nh * 64, dtype=torch.bfloat16, device=device) for _ in range(2)]
+    whole = C.kv_attention_workspace(paged.cache, nh)
+    half = 4096 + (whole.numel() - 4096) // 2
+    C.catq_kv_attention(*args, out[0], nh, whole)
+    ws = torch.zeros_like(whole)
+    ws[half:] = 77
+    C.catq_kv_attention(*args, out[1], nh, ws[:half])
+    torch.cuda.synchronize()
+    assert C.catq_device_status() == 0
+    assert torch.equal(out[0], out[1]) and (ws[half:] == 77).all()

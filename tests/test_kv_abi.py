@@ -244,3 +244,22 @@ def test_oracle_attention_by_hand():
     w = np.exp(8 / np.sqrt(8))
     assert np.allclose(O[0, 0], [2.0] * 4 + [0.0] * 4) and np.allclose(lse[0, 0], 0.0)
     assert np.allclose(O[1, 0], np.array([2.0] * 4 + [4.0 * w] * 4) / (1 + w)) and np.allclose(lse[1, 0], np.log(1 + w))
+
+
+def test_heads_of_64_take_the_workspace_of_tiles_of_32_rows(lib):
+    """The size that the query gives is the tree call's; this call of heads of 64 has no tiles of 128 rows and takes half of
+    the parts' bytes.  (A size that is enough is told from one that is not by the refusal that comes next.)"""
+    whole = lib.catq_kv_attention_workspace_bytes(4, 2, 64)
+    half = 4096 + (whole - 4096) // 2
+    off = 65536 + 64
+
+    def call(n):
+        return attend(lib, c=cache(d=64), ldq=256, ldo=256, ws=off, n=n)
+
+    assert call(half) == call(whole) == ALIGN and call(half - 256) == WORKSPACE
+    c = cache(d=64)
+    tree = [lib.catq_kv_tree_attention(c, 512, 640, 2, 128, 1, 4096, 256, 8, 4, 8192, 256, None, off, n, None)
+            for n in (whole, whole - 256, half)]
+    assert tree == [ALIGN, WORKSPACE, WORKSPACE]
+    whole = lib.catq_kv_attention_workspace_bytes(4, 2, 128)  # (heads of 128 have those tiles in either call)
+    assert attend(lib, ws=off, n=whole) == ALIGN and attend(lib, ws=off, n=whole - 256) == WORKSPACE
