@@ -747,11 +747,15 @@ catq_status catq_kv_tree_attention(const catq_kv_cache* cache, const int32_t* ro
  *     (top_p >= 1: any; at least one token is kept), and
  *   has only tokens with w >= max(1, 2^40 min_p) (min_p <= 0: 1; above 1: 1 is taken).
  * With Z its weight, the token is the first whose cumulated weight exceeds floor(u Z) (at most Z - 1, at least 0).  The products
- * u Z and top_p S are taken in 64-bit floats, all else is exact: no result depends on an order of additions.
+ * u Z and top_p S are taken in 64-bit floats, all else that decides on the token is exact: it depends on no order of additions
+ * and on no other row.
  * temperature, top_p, min_p [R] fp32, top_k [R] int32, each nullable: 1, 1, 0, 0.  T == 0: the first token (no other filter).
  * Temperatures from 2^-60 to 2^60; others above 0 count as the nearer of these.
  * tokens [R] int32, overlapping no input (it holds the kernels' marks in between).  logprob [R] fp32 (nullable): ln(w / Z), the
- * probability with which the token was drawn, with Z to 2^-16 of itself at least; 0 for T == 0.
+ * probability with which the token was drawn; 0 for T == 0.  Where the token is certain before Z is known exactly (no filter ends
+ * what is kept among the row's largest tokens), Z is the middle of two limits at most 2^-15 of it apart.  The limits go with
+ * the number of rows, which sets how a row is shared out: beside another number of rows a logprob may be another within 2^-15;
+ * the same call gives the same bits.
  * Logits of -inf are never drawn.  A row with NaN or +inf, without any finite logit, or with a temperature that is negative
  * or NaN gets token -1 and logprob NaN.  A NaN among the other settings counts as its default (u: as 0).
  * 1 <= V <= 2^20, R < 2^31, ld >= V (else CATQ_ERR_SHAPE); logits aligned to their type (16-byte aligned rows are faster),

@@ -964,7 +964,8 @@ def catq_kv_tree_attention(cache: KVCache, row_start, seq_len, seen, Q, O, n_hea
 
 def catq_sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, stream=None):
     """tokens [R] int32 drawn from logits [R, V] (bf16 or fp32, rows may lie apart) by the random numbers u [R] (fp32);
-    settings a row: temperature, top_p, min_p [R] fp32, top_k [R] int32; logprob [R] fp32 (optional)."""
+    settings a row: temperature, top_p, min_p [R] fp32, top_k [R] int32; logprob [R] fp32 (optional), whose last bits may go
+    with the number of rows (the tokens do not)."""
     w = "catq_sample"
     if logits.dim() != 2:
         raise ValueError(f"{w}: logits have shape {tuple(logits.shape)}, the call needs [R, V]")

@@ -287,3 +287,18 @@ def test_logits_far_from_zero(device, V, ties, base, T):
         at = int(np.searchsorted(upto, int(np.floor(np.float64(u[i]) * np.float64(upto[-1]))), side="right"))
         assert tokens[i] == order[at], (i, u[i], at)
         assert near(lp[i], np.log(w[at] / upto[-1])), (i, lp[i], np.log(w[at] / upto[-1]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [20000, 131072])
+def test_a_row_beside_others(device, dtype, V):
+    """A row by itself and among 64 and 200: the same token; its probability within what Z may be off by, twice."""
+    r = syn.rng(73, f"beside/{V}")
+    x = logits(r, 1, V, "lm")
+    u = r.random(200).astype(np.float32)
+    alone = [run(device, x, dtype, u=u[i:i + 1]) for i in range(12)]
+    for R in (64, 200):
+        _, tokens, lp = run(device, np.repeat(x, R, 0), dtype, u=u[:R])
+        for i, (_, t, p) in enumerate(alone):
+            assert tokens[i] == t[0]
+            assert abs(lp[i] - p[0]) <= 2.0 ** -15 * (1 + 2.0 ** -15) + 2.0 ** -20 * abs(p[0])
