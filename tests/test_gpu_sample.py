@@ -302,3 +302,29 @@ def test_a_row_beside_others(device, dtype, V):
         for i, (_, t, p) in enumerate(alone):
             assert tokens[i] == t[0]
             assert abs(lp[i] - p[0]) <= 2.0 ** -15 * (1 + 2.0 ** -15) + 2.0 ** -20 * abs(p[0])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["flat", "equal", "close"])
+@pytest.mark.parametrize("R", [1, 4, 66])
+def test_the_largest_vocabulary(device, dtype, kind, R):
+    """2^20 logits, by eight CTAs a row, four and one.  close: 400 tokens at the largest, all others one step below, so that
+    what is not listed weighs as much as it can."""
+    V = 1 << 20
+    r = syn.rng(72, f"most/{kind}")
+    x = logits(r, 1, V, kind)[0].astype(np.float32)
+    if kind == "close":
+        x = np.full(V, 1.0 - (2.0 ** -24 if dtype == "f32" else 2.0 ** -8), np.float32)
+        x[r.permutation(V)[:400]] = 1.0
+    u = np.concatenate([[0.5], r.random(R)])[:R].astype(np.float32)
+    if kind == "close":
+        u[::2] *= np.float32(400 / V)  # (the listed ones)
+    read, tokens, lp = run(device, np.repeat(x[None], R, 0), dtype, u=u)
+    x = read[0].astype(np.float64)
+    order = np.lexsort((np.arange(V), -x))
+    w = np.rint(2.0 ** 40 * np.exp(x[order] - x[order[0]])).astype(np.int64)
+    upto = np.cumsum(w)
+    for i in range(R):
+        at = int(np.searchsorted(upto, int(np.floor(np.float64(u[i]) * np.float64(upto[-1]))), side="right"))
+        assert tokens[i] == order[at], (i, u[i], at)
+        assert near(lp[i], np.log(w[at] / upto[-1]))
