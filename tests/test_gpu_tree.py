@@ -583,3 +583,84 @@ def test_drafted_steps_follow_plain_decoding(device, captured):
     for b in range(B):
         assert got[b] == want[b][:len(got[b])].tolist(), (got[b], want[b])
     assert max(max(k) for k in kept_all) >= 3
+
+
+# ------------------------------------------------------------------ beside the causal call; rows without a context
+
+def chained(device, d, nh, nkv, page, lens, news, words):
+    """(tree's and causal attention of the same rows, the larger of the two parts' sums p |v|)."""
+    import torch
+
+    from paper_2606_26650_gb300 import catq as C
+    r = syn.rng(52, f"chain/{d}/{nh}/{nkv}/{lens}/{news}")
+    paged = Paged(r, lens, nkv, page, d, device)
+    rs = starts(news)
+    seen, _ = O.masks(trees(r, news, back=1), rs, lens, words)
+    q = r.standard_normal((rs[-1], nh, d)) * 2.0
+    got, lse, status = attend(paged, rs, lens, seen, q, nh, device)
+    assert status == 0
+    out = torch.full((int(rs[-1]), nh * d), 7.0, dtype=torch.bfloat16, device=device)
+    lse2 = torch.full((int(rs[-1]), nh), 7.0, device=device)
+    C.catq_kv_attention(paged.cache, i32(rs, device), i32(lens, device), bf16(q.reshape(rs[-1], -1), device), out, nh,
+                        C.kv_attention_workspace(paged.cache, nh), lse=lse2)
+    assert done() == 0
+    _, _, mag, low = O.attention(*paged.codes, *paged.scale, paged.table, page, rs, lens, seen,
+                                 syn.round_bf16(np.asarray(q, np.float32)), nh)
+    return got, lse, out.float().cpu().numpy().reshape(got.shape).astype(np.float64), lse2.cpu().numpy(), mag, low
+
+
+@pytest.mark.parametrize("d,nh,nkv,page,lens,news,words", [
+    (128, 4, 2, 64, [100, 128, 3], [2, 4, 3], 1),          # tiles of 8 rows
+    (128, 8, 2, 16, [100, 128, 70], [4, 3, 4], 1),         # of 16
+    (128, 8, 2, 64, [100, 128, 70], [8, 8, 7], 1),         # of 32
+    (128, 8, 2, 64, [128, 127, 100], [33, 40, 60], 2),     # of 128
+    (64, 8, 4, 32, [256, 200, 31], [4, 4, 3], 1),
+    (64, 8, 2, 16, [256, 255, 90], [16, 15, 9], 1),
+])
+def test_chains_of_one_tile_of_tokens_are_causal_attention(device, d, nh, nkv, page, lens, news, words):
+    """Where no row tile's tokens are shared out and both calls take tiles of as many rows, they do the same arithmetic: equal
+    bits."""
+    got, lse, want, want_lse, _, _ = chained(device, d, nh, nkv, page, lens, news, words)
+    assert np.array_equal(got, want) and np.array_equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("d,nh,nkv,page,lens,news,words", [
+    (128, 8, 2, 64, [400, 1000, 70], [24, 24, 24], 1),
+    (128, 8, 1, 16, [9000, 600], [100, 127], 4),
+    (64, 8, 2, 64, [5000, 1000], [30, 17], 1),
+])
+def test_chains_are_causal_attention(device, d, nh, nkv, page, lens, news, words):
+    """Shared out otherwise: two outputs that are each within the oracle's bounds, element by element, and twice the part of these
+    that is not the last rounding."""
+    got, lse, want, want_lse, mag, low = chained(device, d, nh, nkv, page, lens, news, words)
+    bound = 2.0 ** -8 * (np.abs(got) + np.abs(want)) + 2 * ((2.0 ** -8 + 2.0 ** -14) * mag + 2.0 ** -17 * low)
+    assert (np.abs(got - want) <= bound).all()
+    assert (np.abs(lse - want_lse) <= 2.0 ** -15 * (1 + np.abs(want_lse))).all()
+
+
+@pytest.mark.parametrize("d,nh,nkv,page,lens,news", [
+    (128, 1, 1, 64, [256] + [3] * 40, [256] + [1] * 40),    # 8 rows a tile: two tiles of tokens, the first hidden from many rows
+    (128, 2, 1, 16, [256] + [2] * 40, [256] + [2] * 40),    # 16
+    (128, 4, 1, 16, [256] + [5] * 40, [256] + [2] * 40),    # 32
+    (128, 2, 1, 64, [256, 129], [256, 129]),                # 128
+    (64, 2, 1, 16, [256, 200], [256, 200]),
+    (64, 2, 2, 32, [256, 140], [250, 140]),
+])
+@pytest.mark.parametrize("kind", ["alone", "late", "none"])
+def test_rows_from_which_whole_tiles_are_hidden(device, d, nh, nkv, page, lens, news, kind):
+    """Trees without a context (or of a few tokens): rows that see themselves alone, or rows from the 128th on, or nothing."""
+    r = syn.rng(53, f"hidden/{d}/{nh}/{nkv}/{lens[:2]}/{news[:2]}/{kind}")
+    paged = Paged(r, lens, nkv, page, d, device)
+    rs = starts(news)
+    words = 8
+    seen = np.zeros((int(rs[-1]), words), np.uint32)
+    for b, n in enumerate(news):
+        for i in range(n):
+            if kind == "alone":
+                seen[rs[b] + i, i // 32] = np.uint32(1 << (i % 32))
+            elif kind == "late":
+                seen[rs[b] + i, 4:] = r.integers(0, 1 << 32, 4, dtype=np.uint64).astype(np.uint32)
+    q = r.standard_normal((int(rs[-1]), nh, d)) * 2.0
+    got, lse, status = attend(paged, rs, lens, seen, q, nh, device)
+    assert status == 0
+    check(paged, rs, np.array(lens), seen, q, nh, got, lse)
