@@ -1124,8 +1124,9 @@ __global__ void __launch_bounds__(KvLay<HD, R, TREE>::kThreads, KvLay<HD, R, TRE
 // Thread (row, quarter c) has the row's tokens 32 c .. 32 c + 31 of a tile.  The four agree on the row's maximum through
 // shared memory; raising it is lazy, as there, row by row.
 // Two prompts' chunks of 1023 tokens on 6001 and 8191 (32 / 8 heads of 128, 213 GFLOP) take 254 us, 0.84 PFLOP/s, bound by
-// the softmax's arithmetic (265 with the parts of a cut row tile row by row, whose 16 bytes a lane are 32 lines an instruction).  The products by themselves, the softmax's threads only keeping pace, take 188: 1,280 cycles a tile
-// would be 115, the rest is that a tile's scores, its weights and their product follow one another.  In a form with two terms a
+// the softmax's arithmetic (265 with the parts of a cut row tile row by row, whose 16 bytes a lane are 32 lines an instruction).
+// The products by themselves, the softmax's threads only keeping pace, take 188: 1,280 cycles a tile would be 115, the rest is
+// that a tile's scores, its weights and their product follow one another.  In a form with two terms a
 // weight (257 us): two threads a row 284; the accumulators raised before the weights are made, and only those of the rows
 // that have to be, 266; rows read and written by their own lanes 261; the other kernel with tiles of 64 rows 386.
 constexpr float kNominalRows = 14.0f;
@@ -1785,12 +1786,18 @@ cudaError_t run_kv(void (*kern)(CUtensorMap, CUtensorMap, KvTcArgs), int ctas, c
 }
 
 // Rows of a tile: by what an average sequence has a key/value head (any number is right).  16 sequences of 4096 tokens, 8
-// key/value heads, us with tiles of 8 / 16 / 32 / 128 rows: heads of 128, 4 rows 29.2 / 28.7 / 32.9 / 51.8, 12 rows 34.3 /
-// 29.6 / 35.7 / 53, 24 rows 46.3 / 38.3 / 38.7 / 53, 48 rows 102 / 52.4 / 56.8 / 53.9, 64 rows 119 / 69 / 58.8 / 54.5, 96 rows 145 / 104 /
-// 78 / 55.5, 128 rows 193 / 127 / 99 / 57.3; heads of 64 (those of 128 rows: TREE), 4 rows 17.8 / 19.7 / 25.1 / 52, 16 rows 24.6 / 19.5 / 24.9,
-// 32 rows 39 / 32.7 / 30 / 53, 64 rows 69 / 52 / 47.1 / 53.5, 96 rows 96 / 71 / 65.5 / 53.9, 128 rows 125 / 90 / 83.5 / 54.7.  Trees of
-// unlike size in one batch bring the line between the last two down.  The mean is a poor guide to a batch of single tokens
-// with a prompt among them: 128 single tokens on 2048 and a prompt of 512 (32 / 8 heads
+// key/value heads of 4 query heads each, us with tiles of 8 / 16 / 32 / 128 rows.
+//   Causal, heads of 128: 4 rows 30.1 / 29.1 / 32.4 / 51.3, 12 rows 36.9 / 29.7 / 33.8 / 52.1, 24 rows 50.7 / 39.0 / 35.6 / 52.1, 48 rows
+//   104 / 54.5 / 51.8 / 53.1, 64 rows - / 71.3 / 52.8 / 53.6, 96 rows - / 105 / 73.7 / 54.8, 128 rows - / 129 / 92.1 / 56.7.
+//   Causal, heads of 64 (no tiles of 128): 4 rows 21.1 / 20.8 / 25.6, 16 rows 25.8 / 21.7 / 26.4, 32 rows 41.0 / 30.5 / 29.5, 48 rows 56.0 /
+//   40.3 / 43.7, 64 rows - / 50.2 / 46.3, 128 rows - / 86.3 / 80.2.
+//   TREE, heads of 128: 4 rows 30.2 / 29.6 / 31.7 / 51.6, 12 rows 37.2 / 30.4 / 33.3 / 52.1, 24 rows 51.3 / 39.2 / 35.2 / 52.3, 48 rows 103 /
+//   54.7 / 50.8 / 52.8, 64 rows - / 71.0 / 51.5 / 53.4, 96 rows - / 105 / 72.9 / 55.2, 128 rows - / 129 / 90.6 / 57.2.
+//   TREE, heads of 64: 4 rows 21.6 / 21.7 / 27.2 / 53.2, 16 rows 25.8 / 22.7 / 28.0 / 53.3, 32 rows 41.7 / 31.9 / 31.4 / 53.5, 48 rows 56.7 / 42.1 /
+//   46.6 / 53.8, 64 rows - / 52.6 / 49.1 / 53.7, 96 rows - / 72.1 / 67.1 / 54.3, 128 rows - / 90.3 / 85.1 / 54.9.
+// Trees of unlike size in one batch bring the line between the last two down: 16 of 3 to 24 tokens (heads of 128, 55 rows in the
+// mean) 82.9 / 79.7 / 66.8 with tiles of 16 / 32 / 128, 32 of 2 to 61 (heads of 64, 95 rows) 73.4 / 70.4 / 51.8.  The mean is a
+// poor guide to a batch of single tokens with a prompt among them: 128 single tokens on 2048 and a prompt of 512 (32 / 8 heads
 // of 128) take 155 us in one call, 129 in two; 32 on 4096 and a prompt of 2048 171 and 146.
 template <int HD, int R, bool TREE>
 cudaError_t run_few(const KvAttnArgs& a, cudaStream_t st) {

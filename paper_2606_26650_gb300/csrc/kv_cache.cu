@@ -603,7 +603,8 @@ constexpr int kInHand = 2;    // passes over a page's tokens that a warp keeps i
 // is found once.  Page by page, so that a token's slot is never written before it has been read: sources rise strictly, so the
 // j-th kept token's is j or more behind the context.  A page that has to grow is rounded again before what moves inside it.
 // Bound by the chain of loads (rows, path, page numbers, codes and scales), 3 us for one sequence and layer; 16 layers of 64
-// sequences with up to 8 moved tokens each (8 heads of 128) move 19.6 MB in 12.6 us.
+// sequences with up to 8 moved tokens each (8 heads of 128) move 19.6 MB in 14.4 us where no page grows, and take 18.5 where the
+// pages are each at half the scale of the next, so that those that take another's tokens are rounded again.
 template <int D>
 __global__ void __launch_bounds__(32 * kCompactWarps) kv_compact_kernel(const __grid_constant__ KvCompactArgs a, Divisor by_page,
                                                                         int32_t per_cta) {
@@ -859,8 +860,8 @@ cudaError_t launch_kv_compact(KvCompactArgs& a, cudaStream_t st) {
   WaitCtl wc;
   if (!launch_wait_ctl(&wc)) return cudaErrorInvalidDevice;
   a.status = wc.status_word;
-  // A warp takes one (cache, keys or values, head) (16 layers of 64 sequences: 12.6 us, two each 14, four 16.7); as many CTAs a
-  // sequence as a grid's second dimension has.
+  // A warp takes one (cache, keys or values, head) (one layer of one sequence 3.1 us, two each 4.0; 16 layers of 64 sequences
+  // 14.4, two each 14.1, four 17.1); as many CTAs a sequence as a grid's second dimension has.
   const int32_t items = a.n_caches * 2 * a.nkv, per_cta = ((items / kCompactWarps) / 65535 + 1) * kCompactWarps;
   const dim3 grid(a.B, (items + per_cta - 1) / per_cta);
   if (a.d == 64)
